@@ -265,6 +265,111 @@ size_t dll_cnn_forward_workspace_bytes(const dll_net_desc *net);
 dll_status dll_cnn_forward(const dll_net_desc *net, const float *const *params, const float *x,
                            float *logits, float *prob, void *ws, size_t ws_bytes, void *stream);
 
+/* ---------------------------------------------------------------------------------------
+ * Operators of large language models, beside the dense layers, the loss and the update of the
+ * network steps above: a gated feed-forward block, softmax cross entropy over a large
+ * vocabulary, and clipping by the global gradient norm with the momentum step behind it.
+ * The conventions at the top hold: device pointers, row-major and contiguous, 16-byte aligned
+ * (else DLL_ERR_SHAPE) unless stated, caller-owned workspaces, errors before any launch.
+ * Tensors typed `void *` hold the descriptor's dtype.  Sums, softmax statistics and norms are
+ * taken in 32 bits or more; with DLL_BF16 what one product hands to the next is rounded to
+ * bfloat16 once (to nearest), and results are rounded once.  At most 2^24 tokens and 2^20
+ * features, hidden units or classes; a tensor of 2^31 or more elements -> DLL_ERR_UNSUPPORTED.
+ * Results are bit-identical from run to run.  Nothing is allocated or copied from the host, so
+ * every call can be captured into a graph (calls that overlap in time need workspaces of their
+ * own).  Rows of sizes that are no multiple of 16 bytes are copied into the workspace first.
+ * ------------------------------------------------------------------------------------- */
+typedef enum { DLL_FP32 = 0, DLL_BF16 = 1 } dll_dtype;
+
+/* The gate's activation: identity, sigmoid, max(a, 0), a * sigmoid(a), a * Phi(a) with Phi the
+ * normal distribution's cumulative function (not its tanh approximation). */
+typedef enum { DLL_GATE_IDENTITY = 0, DLL_GATE_SIGMOID = 1, DLL_GATE_RELU = 2, DLL_GATE_SILU = 3, DLL_GATE_GELU = 4 } dll_gate;
+
+typedef struct {
+  int tokens, width, hidden;
+  int gate;  /* dll_gate */
+  int dtype; /* dll_dtype of all tensors */
+} dll_gated_desc;
+
+/* Gated feed-forward block over a batch of tokens:
+ *   a = x w_gate^T,  b = x w_up^T,  h = act(a) * b,  y = h w_down^T
+ *   x, y [tokens][width];  w_gate, w_up [hidden][width];  w_down [width][hidden]
+ * gate_pre and up_pre [tokens][hidden] receive a and b, which the backward pass needs (both or
+ * neither; NULL in an inference pass). */
+size_t dll_gated_fwd_workspace_bytes(const dll_gated_desc *d);
+dll_status dll_gated_fwd(const dll_gated_desc *d, const void *x, const void *w_gate, const void *w_up,
+                         const void *w_down, void *y, void *gate_pre, void *up_pre, void *ws,
+                         size_t ws_bytes, void *stream);
+
+/* Its backward pass, dy [tokens][width] the gradient w.r.t. y:
+ *   dh = dy w_down,  da = dh * b * act'(a),  db = dh * act(a)   (act'(0) = 0 for DLL_GATE_RELU)
+ *   dx = da w_gate + db w_up,  dw_gate = da^T x,  dw_up = db^T x,  dw_down = dy^T h
+ * dx, dw_gate, dw_up and dw_down may each be NULL (that gradient is not taken), not all four. */
+size_t dll_gated_bwd_workspace_bytes(const dll_gated_desc *d);
+dll_status dll_gated_bwd(const dll_gated_desc *d, const void *x, const void *w_gate, const void *w_up,
+                         const void *w_down, const void *gate_pre, const void *up_pre, const void *dy,
+                         void *dx, void *dw_gate, void *dw_up, void *dw_down, void *ws, size_t ws_bytes,
+                         void *stream);
+
+typedef struct {
+  int tokens, width, classes;
+  int dtype; /* dll_dtype of x, w, bias and their gradients */
+} dll_vocab_desc;
+
+/* Softmax cross entropy of a linear layer over a large vocabulary; its logits are never stored:
+ *   z = x w^T + bias,  lse_t = ln sum_v exp z[t][v],  loss_t = lse_t - z[t][labels[t]]
+ *   x [tokens][width];  w [classes][width];  bias [classes], may be NULL;  labels [tokens] int32
+ * Rows whose label lies outside [0, classes) (padding) do not count: their row_loss and row_lse are
+ * 0 and nothing of what x holds there is used.  *loss is the mean over the rows that count, 0 if
+ * none does.  row_loss and row_lse [tokens] fp32 may be NULL.  A bias of -infinity takes a class out;
+ * logits that are NaN or +infinity, or a row without a finite one, give a loss of NaN. */
+size_t dll_vocab_loss_fwd_workspace_bytes(const dll_vocab_desc *d);
+dll_status dll_vocab_loss_fwd(const dll_vocab_desc *d, const void *x, const void *w, const void *bias,
+                              const int *labels, float *row_loss, float *row_lse, float *loss, void *ws,
+                              size_t ws_bytes, void *stream);
+
+/* The same with the gradients of scale * loss:
+ *   dz = scale / count * (softmax(z) - onehot(labels)),  dx = dz w,  dw = dz^T x,  dbias = sum_t dz
+ * dx rows that do not count are 0.  dx, dw and dbias may each be NULL (not all three; dbias needs bias).
+ * exp(z) is kept for a piece of the tokens at a time, 1 GiB at most. */
+size_t dll_vocab_loss_grad_workspace_bytes(const dll_vocab_desc *d);
+dll_status dll_vocab_loss_grad(const dll_vocab_desc *d, const void *x, const void *w, const void *bias,
+                               const int *labels, float scale, float *row_loss, float *row_lse,
+                               float *loss, void *dx, void *dw, void *dbias, void *ws, size_t ws_bytes,
+                               void *stream);
+
+/* A list of n tensors, as host arrays that are read during the call only: their numbers of elements
+ * (0 is allowed) and types. */
+typedef struct {
+  int n;
+  const size_t *counts;
+  const int *dtypes; /* dll_dtype of each gradient */
+} dll_tensor_list;
+
+/* The 2-norm over all elements of all gradients, *norm a device scalar.  grads is a host array of n
+ * device pointers (aligned to their elements; NULL only where the count is 0).  Squares are added
+ * in 64 bits in a fixed order. */
+size_t dll_grad_norm_workspace_bytes(const dll_tensor_list *list);
+dll_status dll_grad_norm(const dll_tensor_list *list, const void *const *grads, float *norm, void *ws,
+                         size_t ws_bytes, void *stream);
+
+/* Clipping by the global norm: out = c * grad with c = min(1, max_norm / norm), max_norm > 0 (infinity:
+ * c = 1), out in the gradients' types; out[i] may be grads[i].  Where the norm is not finite c is 1.
+ * Workspace as for dll_grad_norm. */
+dll_status dll_grad_clip(const dll_tensor_list *list, const void *const *grads, void *const *out,
+                         float max_norm, float *norm, void *ws, size_t ws_bytes, void *stream);
+
+/* The momentum step of dll_cnn_train_step_momentum on gradients clipped in passing (they are not written):
+ *   v <- momentum * v - lr * (c * g + weight_decay * theta);   theta <- theta + v
+ * params and velocity are host arrays of n fp32 device pointers; weight_decay a host array of n factors,
+ * or NULL (none).  copies, or NULL, is a host array of n device pointers (each may be NULL) that receive
+ * the new parameters in bfloat16.  Where the norm is not finite no step is taken: only *norm is written. */
+dll_status dll_momentum_update_clipped(const dll_tensor_list *list, float *const *params,
+                                       float *const *velocity, const void *const *grads, float lr,
+                                       float momentum, const float *weight_decay, float max_norm,
+                                       float *norm, void *const *copies, void *ws, size_t ws_bytes,
+                                       void *stream);
+
 #ifdef __cplusplus
 }
 #endif

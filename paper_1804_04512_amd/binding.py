@@ -13,7 +13,7 @@ from typing import List, Optional, Sequence
 
 import torch
 
-from .workloads import ConvSpec, DenseSpec
+from .workloads import ConvSpec, DenseSpec, GatedSpec, VocabSpec
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libdll_conv.so")
@@ -24,9 +24,16 @@ SYMBOLS = ["dll_status_string", "dll_conv_workspace_bytes", "dll_conv_valid_fwd"
            "dll_cnn_workspace_bytes", "dll_cnn_train_step", "dll_cnn_forward_workspace_bytes", "dll_cnn_forward",
            "dll_cnn_train_step_momentum", "dll_crbm_cd1_step_units", "dll_rbm_workspace_bytes", "dll_rbm_cd1_step",
            "dll_conv_full_fft_workspace_bytes", "dll_conv_full_bwd_fft", "dll_conv_valid_wgrad_noalloc",
-           "dll_conv_valid_wgrad_partial", "dll_conv_valid_wgrad_finish"]
+           "dll_conv_valid_wgrad_partial", "dll_conv_valid_wgrad_finish",
+           "dll_gated_fwd_workspace_bytes", "dll_gated_fwd", "dll_gated_bwd_workspace_bytes", "dll_gated_bwd",
+           "dll_vocab_loss_fwd_workspace_bytes", "dll_vocab_loss_fwd", "dll_vocab_loss_grad_workspace_bytes",
+           "dll_vocab_loss_grad", "dll_grad_norm_workspace_bytes", "dll_grad_norm", "dll_grad_clip",
+           "dll_momentum_update_clipped"]
 NOALLOC_SCRATCH_BYTES = 8 << 20   # DLL_NOALLOC_SCRATCH_BYTES of include/dll_conv.h
 VISIBLE = {"binary": 0, "gaussian": 1}
+DTYPE = {"float32": 0, "bfloat16": 1}
+GATE = {"identity": 0, "sigmoid": 1, "relu": 2, "silu": 3, "gelu": 4}
+_TORCH_TYPE = {"float32": torch.float32, "bfloat16": torch.bfloat16}
 
 
 class DllError(RuntimeError):
@@ -42,6 +49,18 @@ class dll_conv_desc(C.Structure):
 
 class dll_dense_desc(C.Structure):
     _fields_ = [("in_", C.c_int), ("out", C.c_int), ("act", C.c_int)]
+
+
+class dll_gated_desc(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("tokens", "width", "hidden", "gate", "dtype")]
+
+
+class dll_vocab_desc(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("tokens", "width", "classes", "dtype")]
+
+
+class dll_tensor_list(C.Structure):
+    _fields_ = [("n", C.c_int), ("counts", C.POINTER(C.c_size_t)), ("dtypes", C.POINTER(C.c_int))]
 
 
 class dll_net_desc(C.Structure):
@@ -89,6 +108,18 @@ def lib() -> C.CDLL:
         L.dll_cnn_forward_workspace_bytes.restype = sz
         L.dll_cnn_forward_workspace_bytes.argtypes = [C.POINTER(dll_net_desc)]
         L.dll_cnn_forward.argtypes = [C.POINTER(dll_net_desc), vp, vp, vp, vp, vp, sz, vp]
+        pg, pv, pl = C.POINTER(dll_gated_desc), C.POINTER(dll_vocab_desc), C.POINTER(dll_tensor_list)
+        for name, arg in (("dll_gated_fwd", pg), ("dll_gated_bwd", pg), ("dll_vocab_loss_fwd", pv), ("dll_vocab_loss_grad", pv),
+                          ("dll_grad_norm", pl)):
+            query = getattr(L, name + "_workspace_bytes")
+            query.restype, query.argtypes = sz, [arg]
+        L.dll_gated_fwd.argtypes = [pg] + [vp] * 8 + [sz, vp]
+        L.dll_gated_bwd.argtypes = [pg] + [vp] * 12 + [sz, vp]
+        L.dll_vocab_loss_fwd.argtypes = [pv] + [vp] * 8 + [sz, vp]
+        L.dll_vocab_loss_grad.argtypes = [pv] + [vp] * 4 + [C.c_float] + [vp] * 7 + [sz, vp]
+        L.dll_grad_norm.argtypes = [pl, vp, vp, vp, sz, vp]
+        L.dll_grad_clip.argtypes = [pl, vp, vp, C.c_float, vp, vp, sz, vp]
+        L.dll_momentum_update_clipped.argtypes = [pl, vp, vp, vp, C.c_float, C.c_float, vp, C.c_float, vp, vp, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -259,3 +290,182 @@ def dll_cnn_train_step_momentum(net: NetHandle, params: List[torch.Tensor], velo
     _ok(lib().dll_cnn_train_step_momentum(C.byref(net.desc), pa, va, ga, _ptr(x), _ptr(labels), C.c_float(lr),
                                           C.c_float(momentum), C.c_float(weight_decay), _ptr(loss), _ptr(logits), ia, _ptr(ws),
                                           0 if ws is None else ws.numel(), _stream(stream)), "dll_cnn_train_step_momentum")
+
+
+# ---------------------------------------------------------------------------------------
+# Large-model operators.  The C calls know addresses only, so what an address must hold (type,
+# shape, device) is checked here.
+# ---------------------------------------------------------------------------------------
+def _tensor(t: Optional[torch.Tensor], shape, dtype: torch.dtype, what: str, device, optional: bool = False):
+    """The address of a tensor that has to have this shape and type and lie on this device."""
+    if t is None:
+        if optional:
+            return None
+        raise ValueError(f"{what}: a tensor is required")
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: {dtype} of shape {tuple(shape)} expected, got {t.dtype} of shape {tuple(t.shape)}")
+    if t.device != device or not t.is_contiguous():
+        raise ValueError(f"{what}: contiguous and on {device} (the device of the call's stream) expected")
+    return t.data_ptr()
+
+
+def _call_stream(stream):
+    s = stream if stream is not None else torch.cuda.current_stream()
+    if s.device != torch.device("cuda", torch.cuda.current_device()):
+        raise ValueError(f"the stream belongs to {s.device}, which is not the current device")
+    return s
+
+
+def _ws(ws: Optional[torch.Tensor], device):
+    if ws is None:
+        return None, 0
+    if ws.device != device or not ws.is_contiguous():
+        raise ValueError(f"ws: contiguous and on {device} expected")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def gated_desc(g: GatedSpec) -> dll_gated_desc:
+    return dll_gated_desc(g.tokens, g.width, g.hidden, GATE[g.gate], DTYPE[g.dtype])
+
+
+def vocab_desc(v: VocabSpec) -> dll_vocab_desc:
+    return dll_vocab_desc(v.tokens, v.width, v.classes, DTYPE[v.dtype])
+
+
+def dll_gated_fwd_workspace_bytes(g: GatedSpec) -> int:
+    return int(lib().dll_gated_fwd_workspace_bytes(C.byref(gated_desc(g))))
+
+
+def dll_gated_fwd(g: GatedSpec, x, w_gate, w_up, w_down, y, gate_pre=None, up_pre=None, ws=None, stream=None) -> None:
+    s = _call_stream(stream)
+    t, dev = _TORCH_TYPE[g.dtype], s.device
+    io, up, kept = (g.tokens, g.width), (g.hidden, g.width), (g.tokens, g.hidden)
+    _ok(lib().dll_gated_fwd(C.byref(gated_desc(g)), _tensor(x, io, t, "x", dev), _tensor(w_gate, up, t, "w_gate", dev),
+                            _tensor(w_up, up, t, "w_up", dev), _tensor(w_down, up[::-1], t, "w_down", dev),
+                            _tensor(y, io, t, "y", dev), _tensor(gate_pre, kept, t, "gate_pre", dev, True),
+                            _tensor(up_pre, kept, t, "up_pre", dev, True), *_ws(ws, dev), s.cuda_stream), "dll_gated_fwd")
+
+
+def dll_gated_bwd_workspace_bytes(g: GatedSpec) -> int:
+    return int(lib().dll_gated_bwd_workspace_bytes(C.byref(gated_desc(g))))
+
+
+def dll_gated_bwd(g: GatedSpec, x, w_gate, w_up, w_down, gate_pre, up_pre, dy, dx=None, dw_gate=None, dw_up=None, dw_down=None,
+                  ws=None, stream=None) -> None:
+    s = _call_stream(stream)
+    t, dev = _TORCH_TYPE[g.dtype], s.device
+    io, up, kept = (g.tokens, g.width), (g.hidden, g.width), (g.tokens, g.hidden)
+    _ok(lib().dll_gated_bwd(C.byref(gated_desc(g)), _tensor(x, io, t, "x", dev), _tensor(w_gate, up, t, "w_gate", dev),
+                            _tensor(w_up, up, t, "w_up", dev), _tensor(w_down, up[::-1], t, "w_down", dev),
+                            _tensor(gate_pre, kept, t, "gate_pre", dev), _tensor(up_pre, kept, t, "up_pre", dev),
+                            _tensor(dy, io, t, "dy", dev), _tensor(dx, io, t, "dx", dev, True),
+                            _tensor(dw_gate, up, t, "dw_gate", dev, True), _tensor(dw_up, up, t, "dw_up", dev, True),
+                            _tensor(dw_down, up[::-1], t, "dw_down", dev, True), *_ws(ws, dev), s.cuda_stream), "dll_gated_bwd")
+
+
+def dll_vocab_loss_fwd_workspace_bytes(v: VocabSpec) -> int:
+    return int(lib().dll_vocab_loss_fwd_workspace_bytes(C.byref(vocab_desc(v))))
+
+
+def _vocab_inputs(v: VocabSpec, x, w, bias, labels, dev):
+    t = _TORCH_TYPE[v.dtype]
+    return (_tensor(x, (v.tokens, v.width), t, "x", dev), _tensor(w, (v.classes, v.width), t, "w", dev),
+            _tensor(bias, (v.classes,), t, "bias", dev, True), _tensor(labels, (v.tokens,), torch.int32, "labels", dev))
+
+
+def _vocab_losses(v: VocabSpec, row_loss, row_lse, loss, dev):
+    f = torch.float32
+    return (_tensor(row_loss, (v.tokens,), f, "row_loss", dev, True), _tensor(row_lse, (v.tokens,), f, "row_lse", dev, True),
+            _tensor(loss, (1,), f, "loss", dev))
+
+
+def dll_vocab_loss_fwd(v: VocabSpec, x, w, bias, labels, row_loss, row_lse, loss, ws=None, stream=None) -> None:
+    s = _call_stream(stream)
+    dev = s.device
+    _ok(lib().dll_vocab_loss_fwd(C.byref(vocab_desc(v)), *_vocab_inputs(v, x, w, bias, labels, dev),
+                                 *_vocab_losses(v, row_loss, row_lse, loss, dev), *_ws(ws, dev), s.cuda_stream), "dll_vocab_loss_fwd")
+
+
+def dll_vocab_loss_grad_workspace_bytes(v: VocabSpec) -> int:
+    return int(lib().dll_vocab_loss_grad_workspace_bytes(C.byref(vocab_desc(v))))
+
+
+def dll_vocab_loss_grad(v: VocabSpec, x, w, bias, labels, scale, row_loss, row_lse, loss, dx=None, dw=None, dbias=None, ws=None,
+                        stream=None) -> None:
+    s = _call_stream(stream)
+    t, dev = _TORCH_TYPE[v.dtype], s.device
+    _ok(lib().dll_vocab_loss_grad(C.byref(vocab_desc(v)), *_vocab_inputs(v, x, w, bias, labels, dev), C.c_float(scale),
+                                  *_vocab_losses(v, row_loss, row_lse, loss, dev),
+                                  _tensor(dx, (v.tokens, v.width), t, "dx", dev, True),
+                                  _tensor(dw, (v.classes, v.width), t, "dw", dev, True),
+                                  _tensor(dbias, (v.classes,), t, "dbias", dev, True), *_ws(ws, dev), s.cuda_stream),
+        "dll_vocab_loss_grad")
+
+
+@dataclass
+class TensorList:
+    """Numbers of elements and types of a list of gradients, kept for the calls on them."""
+    desc: dll_tensor_list
+    counts: object
+    dtypes: object
+    torch_types: List[torch.dtype]
+
+
+def tensor_list(grads: Sequence[torch.Tensor]) -> TensorList:
+    names = {v: k for k, v in _TORCH_TYPE.items()}
+    for g in grads:
+        if g.dtype not in names:
+            raise ValueError(f"gradients are float32 or bfloat16, got {g.dtype}")
+    counts = (C.c_size_t * len(grads))(*[g.numel() for g in grads])
+    dtypes = (C.c_int * len(grads))(*[DTYPE[names[g.dtype]] for g in grads])
+    return TensorList(dll_tensor_list(len(grads), counts, dtypes), counts, dtypes, [g.dtype for g in grads])
+
+
+def _list_ptrs(tensors: Sequence[Optional[torch.Tensor]], l: TensorList, dtypes, what: str, dev, optional: bool = False):
+    """Addresses of one tensor for each entry of the list, of any shape with as many elements."""
+    if len(tensors) != l.desc.n:
+        raise ValueError(f"{what}: {l.desc.n} tensors expected, got {len(tensors)}")
+    for t, n, dtype in zip(tensors, l.counts, dtypes):
+        if t is None:
+            if optional or n == 0:
+                continue
+            raise ValueError(f"{what}: a tensor is required")
+        if t.dtype != dtype or t.numel() != n or t.device != dev or not t.is_contiguous():
+            raise ValueError(f"{what}: contiguous {dtype} with {n} elements on {dev} expected, got {t.dtype} with {t.numel()} on {t.device}")
+    return (C.c_void_p * len(tensors))(*[None if t is None else t.data_ptr() for t in tensors])
+
+
+def dll_grad_norm_workspace_bytes(l: TensorList) -> int:
+    return int(lib().dll_grad_norm_workspace_bytes(C.byref(l.desc)))
+
+
+def dll_grad_norm(l: TensorList, grads, norm, ws=None, stream=None) -> None:
+    s = _call_stream(stream)
+    dev = s.device
+    _ok(lib().dll_grad_norm(C.byref(l.desc), _list_ptrs(grads, l, l.torch_types, "grads", dev),
+                            _tensor(norm, (1,), torch.float32, "norm", dev), *_ws(ws, dev), s.cuda_stream), "dll_grad_norm")
+
+
+def dll_grad_clip(l: TensorList, grads, out, max_norm, norm, ws=None, stream=None) -> None:
+    s = _call_stream(stream)
+    dev = s.device
+    _ok(lib().dll_grad_clip(C.byref(l.desc), _list_ptrs(grads, l, l.torch_types, "grads", dev),
+                            _list_ptrs(out, l, l.torch_types, "out", dev), C.c_float(max_norm),
+                            _tensor(norm, (1,), torch.float32, "norm", dev), *_ws(ws, dev), s.cuda_stream), "dll_grad_clip")
+
+
+def dll_momentum_update_clipped(l: TensorList, params, velocity, grads, lr, momentum, weight_decay, max_norm, norm, copies=None,
+                                ws=None, stream=None) -> None:
+    """weight_decay: one factor a tensor, or None."""
+    s = _call_stream(stream)
+    dev, n = s.device, l.desc.n
+    f = [torch.float32] * n
+    if weight_decay is not None and len(weight_decay) != n:
+        raise ValueError(f"weight_decay: {n} factors expected, got {len(weight_decay)}")
+    _ok(lib().dll_momentum_update_clipped(
+        C.byref(l.desc), _list_ptrs(params, l, f, "params", dev), _list_ptrs(velocity, l, f, "velocity", dev),
+        _list_ptrs(grads, l, l.torch_types, "grads", dev), C.c_float(lr), C.c_float(momentum),
+        None if weight_decay is None else (C.c_float * n)(*weight_decay), C.c_float(max_norm),
+        _tensor(norm, (1,), torch.float32, "norm", dev),
+        None if copies is None else _list_ptrs(copies, l, [torch.bfloat16] * n, "copies", dev, True), *_ws(ws, dev), s.cuda_stream),
+        "dll_momentum_update_clipped")

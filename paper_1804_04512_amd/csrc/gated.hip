@@ -1,0 +1,301 @@
+// Gated feed-forward block, forward and backward:
+//   a = x Wg^T, b = x Wu^T, h = act(a) * b, y = h Wd^T
+//   dh = dy Wd, da = dh * b * act'(a), db = dh * act(a)
+//   dWd = dy^T h, dWg = da^T x, dWu = db^T x, dx = da Wg + db Wu
+// Sums in 32 bits.  With bfloat16 operands h, da and db are rounded to bfloat16 on the way to the next product, as its
+// matrix instructions take nothing wider; a and b are kept for the backward pass in the operands' type.
+#include "large_ops.h"
+#include "tile_product.h"
+
+namespace dllk {
+
+using namespace tile;
+
+namespace {
+
+// act(a) and act'(a)
+__device__ __forceinline__ void gate_both(int gate, float a, float *f, float *d) {
+  switch (gate) {
+    case GATE_SIGMOID: {
+      const float s = 1.0f / (1.0f + expf(-a));
+      *f = s;
+      *d = s * (1.0f - s);
+      return;
+    }
+    case GATE_RELU:
+      *f = a > 0.0f ? a : 0.0f;
+      *d = a > 0.0f ? 1.0f : 0.0f;
+      return;
+    case GATE_SILU: {
+      const float s = 1.0f / (1.0f + expf(-a));
+      *f = a * s;
+      *d = s * (1.0f + a * (1.0f - s));
+      return;
+    }
+    case GATE_GELU: {
+      const float c = 0.5f * (1.0f + erff(a * 0.70710678118654752f));
+      *f = a * c;
+      *d = c + a * expf(-0.5f * a * a) * 0.39894228040143268f;
+      return;
+    }
+    default:
+      *f = a;
+      *d = 1.0f;
+  }
+}
+__device__ __forceinline__ float gate_value(int gate, float a) {
+  float f, d;
+  gate_both(gate, a, &f, &d);
+  return f;
+}
+
+// h = act(a) * b from a piece whose columns 0..31 are a and 32..63 are b of the same hidden units; h in padded rows
+template <class T>
+struct GateEpi {
+  int gate, vec, vec_kept;
+  T *h;
+  long ldh;
+  T *kept_a, *kept_b;   // nullable, [T][H]
+  __device__ __forceinline__ void piece(const float *stage, int m, int n, int M, int H, int, int) const {
+    const int lane = threadIdx.x & 63, col = 8 * (lane & 3);
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const int row = 16 * p + (lane >> 2);
+      if (m + row >= M || n + col >= H) continue;
+      float va[8], vb[8], vh[8];
+      stage8(stage, row, col, va);
+      stage8(stage, row, 32 + col, vb);
+      const int left = H - n - col;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) vh[j] = j < left ? gate_value(gate, va[j]) * vb[j] : 0.0f;
+      store8<T>(h + (long)(m + row) * ldh + n + col, vh, true, 8);
+      if (kept_a) {
+        const long o = (long)(m + row) * H + n + col;
+        store8<T>(kept_a + o, va, vec_kept && left >= 8, left);
+        store8<T>(kept_b + o, vb, vec_kept && left >= 8, left);
+      }
+    }
+  }
+};
+
+// da, db and h from dh and the kept a and b, all three in padded rows
+template <class T>
+struct GateBackEpi {
+  int gate, vec_kept;
+  const T *a, *b;
+  T *da, *db, *h;
+  long ld;
+  __device__ __forceinline__ void piece(const float *stage, int m, int n, int M, int H, int, int) const {
+    const int lane = threadIdx.x & 63, col = 8 * (lane & 7);
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const int row = 8 * p + (lane >> 3);
+      if (m + row >= M || n + col >= H) continue;
+      const int left = H - n - col;
+      const bool whole = vec_kept && left >= 8;
+      float g[8], va[8], vb[8], oa[8], ob[8], oh[8];
+      stage8(stage, row, col, g);
+      load8<T>(a + (long)(m + row) * H + n + col, va, whole, left);
+      load8<T>(b + (long)(m + row) * H + n + col, vb, whole, left);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        float f, d;
+        gate_both(gate, va[j], &f, &d);
+        oa[j] = j < left ? g[j] * vb[j] * d : 0.0f;
+        ob[j] = j < left ? g[j] * f : 0.0f;
+        oh[j] = j < left ? f * vb[j] : 0.0f;
+      }
+      const long o = (long)(m + row) * ld + n + col;
+      store8<T>(da + o, oa, true, 8);
+      store8<T>(db + o, ob, true, 8);
+      store8<T>(h + o, oh, true, 8);
+    }
+  }
+};
+
+template <class T>
+__global__ __launch_bounds__(256) void pad_rows_kernel(const T *src, T *dst, long rows, long cols, long ld) {
+  const long groups = ld / 8, n = rows * groups;
+  for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) {
+    const long r = i / groups, c = (i - r * groups) * 8;
+    const int left = (int)(cols - c < 8 ? cols - c : 8);
+    float v[8];
+    load8<T>(src + r * cols + c, v, false, left);
+    store8<T>(dst + r * ld + c, v, true, 8);
+  }
+}
+
+// The workspace's parts, the same walk for the query and the call
+struct FwdPlan {
+  long ldh, ldd;
+  void *h, *x, *wg, *wu, *wd;
+  float *part;
+  int splits_y;
+  size_t bytes;
+  FwdPlan(int T, int D, int H, int dtype, char *base) {
+    Take take{base};
+    const size_t e = type_bytes(dtype);
+    ldh = padded(H);
+    ldd = padded(D);
+    h = take((size_t)T * ldh * e);
+    x = wg = wu = wd = nullptr;
+    if (!whole_groups(D, dtype)) x = take((size_t)T * ldd * e), wg = take((size_t)H * ldd * e), wu = take((size_t)H * ldd * e);
+    if (!whole_groups(H, dtype)) wd = take((size_t)D * ldh * e);
+    const long tiles = (long)((T + 127) / 128) * ((D + 127) / 128);
+    splits_y = pick_splits(tiles, (ldh * (long)e + kSlabBytes - 1) / kSlabBytes);
+    part = splits_y > 1 ? (float *)take((size_t)splits_y * T * padded(D) * sizeof(float)) : nullptr;
+    bytes = take.used;
+  }
+};
+
+struct BwdPlan {
+  long ldh, ldd;
+  void *da, *db, *h, *x, *wg, *wu, *wd, *dy;
+  float *part;
+  int splits_dx;
+  size_t bytes;
+  BwdPlan(int T, int D, int H, int dtype, char *base) {
+    Take take{base};
+    const size_t e = type_bytes(dtype);
+    ldh = padded(H);
+    ldd = padded(D);
+    da = take((size_t)T * ldh * e);
+    db = take((size_t)T * ldh * e);
+    h = take((size_t)T * ldh * e);
+    x = wg = wu = wd = dy = nullptr;
+    if (!whole_groups(D, dtype)) x = take((size_t)T * ldd * e), dy = take((size_t)T * ldd * e), wg = take((size_t)H * ldd * e), wu = take((size_t)H * ldd * e);
+    if (!whole_groups(H, dtype)) wd = take((size_t)D * ldh * e);
+    const long tiles = (long)((T + 127) / 128) * ((D + 127) / 128);
+    splits_dx = pick_splits(tiles, 2 * ((ldh * (long)e + kSlabBytes - 1) / kSlabBytes));
+    part = splits_dx > 1 ? (float *)take((size_t)splits_dx * T * padded(D) * sizeof(float)) : nullptr;
+    bytes = take.used;
+  }
+};
+
+template <class T>
+hipError_t gated_fwd(const GatedArgs &a, char *scratch, hipStream_t stream) {
+  const FwdPlan p(a.T, a.D, a.H, a.dtype, scratch);
+  const void *x = a.x, *wg = a.w_gate, *wu = a.w_up, *wd = a.w_down;
+  if (p.x) {
+    DLL_TRY(launch_pad_rows(x, p.x, a.T, a.D, a.dtype, stream));
+    DLL_TRY(launch_pad_rows(wg, p.wg, a.H, a.D, a.dtype, stream));
+    DLL_TRY(launch_pad_rows(wu, p.wu, a.H, a.D, a.dtype, stream));
+    x = p.x, wg = p.wg, wu = p.wu;
+  }
+  if (p.wd) {
+    DLL_TRY(launch_pad_rows(wd, p.wd, a.D, a.H, a.dtype, stream));
+    wd = p.wd;
+  }
+  const long ldx = p.x ? p.ldd : a.D, ldd = p.wd ? p.ldh : a.H;
+  ProductArgs g;
+  g.M = a.T;
+  g.N = a.H;
+  g.A[0] = {x, ldx};
+  g.B[0] = {wg, ldx};
+  g.B[1] = {wu, ldx};
+  g.K[0] = (int)ldx;
+  GateEpi<T> ge{a.gate, 1, rows16<T>(a.gate_pre, a.H) && rows16<T>(a.up_pre, a.H), (T *)p.h, p.ldh, (T *)a.gate_pre, (T *)a.up_pre};
+  const long large = (long)((a.T + 255) / 256) * ((a.H + 127) / 128);
+  DLL_TRY((launch_product<T, true, true, true>(g, ge, large >= chip().cus * 3 / 4, stream)));
+  ProductArgs y;
+  y.M = a.T;
+  y.N = a.D;
+  y.A[0] = {p.h, p.ldh};
+  y.B[0] = {wd, ldd};
+  y.K[0] = (int)ldd;
+  StoreEpi<T> out{{(T *)a.y, nullptr}, a.D, rows16<T>(a.y, a.D), nullptr, 0};
+  return product_to<T, true, true>(y, out, p.splits_y, p.part, stream);
+}
+
+template <class T>
+hipError_t gated_bwd(const GatedArgs &a, char *scratch, hipStream_t stream) {
+  const BwdPlan p(a.T, a.D, a.H, a.dtype, scratch);
+  const void *x = a.x, *wg = a.w_gate, *wu = a.w_up, *wd = a.w_down, *dy = a.dy;
+  if (p.x) {
+    DLL_TRY(launch_pad_rows(dy, p.dy, a.T, a.D, a.dtype, stream));
+    dy = p.dy;
+    if (a.dw_gate || a.dw_up) DLL_TRY(launch_pad_rows(x, p.x, a.T, a.D, a.dtype, stream));
+    x = p.x;
+    if (a.dx) {
+      DLL_TRY(launch_pad_rows(wg, p.wg, a.H, a.D, a.dtype, stream));
+      DLL_TRY(launch_pad_rows(wu, p.wu, a.H, a.D, a.dtype, stream));
+      wg = p.wg, wu = p.wu;
+    }
+  }
+  if (p.wd) {
+    DLL_TRY(launch_pad_rows(wd, p.wd, a.D, a.H, a.dtype, stream));
+    wd = p.wd;
+  }
+  const long ldx = p.x ? p.ldd : a.D, ldd = p.wd ? p.ldh : a.H;
+  // dh = dy Wd, leaving as da, db and h
+  ProductArgs g;
+  g.M = a.T;
+  g.N = a.H;
+  g.A[0] = {dy, ldx};
+  g.B[0] = {wd, ldd};
+  g.K[0] = a.D;   // Wd lies across k; where D is no multiple of a 16-byte group, dy's copy has zeros behind it
+  GateBackEpi<T> ge{a.gate, rows16<T>(a.gate_pre, a.H) && rows16<T>(a.up_pre, a.H), (const T *)a.gate_pre, (const T *)a.up_pre,
+                    (T *)p.da, (T *)p.db, (T *)p.h, p.ldh};
+  const long large = (long)((a.T + 255) / 256) * ((a.H + 255) / 256);
+  DLL_TRY((launch_product<T, true, false, false>(g, ge, large >= chip().cus * 3 / 4, stream)));
+  if (a.dw_down) {
+    ProductArgs w;
+    w.M = a.D;
+    w.N = a.H;
+    w.A[0] = {dy, ldx};
+    w.B[0] = {p.h, p.ldh};
+    w.K[0] = a.T;
+    StoreEpi<T> out{{(T *)a.dw_down, nullptr}, a.H, rows16<T>(a.dw_down, a.H), nullptr, 0};
+    DLL_TRY((product_to<T, false, false>(w, out, 1, nullptr, stream)));
+  }
+  if (a.dw_gate || a.dw_up) {
+    ProductArgs w;
+    w.M = a.H;
+    w.N = a.D;
+    w.problems = a.dw_gate && a.dw_up ? 2 : 1;
+    const int first = a.dw_gate ? 0 : 1;
+    const void *d[2] = {p.da, p.db};
+    T *o[2] = {(T *)a.dw_gate, (T *)a.dw_up};
+    w.A[0] = {d[first], p.ldh};
+    w.A[1] = {d[1], p.ldh};
+    w.B[0] = w.B[1] = {x, ldx};
+    w.K[0] = a.T;
+    StoreEpi<T> out{{o[first], o[1]}, a.D, rows16<T>(o[first], a.D) && rows16<T>(o[w.problems - 1], a.D), nullptr, 0};
+    DLL_TRY((product_to<T, false, false>(w, out, 1, nullptr, stream)));
+  }
+  if (a.dx) {
+    ProductArgs w;
+    w.M = a.T;
+    w.N = a.D;
+    w.A[0] = {p.da, p.ldh};
+    w.A[1] = {p.db, p.ldh};
+    w.B[0] = {wg, ldx};
+    w.B[1] = {wu, ldx};
+    w.K[0] = w.K[1] = a.H;
+    StoreEpi<T> out{{(T *)a.dx, nullptr}, a.D, rows16<T>(a.dx, a.D), nullptr, 0};
+    DLL_TRY((product_to<T, true, false>(w, out, p.splits_dx, p.part, stream)));
+  }
+  return hipSuccess;
+}
+
+}  // namespace
+
+hipError_t launch_pad_rows(const void *src, void *dst, long rows, long cols, int dtype, hipStream_t stream) {
+  const long ld = padded(cols), blocks = (rows * (ld / 8) + 255) / 256;
+  const dim3 grid((unsigned)(blocks < 8192 ? blocks : 8192));
+  if (dtype == TYPE_BF16) pad_rows_kernel<bf16><<<grid, dim3(256), 0, stream>>>((const bf16 *)src, (bf16 *)dst, rows, cols, ld);
+  else pad_rows_kernel<float><<<grid, dim3(256), 0, stream>>>((const float *)src, (float *)dst, rows, cols, ld);
+  return hipGetLastError();
+}
+
+size_t gated_fwd_scratch(int T, int D, int H, int dtype) { return FwdPlan(T, D, H, dtype, nullptr).bytes; }
+size_t gated_bwd_scratch(int T, int D, int H, int dtype) { return BwdPlan(T, D, H, dtype, nullptr).bytes; }
+
+hipError_t launch_gated_fwd(const GatedArgs &a, char *scratch, hipStream_t stream) {
+  return a.dtype == TYPE_BF16 ? gated_fwd<bf16>(a, scratch, stream) : gated_fwd<float>(a, scratch, stream);
+}
+hipError_t launch_gated_bwd(const GatedArgs &a, char *scratch, hipStream_t stream) {
+  return a.dtype == TYPE_BF16 ? gated_bwd<bf16>(a, scratch, stream) : gated_bwd<float>(a, scratch, stream);
+}
+
+}  // namespace dllk

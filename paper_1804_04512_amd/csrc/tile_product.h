@@ -1,0 +1,501 @@
+// Matrix products of the large-model operators on MFMA, gfx950: operands in bfloat16 or single precision, sums in 32 bits.
+//
+//   C(m, n) = sum_k A(m, k) * B(n, k)
+//
+// Each operand lies either along k ("KC": element (x, k) at p[x * ld + k]) or across it ("KS": p[k * ld + x]), so the three
+// forms of a layer's products (forward KC KC, data gradient KC KS, weight gradient KS KS) need no transposed copies.
+//
+// A workgroup owns a BM x BN tile of C and walks k in slabs of 128 bytes a row (64 bf16, 32 fp32).  Slabs go from global
+// memory straight into LDS (16 bytes a lane, no registers in between), the next one on its way while the current one is
+// multiplied.  Every access is range checked by the buffer descriptor: rows behind the end read as zeros, and columns
+// behind K are sent out of range where the last slab is not whole, so no operand needs padding to the tile.
+//
+// LDS layouts.  The hardware writes a wavefront's 64 x 16 bytes in lane order, so a swizzle is made by permuting which
+// global bytes a lane fetches.  KC: rows of 128 bytes, 16-byte group c of row r at place c ^ (r & 7); a fragment read
+// (32 rows, one group each) touches every bank the same number of times.  KS bf16: rows of X columns, 64-byte block b of
+// row k at place b ^ g(k) with g from bits 0, 1 and 3 of k; the transposing read ds_read_b64_tr_b16 turns four rows of
+// sixteen columns into four k's a lane.  KS fp32: four 4-byte reads a fragment.
+//
+// MFMA: 32x32x16 bf16, and for fp32 32x32x2 with the four floats of a 16-byte group as four steps (the order of k within a
+// slab is the same permutation for both operands).  B rides on the first operand, so a lane holds one row m of C and runs
+// of four neighbouring n.  The epilogue passes 32 x 64 pieces of C through LDS, one wavefront at a time, so that outputs
+// leave as whole rows of 64 columns.
+#pragma once
+
+#include "large_ops.h"
+
+namespace dllk {
+namespace tile {
+
+typedef __bf16 bf16;
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
+typedef short shortx4 __attribute__((ext_vector_type(4)));
+typedef short shortx8 __attribute__((ext_vector_type(8)));
+
+constexpr int kSlabBytes = 128;              // of one row along k
+constexpr unsigned kOutOfRange = 0xFFFFFFF0u;
+constexpr int kStageLd = 68;                 // floats: row stride of an epilogue piece (64 columns)
+
+template <class T> struct Elem;
+template <> struct Elem<bf16> { static constexpr int kSlab = 64; typedef bf16x8 Frag; };
+template <> struct Elem<float> { static constexpr int kSlab = 32; typedef floatx4 Frag; };
+
+struct Operand {
+  const void *p = nullptr;
+  long ld = 0;   // elements; rows start at multiples of 16 bytes
+};
+
+struct ProductArgs {
+  int M = 0, N = 0;
+  // segment 0 and, where K[1] > 0, a second pair of operands whose products are added to the first's;
+  // or two products of one shape side by side (problems == 2), each with its own operands and outputs
+  Operand A[2], B[2];
+  int K[2] = {0, 0};          // KC operands: multiples of a 16-byte group (padded with zeros by whoever wrote them)
+  int problems = 1;
+  // Rows that exist as the device counts them: M (m_rows) and K[0] (k_rows) become what *p leaves behind `first`.
+  const int *m_rows = nullptr, *k_rows = nullptr;
+  int first = 0;
+  int slabs_per_split = 1 << 30;
+  int tiles_m = 0, tiles_n = 0, splits = 1;
+};
+
+__device__ __forceinline__ int rows_left(const int *rows, int first, int most) {
+  return rows ? max(0, min(most, *rows - first)) : most;
+}
+
+// Workgroups are dealt to the 8 XCDs in turn; each XCD gets a contiguous run of tiles, eight tile rows high, so that the 32
+// tiles it works on at a time share their operands in its L2.
+__device__ __forceinline__ void tile_of(int id, int tiles_m, int tiles_n, int *tm, int *tn) {
+  const int n = tiles_m * tiles_n, q = n >> 3, r = n & 7, xcd = id & 7, i = id >> 3;
+  const int t = xcd * q + min(xcd, r) + i;
+  constexpr int kRows = 8;
+  const int group = t / (kRows * tiles_n), first = group * kRows, rows = min(kRows, tiles_m - first), at = t - group * kRows * tiles_n;
+  *tm = first + at % rows;
+  *tn = at / rows;
+}
+
+// ------------------------------------------------------------------------------------------------ loading
+// A raw buffer's descriptor: 48-bit address, extent in bytes; what lies outside reads as zeros.
+__device__ __forceinline__ uintx4 buffer_of(const char *p, unsigned bytes) {
+  const uint64_t at = (uint64_t)p;
+  return uintx4{(unsigned)__builtin_amdgcn_readfirstlane((int)at), (unsigned)__builtin_amdgcn_readfirstlane((int)(at >> 32) & 0xFFFF),
+                (unsigned)__builtin_amdgcn_readfirstlane((int)bytes), 0x00020000u};
+}
+// 16 bytes a lane from the buffer to 1024 bytes of LDS in lane order.  Written out because the compiler, which sees that the
+// builtin writes LDS, waits for it before any transposing LDS read, of the other slab too.  It has no output register, and
+// the caller waits for it (vmcnt) before the barrier behind which the slab is read.
+__device__ __forceinline__ void load_to_lds(const uintx4 &rs, unsigned off, unsigned lds) {
+  const unsigned at = (unsigned)__builtin_amdgcn_readfirstlane((int)lds);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(off), "s"(rs) : "memory");   // m0 is never the compiler's to keep
+}
+// One operand's slab of X rows (KC) or X columns (KS).
+template <class T, int X, bool KC, int THREADS>
+struct Slab {
+  static constexpr int kK = Elem<T>::kSlab;
+  static constexpr int kBytes = X * kSlabBytes;
+  static constexpr int kIts = kBytes / (16 * THREADS);
+  static constexpr int kRowGroups = KC ? 8 : X * (int)sizeof(T) / 16;   // 16-byte groups of a row in LDS
+  static_assert(kBytes % (16 * THREADS) == 0 && (THREADS / kRowGroups) * kRowGroups == THREADS, "whole rows a step");
+  static constexpr int kStep = THREADS / kRowGroups;                     // rows between a thread's loads
+  static_assert(KC ? kStep % 8 == 0 : (sizeof(T) == 4 || kStep % 4 == 0), "the swizzle does not change between them");
+
+  // the swizzle of a KS bf16 row: which of its 64-byte blocks change places
+  static __device__ __forceinline__ int mix(int k) { return (k & 3) | (X >= 256 ? ((k >> 3) & 1) << 2 : 0); }
+
+  unsigned off[kIts];   // bytes from the slab's first element
+  int along;            // KC: this thread's first k inside the slab
+
+  __device__ __forceinline__ void init(long ld) {
+    const int t = threadIdx.x, place = t % kRowGroups, row0 = t / kRowGroups;
+#pragma unroll
+    for (int it = 0; it < kIts; ++it) {
+      const int row = row0 + it * kStep;
+      int group = place;
+      if (KC) group = place ^ (row & 7);
+      else if (sizeof(T) == 2) group = (((place >> 2) ^ mix(row)) << 2) | (place & 3);
+      off[it] = (unsigned)((long)row * ld * (int)sizeof(T)) + 16u * group;
+      if (it == 0) along = KC ? group * (16 / (int)sizeof(T)) : 0;
+    }
+  }
+  // x0: the tile's first row (KC) or column (KS); k0: the slab's first k; X_, K: extents of the operand
+  __device__ __forceinline__ void load(unsigned lds, const Operand &o, int x0, int X_, int k0, int K) const {
+    const long first = KC ? (long)x0 * o.ld + k0 : (long)k0 * o.ld + x0;
+    const long end = KC ? (long)X_ * o.ld : (long)K * o.ld;
+    long bytes = (end - first) * (long)sizeof(T);
+    bytes = bytes < 0 ? 0 : (bytes > 0xFFFFFF00L ? 0xFFFFFF00L : bytes);
+    const uintx4 rs = buffer_of((const char *)o.p + first * (long)sizeof(T), (unsigned)bytes);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool cut = KC && k0 + kK > K;   // uniform: only a last slab
+    const bool out = cut && k0 + along >= K;
+#pragma unroll
+    for (int it = 0; it < kIts; ++it) load_to_lds(rs, out ? kOutOfRange : off[it], lds + (it * THREADS + wave * 64) * 16);
+  }
+};
+
+// A gate's and an up projection's rows side by side: rows 64 w + 0..31 of the tile are gate rows 32 w + .., the next 32 the
+// same rows of the up projection, so that a wavefront's 64 columns hold both factors of 32 hidden units.
+template <class T, int X, int THREADS>
+struct PairSlab {
+  typedef Slab<T, X, true, THREADS> Base;
+  static constexpr int kBytes = Base::kBytes, kIts = Base::kIts;
+  static_assert(Base::kStep % 32 == 0 || 32 % Base::kStep == 0, "a wavefront's rows lie in one projection");
+  unsigned off[kIts];
+  int along;
+  __device__ __forceinline__ void init(long ld) {
+    const int t = threadIdx.x, place = t & 7, row0 = t >> 3;
+#pragma unroll
+    for (int it = 0; it < kIts; ++it) {
+      const int row = row0 + it * Base::kStep, group = place ^ (row & 7);
+      off[it] = (unsigned)((long)((row >> 6) * 32 + (row & 31)) * ld * (int)sizeof(T)) + 16u * group;
+      if (it == 0) along = group * (16 / (int)sizeof(T));
+    }
+  }
+  // x0: the tile's first hidden unit; H: hidden units
+  __device__ __forceinline__ void load(unsigned lds, const Operand &gate, const Operand &up, int x0, int H, int k0, int K) const {
+    const long first = (long)x0 * gate.ld + k0;
+    long bytes = ((long)H * gate.ld - first) * (long)sizeof(T);
+    bytes = bytes < 0 ? 0 : (bytes > 0xFFFFFF00L ? 0xFFFFFF00L : bytes);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool out = k0 + Base::kK > K && k0 + along >= K;
+#pragma unroll
+    for (int it = 0; it < kIts; ++it) {
+      const bool second = ((wave * 8 + it * Base::kStep) >> 5) & 1;
+      const uintx4 rs = buffer_of((const char *)(second ? up.p : gate.p) + first * (long)sizeof(T), (unsigned)bytes);
+      load_to_lds(rs, out ? kOutOfRange : off[it], lds + (it * THREADS + wave * 64) * 16);
+    }
+  }
+};
+
+// ------------------------------------------------------------------------------------------------ fragments
+// Lane l's part of a 32-row fragment at step s (of 4 a slab): row x0 + l % 32, 16-byte group 2 s + l / 32 along k.
+template <class T, int X, bool KC>
+struct FragReader;
+template <class T, int X>
+struct FragReader<T, X, true> {
+  int row, half, low;
+  __device__ __forceinline__ explicit FragReader(int lane) : row((lane & 31) * kSlabBytes), half(lane >> 5), low(lane & 7) {}
+  __device__ __forceinline__ typename Elem<T>::Frag operator()(const char *lds, int x0, int s) const {
+    return *reinterpret_cast<const typename Elem<T>::Frag *>(lds + x0 * kSlabBytes + row + (((2 * s + half) ^ low) << 4));
+  }
+};
+template <int X>
+struct FragReader<bf16, X, false> {
+  int base, g;
+  __device__ __forceinline__ explicit FragReader(int lane) {
+    const int i = lane & 15, k = 8 * (lane >> 5) + (i >> 2);
+    base = k * X * 2 + (((lane >> 4) & 1) * 16 + 4 * (i & 3)) * 2;
+    g = Slab<bf16, X, false, 256>::mix(k);
+  }
+  __device__ __forceinline__ bf16x8 operator()(const char *lds, int x0, int s) const {
+    typedef __attribute__((address_space(3))) shortx4 *Lp;
+    const char *p = lds + base + s * 16 * X * 2 + (((x0 >> 5) ^ g) << 6);
+    const shortx4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lp)(p)), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lp)(p + 4 * X * 2));
+    const shortx8 v = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    return __builtin_bit_cast(bf16x8, v);
+  }
+};
+template <int X>
+struct FragReader<float, X, false> {
+  int base;
+  __device__ __forceinline__ explicit FragReader(int lane) : base((4 * (lane >> 5) * X + (lane & 31)) * 4) {}
+  __device__ __forceinline__ floatx4 operator()(const char *lds, int x0, int s) const {
+    const float *p = reinterpret_cast<const float *>(lds + base) + s * 8 * X + x0;
+    return floatx4{p[0], p[X], p[2 * X], p[3 * X]};
+  }
+};
+
+__device__ __forceinline__ floatx16 mfma(bf16x8 b, bf16x8 a, floatx16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(b, a, c, 0, 0, 0); }
+__device__ __forceinline__ floatx16 mfma(floatx4 b, floatx4 a, floatx16 c) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(b[j], a[j], c, 0, 0, 0);
+  return c;
+}
+
+// ------------------------------------------------------------------------------------------------ kernel
+// WM x WN wavefronts of (BM / WM) x 64 each.  Epi: `piece(stage, m, n, M, N, problem, split)` takes 32 x 64 sums from the
+// wavefront's LDS area (row stride kStageLd floats), first element C(m, n).
+// PAIR: B[0] and B[1] are the gate and up projections (KC), N counts hidden units, a tile covers BN / 2 of them.
+template <class T, int BM, int BN, int WM, int WN, bool AKC, bool BKC, bool PAIR, class Epi>
+__global__ __launch_bounds__(64 * WM *WN, 2) void product_kernel(const ProductArgs a, const Epi epi) {
+  constexpr int kThreads = 64 * WM * WN, TM = BM / WM / 32, kK = Elem<T>::kSlab;
+  static_assert(BN / WN == 64 && BM % (32 * WM) == 0, "wavefront tiles are 64 columns wide");
+  typedef Slab<T, BM, AKC, kThreads> SA;
+  typedef Slab<T, BN, BKC, kThreads> SB;
+  constexpr int kA = SA::kBytes, kStage = SA::kBytes + SB::kBytes;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * 64;
+  int tm, tn;
+  tile_of(blockIdx.x, a.tiles_m, a.tiles_n, &tm, &tn);
+  const int problem = a.problems > 1 ? blockIdx.z : 0;
+  const int M = rows_left(a.m_rows, a.first, a.M);
+  const int K0 = rows_left(a.k_rows, a.first, a.K[0]);
+  const int m0 = tm * BM, n0 = tn * (PAIR ? BN / 2 : BN);
+  if (m0 >= M) return;
+  const int slabs0 = (K0 + kK - 1) / kK, slabs = slabs0 + (a.K[1] + kK - 1) / kK;
+  const int t0 = min(slabs, (int)blockIdx.y * a.slabs_per_split), t1 = min(slabs, t0 + a.slabs_per_split);
+
+  SA sa;
+  SB sb;
+  PairSlab<T, BN, kThreads> sp;
+  sa.init(a.A[0].ld);
+  if (PAIR) sp.init(a.B[0].ld);
+  else sb.init(a.B[0].ld);
+  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
+  const auto load = [&](int t, unsigned lds) {
+    const bool second = t >= slabs0;
+    const int k0 = (second ? t - slabs0 : t) * kK, K = second ? a.K[1] : K0, which = second ? 1 : problem;
+    sa.load(lds, a.A[which], m0, M, k0, K);
+    if (PAIR) sp.load(lds + kA, a.B[0], a.B[1], n0, a.N, k0, K);
+    else sb.load(lds + kA, a.B[which], n0, a.N, k0, K);
+  };
+
+  floatx16 acc[TM][2];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) acc[i][j] = floatx16{};
+  const FragReader<T, BM, AKC> ra(lane);
+  const FragReader<T, BN, BKC> rb(lane);
+  if (t0 < t1) load(t0, lds0);
+  for (int t = t0; t < t1; ++t) {
+    const char *now = smem + ((t - t0) & 1) * kStage;
+    // this wavefront's loads of slab t have landed, then everyone's; all have also left slab t - 1, whose place t + 1 takes
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (t + 1 < t1) load(t + 1, lds0 + ((t - t0 + 1) & 1) * kStage);
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      typename Elem<T>::Frag fa[TM], fb[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) fb[j] = rb(now + kA, wn + 32 * j, s);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) fa[i] = ra(now, wm + 32 * i, s);
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[i][j] = mfma(fb[j], fa[i], acc[i][j]);
+    }
+  }
+  __syncthreads();   // the slabs' place becomes the epilogue's
+  float *stage = reinterpret_cast<float *>(smem) + wave * 32 * kStageLd;
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        *reinterpret_cast<floatx4 *>(stage + (lane & 31) * kStageLd + 32 * j + 8 * r + 4 * (lane >> 5)) =
+            floatx4{acc[i][j][4 * r], acc[i][j][4 * r + 1], acc[i][j][4 * r + 2], acc[i][j][4 * r + 3]};
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (m0 + wm + 32 * i < M) epi.piece(stage, m0 + wm + 32 * i, PAIR ? n0 + wn / 2 : n0 + wn, M, a.N, problem, (int)blockIdx.y);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ outputs
+__device__ __forceinline__ float to_float(bf16 v) { return (float)v; }
+__device__ __forceinline__ float to_float(float v) { return v; }
+
+// eight neighbours of a row; `whole`: 16-byte aligned and all eight exist
+template <class T> __device__ __forceinline__ void store8(T *p, const float (&v)[8], bool whole, int n);
+template <> __device__ __forceinline__ void store8<bf16>(bf16 *p, const float (&v)[8], bool whole, int n) {
+  if (whole) {
+    bf16x8 o;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = (bf16)v[j];   // to nearest, ties to even
+    *reinterpret_cast<bf16x8 *>(p) = o;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < n) p[j] = (bf16)v[j];
+  }
+}
+template <> __device__ __forceinline__ void store8<float>(float *p, const float (&v)[8], bool whole, int n) {
+  if (whole) {
+    reinterpret_cast<floatx4 *>(p)[0] = floatx4{v[0], v[1], v[2], v[3]};
+    reinterpret_cast<floatx4 *>(p)[1] = floatx4{v[4], v[5], v[6], v[7]};
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < n) p[j] = v[j];
+  }
+}
+template <class T> __device__ __forceinline__ void load8(const T *p, float (&v)[8], bool whole, int n);
+template <> __device__ __forceinline__ void load8<bf16>(const bf16 *p, float (&v)[8], bool whole, int n) {
+  if (whole) {
+    const bf16x8 o = *reinterpret_cast<const bf16x8 *>(p);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (float)o[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < n ? (float)p[j] : 0.f;
+  }
+}
+template <> __device__ __forceinline__ void load8<float>(const float *p, float (&v)[8], bool whole, int n) {
+  if (whole) {
+    const floatx4 a = reinterpret_cast<const floatx4 *>(p)[0], b = reinterpret_cast<const floatx4 *>(p)[1];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = a[j], v[4 + j] = b[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < n ? p[j] : 0.f;
+  }
+}
+__device__ __forceinline__ void stage8(const float *stage, int row, int col, float (&v)[8]) {
+  const floatx4 a = *reinterpret_cast<const floatx4 *>(stage + row * kStageLd + col), b = *reinterpret_cast<const floatx4 *>(stage + row * kStageLd + col + 4);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = a[j], v[4 + j] = b[j];
+}
+// rows of ld elements may be accessed 16 bytes at a time
+template <class T> __host__ __device__ __forceinline__ bool rows16(const void *p, long ld) {
+  return ((uintptr_t)p & 15) == 0 && ld * (long)sizeof(T) % 16 == 0;
+}
+
+// C[problem][m][n] in T, rows optionally through a map; or += to what a former piece left (fp32 sums)
+template <class T>
+struct StoreEpi {
+  T *c[2];
+  long ld;
+  int vec;                 // rows16 of both
+  const int *rows;         // nullable: row m of the product goes to row rows[m]
+  int add;                 // T = float only: add to what is there
+  __device__ __forceinline__ void piece(const float *stage, int m, int n, int M, int N, int problem, int) const {
+    const int lane = threadIdx.x & 63, col = 8 * (lane & 7);
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const int row = 8 * p + (lane >> 3);
+      if (m + row >= M || n + col >= N) continue;
+      float v[8];
+      stage8(stage, row, col, v);
+      T *d = c[problem] + (long)(rows ? rows[m + row] : m + row) * ld + n + col;
+      const int left = N - n - col;
+      const bool whole = vec && left >= 8;
+      if (add) {
+        float o[8];
+        load8<T>(d, o, whole, left);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += o[j];
+      }
+      store8<T>(d, v, whole, left);
+    }
+  }
+};
+
+// Sums of one split of k in fp32, [split][M][N8], N8 = N rounded up to 8
+struct PartialEpi {
+  float *part;
+  long rows;   // of a split (the M of the launch)
+  __device__ __forceinline__ void piece(const float *stage, int m, int n, int M, int N, int, int split) const {
+    const int lane = threadIdx.x & 63, col = 8 * (lane & 7);
+    const long n8 = (N + 7) & ~7;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const int row = 8 * p + (lane >> 3);
+      if (m + row >= M || n + col >= N) continue;
+      float v[8];
+      stage8(stage, row, col, v);
+      store8<float>(part + ((long)split * rows + m + row) * n8 + n + col, v, true, 8);
+    }
+  }
+};
+
+// The splits added up in order, as a StoreEpi of one problem would have stored them
+template <class T>
+__global__ __launch_bounds__(256) void sum_splits_kernel(const float *part, int splits, int M, int N, const int *m_rows, int first, StoreEpi<T> out) {
+  const long n8 = (N + 7) & ~7;
+  const int rows = rows_left(m_rows, first, M), g = (int)(n8 >> 3);
+  for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < (long)rows * g; i += (long)gridDim.x * 256) {
+    const int m = (int)(i / g), n = (int)(i % g) * 8;
+    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) {
+      float o[8];
+      load8<float>(part + ((long)s * M + m) * n8 + n, o, true, 8);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += o[j];
+    }
+    T *d = out.c[0] + (long)(out.rows ? out.rows[m] : m) * out.ld + n;
+    const int left = N - n;
+    const bool whole = out.vec && left >= 8;
+    if (out.add) {
+      float o[8];
+      load8<T>(d, o, whole, left);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += o[j];
+    }
+    store8<T>(d, v, whole, left);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ host
+template <class T, int BM, int BN, int WM, int WN, bool AKC, bool BKC, bool PAIR, class Epi>
+hipError_t launch_shape(ProductArgs a, const Epi &epi, hipStream_t stream) {
+  constexpr int kThreads = 64 * WM * WN;
+  constexpr size_t slabs = 2 * (size_t)(BM + BN) * kSlabBytes, stage = (size_t)WM * WN * 32 * kStageLd * sizeof(float);
+  constexpr size_t lds = slabs > stage ? slabs : stage;
+  const auto kernel = product_kernel<T, BM, BN, WM, WN, AKC, BKC, PAIR, Epi>;
+  hipError_t e = allow_large_lds(reinterpret_cast<const void *>(kernel), lds);
+  if (e != hipSuccess) return e;
+  a.tiles_m = (a.M + BM - 1) / BM;
+  a.tiles_n = (a.N + (PAIR ? BN / 2 : BN) - 1) / (PAIR ? BN / 2 : BN);
+  const long tiles = (long)a.tiles_m * a.tiles_n;
+  if (tiles > kMaxGrid / 2) return hipErrorInvalidValue;
+  kernel<<<dim3((unsigned)tiles, (unsigned)a.splits, (unsigned)a.problems), dim3(kThreads), lds, stream>>>(a, epi);
+  return hipGetLastError();
+}
+
+// Tiles of 256 x 256 (8 wavefronts, 128 KB of LDS, one workgroup a compute unit) where they fill the chip, else 128 x 128
+// (4 wavefronts, 64 KB, two workgroups a compute unit).
+template <class T, bool AKC, bool BKC, bool PAIR, class Epi>
+hipError_t launch_product(const ProductArgs &a, const Epi &epi, bool large, hipStream_t stream) {
+  if (a.M <= 0 || a.N <= 0) return hipSuccess;
+  if (large) return launch_shape<T, 256, 256, 2, 4, AKC, BKC, PAIR, Epi>(a, epi, stream);
+  return launch_shape<T, 128, 128, 2, 2, AKC, BKC, PAIR, Epi>(a, epi, stream);
+}
+
+// How many parts to cut k into so that about two workgroups a compute unit are at work
+inline int pick_splits(long tiles, long slabs) {
+  const long want = 2L * chip().cus;
+  long s = tiles > 0 ? want / tiles : 1;
+  if (s > slabs / 4) s = slabs / 4;
+  if (s > 64) s = 64;
+  return s < 1 ? 1 : (int)s;
+}
+
+struct Take {
+  char *base;
+  size_t used = 0;
+  void *operator()(size_t bytes) {
+    void *p = base ? base + used : nullptr;
+    used += (bytes + 255) / 256 * 256;
+    return p;
+  }
+};
+
+// a product whose k may be split, its sums stored as T
+template <class T, bool AKC, bool BKC>
+hipError_t product_to(ProductArgs p, StoreEpi<T> out, int splits, float *part, hipStream_t stream) {
+  const int slab = Elem<T>::kSlab, slabs = (p.K[0] + slab - 1) / slab + (p.K[1] + slab - 1) / slab;
+  if (splits <= 1) {
+    const long large = (long)((p.M + 255) / 256) * ((p.N + 255) / 256) * p.problems;
+    return launch_product<T, AKC, BKC, false>(p, out, large >= chip().cus * 3 / 4, stream);
+  }
+  p.slabs_per_split = (slabs + splits - 1) / splits;
+  p.splits = splits;
+  hipError_t e = launch_product<T, AKC, BKC, false>(p, PartialEpi{part, p.M}, false, stream);
+  if (e != hipSuccess) return e;
+  const long groups = (long)p.M * (padded(p.N) / 8);
+  const long blocks = (groups + 255) / 256;
+  sum_splits_kernel<T><<<dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, stream>>>(part, splits, p.M, p.N, p.m_rows, p.first, out);
+  return hipGetLastError();
+}
+
+#define DLL_TRY(call) do { const hipError_t e_ = (call); if (e_ != hipSuccess) return e_; } while (0)
+
+}  // namespace tile
+}  // namespace dllk

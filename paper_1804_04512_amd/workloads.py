@@ -74,6 +74,25 @@ class DenseSpec:
     act: str = "identity"
 
 
+@dataclass(frozen=True)
+class GatedSpec:
+    """A gated feed-forward block over `tokens` rows; gate "identity", "sigmoid", "relu", "silu" or "gelu"."""
+    tokens: int
+    width: int
+    hidden: int
+    gate: str = "silu"
+    dtype: str = "bfloat16"
+
+
+@dataclass(frozen=True)
+class VocabSpec:
+    """Softmax cross entropy of `tokens` rows over a vocabulary of `classes`."""
+    tokens: int
+    width: int
+    classes: int
+    dtype: str = "bfloat16"
+
+
 @dataclass
 class ConvWorkload:
     cfg: int
