@@ -130,7 +130,7 @@ struct FwdPlan {
   long ldh, ldd;
   void *h, *x, *wg, *wu, *wd;
   float *part;
-  int splits_y;
+  ProductPlan up, down;
   size_t bytes;
   FwdPlan(int T, int D, int H, int dtype, char *base) {
     Take take{base};
@@ -141,9 +141,9 @@ struct FwdPlan {
     x = wg = wu = wd = nullptr;
     if (!whole_groups(D, dtype)) x = take((size_t)T * ldd * e), wg = take((size_t)H * ldd * e), wu = take((size_t)H * ldd * e);
     if (!whole_groups(H, dtype)) wd = take((size_t)D * ldh * e);
-    const long tiles = (long)((T + 127) / 128) * ((D + 127) / 128);
-    splits_y = pick_splits(tiles, (ldh * (long)e + kSlabBytes - 1) / kSlabBytes);
-    part = splits_y > 1 ? (float *)take((size_t)splits_y * T * padded(D) * sizeof(float)) : nullptr;
+    up = plan_product(dtype, T, H, slabs_of(D, dtype), 1, true, false);
+    down = plan_product(dtype, T, D, slabs_of(H, dtype), 1, false, true);
+    part = down.splits > 1 ? (float *)take((size_t)down.splits * T * padded(D) * sizeof(float)) : nullptr;
     bytes = take.used;
   }
 };
@@ -152,7 +152,7 @@ struct BwdPlan {
   long ldh, ldd;
   void *da, *db, *h, *x, *wg, *wu, *wd, *dy;
   float *part;
-  int splits_dx;
+  ProductPlan dh, dw_down, dw_up, dx;
   size_t bytes;
   BwdPlan(int T, int D, int H, int dtype, char *base) {
     Take take{base};
@@ -165,9 +165,11 @@ struct BwdPlan {
     x = wg = wu = wd = dy = nullptr;
     if (!whole_groups(D, dtype)) x = take((size_t)T * ldd * e), dy = take((size_t)T * ldd * e), wg = take((size_t)H * ldd * e), wu = take((size_t)H * ldd * e);
     if (!whole_groups(H, dtype)) wd = take((size_t)D * ldh * e);
-    const long tiles = (long)((T + 127) / 128) * ((D + 127) / 128);
-    splits_dx = pick_splits(tiles, 2 * ((ldh * (long)e + kSlabBytes - 1) / kSlabBytes));
-    part = splits_dx > 1 ? (float *)take((size_t)splits_dx * T * padded(D) * sizeof(float)) : nullptr;
+    dh = plan_product(dtype, T, H, slabs_of(D, dtype), 1, false, false);
+    dw_down = plan_product(dtype, D, H, slabs_of(T, dtype), 1, false, false);
+    dw_up = plan_product(dtype, H, D, slabs_of(T, dtype), 2, false, false);
+    dx = plan_product(dtype, T, D, 2 * slabs_of(H, dtype), 1, false, true);
+    part = dx.splits > 1 ? (float *)take((size_t)dx.splits * T * padded(D) * sizeof(float)) : nullptr;
     bytes = take.used;
   }
 };
@@ -195,8 +197,7 @@ hipError_t gated_fwd(const GatedArgs &a, char *scratch, hipStream_t stream) {
   g.B[1] = {wu, ldx};
   g.K[0] = (int)ldx;
   GateEpi<T> ge{a.gate, 1, rows16<T>(a.gate_pre, a.H) && rows16<T>(a.up_pre, a.H), (T *)p.h, p.ldh, (T *)a.gate_pre, (T *)a.up_pre};
-  const long large = (long)((a.T + 255) / 256) * ((a.H + 127) / 128);
-  DLL_TRY((launch_product<T, true, true, true>(g, ge, large >= chip().cus * 3 / 4, stream)));
+  DLL_TRY((launch_product<T, true, true, true>(g, ge, p.up.tiling, stream)));
   ProductArgs y;
   y.M = a.T;
   y.N = a.D;
@@ -204,7 +205,7 @@ hipError_t gated_fwd(const GatedArgs &a, char *scratch, hipStream_t stream) {
   y.B[0] = {wd, ldd};
   y.K[0] = (int)ldd;
   StoreEpi<T> out{{(T *)a.y, nullptr}, a.D, rows16<T>(a.y, a.D), nullptr, 0};
-  return product_to<T, true, true>(y, out, p.splits_y, p.part, stream);
+  return product_to<T, true, true>(y, out, p.down, p.part, stream);
 }
 
 template <class T>
@@ -236,8 +237,7 @@ hipError_t gated_bwd(const GatedArgs &a, char *scratch, hipStream_t stream) {
   g.K[0] = a.D;   // Wd lies across k; where D is no multiple of a 16-byte group, dy's copy has zeros behind it
   GateBackEpi<T> ge{a.gate, rows16<T>(a.gate_pre, a.H) && rows16<T>(a.up_pre, a.H), (const T *)a.gate_pre, (const T *)a.up_pre,
                     (T *)p.da, (T *)p.db, (T *)p.h, p.ldh};
-  const long large = (long)((a.T + 255) / 256) * ((a.H + 255) / 256);
-  DLL_TRY((launch_product<T, true, false, false>(g, ge, large >= chip().cus * 3 / 4, stream)));
+  DLL_TRY((launch_product<T, true, false, false>(g, ge, p.dh.tiling, stream)));
   if (a.dw_down) {
     ProductArgs w;
     w.M = a.D;
@@ -246,7 +246,7 @@ hipError_t gated_bwd(const GatedArgs &a, char *scratch, hipStream_t stream) {
     w.B[0] = {p.h, p.ldh};
     w.K[0] = a.T;
     StoreEpi<T> out{{(T *)a.dw_down, nullptr}, a.H, rows16<T>(a.dw_down, a.H), nullptr, 0};
-    DLL_TRY((product_to<T, false, false>(w, out, 1, nullptr, stream)));
+    DLL_TRY((launch_product<T, false, false, false>(w, out, p.dw_down.tiling, stream)));
   }
   if (a.dw_gate || a.dw_up) {
     ProductArgs w;
@@ -261,7 +261,7 @@ hipError_t gated_bwd(const GatedArgs &a, char *scratch, hipStream_t stream) {
     w.B[0] = w.B[1] = {x, ldx};
     w.K[0] = a.T;
     StoreEpi<T> out{{o[first], o[1]}, a.D, rows16<T>(o[first], a.D) && rows16<T>(o[w.problems - 1], a.D), nullptr, 0};
-    DLL_TRY((product_to<T, false, false>(w, out, 1, nullptr, stream)));
+    DLL_TRY((launch_product<T, false, false, false>(w, out, p.dw_up.tiling, stream)));
   }
   if (a.dx) {
     ProductArgs w;
@@ -273,7 +273,7 @@ hipError_t gated_bwd(const GatedArgs &a, char *scratch, hipStream_t stream) {
     w.B[1] = {wu, ldx};
     w.K[0] = w.K[1] = a.H;
     StoreEpi<T> out{{(T *)a.dx, nullptr}, a.D, rows16<T>(a.dx, a.D), nullptr, 0};
-    DLL_TRY((product_to<T, true, false>(w, out, p.splits_dx, p.part, stream)));
+    DLL_TRY((product_to<T, true, false>(w, out, p.dx, p.part, stream)));
   }
   return hipSuccess;
 }

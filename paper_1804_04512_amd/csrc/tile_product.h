@@ -11,10 +11,11 @@
 // behind K are sent out of range where the last slab is not whole, so no operand needs padding to the tile.
 //
 // LDS layouts.  The hardware writes a wavefront's 64 x 16 bytes in lane order, so a swizzle is made by permuting which
-// global bytes a lane fetches.  KC: rows of 128 bytes, 16-byte group c of row r at place c ^ (r & 7); a fragment read
-// (32 rows, one group each) touches every bank the same number of times.  KS bf16: rows of X columns, 64-byte block b of
+// global bytes a lane fetches.  KC: rows of 128 bytes, 16-byte group c of row r at place c ^ ((r >> 1) & 7), so that the
+// sixteen lanes that read at a time (16 rows, one group each) touch all 64 banks once (c ^ (r & 7), made for 32 banks, had two
+// lanes on each: half of all LDS cycles).  KS bf16: rows of X columns, 64-byte block b of
 // row k at place b ^ g(k) with g from bits 0, 1 and 3 of k; the transposing read ds_read_b64_tr_b16 turns four rows of
-// sixteen columns into four k's a lane.  KS fp32: four 4-byte reads a fragment.
+// sixteen columns into four k's a lane.  KS fp32: four 4-byte reads a fragment, 128-byte block b of row k at b ^ bit 2 of k.
 //
 // MFMA: 32x32x16 bf16, and for fp32 32x32x2 with the four floats of a 16-byte group as four steps (the order of k within a
 // slab is the same permutation for both operands).  B rides on the first operand, so a lane holds one row m of C and runs
@@ -92,6 +93,10 @@ __device__ __forceinline__ void load_to_lds(const uintx4 &rs, unsigned off, unsi
   const unsigned at = (unsigned)__builtin_amdgcn_readfirstlane((int)lds);
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(off), "s"(rs) : "memory");   // m0 is never the compiler's to keep
 }
+// the swizzle of a KS bf16 row of X columns: which of its 64-byte blocks change places
+template <int X>
+__device__ __forceinline__ int mix(int k) { return X >= 256 ? (k & 3) | ((k >> 1) & 4) : X >= 128 ? k & 3 : X >= 64 ? (k >> 1) & 1 : 0; }
+
 // One operand's slab of X rows (KC) or X columns (KS).
 template <class T, int X, bool KC, int THREADS>
 struct Slab {
@@ -101,38 +106,40 @@ struct Slab {
   static constexpr int kRowGroups = KC ? 8 : X * (int)sizeof(T) / 16;   // 16-byte groups of a row in LDS
   static_assert(kBytes % (16 * THREADS) == 0 && (THREADS / kRowGroups) * kRowGroups == THREADS, "whole rows a step");
   static constexpr int kStep = THREADS / kRowGroups;                     // rows between a thread's loads
-  static_assert(KC ? kStep % 8 == 0 : (sizeof(T) == 4 || kStep % 4 == 0), "the swizzle does not change between them");
-
-  // the swizzle of a KS bf16 row: which of its 64-byte blocks change places
-  static __device__ __forceinline__ int mix(int k) { return (k & 3) | (X >= 256 ? ((k >> 3) & 1) << 2 : 0); }
 
   unsigned off[kIts];   // bytes from the slab's first element
-  int along;            // KC: this thread's first k inside the slab
 
-  __device__ __forceinline__ void init(long ld) {
-    const int t = threadIdx.x, place = t % kRowGroups, row0 = t / kRowGroups;
+  static __device__ __forceinline__ int group_of(int row, int place) {
+    if (KC) return place ^ ((row >> 1) & 7);
+    if (sizeof(T) == 2) return (((place >> 2) ^ mix<X>(row)) << 2) | (place & 3);
+    return X >= 64 ? place ^ (((row >> 2) & 1) << 3) : place;
+  }
+  __device__ __forceinline__ void init(long ld, int t) {   // t: the thread among the THREADS that load this slab
+    const int place = t % kRowGroups, row0 = t / kRowGroups;
 #pragma unroll
     for (int it = 0; it < kIts; ++it) {
       const int row = row0 + it * kStep;
-      int group = place;
-      if (KC) group = place ^ (row & 7);
-      else if (sizeof(T) == 2) group = (((place >> 2) ^ mix(row)) << 2) | (place & 3);
-      off[it] = (unsigned)((long)row * ld * (int)sizeof(T)) + 16u * group;
-      if (it == 0) along = KC ? group * (16 / (int)sizeof(T)) : 0;
+      off[it] = (unsigned)((long)row * ld * (int)sizeof(T)) + 16u * group_of(row, place);
     }
   }
   // x0: the tile's first row (KC) or column (KS); k0: the slab's first k; X_, K: extents of the operand
-  __device__ __forceinline__ void load(unsigned lds, const Operand &o, int x0, int X_, int k0, int K) const {
+  __device__ __forceinline__ void load(unsigned lds, int wave, const Operand &o, int x0, int X_, int k0, int K) const {
     const long first = KC ? (long)x0 * o.ld + k0 : (long)k0 * o.ld + x0;
     const long end = KC ? (long)X_ * o.ld : (long)K * o.ld;
     long bytes = (end - first) * (long)sizeof(T);
     bytes = bytes < 0 ? 0 : (bytes > 0xFFFFFF00L ? 0xFFFFFF00L : bytes);
     const uintx4 rs = buffer_of((const char *)o.p + first * (long)sizeof(T), (unsigned)bytes);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const bool cut = KC && k0 + kK > K;   // uniform: only a last slab
-    const bool out = cut && k0 + along >= K;
+    if (KC && k0 + kK > K) {   // uniform: only a last slab
+      const int t = (int)(threadIdx.x % THREADS), place = t % kRowGroups, row0 = t / kRowGroups;
 #pragma unroll
-    for (int it = 0; it < kIts; ++it) load_to_lds(rs, out ? kOutOfRange : off[it], lds + (it * THREADS + wave * 64) * 16);
+      for (int it = 0; it < kIts; ++it) {
+        const bool out = k0 + group_of(row0 + it * kStep, place) * (16 / (int)sizeof(T)) >= K;
+        load_to_lds(rs, out ? kOutOfRange : off[it], lds + (it * THREADS + wave * 64) * 16);
+      }
+      return;
+    }
+#pragma unroll
+    for (int it = 0; it < kIts; ++it) load_to_lds(rs, off[it], lds + (it * THREADS + wave * 64) * 16);
   }
 };
 
@@ -144,27 +151,26 @@ struct PairSlab {
   static constexpr int kBytes = Base::kBytes, kIts = Base::kIts;
   static_assert(Base::kStep % 32 == 0 || 32 % Base::kStep == 0, "a wavefront's rows lie in one projection");
   unsigned off[kIts];
-  int along;
-  __device__ __forceinline__ void init(long ld) {
-    const int t = threadIdx.x, place = t & 7, row0 = t >> 3;
+  __device__ __forceinline__ void init(long ld, int t) {
+    const int place = t & 7, row0 = t >> 3;
 #pragma unroll
     for (int it = 0; it < kIts; ++it) {
-      const int row = row0 + it * Base::kStep, group = place ^ (row & 7);
-      off[it] = (unsigned)((long)((row >> 6) * 32 + (row & 31)) * ld * (int)sizeof(T)) + 16u * group;
-      if (it == 0) along = group * (16 / (int)sizeof(T));
+      const int row = row0 + it * Base::kStep;
+      off[it] = (unsigned)((long)((row >> 6) * 32 + (row & 31)) * ld * (int)sizeof(T)) + 16u * Base::group_of(row, place);
     }
   }
   // x0: the tile's first hidden unit; H: hidden units
-  __device__ __forceinline__ void load(unsigned lds, const Operand &gate, const Operand &up, int x0, int H, int k0, int K) const {
+  __device__ __forceinline__ void load(unsigned lds, int wave, const Operand &gate, const Operand &up, int x0, int H, int k0, int K) const {
     const long first = (long)x0 * gate.ld + k0;
     long bytes = ((long)H * gate.ld - first) * (long)sizeof(T);
     bytes = bytes < 0 ? 0 : (bytes > 0xFFFFFF00L ? 0xFFFFFF00L : bytes);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const bool out = k0 + Base::kK > K && k0 + along >= K;
+    const bool cut = k0 + Base::kK > K;   // uniform
+    const int t = (int)(threadIdx.x % THREADS), place = t & 7, row0 = t >> 3;
 #pragma unroll
     for (int it = 0; it < kIts; ++it) {
       const bool second = ((wave * 8 + it * Base::kStep) >> 5) & 1;
       const uintx4 rs = buffer_of((const char *)(second ? up.p : gate.p) + first * (long)sizeof(T), (unsigned)bytes);
+      const bool out = cut && k0 + Base::group_of(row0 + it * Base::kStep, place) * (16 / (int)sizeof(T)) >= K;
       load_to_lds(rs, out ? kOutOfRange : off[it], lds + (it * THREADS + wave * 64) * 16);
     }
   }
@@ -177,7 +183,7 @@ struct FragReader;
 template <class T, int X>
 struct FragReader<T, X, true> {
   int row, half, low;
-  __device__ __forceinline__ explicit FragReader(int lane) : row((lane & 31) * kSlabBytes), half(lane >> 5), low(lane & 7) {}
+  __device__ __forceinline__ explicit FragReader(int lane) : row((lane & 31) * kSlabBytes), half(lane >> 5), low((lane >> 1) & 7) {}
   __device__ __forceinline__ typename Elem<T>::Frag operator()(const char *lds, int x0, int s) const {
     return *reinterpret_cast<const typename Elem<T>::Frag *>(lds + x0 * kSlabBytes + row + (((2 * s + half) ^ low) << 4));
   }
@@ -188,7 +194,7 @@ struct FragReader<bf16, X, false> {
   __device__ __forceinline__ explicit FragReader(int lane) {
     const int i = lane & 15, k = 8 * (lane >> 5) + (i >> 2);
     base = k * X * 2 + (((lane >> 4) & 1) * 16 + 4 * (i & 3)) * 2;
-    g = Slab<bf16, X, false, 256>::mix(k);
+    g = mix<X>(k);
   }
   __device__ __forceinline__ bf16x8 operator()(const char *lds, int x0, int s) const {
     typedef __attribute__((address_space(3))) shortx4 *Lp;
@@ -200,10 +206,10 @@ struct FragReader<bf16, X, false> {
 };
 template <int X>
 struct FragReader<float, X, false> {
-  int base;
-  __device__ __forceinline__ explicit FragReader(int lane) : base((4 * (lane >> 5) * X + (lane & 31)) * 4) {}
+  int base, flip;
+  __device__ __forceinline__ explicit FragReader(int lane) : base((4 * (lane >> 5) * X + (lane & 31)) * 4), flip(X >= 64 ? lane & 32 : 0) {}
   __device__ __forceinline__ floatx4 operator()(const char *lds, int x0, int s) const {
-    const float *p = reinterpret_cast<const float *>(lds + base) + s * 8 * X + x0;
+    const float *p = reinterpret_cast<const float *>(lds + base) + s * 8 * X + (x0 ^ flip);
     return floatx4{p[0], p[X], p[2 * X], p[3 * X]};
   }
 };
@@ -216,18 +222,20 @@ __device__ __forceinline__ floatx16 mfma(floatx4 b, floatx4 a, floatx16 c) {
 }
 
 // ------------------------------------------------------------------------------------------------ kernel
-// WM x WN wavefronts of (BM / WM) x 64 each.  Epi: `piece(stage, m, n, M, N, problem, split)` takes 32 x 64 sums from the
-// wavefront's LDS area (row stride kStageLd floats), first element C(m, n).
+// WK groups of WM x WN wavefronts of (BM / WM) x 64 each; the groups take the slabs in turn and their sums are added in LDS in
+// group order (products with too few tiles to fill the chip: the chain of slabs is WK times shorter).
+// Epi: `piece(stage, m, n, M, N, problem, split)` takes 32 x 64 sums from the wavefront's LDS area (row stride kStageLd
+// floats), first element C(m, n).
 // PAIR: B[0] and B[1] are the gate and up projections (KC), N counts hidden units, a tile covers BN / 2 of them.
-template <class T, int BM, int BN, int WM, int WN, bool AKC, bool BKC, bool PAIR, class Epi>
-__global__ __launch_bounds__(64 * WM *WN, 2) void product_kernel(const ProductArgs a, const Epi epi) {
+template <class T, int BM, int BN, int WM, int WN, int WK, bool AKC, bool BKC, bool PAIR, class Epi>
+__global__ __launch_bounds__(64 * WM *WN *WK, 2) void product_kernel(const ProductArgs a, const Epi epi) {
   constexpr int kThreads = 64 * WM * WN, TM = BM / WM / 32, kK = Elem<T>::kSlab;
   static_assert(BN / WN == 64 && BM % (32 * WM) == 0, "wavefront tiles are 64 columns wide");
   typedef Slab<T, BM, AKC, kThreads> SA;
   typedef Slab<T, BN, BKC, kThreads> SB;
   constexpr int kA = SA::kBytes, kStage = SA::kBytes + SB::kBytes;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = all % (WM * WN), group = all / (WM * WN);
   const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * 64;
   int tm, tn;
   tile_of(blockIdx.x, a.tiles_m, a.tiles_n, &tm, &tn);
@@ -238,20 +246,25 @@ __global__ __launch_bounds__(64 * WM *WN, 2) void product_kernel(const ProductAr
   if (m0 >= M) return;
   const int slabs0 = (K0 + kK - 1) / kK, slabs = slabs0 + (a.K[1] + kK - 1) / kK;
   const int t0 = min(slabs, (int)blockIdx.y * a.slabs_per_split), t1 = min(slabs, t0 + a.slabs_per_split);
+  const int turns = (t1 - t0 + WK - 1) / WK;   // a group's slabs: t0 + group, then every WK-th
 
   SA sa;
   SB sb;
   PairSlab<T, BN, kThreads> sp;
-  sa.init(a.A[0].ld);
-  if (PAIR) sp.init(a.B[0].ld);
-  else sb.init(a.B[0].ld);
-  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
-  const auto load = [&](int t, unsigned lds) {
+  sa.init(a.A[0].ld, threadIdx.x % kThreads);
+  if (PAIR) sp.init(a.B[0].ld, threadIdx.x % kThreads);
+  else sb.init(a.B[0].ld, threadIdx.x % kThreads);
+  char *mine = smem + group * 2 * kStage;
+  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)mine;
+  const auto load = [&](int turn) {
+    const int t = t0 + turn * WK + group;
+    if (t >= t1) return;
+    const unsigned lds = lds0 + (turn & 1) * kStage;
     const bool second = t >= slabs0;
     const int k0 = (second ? t - slabs0 : t) * kK, K = second ? a.K[1] : K0, which = second ? 1 : problem;
-    sa.load(lds, a.A[which], m0, M, k0, K);
-    if (PAIR) sp.load(lds + kA, a.B[0], a.B[1], n0, a.N, k0, K);
-    else sb.load(lds + kA, a.B[which], n0, a.N, k0, K);
+    sa.load(lds, wave, a.A[which], m0, M, k0, K);
+    if (PAIR) sp.load(lds + kA, wave, a.B[0], a.B[1], n0, a.N, k0, K);
+    else sb.load(lds + kA, wave, a.B[which], n0, a.N, k0, K);
   };
 
   floatx16 acc[TM][2];
@@ -261,39 +274,85 @@ __global__ __launch_bounds__(64 * WM *WN, 2) void product_kernel(const ProductAr
     for (int j = 0; j < 2; ++j) acc[i][j] = floatx16{};
   const FragReader<T, BM, AKC> ra(lane);
   const FragReader<T, BN, BKC> rb(lane);
-  if (t0 < t1) load(t0, lds0);
-  for (int t = t0; t < t1; ++t) {
-    const char *now = smem + ((t - t0) & 1) * kStage;
-    // this wavefront's loads of slab t have landed, then everyone's; all have also left slab t - 1, whose place t + 1 takes
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  // Fragments are read one step ahead of the products that take them.  The one barrier of a slab stands before its last
+  // step: by then every wavefront holds its last fragments of this slab, so its place can take the slab after the next, and has
+  // seen its part of the next slab land, whose first fragments are read behind the barrier while the last step multiplies.
+  typename Elem<T>::Frag fa[2][TM], fb[2][2];
+  const auto read = [&](int set, const char *lds, int s) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) fb[set][j] = rb(lds + kA, wn + 32 * j, s);
+#pragma unroll
+    for (int i = 0; i < TM; ++i) fa[set][i] = ra(lds, wm + 32 * i, s);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  const auto multiply = [&](int set) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) acc[i][j] = mfma(fb[set][j], fa[set][i], acc[i][j]);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  if (turns > 0) {
+    load(0);
+    load(1);
+    if (turns > 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(SA::kIts + SB::kIts) : "memory");
+    if (turns == 1 || (WK > 1 && t0 + WK + group >= t1)) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (t + 1 < t1) load(t + 1, lds0 + ((t - t0 + 1) & 1) * kStage);
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      typename Elem<T>::Frag fa[TM], fb[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) fb[j] = rb(now + kA, wn + 32 * j, s);
-#pragma unroll
-      for (int i = 0; i < TM; ++i) fa[i] = ra(now, wm + 32 * i, s);
-#pragma unroll
-      for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) acc[i][j] = mfma(fb[j], fa[i], acc[i][j]);
+    if (WK == 1 || t0 + group < t1) read(0, mine, 0);
+  }
+  for (int turn = 0; turn < turns; ++turn) {
+    const char *now = mine + (turn & 1) * kStage, *next = mine + ((turn + 1) & 1) * kStage;
+    const bool has = WK == 1 || t0 + turn * WK + group < t1;   // a group may have no slab in the last turn
+    if (has) {
+      read(1, now, 1);
+      multiply(0);
+      read(0, now, 2);
+      multiply(1);
+      read(1, now, 3);
+      multiply(0);
     }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (turn + 2 < turns) load(turn + 2);
+    if (turn + 1 < turns && (WK == 1 || t0 + (turn + 1) * WK + group < t1)) read(0, next, 0);
+    if (has) multiply(1);
   }
   __syncthreads();   // the slabs' place becomes the epilogue's
-  float *stage = reinterpret_cast<float *>(smem) + wave * 32 * kStageLd;
-#pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  constexpr int kPiece = 32 * kStageLd;
+  float *stage = reinterpret_cast<float *>(smem) + all * kPiece;
+  const auto to_stage = [&](const floatx16 (&c)[2]) {
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
         *reinterpret_cast<floatx4 *>(stage + (lane & 31) * kStageLd + 32 * j + 8 * r + 4 * (lane >> 5)) =
-            floatx4{acc[i][j][4 * r], acc[i][j][4 * r + 1], acc[i][j][4 * r + 2], acc[i][j][4 * r + 3]};
+            floatx4{c[j][4 * r], c[j][4 * r + 1], c[j][4 * r + 2], c[j][4 * r + 3]};
+  };
+  if constexpr (WK > 1) {
+    static_assert(TM == 1, "one piece a wavefront");
+    to_stage(acc[0]);
+    __syncthreads();
+    if (group > 0 || m0 + wm >= M) return;
+#pragma unroll
+    for (int e = 0; e < 32; e += 4) {   // four rows of 16 lanes' 16 bytes a step
+      float *p = stage + (e + (lane >> 4)) * kStageLd + 4 * (lane & 15);
+      floatx4 v = *reinterpret_cast<floatx4 *>(p);
+#pragma unroll
+      for (int g = 1; g < WK; ++g) v += *reinterpret_cast<floatx4 *>(p + g * WM * WN * kPiece);
+      *reinterpret_cast<floatx4 *>(p) = v;
+    }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (m0 + wm + 32 * i < M) epi.piece(stage, m0 + wm + 32 * i, PAIR ? n0 + wn / 2 : n0 + wn, M, a.N, problem, (int)blockIdx.y);
+    epi.piece(stage, m0 + wm, PAIR ? n0 + wn / 2 : n0 + wn, M, a.N, problem, (int)blockIdx.y);
+  } else {
+#pragma unroll 1   // one copy of the epilogue; the sums' registers are chosen by uniform branches
+    for (int q = 0; q < TM; ++q) {
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+        if (i == q) to_stage(acc[i]);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      if (m0 + wm + 32 * q < M) epi.piece(stage, m0 + wm + 32 * q, PAIR ? n0 + wn / 2 : n0 + wn, M, a.N, problem, (int)blockIdx.y);
+    }
   }
 }
 
@@ -433,38 +492,75 @@ __global__ __launch_bounds__(256) void sum_splits_kernel(const float *part, int 
 }
 
 // ------------------------------------------------------------------------------------------------ host
-template <class T, int BM, int BN, int WM, int WN, bool AKC, bool BKC, bool PAIR, class Epi>
-hipError_t launch_shape(ProductArgs a, const Epi &epi, hipStream_t stream) {
-  constexpr int kThreads = 64 * WM * WN;
-  constexpr size_t slabs = 2 * (size_t)(BM + BN) * kSlabBytes, stage = (size_t)WM * WN * 32 * kStageLd * sizeof(float);
+// The tilings of a product: tile edges, and how many groups of wavefronts take the slabs in turn.
+enum Tiling { TILE_256 = 0, TILE_128, TILE_64_K2, TILE_64_K4, TILE_32_K4, TILINGS };
+struct ProductPlan { int tiling = TILE_128, splits = 1; };
+
+// What a tiling costs, in microseconds, as measured on products of 512 to 8192 rows and columns: a workgroup's share of a
+// compute unit for one turn (a slab for each group) with the unit full, the least time of a turn's chain of load, barrier and
+// products, what a workgroup takes besides its turns, and how many a unit holds.
+struct TilingCost { int bm, bn, groups, resident; double share[2], chain[2], besides[2]; };   // [fp32, bf16]
+constexpr TilingCost kTilings[TILINGS] = {
+    {256, 256, 1, 1, {7.8, 1.62}, {7.4, 1.3}, {6.0, 8.0}},
+    {128, 128, 1, 2, {2.08, 0.55}, {2.05, 0.66}, {4.0, 4.0}},
+    {64, 64, 2, 2, {1.07, 0.42}, {1.15, 0.7}, {3.0, 3.0}},
+    {64, 64, 4, 1, {2.1, 0.92}, {2.2, 0.95}, {3.5, 2.7}},
+    {32, 64, 4, 1, {1.05, 0.6}, {1.1, 0.75}, {3.0, 2.5}},
+};
+
+// The tiling and the number of parts of k with the least estimated time.  Parts of k cost their sums' way to memory and back and
+// a second launch.
+inline ProductPlan plan_product(int dtype, int M, int N, long slabs, int problems, bool pair, bool may_split) {
+  ProductPlan best;
+  double least = 1e30;
+  const int type = dtype == TYPE_BF16 ? 1 : 0, cus = chip().cus;
+  for (int i = 0; i < TILINGS; ++i) {
+    const TilingCost &c = kTilings[i];
+    const long nn = pair ? 2L * N : N, tiles = (long)((M + c.bm - 1) / c.bm) * ((nn + c.bn - 1) / c.bn) * problems;
+    for (int s = 1; s <= (may_split ? 32 : 1); s *= 2) {
+      if (s > 1 && (slabs < 4L * s || tiles * s > 4L * cus * c.resident)) break;
+      const long each = ((slabs + s - 1) / s + c.groups - 1) / c.groups, n = (tiles * s + cus - 1) / cus, full = n / c.resident, rest = n % c.resident;
+      const double whole = c.resident * c.share[type] > c.chain[type] ? c.resident * c.share[type] : c.chain[type];
+      const double part = rest * c.share[type] > c.chain[type] ? rest * c.share[type] : c.chain[type];
+      double t = full * (each * whole + c.besides[type]) + (rest ? each * part + c.besides[type] : 0.0);
+      if (s > 1) t += 5.0 + (double)s * M * N * 8.0 / 4.0e6;
+      if (t < least) {
+        least = t;
+        best.tiling = i;
+        best.splits = s;
+      }
+    }
+  }
+  return best;
+}
+inline long slabs_of(long k, int dtype) { return (k * (long)type_bytes(dtype) + kSlabBytes - 1) / kSlabBytes; }
+
+template <class T, int BM, int BN, int WM, int WN, int WK, bool AKC, bool BKC, bool PAIR, class Epi>
+hipError_t launch_tiling(ProductArgs a, const Epi &epi, hipStream_t stream) {
+  constexpr int kThreads = 64 * WM * WN * WK;
+  constexpr size_t slabs = 2 * (size_t)WK * (BM + BN) * kSlabBytes, stage = (size_t)WM * WN * WK * 32 * kStageLd * sizeof(float);
   constexpr size_t lds = slabs > stage ? slabs : stage;
-  const auto kernel = product_kernel<T, BM, BN, WM, WN, AKC, BKC, PAIR, Epi>;
+  const auto kernel = product_kernel<T, BM, BN, WM, WN, WK, AKC, BKC, PAIR, Epi>;
   hipError_t e = allow_large_lds(reinterpret_cast<const void *>(kernel), lds);
   if (e != hipSuccess) return e;
   a.tiles_m = (a.M + BM - 1) / BM;
   a.tiles_n = (a.N + (PAIR ? BN / 2 : BN) - 1) / (PAIR ? BN / 2 : BN);
   const long tiles = (long)a.tiles_m * a.tiles_n;
-  if (tiles > kMaxGrid / 2) return hipErrorInvalidValue;
+  if (tiles * kThreads >= (1L << 32)) return hipErrorInvalidValue;
   kernel<<<dim3((unsigned)tiles, (unsigned)a.splits, (unsigned)a.problems), dim3(kThreads), lds, stream>>>(a, epi);
   return hipGetLastError();
 }
 
-// Tiles of 256 x 256 (8 wavefronts, 128 KB of LDS, one workgroup a compute unit) where they fill the chip, else 128 x 128
-// (4 wavefronts, 64 KB, two workgroups a compute unit).
 template <class T, bool AKC, bool BKC, bool PAIR, class Epi>
-hipError_t launch_product(const ProductArgs &a, const Epi &epi, bool large, hipStream_t stream) {
+hipError_t launch_product(const ProductArgs &a, const Epi &epi, int tiling, hipStream_t stream) {
   if (a.M <= 0 || a.N <= 0) return hipSuccess;
-  if (large) return launch_shape<T, 256, 256, 2, 4, AKC, BKC, PAIR, Epi>(a, epi, stream);
-  return launch_shape<T, 128, 128, 2, 2, AKC, BKC, PAIR, Epi>(a, epi, stream);
-}
-
-// How many parts to cut k into so that about two workgroups a compute unit are at work
-inline int pick_splits(long tiles, long slabs) {
-  const long want = 2L * chip().cus;
-  long s = tiles > 0 ? want / tiles : 1;
-  if (s > slabs / 4) s = slabs / 4;
-  if (s > 64) s = 64;
-  return s < 1 ? 1 : (int)s;
+  switch (tiling) {
+    case TILE_256: return launch_tiling<T, 256, 256, 2, 4, 1, AKC, BKC, PAIR, Epi>(a, epi, stream);
+    case TILE_128: return launch_tiling<T, 128, 128, 2, 2, 1, AKC, BKC, PAIR, Epi>(a, epi, stream);
+    case TILE_64_K2: return launch_tiling<T, 64, 64, 2, 1, 2, AKC, BKC, PAIR, Epi>(a, epi, stream);
+    case TILE_64_K4: return launch_tiling<T, 64, 64, 2, 1, 4, AKC, BKC, PAIR, Epi>(a, epi, stream);
+    default: return launch_tiling<T, 32, 64, 1, 1, 4, AKC, BKC, PAIR, Epi>(a, epi, stream);
+  }
 }
 
 struct Take {
@@ -479,19 +575,15 @@ struct Take {
 
 // a product whose k may be split, its sums stored as T
 template <class T, bool AKC, bool BKC>
-hipError_t product_to(ProductArgs p, StoreEpi<T> out, int splits, float *part, hipStream_t stream) {
+hipError_t product_to(ProductArgs p, StoreEpi<T> out, const ProductPlan &plan, float *part, hipStream_t stream) {
+  if (plan.splits <= 1) return launch_product<T, AKC, BKC, false>(p, out, plan.tiling, stream);
   const int slab = Elem<T>::kSlab, slabs = (p.K[0] + slab - 1) / slab + (p.K[1] + slab - 1) / slab;
-  if (splits <= 1) {
-    const long large = (long)((p.M + 255) / 256) * ((p.N + 255) / 256) * p.problems;
-    return launch_product<T, AKC, BKC, false>(p, out, large >= chip().cus * 3 / 4, stream);
-  }
-  p.slabs_per_split = (slabs + splits - 1) / splits;
-  p.splits = splits;
-  hipError_t e = launch_product<T, AKC, BKC, false>(p, PartialEpi{part, p.M}, false, stream);
+  p.slabs_per_split = (slabs + plan.splits - 1) / plan.splits;
+  p.splits = plan.splits;
+  hipError_t e = launch_product<T, AKC, BKC, false>(p, PartialEpi{part, p.M}, plan.tiling, stream);
   if (e != hipSuccess) return e;
-  const long groups = (long)p.M * (padded(p.N) / 8);
-  const long blocks = (groups + 255) / 256;
-  sum_splits_kernel<T><<<dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, stream>>>(part, splits, p.M, p.N, p.m_rows, p.first, out);
+  const long groups = (long)p.M * (padded(p.N) / 8), blocks = (groups + 255) / 256;
+  sum_splits_kernel<T><<<dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, stream>>>(part, plan.splits, p.M, p.N, p.m_rows, p.first, out);
   return hipGetLastError();
 }
 

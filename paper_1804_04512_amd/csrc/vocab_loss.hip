@@ -238,7 +238,8 @@ __global__ __launch_bounds__(256) void convert_kernel(const float *src, T *dst, 
 
 struct Plan {
   long ldd, lde;
-  int groups, piece, pieces, splits_dx;
+  int groups, piece, pieces;
+  ProductPlan z, dx, dw;
   int *count, *rows, *labels;
   void *x, *w, *e;
   float2 *stats;
@@ -266,16 +267,16 @@ struct Plan {
     hit = (float *)take((size_t)piece * sizeof(float));
     loss = (float *)take((size_t)T * sizeof(float));
     lse = nullptr, e = nullptr, sums = bias_sum = dw_sum = part = nullptr;
-    splits_dx = 1;
+    z = plan_product(dtype, piece, V, slabs_of(D, dtype), 1, false, false);
     if (grad) {
       lse = (float *)take((size_t)piece * sizeof(float));
       e = take(slab_rows * lde * b);
       sums = (float *)take(slab_rows / 64 * lde * sizeof(float));
       bias_sum = (float *)take((size_t)V * sizeof(float));
       if (pieces > 1 && dtype == TYPE_BF16) dw_sum = (float *)take((size_t)V * D * sizeof(float));
-      const long tiles = (long)((piece + 127) / 128) * ((D + 127) / 128);
-      splits_dx = pick_splits(tiles, (lde * (long)b + kSlabBytes - 1) / kSlabBytes);
-      if (splits_dx > 1) part = (float *)take((size_t)splits_dx * piece * ldd * sizeof(float));
+      dx = plan_product(dtype, piece, D, slabs_of(V, dtype), 1, false, true);
+      dw = plan_product(dtype, V, D, slabs_of(piece, dtype), 1, false, false);
+      if (dx.splits > 1) part = (float *)take((size_t)dx.splits * piece * ldd * sizeof(float));
     }
     bytes = take.used;
   }
@@ -312,8 +313,7 @@ hipError_t logits(const VocabArgs &a, const Plan &p, int first, const void *w, l
   g.m_rows = p.count;
   g.first = first;
   const LogitEpi<T, KEEP> epi{(const T *)a.bias, p.labels + first, p.count, first, p.stats, p.groups, p.hit, (T *)p.e, p.lde};
-  const long large = (long)((g.M + 255) / 256) * ((a.V + 255) / 256);
-  DLL_TRY((launch_product<T, true, true, false>(g, epi, large >= chip().cus * 3 / 4, stream)));
+  DLL_TRY((launch_product<T, true, true, false>(g, epi, p.z.tiling, stream)));
   join_groups_kernel<<<dim3((unsigned)((g.M + 3) / 4)), dim3(256), 0, stream>>>(p.stats, p.groups, p.hit, g.M, p.count, first, p.rows + first, p.lse,
                                                                                    p.loss + first, a.row_loss, a.row_lse);
   return hipGetLastError();
@@ -359,7 +359,7 @@ hipError_t vocab_grad(const VocabArgs &a, char *scratch, hipStream_t stream) {
       g.m_rows = p.count;
       g.first = first;
       const StoreEpi<T> out{{(T *)a.dx, nullptr}, a.D, rows16<T>(a.dx, a.D), p.rows + first, 0};
-      DLL_TRY((product_to<T, true, false>(g, out, p.splits_dx, p.part, stream)));
+      DLL_TRY((product_to<T, true, false>(g, out, p.dx, p.part, stream)));
     }
     if (a.dw) {
       ProductArgs g;
@@ -370,10 +370,9 @@ hipError_t vocab_grad(const VocabArgs &a, char *scratch, hipStream_t stream) {
       g.K[0] = M;
       g.k_rows = p.count;
       g.first = first;
-      const long large = (long)((a.V + 255) / 256) * ((a.D + 255) / 256);
       if (p.dw_sum) {   // pieces of bfloat16 products add up in 32 bits
         const StoreEpi<float> out{{p.dw_sum, nullptr}, a.D, rows16<float>(p.dw_sum, a.D), nullptr, first > 0};
-        DLL_TRY((launch_product<T, false, false, false>(g, out, large >= chip().cus * 3 / 4, stream)));
+        DLL_TRY((launch_product<T, false, false, false>(g, out, p.dw.tiling, stream)));
         if (last) {
           const long n = (long)a.V * a.D, blocks = (n + 255) / 256;
           convert_kernel<T><<<dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, stream>>>(p.dw_sum, (T *)a.dw, n);
@@ -381,7 +380,7 @@ hipError_t vocab_grad(const VocabArgs &a, char *scratch, hipStream_t stream) {
         }
       } else {
         const StoreEpi<T> out{{(T *)a.dw, nullptr}, a.D, rows16<T>(a.dw, a.D), nullptr, first > 0};
-        DLL_TRY((launch_product<T, false, false, false>(g, out, large >= chip().cus * 3 / 4, stream)));
+        DLL_TRY((launch_product<T, false, false, false>(g, out, p.dw.tiling, stream)));
       }
     }
   }
