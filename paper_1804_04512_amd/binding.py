@@ -7,6 +7,7 @@ no CPU fallback: a missing library or a non-OK status raises.
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import os
 from dataclasses import dataclass
 from typing import List, Optional, Sequence
@@ -302,7 +303,7 @@ def _tensor(t: Optional[torch.Tensor], shape, dtype: torch.dtype, what: str, dev
         if optional:
             return None
         raise ValueError(f"{what}: a tensor is required")
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+    if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{what}: {dtype} of shape {tuple(shape)} expected, got {t.dtype} of shape {tuple(t.shape)}")
     if t.device != device or not t.is_contiguous():
         raise ValueError(f"{what}: contiguous and on {device} (the device of the call's stream) expected")
@@ -310,7 +311,9 @@ def _tensor(t: Optional[torch.Tensor], shape, dtype: torch.dtype, what: str, dev
 
 
 def _call_stream(stream):
-    s = stream if stream is not None else torch.cuda.current_stream()
+    if stream is None:
+        return torch.cuda.current_stream()
+    s = stream
     if s.device != torch.device("cuda", torch.cuda.current_device()):
         raise ValueError(f"the stream belongs to {s.device}, which is not the current device")
     return s
@@ -402,6 +405,11 @@ def dll_vocab_loss_grad(v: VocabSpec, x, w, bias, labels, scale, row_loss, row_l
         "dll_vocab_loss_grad")
 
 
+_DTYPE_OF = operator.attrgetter("dtype")
+_NUMEL, _CONTIGUOUS = torch.Tensor.numel, torch.Tensor.is_contiguous
+_DEVICE_OF, _ADDRESS = torch.Tensor.get_device, torch.Tensor.data_ptr
+
+
 @dataclass
 class TensorList:
     """Numbers of elements and types of a list of gradients, kept for the calls on them."""
@@ -409,6 +417,8 @@ class TensorList:
     counts: object
     dtypes: object
     torch_types: List[torch.dtype]
+    numels: List[int]
+    array: type   # of n addresses
 
 
 def tensor_list(grads: Sequence[torch.Tensor]) -> TensorList:
@@ -418,21 +428,29 @@ def tensor_list(grads: Sequence[torch.Tensor]) -> TensorList:
             raise ValueError(f"gradients are float32 or bfloat16, got {g.dtype}")
     counts = (C.c_size_t * len(grads))(*[g.numel() for g in grads])
     dtypes = (C.c_int * len(grads))(*[DTYPE[names[g.dtype]] for g in grads])
-    return TensorList(dll_tensor_list(len(grads), counts, dtypes), counts, dtypes, [g.dtype for g in grads])
+    return TensorList(dll_tensor_list(len(grads), counts, dtypes), counts, dtypes, [g.dtype for g in grads],
+                      list(counts), C.c_void_p * len(grads))
 
 
 def _list_ptrs(tensors: Sequence[Optional[torch.Tensor]], l: TensorList, dtypes, what: str, dev, optional: bool = False):
     """Addresses of one tensor for each entry of the list, of any shape with as many elements."""
-    if len(tensors) != l.desc.n:
-        raise ValueError(f"{what}: {l.desc.n} tensors expected, got {len(tensors)}")
-    for t, n, dtype in zip(tensors, l.counts, dtypes):
+    n = l.desc.n
+    if len(tensors) != n:
+        raise ValueError(f"{what}: {n} tensors expected, got {len(tensors)}")
+    if not any(t is None for t in tensors):
+        # the whole list at a time: a call over hundreds of tensors would spend longer on checks one by one than on the GPU
+        index = -1 if dev.type == "cpu" else dev.index
+        if (list(map(_DTYPE_OF, tensors)) == dtypes and list(map(_NUMEL, tensors)) == l.numels and all(map(_CONTIGUOUS, tensors))
+                and list(map(_DEVICE_OF, tensors)).count(index) == n):
+            return l.array(*map(_ADDRESS, tensors))
+    for t, k, dtype in zip(tensors, l.numels, dtypes):
         if t is None:
-            if optional or n == 0:
+            if optional or k == 0:
                 continue
             raise ValueError(f"{what}: a tensor is required")
-        if t.dtype != dtype or t.numel() != n or t.device != dev or not t.is_contiguous():
-            raise ValueError(f"{what}: contiguous {dtype} with {n} elements on {dev} expected, got {t.dtype} with {t.numel()} on {t.device}")
-    return (C.c_void_p * len(tensors))(*[None if t is None else t.data_ptr() for t in tensors])
+        if t.dtype != dtype or t.numel() != k or t.device != dev or not t.is_contiguous():
+            raise ValueError(f"{what}: contiguous {dtype} with {k} elements on {dev} expected, got {t.dtype} with {t.numel()} on {t.device}")
+    return l.array(*[None if t is None else t.data_ptr() for t in tensors])
 
 
 def dll_grad_norm_workspace_bytes(l: TensorList) -> int:

@@ -49,22 +49,26 @@ __device__ __forceinline__ float gate_value(int gate, float a) {
   return f;
 }
 
-// h = act(a) * b from a piece whose columns 0..31 are a and 32..63 are b of the same hidden units; h in padded rows
+// h = act(a) * b from a piece whose first half's columns are a and whose second half's are b of the same hidden units; h in
+// padded rows
 template <class T>
-struct GateEpi {
-  int gate, vec, vec_kept;
+struct GateEpi : NothingAhead {
+  GateEpi(int gate_, int vec_kept_, T *h_, long ldh_, T *a_, T *b_) : gate(gate_), vec_kept(vec_kept_), h(h_), ldh(ldh_), kept_a(a_), kept_b(b_) {}
+  int gate, vec_kept;
   T *h;
   long ldh;
   T *kept_a, *kept_b;   // nullable, [T][H]
-  __device__ __forceinline__ void piece(const float *stage, int m, int n, int M, int H, int, int) const {
-    const int lane = threadIdx.x & 63, col = 8 * (lane & 3);
+  template <int WC>
+  __device__ __forceinline__ void piece(const float *stage, int m, int n, int M, int H, int, int, int, Nothing) const {
+    const Lanes<WC / 2> l;
+    const int col = l.col;
 #pragma unroll
-    for (int p = 0; p < 2; ++p) {
-      const int row = 16 * p + (lane >> 2);
+    for (int p = 0; p < l.kPasses; ++p) {
+      const int row = l.kRows * p + l.row;
       if (m + row >= M || n + col >= H) continue;
       float va[8], vb[8], vh[8];
       stage8(stage, row, col, va);
-      stage8(stage, row, 32 + col, vb);
+      stage8(stage, row, WC / 2 + col, vb);
       const int left = H - n - col;
 #pragma unroll
       for (int j = 0; j < 8; ++j) vh[j] = j < left ? gate_value(gate, va[j]) * vb[j] : 0.0f;
@@ -80,30 +84,40 @@ struct GateEpi {
 
 // da, db and h from dh and the kept a and b, all three in padded rows
 template <class T>
-struct GateBackEpi {
+struct GateBackEpi : NothingAhead {
+  GateBackEpi(int gate_, int vec_kept_, const T *a_, const T *b_, T *da_, T *db_, T *h_, long ld_)
+      : gate(gate_), vec_kept(vec_kept_), a(a_), b(b_), da(da_), db(db_), h(h_), ld(ld_) {}
   int gate, vec_kept;
   const T *a, *b;
   T *da, *db, *h;
   long ld;
-  __device__ __forceinline__ void piece(const float *stage, int m, int n, int M, int H, int, int) const {
-    const int lane = threadIdx.x & 63, col = 8 * (lane & 7);
+  template <int WC>
+  __device__ __forceinline__ void piece(const float *stage, int m, int n, int M, int H, int, int, int, Nothing) const {
+    const Lanes<WC> l;
+    const int col = l.col, left = H - n - col;
+    if (left <= 0) return;
+    const bool whole = vec_kept && left >= 8;
+    Eight<T> va[l.kPasses], vb[l.kPasses];   // all loads of the piece go out together
 #pragma unroll
-    for (int p = 0; p < 4; ++p) {
-      const int row = 8 * p + (lane >> 3);
-      if (m + row >= M || n + col >= H) continue;
-      const int left = H - n - col;
-      const bool whole = vec_kept && left >= 8;
-      float g[8], va[8], vb[8], oa[8], ob[8], oh[8];
+    for (int p = 0; p < l.kPasses; ++p) {
+      const int row = min(m + l.kRows * p + l.row, M - 1);
+      va[p].load(a + (long)row * H + n + col, whole, left);
+      vb[p].load(b + (long)row * H + n + col, whole, left);
+    }
+#pragma unroll
+    for (int p = 0; p < l.kPasses; ++p) {
+      const int row = l.kRows * p + l.row;
+      if (m + row >= M) continue;
+      float g[8], oa[8], ob[8], oh[8];
       stage8(stage, row, col, g);
-      load8<T>(a + (long)(m + row) * H + n + col, va, whole, left);
-      load8<T>(b + (long)(m + row) * H + n + col, vb, whole, left);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
+        const float va_ = (float)va[p].v[j], vb_ = (float)vb[p].v[j];
         float f, d;
-        gate_both(gate, va[j], &f, &d);
-        oa[j] = j < left ? g[j] * vb[j] * d : 0.0f;
+        gate_both(gate, va_, &f, &d);
+        oa[j] = j < left ? g[j] * vb_ * d : 0.0f;
         ob[j] = j < left ? g[j] * f : 0.0f;
-        oh[j] = j < left ? f * vb[j] : 0.0f;
+        oh[j] = j < left ? f * vb_ : 0.0f;
       }
       const long o = (long)(m + row) * ld + n + col;
       store8<T>(da + o, oa, true, 8);
@@ -118,9 +132,9 @@ __global__ __launch_bounds__(256) void pad_rows_kernel(const T *src, T *dst, lon
   const long groups = ld / 8, n = rows * groups;
   for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) {
     const long r = i / groups, c = (i - r * groups) * 8;
-    const int left = (int)(cols - c < 8 ? cols - c : 8);
+    const int left = (int)(cols - c < 8 ? cols - c : 8);   // negative in the padding
     float v[8];
-    load8<T>(src + r * cols + c, v, false, left);
+    load8<T>(src + r * cols + (left > 0 ? c : 0), v, false, left);
     store8<T>(dst + r * ld + c, v, true, 8);
   }
 }
@@ -143,7 +157,7 @@ struct FwdPlan {
     if (!whole_groups(H, dtype)) wd = take((size_t)D * ldh * e);
     up = plan_product(dtype, T, H, slabs_of(D, dtype), 1, true, false);
     down = plan_product(dtype, T, D, slabs_of(H, dtype), 1, false, true);
-    part = down.splits > 1 ? (float *)take((size_t)down.splits * T * padded(D) * sizeof(float)) : nullptr;
+    part = (float *)take(partial_bytes(down.splits, T, D));
     bytes = take.used;
   }
 };
@@ -152,7 +166,7 @@ struct BwdPlan {
   long ldh, ldd;
   void *da, *db, *h, *x, *wg, *wu, *wd, *dy;
   float *part;
-  ProductPlan dh, dw_down, dw_up, dx;
+  ProductPlan dh, gradients;
   size_t bytes;
   BwdPlan(int T, int D, int H, int dtype, char *base) {
     Take take{base};
@@ -166,10 +180,10 @@ struct BwdPlan {
     if (!whole_groups(D, dtype)) x = take((size_t)T * ldd * e), dy = take((size_t)T * ldd * e), wg = take((size_t)H * ldd * e), wu = take((size_t)H * ldd * e);
     if (!whole_groups(H, dtype)) wd = take((size_t)D * ldh * e);
     dh = plan_product(dtype, T, H, slabs_of(D, dtype), 1, false, false);
-    dw_down = plan_product(dtype, D, H, slabs_of(T, dtype), 1, false, false);
-    dw_up = plan_product(dtype, H, D, slabs_of(T, dtype), 2, false, false);
-    dx = plan_product(dtype, T, D, 2 * slabs_of(H, dtype), 1, false, true);
-    part = dx.splits > 1 ? (float *)take((size_t)dx.splits * T * padded(D) * sizeof(float)) : nullptr;
+    const long tokens = slabs_of(T, dtype);
+    const GradientShape shape[3] = {{T, D, 2 * slabs_of(H, dtype), 1, true}, {H, D, tokens, 2, false}, {D, H, tokens, 1, false}};
+    gradients = plan_gradients(dtype, shape, 3);
+    part = (float *)take(partial_bytes(gradients.splits, T, D));
     bytes = take.used;
   }
 };
@@ -195,16 +209,16 @@ hipError_t gated_fwd(const GatedArgs &a, char *scratch, hipStream_t stream) {
   g.A[0] = {x, ldx};
   g.B[0] = {wg, ldx};
   g.B[1] = {wu, ldx};
-  g.K[0] = (int)ldx;
-  GateEpi<T> ge{a.gate, 1, rows16<T>(a.gate_pre, a.H) && rows16<T>(a.up_pre, a.H), (T *)p.h, p.ldh, (T *)a.gate_pre, (T *)a.up_pre};
+  g.K[0] = a.D;
+  const GateEpi<T> ge(a.gate, rows16<T>(a.gate_pre, a.H) && rows16<T>(a.up_pre, a.H), (T *)p.h, p.ldh, (T *)a.gate_pre, (T *)a.up_pre);
   DLL_TRY((launch_product<T, true, true, true>(g, ge, p.up.tiling, stream)));
   ProductArgs y;
   y.M = a.T;
   y.N = a.D;
   y.A[0] = {p.h, p.ldh};
   y.B[0] = {wd, ldd};
-  y.K[0] = (int)ldd;
-  StoreEpi<T> out{{(T *)a.y, nullptr}, a.D, rows16<T>(a.y, a.D), nullptr, 0};
+  y.K[0] = a.H;
+  StoreEpi<T> out((T *)a.y, nullptr, a.D, rows16<T>(a.y, a.D), nullptr, 0);
   return product_to<T, true, true>(y, out, p.down, p.part, stream);
 }
 
@@ -235,18 +249,22 @@ hipError_t gated_bwd(const GatedArgs &a, char *scratch, hipStream_t stream) {
   g.A[0] = {dy, ldx};
   g.B[0] = {wd, ldd};
   g.K[0] = a.D;   // Wd lies across k; where D is no multiple of a 16-byte group, dy's copy has zeros behind it
-  GateBackEpi<T> ge{a.gate, rows16<T>(a.gate_pre, a.H) && rows16<T>(a.up_pre, a.H), (const T *)a.gate_pre, (const T *)a.up_pre,
-                    (T *)p.da, (T *)p.db, (T *)p.h, p.ldh};
+  const GateBackEpi<T> ge(a.gate, rows16<T>(a.gate_pre, a.H) && rows16<T>(a.up_pre, a.H), (const T *)a.gate_pre, (const T *)a.up_pre,
+                    (T *)p.da, (T *)p.db, (T *)p.h, p.ldh);
   DLL_TRY((launch_product<T, true, false, false>(g, ge, p.dh.tiling, stream)));
-  if (a.dw_down) {
+  GradientJobs<T> jobs;
+  jobs.plan = p.gradients;
+  jobs.partial = p.part;
+  if (a.dx) {
     ProductArgs w;
-    w.M = a.D;
-    w.N = a.H;
-    w.A[0] = {dy, ldx};
-    w.B[0] = {p.h, p.ldh};
-    w.K[0] = a.T;
-    StoreEpi<T> out{{(T *)a.dw_down, nullptr}, a.H, rows16<T>(a.dw_down, a.H), nullptr, 0};
-    DLL_TRY((launch_product<T, false, false, false>(w, out, p.dw_down.tiling, stream)));
+    w.M = a.T;
+    w.N = a.D;
+    w.A[0] = {p.da, p.ldh};
+    w.A[1] = {p.db, p.ldh};
+    w.B[0] = {wg, ldx};
+    w.B[1] = {wu, ldx};
+    w.K[0] = w.K[1] = a.H;
+    jobs.add(w, StoreEpi<T>((T *)a.dx, nullptr, a.D, rows16<T>(a.dx, a.D), nullptr, 0), true);
   }
   if (a.dw_gate || a.dw_up) {
     ProductArgs w;
@@ -260,22 +278,18 @@ hipError_t gated_bwd(const GatedArgs &a, char *scratch, hipStream_t stream) {
     w.A[1] = {d[1], p.ldh};
     w.B[0] = w.B[1] = {x, ldx};
     w.K[0] = a.T;
-    StoreEpi<T> out{{o[first], o[1]}, a.D, rows16<T>(o[first], a.D) && rows16<T>(o[w.problems - 1], a.D), nullptr, 0};
-    DLL_TRY((launch_product<T, false, false, false>(w, out, p.dw_up.tiling, stream)));
+    jobs.add(w, StoreEpi<T>(o[first], o[1], a.D, rows16<T>(o[first], a.D) && rows16<T>(o[w.problems - 1], a.D), nullptr, 0), false);
   }
-  if (a.dx) {
+  if (a.dw_down) {
     ProductArgs w;
-    w.M = a.T;
-    w.N = a.D;
-    w.A[0] = {p.da, p.ldh};
-    w.A[1] = {p.db, p.ldh};
-    w.B[0] = {wg, ldx};
-    w.B[1] = {wu, ldx};
-    w.K[0] = w.K[1] = a.H;
-    StoreEpi<T> out{{(T *)a.dx, nullptr}, a.D, rows16<T>(a.dx, a.D), nullptr, 0};
-    DLL_TRY((product_to<T, true, false>(w, out, p.dx, p.part, stream)));
+    w.M = a.D;
+    w.N = a.H;
+    w.A[0] = {dy, ldx};
+    w.B[0] = {p.h, p.ldh};
+    w.K[0] = a.T;
+    jobs.add(w, StoreEpi<T>((T *)a.dw_down, nullptr, a.H, rows16<T>(a.dw_down, a.H), nullptr, 0), false);
   }
-  return hipSuccess;
+  return launch_gradients<T>(jobs, stream);
 }
 
 }  // namespace

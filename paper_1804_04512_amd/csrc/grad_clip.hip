@@ -5,7 +5,7 @@
 // The tensors' addresses travel in the kernel arguments (kTable of them a launch), so a call copies nothing and can be
 // captured.  Squares are added in 64 bits: no gradient overflows or vanishes in the sum, whose order is fixed.  What bounds
 // both kernels is memory: the norm reads the gradients once; the second kernel adds the few partial sums again in
-// every workgroup, which saves a launch between the two.
+// every workgroup, which saves a launch between the two.  Small networks' gradients stay in one workgroup's registers.
 #include "large_ops.h"
 #include "tile_product.h"
 
@@ -17,7 +17,9 @@ namespace {
 
 constexpr int kTable = 64;          // tensors of a launch
 constexpr int kChunk = 8192;        // elements a workgroup takes at a time
-constexpr int kPartials = 1024;     // workgroups of the norm, over all its launches
+constexpr int kPartials = 1024;     // workgroups of a launch of the norm: four a compute unit
+constexpr int kJoinAt = 2048;       // more partial sums than this are added up by a launch of their own
+constexpr int kFewGroups = 4096;    // runs of eight elements that one workgroup keeps in registers
 
 struct NormTable {
   int n, chunks;
@@ -91,11 +93,43 @@ __global__ __launch_bounds__(256) void grad_squares_kernel(const NormTable t, do
   if (threadIdx.x == 0) partial[blockIdx.x] = s;
 }
 
+__device__ __forceinline__ const NormTable &table_of(const NormTable &t) { return t; }
+__device__ __forceinline__ const NormTable &table_of(const ClipTable &t) { return t.t; }
+__device__ __forceinline__ const NormTable &table_of(const StepTable &t) { return t.t; }
+__device__ __forceinline__ void few_apply(const NormTable &, int, long, int, float (&)[8], float, float, float) {}
+__device__ __forceinline__ void few_apply(const ClipTable &a, int i, long at, int left, float (&g)[8], float c, float, float) {
+  if (c == 1.0f && a.out[i] == a.t.g[i]) return;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) g[j] *= c;
+  if (a.t.type[i] == TYPE_BF16) store8<bf16>((bf16 *)a.out[i] + at, g, a.t.vec[i] && left == 8, left);
+  else store8<float>((float *)a.out[i] + at, g, a.t.vec[i] && left == 8, left);
+}
+__device__ __forceinline__ void few_apply(const StepTable &a, int i, long at, int left, float (&g)[8], float c, float step, float mu) {
+  const bool whole = a.t.vec[i] && left == 8;
+  float p[8], v[8];
+  load8<float>(a.p[i] + at, p, whole, left);
+  load8<float>(a.v[i] + at, v, whole, left);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) update_param(&p[j], &v[j], g[j] * c, step, mu, a.decay[i]);
+  store8<float>(a.p[i] + at, p, whole, left);
+  store8<float>(a.v[i] + at, v, whole, left);
+  if (a.copy[i]) store8<bf16>(a.copy[i] + at, p, whole, left);
+}
+
 // the norm from the partial sums, the same in every workgroup
 __device__ __forceinline__ double norm_of(const double *partial, int n) {
   double s = 0.0;
+#pragma unroll 8
   for (int i = threadIdx.x; i < n; i += 256) s += partial[i];
   return sqrt(group_sum(s));
+}
+
+__global__ __launch_bounds__(256) void join_squares_kernel(const double *partial, int n, double *sum) {
+  double s = 0.0;
+#pragma unroll 8
+  for (int i = threadIdx.x; i < n; i += 256) s += partial[i];
+  s = group_sum(s);
+  if (threadIdx.x == 0) *sum = s;
 }
 
 __global__ __launch_bounds__(256) void norm_kernel(const double *partial, int n, float *norm) {
@@ -177,14 +211,64 @@ __global__ __launch_bounds__(256) void momentum_step_kernel(const StepTable a, c
   }
 }
 
+// All gradients in one workgroup's registers: norm and what follows it in one launch.  A thread takes up to four runs of eight
+// elements; runs are numbered through the tensors (t.first counts runs here).
+enum { kFewNorm = 0, kFewClip, kFewStep };
+template <int WHAT, class Table>
+__global__ __launch_bounds__(1024) void few_kernel(const Table a, float max_norm, float step, float mu, float *norm) {
+  __shared__ double part[16];
+  const NormTable &t = table_of(a);
+  float g[4][8];
+  int tensor[4];
+  double s = 0.0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int run = k * 1024 + (int)threadIdx.x;
+    tensor[k] = run < t.chunks ? tensor_of(t, run) : -1;
+    if (tensor[k] >= 0) {
+      const int i = tensor[k];
+      const long at = (long)(run - t.first[i]) * 8;
+      const int left = (int)min(8L, t.count[i] - at);
+      if (t.type[i] == TYPE_BF16) load8<bf16>((const bf16 *)t.g[i] + at, g[k], t.vec[i] && left == 8, left);
+      else load8<float>((const float *)t.g[i] + at, g[k], t.vec[i] && left == 8, left);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) g[k][j] = 0.0f;
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s += (double)g[k][j] * (double)g[k][j];
+#pragma unroll
+  for (int k = 32; k > 0; k >>= 1) s += __shfl_xor(s, k);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+  __syncthreads();
+  s = 0.0;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) s += part[w];
+  const double x = sqrt(s);
+  if (threadIdx.x == 0) *norm = (float)x;
+  if (WHAT == kFewNorm || (WHAT == kFewStep && !isfinite(x))) return;
+  const float c = x > (double)max_norm && isfinite(x) ? (float)((double)max_norm / x) : 1.0f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int i = tensor[k];
+    if (i < 0) continue;
+    const long at = (long)(k * 1024 + (int)threadIdx.x - t.first[i]) * 8;
+    const int left = (int)min(8L, t.count[i] - at);
+    few_apply(a, i, at, left, g[k], c, step, mu);
+  }
+}
+
 bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 
 // Tensors [at, at + kTable) of the list that hold anything; returns where the next table starts
-int fill(NormTable &t, const GradList &l, const void *const *grads, int at, int *which) {
+int fill(NormTable &t, const GradList &l, const void *const *grads, int at, int *which, int chunk = kChunk) {
   t.n = t.chunks = 0;
   for (; at < l.n && t.n < kTable; ++at) {
     if (l.counts[at] == 0) continue;
-    const long chunks = ((long)l.counts[at] + kChunk - 1) / kChunk;
+    const long chunks = ((long)l.counts[at] + chunk - 1) / chunk;
     if (t.chunks + chunks > 0x40000000L) break;   // of one launch; a tensor has 2^31 elements at most
     which[t.n] = at;
     t.g[t.n] = grads[at];
@@ -199,36 +283,58 @@ int fill(NormTable &t, const GradList &l, const void *const *grads, int at, int 
   return at;
 }
 
-hipError_t launch_squares(const GradList &l, const void *const *grads, double *partial, int *used, hipStream_t stream) {
-  long total = 0;
-  for (int i = 0; i < l.n; ++i) total += ((long)l.counts[i] + kChunk - 1) / kChunk;
+// The partial sums of all gradients' squares: `used` of them from *partial, joined to one where they are many
+hipError_t launch_squares(const GradList &l, const void *const *grads, double **partial, int *used, hipStream_t stream) {
   *used = 0;
   int which[kTable];
   for (int at = 0; at < l.n;) {
     NormTable t;
     at = fill(t, l, grads, at, which);
     if (t.n == 0) break;
-    // workgroups in proportion to the work, all launches together at most kPartials (and one each)
-    long blocks = total <= kPartials / 2 ? t.chunks : (long)((double)t.chunks / total * (kPartials / 2));
-    if (blocks < 1) blocks = 1;
-    grad_squares_kernel<<<dim3((unsigned)blocks), dim3(256), 0, stream>>>(t, partial + *used);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    *used += (int)blocks;
+    const int blocks = t.chunks < kPartials ? t.chunks : kPartials;
+    grad_squares_kernel<<<dim3((unsigned)blocks), dim3(256), 0, stream>>>(t, *partial + *used);
+    DLL_TRY(hipGetLastError());
+    *used += blocks;
+  }
+  if (*used > kJoinAt) {
+    double *sum = *partial + *used;
+    join_squares_kernel<<<dim3(1), dim3(256), 0, stream>>>(*partial, *used, sum);
+    DLL_TRY(hipGetLastError());
+    *partial = sum;
+    *used = 1;
   }
   return hipSuccess;
 }
 
-unsigned apply_blocks(int chunks) { return (unsigned)(chunks < 8 * chip().cus ? chunks : 8 * chip().cus); }
+// Whether few_kernel takes the list: at most kTable tensors that hold anything, kFewGroups runs
+bool is_few(const GradList &l) {
+  long runs = 0;
+  int n = 0;
+  for (int i = 0; i < l.n; ++i) {
+    runs += ((long)l.counts[i] + 7) / 8;
+    n += l.counts[i] > 0;
+    if (runs > kFewGroups || n > kTable) return false;
+  }
+  return true;
+}
+
+unsigned apply_blocks(int chunks) { return (unsigned)(chunks < 1 ? 1 : chunks < 8 * chip().cus ? chunks : 8 * chip().cus); }
 
 }  // namespace
 
-size_t grad_norm_scratch(const GradList &l) { return ((size_t)kPartials + l.n / kTable + 1) * sizeof(double); }
+size_t grad_norm_scratch(const GradList &l) { return ((size_t)kPartials * (l.n / kTable + 1) + 1) * sizeof(double); }
 
 hipError_t launch_grad_norm(const GradList &l, const void *const *grads, float *norm, char *scratch, hipStream_t stream) {
   double *partial = (double *)scratch;
   int used = 0;
-  DLL_TRY(launch_squares(l, grads, partial, &used, stream));
+  if (is_few(l)) {
+    NormTable t;
+    int which[kTable];
+    fill(t, l, grads, 0, which, 8);
+    few_kernel<kFewNorm, NormTable><<<dim3(1), dim3(1024), 0, stream>>>(t, 0.0f, 0.0f, 0.0f, norm);
+    return hipGetLastError();
+  }
+  DLL_TRY(launch_squares(l, grads, &partial, &used, stream));
   norm_kernel<<<dim3(1), dim3(256), 0, stream>>>(partial, used, norm);
   return hipGetLastError();
 }
@@ -236,15 +342,17 @@ hipError_t launch_grad_norm(const GradList &l, const void *const *grads, float *
 hipError_t launch_grad_clip(const GradList &l, const void *const *grads, void *const *out, float max_norm, float *norm, char *scratch, hipStream_t stream) {
   double *partial = (double *)scratch;
   int used = 0, which[kTable], at = 0;
-  DLL_TRY(launch_squares(l, grads, partial, &used, stream));
+  const bool few = is_few(l);
+  if (!few) DLL_TRY(launch_squares(l, grads, &partial, &used, stream));
   do {
     ClipTable a;
-    at = fill(a.t, l, grads, at, which);
+    at = fill(a.t, l, grads, at, which, few ? 8 : kChunk);
     for (int i = 0; i < a.t.n; ++i) {
       a.out[i] = out[which[i]];
       a.t.vec[i] = a.t.vec[i] && aligned16(a.out[i]);
     }
-    grad_scale_kernel<<<dim3(a.t.n ? apply_blocks(a.t.chunks) : 1), dim3(256), 0, stream>>>(a, partial, used, max_norm, norm);
+    if (few) few_kernel<kFewClip, ClipTable><<<dim3(1), dim3(1024), 0, stream>>>(a, max_norm, 0.0f, 0.0f, norm);
+    else grad_scale_kernel<<<dim3(apply_blocks(a.t.chunks)), dim3(256), 0, stream>>>(a, partial, used, max_norm, norm);
     DLL_TRY(hipGetLastError());
   } while (at < l.n);
   return hipSuccess;
@@ -254,10 +362,11 @@ hipError_t launch_momentum_clipped(const GradList &l, float *const *params, floa
                                    float max_norm, float *norm, void *const *copies, char *scratch, hipStream_t stream) {
   double *partial = (double *)scratch;
   int used = 0, which[kTable], at = 0;
-  DLL_TRY(launch_squares(l, grads, partial, &used, stream));
+  const bool few = is_few(l);
+  if (!few) DLL_TRY(launch_squares(l, grads, &partial, &used, stream));
   do {
     StepTable a;
-    at = fill(a.t, l, grads, at, which);
+    at = fill(a.t, l, grads, at, which, few ? 8 : kChunk);
     for (int i = 0; i < a.t.n; ++i) {
       const int k = which[i];
       a.p[i] = params[k];
@@ -266,7 +375,8 @@ hipError_t launch_momentum_clipped(const GradList &l, float *const *params, floa
       a.decay[i] = decay ? decay[k] : 0.0f;
       a.t.vec[i] = a.t.vec[i] && aligned16(a.p[i]) && aligned16(a.v[i]) && aligned16(a.copy[i]);
     }
-    momentum_step_kernel<<<dim3(a.t.n ? apply_blocks(a.t.chunks) : 1), dim3(256), 0, stream>>>(a, partial, used, max_norm, -lr, mu, norm);
+    if (few) few_kernel<kFewStep, StepTable><<<dim3(1), dim3(1024), 0, stream>>>(a, max_norm, -lr, mu, norm);
+    else momentum_step_kernel<<<dim3(apply_blocks(a.t.chunks)), dim3(256), 0, stream>>>(a, partial, used, max_norm, -lr, mu, norm);
     DLL_TRY(hipGetLastError());
   } while (at < l.n);
   return hipSuccess;

@@ -10,8 +10,8 @@ enum { TYPE_F32 = 0, TYPE_BF16 = 1 };
 enum { GATE_IDENTITY = 0, GATE_SIGMOID = 1, GATE_RELU = 2, GATE_SILU = 3, GATE_GELU = 4 };
 
 inline size_t type_bytes(int dtype) { return dtype == TYPE_BF16 ? 2 : 4; }
-// Elements of a row that is kept in the workspace: whole 16-byte groups (of either type).
-inline long padded(long n) { return (n + 7) & ~7L; }
+// Elements of a row that is kept in the workspace: whole 128-byte lines (of either type), so that no slab's row takes two.
+inline long padded(long n) { return (n + 63) & ~63L; }
 // Rows of n elements that a product can load as they are; others are copied into padded rows first.
 inline bool whole_groups(long n, int dtype) { return n * (long)type_bytes(dtype) % 16 == 0; }
 

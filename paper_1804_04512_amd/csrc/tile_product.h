@@ -39,7 +39,7 @@ typedef short shortx8 __attribute__((ext_vector_type(8)));
 
 constexpr int kSlabBytes = 128;              // of one row along k
 constexpr unsigned kOutOfRange = 0xFFFFFFF0u;
-constexpr int kStageLd = 68;                 // floats: row stride of an epilogue piece (64 columns)
+constexpr int kStageLd = 68;                 // floats: row stride of an epilogue piece (64 or 32 columns)
 
 template <class T> struct Elem;
 template <> struct Elem<bf16> { static constexpr int kSlab = 64; typedef bf16x8 Frag; };
@@ -68,11 +68,13 @@ __device__ __forceinline__ int rows_left(const int *rows, int first, int most) {
   return rows ? max(0, min(most, *rows - first)) : most;
 }
 
-// Workgroups are dealt to the 8 XCDs in turn; each XCD gets a contiguous run of tiles, eight tile rows high, so that the 32
-// tiles it works on at a time share their operands in its L2.
-__device__ __forceinline__ void tile_of(int id, int tiles_m, int tiles_n, int *tm, int *tn) {
-  const int n = tiles_m * tiles_n, q = n >> 3, r = n & 7, xcd = id & 7, i = id >> 3;
-  const int t = xcd * q + min(xcd, r) + i;
+// Workgroups are dealt to the 8 XCDs in turn; each XCD gets a contiguous run of tiles (of one part of k or problem after the
+// other), eight tile rows high, so that the 32 tiles it works on at a time share their operands in its L2.
+__device__ __forceinline__ void tile_of(int id, int tiles_m, int tiles_n, int units, int *tm, int *tn, int *unit) {
+  const int tiles = tiles_m * tiles_n, n = tiles * units, q = n >> 3, r = n & 7, xcd = id & 7, i = id >> 3;
+  int t = xcd * q + min(xcd, r) + i;
+  *unit = t / tiles;
+  t -= *unit * tiles;
   constexpr int kRows = 8;
   const int group = t / (kRows * tiles_n), first = group * kRows, rows = min(kRows, tiles_m - first), at = t - group * kRows * tiles_n;
   *tm = first + at % rows;
@@ -143,20 +145,20 @@ struct Slab {
   }
 };
 
-// A gate's and an up projection's rows side by side: rows 64 w + 0..31 of the tile are gate rows 32 w + .., the next 32 the
-// same rows of the up projection, so that a wavefront's 64 columns hold both factors of 32 hidden units.
-template <class T, int X, int THREADS>
+// A gate's and an up projection's rows side by side: of each wavefront's WC columns the first half are gate rows and the
+// second half the same rows of the up projection, so that a wavefront holds both factors of WC / 2 hidden units.
+template <class T, int X, int WC, int THREADS>
 struct PairSlab {
   typedef Slab<T, X, true, THREADS> Base;
   static constexpr int kBytes = Base::kBytes, kIts = Base::kIts;
-  static_assert(Base::kStep % 32 == 0 || 32 % Base::kStep == 0, "a wavefront's rows lie in one projection");
+  static_assert(WC % 16 == 0, "the eight rows of a wavefront's load lie in one projection");
   unsigned off[kIts];
   __device__ __forceinline__ void init(long ld, int t) {
     const int place = t & 7, row0 = t >> 3;
 #pragma unroll
     for (int it = 0; it < kIts; ++it) {
       const int row = row0 + it * Base::kStep;
-      off[it] = (unsigned)((long)((row >> 6) * 32 + (row & 31)) * ld * (int)sizeof(T)) + 16u * Base::group_of(row, place);
+      off[it] = (unsigned)((long)((row / WC) * (WC / 2) + row % (WC / 2)) * ld * (int)sizeof(T)) + 16u * Base::group_of(row, place);
     }
   }
   // x0: the tile's first hidden unit; H: hidden units
@@ -168,7 +170,7 @@ struct PairSlab {
     const int t = (int)(threadIdx.x % THREADS), place = t & 7, row0 = t >> 3;
 #pragma unroll
     for (int it = 0; it < kIts; ++it) {
-      const bool second = ((wave * 8 + it * Base::kStep) >> 5) & 1;
+      const bool second = (wave * 8 + it * Base::kStep) % WC >= WC / 2;
       const uintx4 rs = buffer_of((const char *)(second ? up.p : gate.p) + first * (long)sizeof(T), (unsigned)bytes);
       const bool out = cut && k0 + Base::group_of(row0 + it * Base::kStep, place) * (16 / (int)sizeof(T)) >= K;
       load_to_lds(rs, out ? kOutOfRange : off[it], lds + (it * THREADS + wave * 64) * 16);
@@ -222,35 +224,34 @@ __device__ __forceinline__ floatx16 mfma(floatx4 b, floatx4 a, floatx16 c) {
 }
 
 // ------------------------------------------------------------------------------------------------ kernel
-// WK groups of WM x WN wavefronts of (BM / WM) x 64 each; the groups take the slabs in turn and their sums are added in LDS in
+// WK groups of WM x WN wavefronts of (BM / WM) x (BN / WN) each; the groups take the slabs in turn and their sums are added in LDS in
 // group order (products with too few tiles to fill the chip: the chain of slabs is WK times shorter).
-// Epi: `piece(stage, m, n, M, N, problem, split)` takes 32 x 64 sums from the wavefront's LDS area (row stride kStageLd
-// floats), first element C(m, n).
+// Epi: `piece<WC>(stage, m, n, M, N, problem, split, q, ahead)` takes 32 x WC sums (WC = 64 or 32) from the wavefront's LDS area
+// (row stride kStageLd floats), first element C(m, n), the wavefront's q-th piece along m; `ahead(m, M, lane)` is called before the products.
 // PAIR: B[0] and B[1] are the gate and up projections (KC), N counts hidden units, a tile covers BN / 2 of them.
 template <class T, int BM, int BN, int WM, int WN, int WK, bool AKC, bool BKC, bool PAIR, class Epi>
-__global__ __launch_bounds__(64 * WM *WN *WK, 2) void product_kernel(const ProductArgs a, const Epi epi) {
-  constexpr int kThreads = 64 * WM * WN, TM = BM / WM / 32, kK = Elem<T>::kSlab;
-  static_assert(BN / WN == 64 && BM % (32 * WM) == 0, "wavefront tiles are 64 columns wide");
+__device__ __forceinline__ void product_tile(const ProductArgs &a, const Epi &epi, int id, char *smem) {
+  constexpr int kThreads = 64 * WM * WN, TM = BM / WM / 32, WC = BN / WN, TN = WC / 32, kK = Elem<T>::kSlab;
+  static_assert((WC == 64 || WC == 32) && BM % (32 * WM) == 0, "wavefront tiles are 64 or 32 columns wide");
   typedef Slab<T, BM, AKC, kThreads> SA;
   typedef Slab<T, BN, BKC, kThreads> SB;
   constexpr int kA = SA::kBytes, kStage = SA::kBytes + SB::kBytes;
-  extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = all % (WM * WN), group = all / (WM * WN);
-  const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * 64;
-  int tm, tn;
-  tile_of(blockIdx.x, a.tiles_m, a.tiles_n, &tm, &tn);
-  const int problem = a.problems > 1 ? blockIdx.z : 0;
+  const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * WC;
+  int tm, tn, unit;
+  tile_of(id, a.tiles_m, a.tiles_n, a.splits * a.problems, &tm, &tn, &unit);
+  const int problem = unit / a.splits, split = unit % a.splits;
   const int M = rows_left(a.m_rows, a.first, a.M);
   const int K0 = rows_left(a.k_rows, a.first, a.K[0]);
   const int m0 = tm * BM, n0 = tn * (PAIR ? BN / 2 : BN);
   if (m0 >= M) return;
   const int slabs0 = (K0 + kK - 1) / kK, slabs = slabs0 + (a.K[1] + kK - 1) / kK;
-  const int t0 = min(slabs, (int)blockIdx.y * a.slabs_per_split), t1 = min(slabs, t0 + a.slabs_per_split);
+  const int t0 = min(slabs, split * a.slabs_per_split), t1 = min(slabs, t0 + a.slabs_per_split);
   const int turns = (t1 - t0 + WK - 1) / WK;   // a group's slabs: t0 + group, then every WK-th
 
   SA sa;
   SB sb;
-  PairSlab<T, BN, kThreads> sp;
+  PairSlab<T, BN, WC, kThreads> sp;
   sa.init(a.A[0].ld, threadIdx.x % kThreads);
   if (PAIR) sp.init(a.B[0].ld, threadIdx.x % kThreads);
   else sb.init(a.B[0].ld, threadIdx.x % kThreads);
@@ -267,20 +268,21 @@ __global__ __launch_bounds__(64 * WM *WN *WK, 2) void product_kernel(const Produ
     else sb.load(lds + kA, wave, a.B[which], n0, a.N, k0, K);
   };
 
-  floatx16 acc[TM][2];
+  floatx16 acc[TM][TN];
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) acc[i][j] = floatx16{};
+    for (int j = 0; j < TN; ++j) acc[i][j] = floatx16{};
+  const typename Epi::Ahead ahead = epi.ahead(m0 + wm, M, lane);   // what the epilogue wants on its way during the products
   const FragReader<T, BM, AKC> ra(lane);
   const FragReader<T, BN, BKC> rb(lane);
   // Fragments are read one step ahead of the products that take them.  The one barrier of a slab stands before its last
   // step: by then every wavefront holds its last fragments of this slab, so its place can take the slab after the next, and has
   // seen its part of the next slab land, whose first fragments are read behind the barrier while the last step multiplies.
-  typename Elem<T>::Frag fa[2][TM], fb[2][2];
+  typename Elem<T>::Frag fa[2][TM], fb[2][TN];
   const auto read = [&](int set, const char *lds, int s) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) fb[set][j] = rb(lds + kA, wn + 32 * j, s);
+    for (int j = 0; j < TN; ++j) fb[set][j] = rb(lds + kA, wn + 32 * j, s);
 #pragma unroll
     for (int i = 0; i < TM; ++i) fa[set][i] = ra(lds, wm + 32 * i, s);
     __builtin_amdgcn_sched_barrier(0);
@@ -289,7 +291,7 @@ __global__ __launch_bounds__(64 * WM *WN *WK, 2) void product_kernel(const Produ
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) acc[i][j] = mfma(fb[set][j], fa[set][i], acc[i][j]);
+      for (int j = 0; j < TN; ++j) acc[i][j] = mfma(fb[set][j], fa[set][i], acc[i][j]);
     __builtin_amdgcn_sched_barrier(0);
   };
   if (turns > 0) {
@@ -320,9 +322,9 @@ __global__ __launch_bounds__(64 * WM *WN *WK, 2) void product_kernel(const Produ
   __syncthreads();   // the slabs' place becomes the epilogue's
   constexpr int kPiece = 32 * kStageLd;
   float *stage = reinterpret_cast<float *>(smem) + all * kPiece;
-  const auto to_stage = [&](const floatx16 (&c)[2]) {
+  const auto to_stage = [&](const floatx16 (&c)[TN]) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < TN; ++j)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
         *reinterpret_cast<floatx4 *>(stage + (lane & 31) * kStageLd + 32 * j + 8 * r + 4 * (lane >> 5)) =
@@ -334,15 +336,15 @@ __global__ __launch_bounds__(64 * WM *WN *WK, 2) void product_kernel(const Produ
     __syncthreads();
     if (group > 0 || m0 + wm >= M) return;
 #pragma unroll
-    for (int e = 0; e < 32; e += 4) {   // four rows of 16 lanes' 16 bytes a step
-      float *p = stage + (e + (lane >> 4)) * kStageLd + 4 * (lane & 15);
+    for (int e = 0; e < 32; e += 256 / WC) {   // 16 bytes a lane
+      float *p = stage + (e + lane / (WC / 4)) * kStageLd + 4 * (lane % (WC / 4));
       floatx4 v = *reinterpret_cast<floatx4 *>(p);
 #pragma unroll
       for (int g = 1; g < WK; ++g) v += *reinterpret_cast<floatx4 *>(p + g * WM * WN * kPiece);
       *reinterpret_cast<floatx4 *>(p) = v;
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    epi.piece(stage, m0 + wm, PAIR ? n0 + wn / 2 : n0 + wn, M, a.N, problem, (int)blockIdx.y);
+    epi.template piece<WC>(stage, m0 + wm, PAIR ? n0 + wn / 2 : n0 + wn, M, a.N, problem, split, 0, ahead);
   } else {
 #pragma unroll 1   // one copy of the epilogue; the sums' registers are chosen by uniform branches
     for (int q = 0; q < TM; ++q) {
@@ -351,9 +353,15 @@ __global__ __launch_bounds__(64 * WM *WN *WK, 2) void product_kernel(const Produ
       for (int i = 0; i < TM; ++i)
         if (i == q) to_stage(acc[i]);
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      if (m0 + wm + 32 * q < M) epi.piece(stage, m0 + wm + 32 * q, PAIR ? n0 + wn / 2 : n0 + wn, M, a.N, problem, (int)blockIdx.y);
+      if (m0 + wm + 32 * q < M) epi.template piece<WC>(stage, m0 + wm + 32 * q, PAIR ? n0 + wn / 2 : n0 + wn, M, a.N, problem, split, q, ahead);
     }
   }
+}
+
+template <class T, int BM, int BN, int WM, int WN, int WK, bool AKC, bool BKC, bool PAIR, class Epi>
+__global__ __launch_bounds__(64 * WM *WN *WK, 2) void product_kernel(const ProductArgs a, const Epi epi) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  product_tile<T, BM, BN, WM, WN, WK, AKC, BKC, PAIR, Epi>(a, epi, blockIdx.x, smem);
 }
 
 // ------------------------------------------------------------------------------------------------ outputs
@@ -410,24 +418,55 @@ __device__ __forceinline__ void stage8(const float *stage, int row, int col, flo
 #pragma unroll
   for (int j = 0; j < 4; ++j) v[j] = a[j], v[4 + j] = b[j];
 }
+// eight neighbours of a row as they lie in memory
+template <class T> struct Eight {
+  typedef T V __attribute__((ext_vector_type(8)));
+  V v;
+  __device__ __forceinline__ void load(const T *p, bool whole, int n) {
+    if (whole) {
+      typedef V At16 __attribute__((aligned(16)));
+      v = *reinterpret_cast<const At16 *>(p);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = j < n ? p[j] : (T)0.0f;
+    }
+  }
+};
 // rows of ld elements may be accessed 16 bytes at a time
 template <class T> __host__ __device__ __forceinline__ bool rows16(const void *p, long ld) {
   return ((uintptr_t)p & 15) == 0 && ld * (long)sizeof(T) % 16 == 0;
 }
 
+// How a wavefront's lanes take a piece of 32 rows x WC columns: eight columns a lane, whole rows side by side, so that outputs leave
+// as full lines (runs of eight straight from the products' registers, 32 rows at a time, made the epilogues' stores 1.5 to 3
+// times as slow)
+template <int WC> struct Lanes {
+  static constexpr int kARow = WC / 8, kRows = 64 / kARow, kPasses = 32 / kRows;
+  int row, col;
+  __device__ __forceinline__ Lanes() : row((int)(threadIdx.x & 63) / kARow), col(8 * ((int)(threadIdx.x & 63) % kARow)) {}
+};
+struct Nothing {};
+struct NothingAhead {
+  typedef Nothing Ahead;
+  __device__ __forceinline__ Nothing ahead(int, int, int) const { return Nothing{}; }
+};
+
 // C[problem][m][n] in T, rows optionally through a map; or += to what a former piece left (fp32 sums)
 template <class T>
-struct StoreEpi {
+struct StoreEpi : NothingAhead {
+  StoreEpi(T *c0, T *c1, long ld_, int vec_, const int *rows_, int add_) : c{c0, c1}, ld(ld_), vec(vec_), rows(rows_), add(add_) {}
   T *c[2];
   long ld;
   int vec;                 // rows16 of both
   const int *rows;         // nullable: row m of the product goes to row rows[m]
   int add;                 // T = float only: add to what is there
-  __device__ __forceinline__ void piece(const float *stage, int m, int n, int M, int N, int problem, int) const {
-    const int lane = threadIdx.x & 63, col = 8 * (lane & 7);
+  template <int WC>
+  __device__ __forceinline__ void piece(const float *stage, int m, int n, int M, int N, int problem, int, int, Nothing) const {
+    const Lanes<WC> l;
+    const int col = l.col;
 #pragma unroll
-    for (int p = 0; p < 4; ++p) {
-      const int row = 8 * p + (lane >> 3);
+    for (int p = 0; p < l.kPasses; ++p) {
+      const int row = l.kRows * p + l.row;
       if (m + row >= M || n + col >= N) continue;
       float v[8];
       stage8(stage, row, col, v);
@@ -446,15 +485,18 @@ struct StoreEpi {
 };
 
 // Sums of one split of k in fp32, [split][M][N8], N8 = N rounded up to 8
-struct PartialEpi {
+struct PartialEpi : NothingAhead {
+  PartialEpi(float *part_, long rows_) : part(part_), rows(rows_) {}
   float *part;
   long rows;   // of a split (the M of the launch)
-  __device__ __forceinline__ void piece(const float *stage, int m, int n, int M, int N, int, int split) const {
-    const int lane = threadIdx.x & 63, col = 8 * (lane & 7);
+  template <int WC>
+  __device__ __forceinline__ void piece(const float *stage, int m, int n, int M, int N, int, int split, int, Nothing) const {
+    const Lanes<WC> l;
+    const int col = l.col;
     const long n8 = (N + 7) & ~7;
 #pragma unroll
-    for (int p = 0; p < 4; ++p) {
-      const int row = 8 * p + (lane >> 3);
+    for (int p = 0; p < l.kPasses; ++p) {
+      const int row = l.kRows * p + l.row;
       if (m + row >= M || n + col >= N) continue;
       float v[8];
       stage8(stage, row, col, v);
@@ -493,7 +535,7 @@ __global__ __launch_bounds__(256) void sum_splits_kernel(const float *part, int 
 
 // ------------------------------------------------------------------------------------------------ host
 // The tilings of a product: tile edges, and how many groups of wavefronts take the slabs in turn.
-enum Tiling { TILE_256 = 0, TILE_128, TILE_64_K2, TILE_64_K4, TILE_32_K4, TILINGS };
+enum Tiling { TILE_256 = 0, TILE_128, TILE_64_K2, TILE_64_K4, TILE_32_K4, TILE_32_K8, TILINGS };
 struct ProductPlan { int tiling = TILE_128, splits = 1; };
 
 // What a tiling costs, in microseconds, as measured on products of 512 to 8192 rows and columns: a workgroup's share of a
@@ -505,7 +547,8 @@ constexpr TilingCost kTilings[TILINGS] = {
     {128, 128, 1, 2, {2.08, 0.55}, {2.05, 0.66}, {4.0, 4.0}},
     {64, 64, 2, 2, {1.07, 0.42}, {1.15, 0.7}, {3.0, 3.0}},
     {64, 64, 4, 1, {2.1, 0.92}, {2.2, 0.95}, {3.5, 2.7}},
-    {32, 64, 4, 1, {1.05, 0.6}, {1.1, 0.75}, {3.0, 2.5}},
+    {32, 64, 4, 1, {1.35, 0.6}, {1.35, 0.75}, {3.5, 2.5}},
+    {32, 32, 8, 1, {1.1, 0.7}, {1.1, 0.8}, {3.5, 3.0}},   // 32 columns a wavefront
 };
 
 // The tiling and the number of parts of k with the least estimated time.  Parts of k cost their sums' way to memory and back and
@@ -533,6 +576,8 @@ inline ProductPlan plan_product(int dtype, int M, int N, long slabs, int problem
   }
   return best;
 }
+// columns of a wavefront's pieces
+inline int piece_columns(int tiling) { return tiling == TILE_32_K8 ? 32 : 64; }
 inline long slabs_of(long k, int dtype) { return (k * (long)type_bytes(dtype) + kSlabBytes - 1) / kSlabBytes; }
 
 template <class T, int BM, int BN, int WM, int WN, int WK, bool AKC, bool BKC, bool PAIR, class Epi>
@@ -545,9 +590,9 @@ hipError_t launch_tiling(ProductArgs a, const Epi &epi, hipStream_t stream) {
   if (e != hipSuccess) return e;
   a.tiles_m = (a.M + BM - 1) / BM;
   a.tiles_n = (a.N + (PAIR ? BN / 2 : BN) - 1) / (PAIR ? BN / 2 : BN);
-  const long tiles = (long)a.tiles_m * a.tiles_n;
-  if (tiles * kThreads >= (1L << 32)) return hipErrorInvalidValue;
-  kernel<<<dim3((unsigned)tiles, (unsigned)a.splits, (unsigned)a.problems), dim3(kThreads), lds, stream>>>(a, epi);
+  const long tiles = (long)a.tiles_m * a.tiles_n * a.splits * a.problems;
+  if (tiles * kThreads >= (1L << 31)) return hipErrorInvalidValue;
+  kernel<<<dim3((unsigned)tiles), dim3(kThreads), lds, stream>>>(a, epi);
   return hipGetLastError();
 }
 
@@ -559,7 +604,8 @@ hipError_t launch_product(const ProductArgs &a, const Epi &epi, int tiling, hipS
     case TILE_128: return launch_tiling<T, 128, 128, 2, 2, 1, AKC, BKC, PAIR, Epi>(a, epi, stream);
     case TILE_64_K2: return launch_tiling<T, 64, 64, 2, 1, 2, AKC, BKC, PAIR, Epi>(a, epi, stream);
     case TILE_64_K4: return launch_tiling<T, 64, 64, 2, 1, 4, AKC, BKC, PAIR, Epi>(a, epi, stream);
-    default: return launch_tiling<T, 32, 64, 1, 1, 4, AKC, BKC, PAIR, Epi>(a, epi, stream);
+    case TILE_32_K4: return launch_tiling<T, 32, 64, 1, 1, 4, AKC, BKC, PAIR, Epi>(a, epi, stream);
+    default: return launch_tiling<T, 32, 32, 1, 1, 8, AKC, BKC, PAIR, Epi>(a, epi, stream);
   }
 }
 
@@ -573,6 +619,14 @@ struct Take {
   }
 };
 
+template <class T>
+hipError_t launch_sum_splits(const ProductArgs &p, const StoreEpi<T> &out, int splits, const float *part, hipStream_t stream) {
+  const long groups = (long)p.M * ((p.N + 7) / 8), blocks = (groups + 255) / 256;
+  sum_splits_kernel<T><<<dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, stream>>>(part, splits, p.M, p.N, p.m_rows, p.first, out);
+  return hipGetLastError();
+}
+inline size_t partial_bytes(int splits, int M, int N) { return splits > 1 ? (size_t)splits * M * ((N + 7) & ~7) * sizeof(float) : 0; }
+
 // a product whose k may be split, its sums stored as T
 template <class T, bool AKC, bool BKC>
 hipError_t product_to(ProductArgs p, StoreEpi<T> out, const ProductPlan &plan, float *part, hipStream_t stream) {
@@ -580,11 +634,143 @@ hipError_t product_to(ProductArgs p, StoreEpi<T> out, const ProductPlan &plan, f
   const int slab = Elem<T>::kSlab, slabs = (p.K[0] + slab - 1) / slab + (p.K[1] + slab - 1) / slab;
   p.slabs_per_split = (slabs + plan.splits - 1) / plan.splits;
   p.splits = plan.splits;
-  hipError_t e = launch_product<T, AKC, BKC, false>(p, PartialEpi{part, p.M}, plan.tiling, stream);
+  hipError_t e = launch_product<T, AKC, BKC, false>(p, PartialEpi(part, p.M), plan.tiling, stream);
   if (e != hipSuccess) return e;
-  const long groups = (long)p.M * (padded(p.N) / 8), blocks = (groups + 255) / 256;
-  sum_splits_kernel<T><<<dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, stream>>>(part, plan.splits, p.M, p.N, p.m_rows, p.first, out);
-  return hipGetLastError();
+  return launch_sum_splits<T>(p, out, plan.splits, part, stream);
+}
+
+// The products of a backward pass that do not wait for each other, in one launch: a data gradient (A along k, B across it), whose k
+// may be split, and up to two kinds of weight gradients (both across k).  Those with the longest chains of slabs come first, the
+// others fill the compute units that these leave.
+template <class T>
+struct GradientEpi : NothingAhead {
+  GradientEpi() : store(nullptr, nullptr, 0, 0, nullptr, 0), part(nullptr, 0), partial(0) {}
+  StoreEpi<T> store;
+  PartialEpi part;
+  int partial;
+  template <int WC>
+  __device__ __forceinline__ void piece(const float *stage, int m, int n, int M, int N, int problem, int split, int q, Nothing a) const {
+    if (partial) part.template piece<WC>(stage, m, n, M, N, problem, split, q, a);
+    else store.template piece<WC>(stage, m, n, M, N, problem, split, q, a);
+  }
+};
+template <class T>
+struct GradientJobs {
+  int n = 0;
+  struct Job { ProductArgs a; GradientEpi<T> epi; int data = 0, begin = 0; } job[3];
+  ProductPlan plan;
+  float *partial = nullptr;
+  void add(const ProductArgs &a, const StoreEpi<T> &out, bool data) {
+    Job &j = job[n++];
+    j.a = a;
+    j.epi.store = out;
+    j.data = data;
+  }
+};
+
+template <class T, int BM, int BN, int WM, int WN, int WK>
+__global__ __launch_bounds__(64 * WM *WN *WK, 2) void gradient_kernel(const GradientJobs<T> g) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int id = blockIdx.x, k = g.n > 2 && id >= g.job[2].begin ? 2 : g.n > 1 && id >= g.job[1].begin ? 1 : 0;
+  const typename GradientJobs<T>::Job &j = g.job[k];
+  if (j.data) product_tile<T, BM, BN, WM, WN, WK, true, false, false, GradientEpi<T>>(j.a, j.epi, id - j.begin, smem);
+  else product_tile<T, BM, BN, WM, WN, WK, false, false, false, GradientEpi<T>>(j.a, j.epi, id - j.begin, smem);
+}
+
+struct GradientShape { int M, N; long slabs; int problems; bool data; };
+
+// As plan_product, for the launch as a whole: the longest chain, or all work spread over the chip and half a workgroup's tail
+inline ProductPlan plan_gradients(int dtype, const GradientShape *shape, int n) {
+  ProductPlan best;
+  double least = 1e30;
+  const int type = dtype == TYPE_BF16 ? 1 : 0, cus = chip().cus;
+  for (int i = 0; i < TILINGS; ++i) {
+    const TilingCost &c = kTilings[i];
+    for (int s = 1; s <= 32; s *= 2) {
+      double all = 0, longest = 0, shortest = 1e30, extra = 0;
+      bool ok = true;
+      for (int k = 0; k < n; ++k) {
+        const GradientShape &g = shape[k];
+        const int parts = g.data ? s : 1;
+        if (parts > 1 && g.slabs < 4L * parts) ok = false;
+        const double units = (double)((g.M + c.bm - 1) / c.bm) * ((g.N + c.bn - 1) / c.bn) * g.problems * parts;
+        const long each = ((g.slabs + parts - 1) / parts + c.groups - 1) / c.groups;
+        const double turn = c.resident * c.share[type] > c.chain[type] ? c.resident * c.share[type] : c.chain[type], time = each * turn + c.besides[type];
+        all += units * time / c.resident;
+        if (time > longest) longest = time;
+        if (time < shortest) shortest = time;
+        if (parts > 1) extra = 5.0 + (double)parts * g.M * g.N * 8.0 / 4.0e6;
+      }
+      if (!ok) break;
+      const double spread = all / cus + 0.5 * shortest, t = (spread > longest ? spread : longest) + extra;
+      if (t < least) {
+        least = t;
+        best.tiling = i;
+        best.splits = s;
+      }
+      bool data = false;
+      for (int k = 0; k < n; ++k) data = data || shape[k].data;
+      if (!data) break;
+    }
+  }
+  return best;
+}
+
+template <class T, int BM, int BN, int WM, int WN, int WK>
+hipError_t launch_gradients_as(GradientJobs<T> g, hipStream_t stream) {
+  constexpr size_t slabs = 2 * (size_t)WK * (BM + BN) * kSlabBytes, stage = (size_t)WM * WN * WK * 32 * kStageLd * sizeof(float);
+  constexpr size_t lds = slabs > stage ? slabs : stage;
+  const auto kernel = gradient_kernel<T, BM, BN, WM, WN, WK>;
+  hipError_t e = allow_large_lds(reinterpret_cast<const void *>(kernel), lds);
+  if (e != hipSuccess) return e;
+  long chain[3], begin = 0;
+  for (int k = 0; k < g.n; ++k) {
+    ProductArgs &a = g.job[k].a;
+    a.tiles_m = (a.M + BM - 1) / BM;
+    a.tiles_n = (a.N + BN - 1) / BN;
+    const int slab = Elem<T>::kSlab, all = (a.K[0] + slab - 1) / slab + (a.K[1] + slab - 1) / slab;
+    chain[k] = all;
+    if (g.job[k].data && g.plan.splits > 1) {
+      a.splits = g.plan.splits;
+      a.slabs_per_split = (all + a.splits - 1) / a.splits;
+      g.job[k].epi.part = PartialEpi(g.partial, a.M);
+      g.job[k].epi.partial = 1;
+      chain[k] = a.slabs_per_split;
+    }
+  }
+  for (int i = 0; i < g.n; ++i)   // the longest first
+    for (int k = i + 1; k < g.n; ++k)
+      if (chain[k] > chain[i]) {
+        const typename GradientJobs<T>::Job j = g.job[i];
+        g.job[i] = g.job[k];
+        g.job[k] = j;
+        const long c = chain[i];
+        chain[i] = chain[k];
+        chain[k] = c;
+      }
+  for (int k = 0; k < g.n; ++k) {
+    g.job[k].begin = (int)begin;
+    begin += (long)g.job[k].a.tiles_m * g.job[k].a.tiles_n * g.job[k].a.splits * g.job[k].a.problems;
+    if (begin * 64 * WM * WN * WK >= (1L << 31)) return hipErrorInvalidValue;
+  }
+  kernel<<<dim3((unsigned)begin), dim3(64 * WM * WN * WK), lds, stream>>>(g);
+  e = hipGetLastError();
+  for (int k = 0; k < g.n && e == hipSuccess; ++k)
+    if (g.job[k].epi.partial) e = launch_sum_splits<T>(g.job[k].a, g.job[k].epi.store, g.plan.splits, g.partial, stream);
+  return e;
+}
+
+template <class T>
+hipError_t launch_gradients(const GradientJobs<T> &g, hipStream_t stream) {
+  if (g.n == 0) return hipSuccess;
+  switch (g.plan.tiling) {
+    case TILE_256: return launch_gradients_as<T, 256, 256, 2, 4, 1>(g, stream);
+    case TILE_128: return launch_gradients_as<T, 128, 128, 2, 2, 1>(g, stream);
+    case TILE_64_K2: return launch_gradients_as<T, 64, 64, 2, 1, 2>(g, stream);
+    case TILE_64_K4: return launch_gradients_as<T, 64, 64, 2, 1, 4>(g, stream);
+    case TILE_32_K4: return launch_gradients_as<T, 32, 64, 1, 1, 4>(g, stream);
+    default: return launch_gradients_as<T, 32, 32, 1, 1, 8>(g, stream);
+  }
 }
 
 #define DLL_TRY(call) do { const hipError_t e_ = (call); if (e_ != hipSuccess) return e_; } while (0)
