@@ -5,7 +5,7 @@
 // Sums in 32 bits.  With bfloat16 operands h, da and db are rounded to bfloat16 on the way to the next product, as its
 // matrix instructions take nothing wider; a and b are kept for the backward pass in the operands' type.
 #include "large_ops.h"
-#include "tile_product.h"
+#include "skinny_product.h"
 
 namespace dllk {
 
@@ -13,11 +13,27 @@ using namespace tile;
 
 namespace {
 
+// 1 / (1 + exp(-a)) through the hardware's 2^x and reciprocal: off by 1.5 |a| 2^-24 and two last digits, relative
+__device__ __forceinline__ float sigmoid(float a) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896341f * a)); }
+
+// The normal distribution's cumulative function.  Where its product is rounded to bfloat16, erf by the formula 7.1.26 of Abramowitz
+// and Stegun's handbook (absolute error 1.5e-7), a third of the library function's instructions: 40 of these an element were a
+// quarter of the forward kernel at 777 x 1000 x 2730.
+template <class T>
+__device__ __forceinline__ float normal_cdf(float a) {
+  if (sizeof(T) == 4) return 0.5f * (1.0f + erff(a * 0.70710678118654752f));
+  const float x = fabsf(a) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * x);
+  const float poly = t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+  const float half = 0.5f * poly * __builtin_amdgcn_exp2f(-1.44269504088896341f * x * x);   // (1 - erf(x)) / 2
+  return a < 0.0f ? half : 1.0f - half;
+}
+
 // act(a) and act'(a)
+template <class T>
 __device__ __forceinline__ void gate_both(int gate, float a, float *f, float *d) {
   switch (gate) {
     case GATE_SIGMOID: {
-      const float s = 1.0f / (1.0f + expf(-a));
+      const float s = sigmoid(a);
       *f = s;
       *d = s * (1.0f - s);
       return;
@@ -27,15 +43,15 @@ __device__ __forceinline__ void gate_both(int gate, float a, float *f, float *d)
       *d = a > 0.0f ? 1.0f : 0.0f;
       return;
     case GATE_SILU: {
-      const float s = 1.0f / (1.0f + expf(-a));
+      const float s = sigmoid(a);
       *f = a * s;
       *d = s * (1.0f + a * (1.0f - s));
       return;
     }
     case GATE_GELU: {
-      const float c = 0.5f * (1.0f + erff(a * 0.70710678118654752f));
+      const float c = normal_cdf<T>(a);
       *f = a * c;
-      *d = c + a * expf(-0.5f * a * a) * 0.39894228040143268f;
+      *d = c + a * __builtin_amdgcn_exp2f(-0.72134752044448170f * a * a) * 0.39894228040143268f;
       return;
     }
     default:
@@ -43,9 +59,10 @@ __device__ __forceinline__ void gate_both(int gate, float a, float *f, float *d)
       *d = 1.0f;
   }
 }
+template <class T>
 __device__ __forceinline__ float gate_value(int gate, float a) {
   float f, d;
-  gate_both(gate, a, &f, &d);
+  gate_both<T>(gate, a, &f, &d);
   return f;
 }
 
@@ -71,13 +88,48 @@ struct GateEpi : NothingAhead {
       stage8(stage, row, WC / 2 + col, vb);
       const int left = H - n - col;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) vh[j] = j < left ? gate_value(gate, va[j]) * vb[j] : 0.0f;
+      for (int j = 0; j < 8; ++j) vh[j] = j < left ? gate_value<T>(gate, va[j]) * vb[j] : 0.0f;
       store8<T>(h + (long)(m + row) * ldh + n + col, vh, true, 8);
-      if (kept_a) {
+      if (kept_a && vec_kept) {
         const long o = (long)(m + row) * H + n + col;
-        store8<T>(kept_a + o, va, vec_kept && left >= 8, left);
-        store8<T>(kept_b + o, vb, vec_kept && left >= 8, left);
+        store8<T>(kept_a + o, va, left >= 8, left);
+        store8<T>(kept_b + o, vb, left >= 8, left);
       }
+    }
+    if (kept_a && !vec_kept) {   // rows that start anywhere: a column a lane
+      const int lane = threadIdx.x & 63, at = lane % (WC / 2);
+      T *const kept = lane % WC < WC / 2 ? kept_a : kept_b;
+      if (n + at >= H) return;
+#pragma unroll 8
+      for (int row = lane / WC; row < 32; row += 64 / WC) {
+        if (m + row >= M) break;
+        kept[(long)(m + row) * H + n + at] = (T)stage[row * kStageLd + lane % WC];
+      }
+    }
+  }
+};
+
+// The same for a few tokens; h in rows of H
+template <class T>
+struct SkinnyGate {
+  int gate;
+  T *h, *kept_a, *kept_b;   // kept_*: nullable
+  template <int R>
+  __device__ __forceinline__ void tile(const floatx4 (&v)[R], int m, int n, int M, int H) const {
+    static_assert(R == 2, "a and b");
+    if (m >= M || n >= H) return;
+    float a[4], b[4], o[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      a[j] = v[0][j];
+      b[j] = v[1][j];
+      o[j] = gate_value<T>(gate, a[j]) * b[j];
+    }
+    const long at = (long)m * H + n;
+    store4<T>(h + at, o, H - n);
+    if (kept_a) {
+      store4<T>(kept_a + at, a, H - n);
+      store4<T>(kept_b + at, b, H - n);
     }
   }
 };
@@ -93,10 +145,26 @@ struct GateBackEpi : NothingAhead {
   long ld;
   template <int WC>
   __device__ __forceinline__ void piece(const float *stage, int m, int n, int M, int H, int, int, int, Nothing) const {
+    if (!vec_kept) {   // rows that start anywhere: a column a lane, zeros up to the next whole run of eight
+      const int lane = threadIdx.x & 63, at = n + lane % WC;
+      if (at >= ((H + 7) & ~7)) return;
+#pragma unroll 8
+      for (int row = lane / WC; row < 32; row += 64 / WC) {
+        if (m + row >= M) break;
+        const long from = (long)(m + row) * H + at, to = (long)(m + row) * ld + at;
+        const float va = at < H ? to_float(a[from]) : 0.0f, vb = at < H ? to_float(b[from]) : 0.0f, dh = at < H ? stage[row * kStageLd + lane % WC] : 0.0f;
+        float f, d;
+        gate_both<T>(gate, va, &f, &d);
+        da[to] = (T)(dh * vb * d);
+        db[to] = (T)(dh * f);
+        h[to] = (T)(f * vb);
+      }
+      return;
+    }
     const Lanes<WC> l;
     const int col = l.col, left = H - n - col;
     if (left <= 0) return;
-    const bool whole = vec_kept && left >= 8;
+    const bool whole = left >= 8;
     Eight<T> va[l.kPasses], vb[l.kPasses];   // all loads of the piece go out together
 #pragma unroll
     for (int p = 0; p < l.kPasses; ++p) {
@@ -114,7 +182,7 @@ struct GateBackEpi : NothingAhead {
       for (int j = 0; j < 8; ++j) {
         const float va_ = (float)va[p].v[j], vb_ = (float)vb[p].v[j];
         float f, d;
-        gate_both(gate, va_, &f, &d);
+        gate_both<T>(gate, va_, &f, &d);
         oa[j] = j < left ? g[j] * vb_ * d : 0.0f;
         ob[j] = j < left ? g[j] * f : 0.0f;
         oh[j] = j < left ? f * vb_ : 0.0f;
@@ -128,15 +196,22 @@ struct GateBackEpi : NothingAhead {
 };
 
 template <class T>
-__global__ __launch_bounds__(256) void pad_rows_kernel(const T *src, T *dst, long rows, long cols, long ld) {
-  const long groups = ld / 8, n = rows * groups;
-  for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) {
-    const long r = i / groups, c = (i - r * groups) * 8;
-    const int left = (int)(cols - c < 8 ? cols - c : 8);   // negative in the padding
-    float v[8];
-    load8<T>(src + r * cols + (left > 0 ? c : 0), v, false, left);
-    store8<T>(dst + r * ld + c, v, true, 8);
-  }
+__global__ __launch_bounds__(256) void pad_rows_kernel(const T *src, T *dst, int rows, int cols, long ld) {
+  for (long r = blockIdx.y * 4 + (threadIdx.x >> 6); r < rows; r += gridDim.y * 4)
+#pragma unroll 8
+    for (int c = blockIdx.x * 512 + (threadIdx.x & 63); c < min((int)ld, (int)blockIdx.x * 512 + 512); c += 64)
+      {
+      const T v = src[r * cols + min(c, cols - 1)];   // no load behind a branch of its own
+      dst[r * ld + c] = c < cols ? v : (T)0.0f;
+    }
+}
+
+// A few tokens: the weights straight from memory.  Up to 16 always (2048 x 8192 bf16, one token: 25.6 us against 30 on tiles with k
+// in parts); up to 32 where the weights are small (24 x 1000 x 2730: 12.6 against 21; at 2048 x 8192 the tiles' 28 against 39, as
+// every workgroup reads the tokens again) or lie in rows of odd sizes, which the tiles would have copied first.
+bool skinny(int T, int D, int H, int dtype) {
+  if (T > kSkinnyRows || D < kSkinnyLeastK || H < kSkinnyLeastK) return false;
+  return T <= 16 || (long)D * H <= (1L << 22) || !whole_groups(D, dtype) || !whole_groups(H, dtype);
 }
 
 // The workspace's parts, the same walk for the query and the call
@@ -153,6 +228,11 @@ struct FwdPlan {
     ldd = padded(D);
     h = take((size_t)T * ldh * e);
     x = wg = wu = wd = nullptr;
+    part = nullptr;
+    if (skinny(T, D, H, dtype)) {   // nothing else
+      bytes = take.used;
+      return;
+    }
     if (!whole_groups(D, dtype)) x = take((size_t)T * ldd * e), wg = take((size_t)H * ldd * e), wu = take((size_t)H * ldd * e);
     if (!whole_groups(H, dtype)) wd = take((size_t)D * ldh * e);
     up = plan_product(dtype, T, H, slabs_of(D, dtype), 1, true, false);
@@ -191,6 +271,21 @@ struct BwdPlan {
 template <class T>
 hipError_t gated_fwd(const GatedArgs &a, char *scratch, hipStream_t stream) {
   const FwdPlan p(a.T, a.D, a.H, a.dtype, scratch);
+  if (skinny(a.T, a.D, a.H, a.dtype)) {
+    SkinnyArgs s;
+    s.M = a.T;
+    s.N = a.H;
+    s.K = a.D;
+    s.x = a.x;
+    s.w[0] = a.w_gate;
+    s.w[1] = a.w_up;
+    DLL_TRY((launch_skinny<T, 2, true>(s, SkinnyGate<T>{a.gate, (T *)p.h, (T *)a.gate_pre, (T *)a.up_pre}, stream)));
+    s.N = a.D;
+    s.K = a.H;
+    s.x = p.h;
+    s.w[0] = a.w_down;
+    return launch_skinny<T, 1, false>(s, SkinnyStore<T>{(T *)a.y}, stream);
+  }
   const void *x = a.x, *wg = a.w_gate, *wu = a.w_up, *wd = a.w_down;
   if (p.x) {
     DLL_TRY(launch_pad_rows(x, p.x, a.T, a.D, a.dtype, stream));
@@ -295,10 +390,10 @@ hipError_t gated_bwd(const GatedArgs &a, char *scratch, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_pad_rows(const void *src, void *dst, long rows, long cols, int dtype, hipStream_t stream) {
-  const long ld = padded(cols), blocks = (rows * (ld / 8) + 255) / 256;
-  const dim3 grid((unsigned)(blocks < 8192 ? blocks : 8192));
-  if (dtype == TYPE_BF16) pad_rows_kernel<bf16><<<grid, dim3(256), 0, stream>>>((const bf16 *)src, (bf16 *)dst, rows, cols, ld);
-  else pad_rows_kernel<float><<<grid, dim3(256), 0, stream>>>((const float *)src, (float *)dst, rows, cols, ld);
+  const long ld = padded(cols), fours = (rows + 3) / 4;
+  const dim3 grid((unsigned)((ld + 511) / 512), (unsigned)(fours < 32768 ? fours : 32768));
+  if (dtype == TYPE_BF16) pad_rows_kernel<bf16><<<grid, dim3(256), 0, stream>>>((const bf16 *)src, (bf16 *)dst, (int)rows, (int)cols, ld);
+  else pad_rows_kernel<float><<<grid, dim3(256), 0, stream>>>((const float *)src, (float *)dst, (int)rows, (int)cols, ld);
   return hipGetLastError();
 }
 

@@ -462,6 +462,18 @@ struct StoreEpi : NothingAhead {
   int add;                 // T = float only: add to what is there
   template <int WC>
   __device__ __forceinline__ void piece(const float *stage, int m, int n, int M, int N, int problem, int, int, Nothing) const {
+    if (!vec) {   // rows that start anywhere: a column a lane
+      const int lane = threadIdx.x & 63, col = lane % WC;
+      if (n + col >= N) return;
+#pragma unroll 8
+      for (int row = lane / WC; row < 32; row += 64 / WC) {
+        if (m + row >= M) break;
+        T *d = c[problem] + (long)(rows ? rows[m + row] : m + row) * ld + n + col;
+        const float v = stage[row * kStageLd + col];
+        *d = (T)(add ? to_float(*d) + v : v);
+      }
+      return;
+    }
     const Lanes<WC> l;
     const int col = l.col;
 #pragma unroll
@@ -510,6 +522,17 @@ template <class T>
 __global__ __launch_bounds__(256) void sum_splits_kernel(const float *part, int splits, int M, int N, const int *m_rows, int first, StoreEpi<T> out) {
   const long n8 = (N + 7) & ~7;
   const int rows = rows_left(m_rows, first, M), g = (int)(n8 >> 3);
+  if (!out.vec) {
+    for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < (long)rows * N; i += (long)gridDim.x * 256) {
+      const int m = (int)(i / N), n = (int)(i - (long)m * N);
+      float v = 0.0f;
+#pragma unroll 4
+      for (int s = 0; s < splits; ++s) v += part[((long)s * M + m) * n8 + n];
+      T *d = out.c[0] + (long)(out.rows ? out.rows[m] : m) * out.ld + n;
+      *d = (T)(out.add ? to_float(*d) + v : v);
+    }
+    return;
+  }
   for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < (long)rows * g; i += (long)gridDim.x * 256) {
     const int m = (int)(i / g), n = (int)(i % g) * 8;
     float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
@@ -621,7 +644,7 @@ struct Take {
 
 template <class T>
 hipError_t launch_sum_splits(const ProductArgs &p, const StoreEpi<T> &out, int splits, const float *part, hipStream_t stream) {
-  const long groups = (long)p.M * ((p.N + 7) / 8), blocks = (groups + 255) / 256;
+  const long groups = (long)p.M * (out.vec ? (p.N + 7) / 8 : p.N), blocks = (groups + 255) / 256;
   sum_splits_kernel<T><<<dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, stream>>>(part, splits, p.M, p.N, p.m_rows, p.first, out);
   return hipGetLastError();
 }

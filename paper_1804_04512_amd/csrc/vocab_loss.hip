@@ -11,7 +11,7 @@
 // after exp).  This takes three products of T D V; forming the logits again for the gradients would take four.
 // The exponentials are kept for a piece of the tokens at a time, 1 GiB at most.
 #include "large_ops.h"
-#include "tile_product.h"
+#include "skinny_product.h"
 
 namespace dllk {
 
@@ -100,6 +100,46 @@ struct LogitEpi {
       }
       if (KEEP && n + col < ld) store8<T>(e + (long)row * ld + n + col, e8, true, 8);
     }
+  }
+};
+
+// The statistics alone for a few tokens: groups of 32 columns, four neighbours a lane and 16 columns an accumulator.
+template <class T>
+struct SkinnyLogits {
+  const T *bias;
+  const int *labels;
+  float2 *stats;
+  long rows_ld;
+  float *hit;
+  template <int R>
+  __device__ __forceinline__ void tile(const floatx4 (&v)[R], int m, int n, int M, int V) const {
+    static_assert(R == 2, "groups of 32 columns");
+    float z[R][4], top = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int at = n + kSkinnyColumns * r + j;
+        z[r][j] = at < V ? v[r][j] + (bias ? to_float(bias[at]) : 0.0f) : -INFINITY;
+        top = fmaxf(top, z[r][j]);
+      }
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float from = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum += exp_below(z[r][j] - from);
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if (m >= M) return;
+    if ((threadIdx.x & 63) < 16) stats[(long)(n / (R * kSkinnyColumns)) * rows_ld + m] = make_float2(top, sum);
+    const int label = labels[m];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (label == n + kSkinnyColumns * r + j && label < V) hit[m] = z[r][j];
   }
 };
 
@@ -360,6 +400,10 @@ __global__ __launch_bounds__(256) void convert_kernel(const float *src, T *dst, 
   for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) dst[i] = (T)src[i];
 }
 
+// Weights in rows of odd sizes, which the tiles would have copied first (16 x 1024 x 32000 in whole rows: 15 us on either way, and
+// half as many groups to join on the tiles').
+bool skinny(int T, int D, int dtype) { return T <= kSkinnyRows && D >= kSkinnyLeastK && !whole_groups(D, dtype); }
+
 struct Plan {
   long ldd, lde;
   int group, groups, piece, pieces;   // group: columns of a row that share a maximum
@@ -381,7 +425,7 @@ struct Plan {
     piece = (size_t)T < most ? T : (int)most;
     pieces = (T + piece - 1) / piece;
     z = plan_product(dtype, piece, V, slabs_of(D, dtype), 1, false, false);
-    group = piece_columns(z.tiling);
+    group = !grad && skinny(T, D, dtype) ? 2 * kSkinnyColumns : piece_columns(z.tiling);
     groups = (V + group - 1) / group;
     const size_t slab_rows = (size_t)(piece + 63) / 64 * 64;
     count = (int *)take(sizeof(int));
@@ -454,6 +498,18 @@ hipError_t logits(const VocabArgs &a, const Plan &p, int first, const void *w, l
 template <class T>
 hipError_t few_rows_fwd(const VocabArgs &a, const Plan &p, hipStream_t stream) {
   const void *x = a.x, *w = a.w;
+  if (skinny(a.T, a.D, a.dtype)) {
+    SkinnyArgs s;
+    s.M = a.T;
+    s.N = a.V;
+    s.K = a.D;
+    s.x = x;
+    s.w[0] = w;
+    DLL_TRY((launch_skinny<T, 2, false>(s, SkinnyLogits<T>{(const T *)a.bias, a.labels, p.stats, p.piece, p.hit}, stream)));
+    join_groups_kernel<<<dim3(1), dim3(1024), 0, stream>>>(p.stats, p.groups, p.piece, p.hit, a.T, nullptr, 0, nullptr, nullptr, nullptr, a.row_loss, a.row_lse,
+                                                               a.labels, a.V, a.loss);
+    return hipGetLastError();
+  }
   if (p.w) {
     DLL_TRY(launch_pad_rows(a.x, p.x, a.T, a.D, a.dtype, stream));
     DLL_TRY(launch_pad_rows(a.w, p.w, a.V, a.D, a.dtype, stream));
