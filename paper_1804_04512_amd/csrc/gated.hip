@@ -197,13 +197,15 @@ struct GateBackEpi : NothingAhead {
 
 template <class T>
 __global__ __launch_bounds__(256) void pad_rows_kernel(const T *src, T *dst, int rows, int cols, long ld) {
-  for (long r = blockIdx.y * 4 + (threadIdx.x >> 6); r < rows; r += gridDim.y * 4)
-#pragma unroll 8
-    for (int c = blockIdx.x * 512 + (threadIdx.x & 63); c < min((int)ld, (int)blockIdx.x * 512 + 512); c += 64)
-      {
-      const T v = src[r * cols + min(c, cols - 1)];   // no load behind a branch of its own
-      dst[r * ld + c] = c < cols ? v : (T)0.0f;
-    }
+  const int c0 = blockIdx.x * 512 + (threadIdx.x & 63);
+  for (long r = blockIdx.y * 4 + (threadIdx.x >> 6); r < rows; r += gridDim.y * 4) {
+    T v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = src[r * cols + min(c0 + 64 * j, cols - 1)];   // all on their way before the first is stored
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (c0 + 64 * j < ld) dst[r * ld + c0 + 64 * j] = c0 + 64 * j < cols ? v[j] : (T)0.0f;
+  }
 }
 
 // A few tokens: the weights straight from memory.  Up to 16 always (2048 x 8192 bf16, one token: 25.6 us against 30 on tiles with k

@@ -178,6 +178,13 @@ struct PairSlab {
   }
 };
 
+// A workgroup barrier that waits for nothing by itself (the callers count their loads) and that no LDS access moves across
+__device__ __forceinline__ void barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 // ------------------------------------------------------------------------------------------------ fragments
 // Lane l's part of a 32-row fragment at step s (of 4 a slab): row x0 + l % 32, 16-byte group 2 s + l / 32 along k.
 template <class T, int X, bool KC>
@@ -229,13 +236,13 @@ __device__ __forceinline__ floatx16 mfma(floatx4 b, floatx4 a, floatx16 c) {
 // Epi: `piece<WC>(stage, m, n, M, N, problem, split, q, ahead)` takes 32 x WC sums (WC = 64 or 32) from the wavefront's LDS area
 // (row stride kStageLd floats), first element C(m, n), the wavefront's q-th piece along m; `ahead(m, M, lane)` is called before the products.
 // PAIR: B[0] and B[1] are the gate and up projections (KC), N counts hidden units, a tile covers BN / 2 of them.
-template <class T, int BM, int BN, int WM, int WN, int WK, bool AKC, bool BKC, bool PAIR, class Epi>
+template <class T, int BM, int BN, int WM, int WN, int WK, int STAGES, bool AKC, bool BKC, bool PAIR, class Epi>
 __device__ __forceinline__ void product_tile(const ProductArgs &a, const Epi &epi, int id, char *smem) {
   constexpr int kThreads = 64 * WM * WN, TM = BM / WM / 32, WC = BN / WN, TN = WC / 32, kK = Elem<T>::kSlab;
   static_assert((WC == 64 || WC == 32) && BM % (32 * WM) == 0, "wavefront tiles are 64 or 32 columns wide");
   typedef Slab<T, BM, AKC, kThreads> SA;
   typedef Slab<T, BN, BKC, kThreads> SB;
-  constexpr int kA = SA::kBytes, kStage = SA::kBytes + SB::kBytes;
+  constexpr int kA = SA::kBytes, kStage = SA::kBytes + SB::kBytes, kLoads = SA::kIts + SB::kIts;
   const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = all % (WM * WN), group = all / (WM * WN);
   const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * WC;
   int tm, tn, unit;
@@ -255,14 +262,15 @@ __device__ __forceinline__ void product_tile(const ProductArgs &a, const Epi &ep
   sa.init(a.A[0].ld, threadIdx.x % kThreads);
   if (PAIR) sp.init(a.B[0].ld, threadIdx.x % kThreads);
   else sb.init(a.B[0].ld, threadIdx.x % kThreads);
-  char *mine = smem + group * 2 * kStage;
+  char *mine = smem + group * STAGES * kStage;
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)mine;
-  const auto load = [&](int turn) {
+  // A slab behind the last is loaded as zeros, out of range of everything: the number of loads on their way stays the same, and a
+  // group without a slab in the last turn adds nothing.
+  const auto load = [&](int turn, int stage) {
     const int t = t0 + turn * WK + group;
-    if (t >= t1) return;
-    const unsigned lds = lds0 + (turn & 1) * kStage;
+    const unsigned lds = lds0 + stage * kStage;
     const bool second = t >= slabs0;
-    const int k0 = (second ? t - slabs0 : t) * kK, K = second ? a.K[1] : K0, which = second ? 1 : problem;
+    const int k0 = (second ? t - slabs0 : t) * kK, K = t >= t1 ? 0 : second ? a.K[1] : K0, which = second && a.K[1] > 0 ? 1 : problem;
     sa.load(lds, wave, a.A[which], m0, M, k0, K);
     if (PAIR) sp.load(lds + kA, wave, a.B[0], a.B[1], n0, a.N, k0, K);
     else sb.load(lds + kA, wave, a.B[which], n0, a.N, k0, K);
@@ -277,7 +285,7 @@ __device__ __forceinline__ void product_tile(const ProductArgs &a, const Epi &ep
   const FragReader<T, BM, AKC> ra(lane);
   const FragReader<T, BN, BKC> rb(lane);
   // Fragments are read one step ahead of the products that take them.  The one barrier of a slab stands before its last
-  // step: by then every wavefront holds its last fragments of this slab, so its place can take the slab after the next, and has
+  // step: by then every wavefront holds its last fragments of this slab, so its place can take the slab STAGES turns on, and has
   // seen its part of the next slab land, whose first fragments are read behind the barrier while the last step multiplies.
   typename Elem<T>::Frag fa[2][TM], fb[2][TN];
   const auto read = [&](int set, const char *lds, int s) {
@@ -295,29 +303,29 @@ __device__ __forceinline__ void product_tile(const ProductArgs &a, const Epi &ep
     __builtin_amdgcn_sched_barrier(0);
   };
   if (turns > 0) {
-    load(0);
-    load(1);
-    if (turns > 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(SA::kIts + SB::kIts) : "memory");
-    if (turns == 1 || (WK > 1 && t0 + WK + group >= t1)) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (WK == 1 || t0 + group < t1) read(0, mine, 0);
-  }
-  for (int turn = 0; turn < turns; ++turn) {
-    const char *now = mine + (turn & 1) * kStage, *next = mine + ((turn + 1) & 1) * kStage;
-    const bool has = WK == 1 || t0 + turn * WK + group < t1;   // a group may have no slab in the last turn
-    if (has) {
+#pragma unroll
+    for (int p = 0; p < STAGES; ++p) load(p, p);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads * (STAGES - 1)) : "memory");
+    barrier();
+    read(0, mine, 0);
+    int stage = 0;
+    for (int turn = 0; turn < turns; ++turn) {
+      const int next = STAGES == 2 ? stage ^ 1 : stage + 1 == STAGES ? 0 : stage + 1;
+      const char *now = mine + stage * kStage;
       read(1, now, 1);
       multiply(0);
       read(0, now, 2);
       multiply(1);
       read(1, now, 3);
       multiply(0);
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLoads * (STAGES - 2)) : "memory");
+      barrier();
+      load(turn + STAGES, stage);
+      read(0, mine + next * kStage, 0);
+      multiply(1);
+      stage = next;
     }
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (turn + 2 < turns) load(turn + 2);
-    if (turn + 1 < turns && (WK == 1 || t0 + (turn + 1) * WK + group < t1)) read(0, next, 0);
-    if (has) multiply(1);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // of the slabs of zeros too
   }
   __syncthreads();   // the slabs' place becomes the epilogue's
   constexpr int kPiece = 32 * kStageLd;
@@ -358,10 +366,10 @@ __device__ __forceinline__ void product_tile(const ProductArgs &a, const Epi &ep
   }
 }
 
-template <class T, int BM, int BN, int WM, int WN, int WK, bool AKC, bool BKC, bool PAIR, class Epi>
+template <class T, int BM, int BN, int WM, int WN, int WK, int STAGES, bool AKC, bool BKC, bool PAIR, class Epi>
 __global__ __launch_bounds__(64 * WM *WN *WK, 2) void product_kernel(const ProductArgs a, const Epi epi) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  product_tile<T, BM, BN, WM, WN, WK, AKC, BKC, PAIR, Epi>(a, epi, blockIdx.x, smem);
+  product_tile<T, BM, BN, WM, WN, WK, STAGES, AKC, BKC, PAIR, Epi>(a, epi, blockIdx.x, smem);
 }
 
 // ------------------------------------------------------------------------------------------------ outputs
@@ -557,21 +565,25 @@ __global__ __launch_bounds__(256) void sum_splits_kernel(const float *part, int 
 }
 
 // ------------------------------------------------------------------------------------------------ host
-// The tilings of a product: tile edges, and how many groups of wavefronts take the slabs in turn.
-enum Tiling { TILE_256 = 0, TILE_128, TILE_64_K2, TILE_64_K4, TILE_32_K4, TILE_32_K8, TILINGS };
+// The tilings of a product: tile edges, groups of wavefronts that take the slabs in turn, slabs on their way.  256 x 256 keeps two
+// slabs (128 KB of LDS, a workgroup a compute unit); 128 x 128 and 64 x 64 two with two workgroups a unit, or four with one, as
+// operands that come from memory rather than L2 take longer to arrive than a slab to multiply (on cold weights 2048 x 2048 x
+// 2048 takes 28 us with four slabs of 128 x 128 and 34 with two, but 777 x 5472 x 1000, with two tiles for some units, 32 against 23).
+enum Tiling { TILE_256 = 0, TILE_128, TILE_128_DEEP, TILE_64_K2, TILE_64_K2_DEEP, TILE_32_K4, TILE_32_K8, TILINGS };
 struct ProductPlan { int tiling = TILE_128, splits = 1; };
 
-// What a tiling costs, in microseconds, as measured on products of 512 to 8192 rows and columns: a workgroup's share of a
+// What a tiling costs, in microseconds, as measured on products of 32 to 8192 rows and columns: a workgroup's share of a
 // compute unit for one turn (a slab for each group) with the unit full, the least time of a turn's chain of load, barrier and
 // products, what a workgroup takes besides its turns, and how many a unit holds.
 struct TilingCost { int bm, bn, groups, resident; double share[2], chain[2], besides[2]; };   // [fp32, bf16]
 constexpr TilingCost kTilings[TILINGS] = {
-    {256, 256, 1, 1, {7.8, 1.62}, {7.4, 1.3}, {6.0, 8.0}},
-    {128, 128, 1, 2, {2.08, 0.55}, {2.05, 0.66}, {4.0, 4.0}},
-    {64, 64, 2, 2, {1.07, 0.42}, {1.15, 0.7}, {3.0, 3.0}},
-    {64, 64, 4, 1, {2.1, 0.92}, {2.2, 0.95}, {3.5, 2.7}},
-    {32, 64, 4, 1, {1.35, 0.6}, {1.35, 0.75}, {3.5, 2.5}},
-    {32, 32, 8, 1, {1.1, 0.7}, {1.1, 0.8}, {3.5, 3.0}},   // 32 columns a wavefront
+    {256, 256, 1, 1, {7.8, 1.62}, {7.4, 1.5}, {6.0, 8.0}},
+    {128, 128, 1, 2, {2.08, 0.55}, {2.05, 1.0}, {4.0, 4.0}},
+    {128, 128, 1, 1, {2.1, 0.78}, {2.1, 0.78}, {3.5, 3.0}},
+    {64, 64, 2, 2, {1.07, 0.45}, {1.15, 0.88}, {3.0, 2.5}},
+    {64, 64, 2, 1, {1.12, 0.62}, {1.12, 0.62}, {3.0, 2.5}},
+    {32, 64, 4, 1, {1.3, 0.9}, {1.3, 0.9}, {3.5, 2.5}},
+    {32, 32, 8, 1, {1.1, 0.9}, {1.1, 0.9}, {3.5, 3.0}},   // 32 columns a wavefront
 };
 
 // The tiling and the number of parts of k with the least estimated time.  Parts of k cost their sums' way to memory and back and
@@ -603,12 +615,19 @@ inline ProductPlan plan_product(int dtype, int M, int N, long slabs, int problem
 inline int piece_columns(int tiling) { return tiling == TILE_32_K8 ? 32 : 64; }
 inline long slabs_of(long k, int dtype) { return (k * (long)type_bytes(dtype) + kSlabBytes - 1) / kSlabBytes; }
 
-template <class T, int BM, int BN, int WM, int WN, int WK, bool AKC, bool BKC, bool PAIR, class Epi>
+// LDS of a workgroup: its slabs, or in their place a piece of sums for each wavefront
+template <int BM, int BN, int WM, int WN, int WK, int STAGES>
+constexpr size_t product_lds() {
+  constexpr size_t slabs = (size_t)STAGES * WK * (BM + BN) * kSlabBytes, stage = (size_t)WM * WN * WK * 32 * kStageLd * sizeof(float);
+  static_assert(slabs <= 160 * 1024 && stage <= 160 * 1024, "a compute unit's LDS");
+  return slabs > stage ? slabs : stage;
+}
+
+template <class T, int BM, int BN, int WM, int WN, int WK, int STAGES, bool AKC, bool BKC, bool PAIR, class Epi>
 hipError_t launch_tiling(ProductArgs a, const Epi &epi, hipStream_t stream) {
   constexpr int kThreads = 64 * WM * WN * WK;
-  constexpr size_t slabs = 2 * (size_t)WK * (BM + BN) * kSlabBytes, stage = (size_t)WM * WN * WK * 32 * kStageLd * sizeof(float);
-  constexpr size_t lds = slabs > stage ? slabs : stage;
-  const auto kernel = product_kernel<T, BM, BN, WM, WN, WK, AKC, BKC, PAIR, Epi>;
+  constexpr size_t lds = product_lds<BM, BN, WM, WN, WK, STAGES>();
+  const auto kernel = product_kernel<T, BM, BN, WM, WN, WK, STAGES, AKC, BKC, PAIR, Epi>;
   hipError_t e = allow_large_lds(reinterpret_cast<const void *>(kernel), lds);
   if (e != hipSuccess) return e;
   a.tiles_m = (a.M + BM - 1) / BM;
@@ -623,12 +642,13 @@ template <class T, bool AKC, bool BKC, bool PAIR, class Epi>
 hipError_t launch_product(const ProductArgs &a, const Epi &epi, int tiling, hipStream_t stream) {
   if (a.M <= 0 || a.N <= 0) return hipSuccess;
   switch (tiling) {
-    case TILE_256: return launch_tiling<T, 256, 256, 2, 4, 1, AKC, BKC, PAIR, Epi>(a, epi, stream);
-    case TILE_128: return launch_tiling<T, 128, 128, 2, 2, 1, AKC, BKC, PAIR, Epi>(a, epi, stream);
-    case TILE_64_K2: return launch_tiling<T, 64, 64, 2, 1, 2, AKC, BKC, PAIR, Epi>(a, epi, stream);
-    case TILE_64_K4: return launch_tiling<T, 64, 64, 2, 1, 4, AKC, BKC, PAIR, Epi>(a, epi, stream);
-    case TILE_32_K4: return launch_tiling<T, 32, 64, 1, 1, 4, AKC, BKC, PAIR, Epi>(a, epi, stream);
-    default: return launch_tiling<T, 32, 32, 1, 1, 8, AKC, BKC, PAIR, Epi>(a, epi, stream);
+    case TILE_256: return launch_tiling<T, 256, 256, 2, 4, 1, 2, AKC, BKC, PAIR, Epi>(a, epi, stream);
+    case TILE_128: return launch_tiling<T, 128, 128, 2, 2, 1, 2, AKC, BKC, PAIR, Epi>(a, epi, stream);
+    case TILE_128_DEEP: return launch_tiling<T, 128, 128, 2, 2, 1, 4, AKC, BKC, PAIR, Epi>(a, epi, stream);
+    case TILE_64_K2: return launch_tiling<T, 64, 64, 2, 1, 2, 2, AKC, BKC, PAIR, Epi>(a, epi, stream);
+    case TILE_64_K2_DEEP: return launch_tiling<T, 64, 64, 2, 1, 2, 4, AKC, BKC, PAIR, Epi>(a, epi, stream);
+    case TILE_32_K4: return launch_tiling<T, 32, 64, 1, 1, 4, 3, AKC, BKC, PAIR, Epi>(a, epi, stream);
+    default: return launch_tiling<T, 32, 32, 1, 1, 8, 2, AKC, BKC, PAIR, Epi>(a, epi, stream);
   }
 }
 
@@ -691,13 +711,13 @@ struct GradientJobs {
   }
 };
 
-template <class T, int BM, int BN, int WM, int WN, int WK>
+template <class T, int BM, int BN, int WM, int WN, int WK, int STAGES>
 __global__ __launch_bounds__(64 * WM *WN *WK, 2) void gradient_kernel(const GradientJobs<T> g) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int id = blockIdx.x, k = g.n > 2 && id >= g.job[2].begin ? 2 : g.n > 1 && id >= g.job[1].begin ? 1 : 0;
   const typename GradientJobs<T>::Job &j = g.job[k];
-  if (j.data) product_tile<T, BM, BN, WM, WN, WK, true, false, false, GradientEpi<T>>(j.a, j.epi, id - j.begin, smem);
-  else product_tile<T, BM, BN, WM, WN, WK, false, false, false, GradientEpi<T>>(j.a, j.epi, id - j.begin, smem);
+  if (j.data) product_tile<T, BM, BN, WM, WN, WK, STAGES, true, false, false, GradientEpi<T>>(j.a, j.epi, id - j.begin, smem);
+  else product_tile<T, BM, BN, WM, WN, WK, STAGES, false, false, false, GradientEpi<T>>(j.a, j.epi, id - j.begin, smem);
 }
 
 struct GradientShape { int M, N; long slabs; int problems; bool data; };
@@ -739,11 +759,10 @@ inline ProductPlan plan_gradients(int dtype, const GradientShape *shape, int n) 
   return best;
 }
 
-template <class T, int BM, int BN, int WM, int WN, int WK>
+template <class T, int BM, int BN, int WM, int WN, int WK, int STAGES>
 hipError_t launch_gradients_as(GradientJobs<T> g, hipStream_t stream) {
-  constexpr size_t slabs = 2 * (size_t)WK * (BM + BN) * kSlabBytes, stage = (size_t)WM * WN * WK * 32 * kStageLd * sizeof(float);
-  constexpr size_t lds = slabs > stage ? slabs : stage;
-  const auto kernel = gradient_kernel<T, BM, BN, WM, WN, WK>;
+  constexpr size_t lds = product_lds<BM, BN, WM, WN, WK, STAGES>();
+  const auto kernel = gradient_kernel<T, BM, BN, WM, WN, WK, STAGES>;
   hipError_t e = allow_large_lds(reinterpret_cast<const void *>(kernel), lds);
   if (e != hipSuccess) return e;
   long chain[3], begin = 0;
@@ -787,12 +806,13 @@ template <class T>
 hipError_t launch_gradients(const GradientJobs<T> &g, hipStream_t stream) {
   if (g.n == 0) return hipSuccess;
   switch (g.plan.tiling) {
-    case TILE_256: return launch_gradients_as<T, 256, 256, 2, 4, 1>(g, stream);
-    case TILE_128: return launch_gradients_as<T, 128, 128, 2, 2, 1>(g, stream);
-    case TILE_64_K2: return launch_gradients_as<T, 64, 64, 2, 1, 2>(g, stream);
-    case TILE_64_K4: return launch_gradients_as<T, 64, 64, 2, 1, 4>(g, stream);
-    case TILE_32_K4: return launch_gradients_as<T, 32, 64, 1, 1, 4>(g, stream);
-    default: return launch_gradients_as<T, 32, 32, 1, 1, 8>(g, stream);
+    case TILE_256: return launch_gradients_as<T, 256, 256, 2, 4, 1, 2>(g, stream);
+    case TILE_128: return launch_gradients_as<T, 128, 128, 2, 2, 1, 2>(g, stream);
+    case TILE_128_DEEP: return launch_gradients_as<T, 128, 128, 2, 2, 1, 4>(g, stream);
+    case TILE_64_K2: return launch_gradients_as<T, 64, 64, 2, 1, 2, 2>(g, stream);
+    case TILE_64_K2_DEEP: return launch_gradients_as<T, 64, 64, 2, 1, 2, 4>(g, stream);
+    case TILE_32_K4: return launch_gradients_as<T, 32, 64, 1, 1, 4, 3>(g, stream);
+    default: return launch_gradients_as<T, 32, 32, 1, 1, 8, 2>(g, stream);
   }
 }
 
