@@ -17,13 +17,15 @@
 // row k at place b ^ g(k) with g from bits 0, 1 and 3 of k; the transposing read ds_read_b64_tr_b16 turns four rows of
 // sixteen columns into four k's a lane.  KS fp32: four 4-byte reads a fragment, 128-byte block b of row k at b ^ bit 2 of k.
 //
-// MFMA: 32x32x16 bf16, and for fp32 32x32x2 with the four floats of a 16-byte group as four steps (the order of k within a
-// slab is the same permutation for both operands).  B rides on the first operand, so a lane holds one row m of C and runs
+// MFMA: 32x32x16 bf16; for fp32 the same on numbers split into three bf16 parts, or 32x32x2 with the four floats of a 16-byte group
+// as four steps (the order of k within a slab is the same permutation for both operands).  B rides on the first operand, so a lane holds one row m of C and runs
 // of four neighbouring n.  The epilogue passes 32 x 64 pieces of C through LDS, one wavefront at a time, so that outputs
 // leave as whole rows of 64 columns.
 #pragma once
 
 #include "large_ops.h"
+
+#include <type_traits>
 
 namespace dllk {
 namespace tile {
@@ -230,6 +232,43 @@ __device__ __forceinline__ floatx16 mfma(floatx4 b, floatx4 a, floatx16 c) {
   return c;
 }
 
+// Single precision on the bfloat16 matrix pipe, which has 16 times the rate: x = hi + mid + lo up to 2^-24 |x|, each the rest so far
+// rounded to nearest (the rests are exact), and of the nine products of two such sums the six that reach 2^-24 of the whole.
+// dot2 takes a number off its rounded pair without unpacking it.
+typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
+struct Split { bf16x8 p[3]; };
+__device__ __forceinline__ Split split3(floatx4 x, floatx4 y) {
+  unsigned lo_ = 0xBF80u, hi_ = 0xBF800000u;   // (-1, 0) and (0, -1), in registers: as inline constants they are single precision's
+  asm("" : "+s"(lo_), "+s"(hi_));
+  const bf16x2 first = __builtin_bit_cast(bf16x2, lo_), second = __builtin_bit_cast(bf16x2, hi_);
+  Split s;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    float a = j < 2 ? x[2 * j] : y[2 * j - 4], b = j < 2 ? x[2 * j + 1] : y[2 * j - 3];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      bf16x2 h;
+      h[0] = (bf16)a;
+      h[1] = (bf16)b;
+      s.p[k][2 * j] = h[0];
+      s.p[k][2 * j + 1] = h[1];
+      if (k < 2) {
+        a = __builtin_amdgcn_fdot2_f32_bf16(h, first, a, false);
+        b = __builtin_amdgcn_fdot2_f32_bf16(h, second, b, false);
+      }
+    }
+  }
+  return s;
+}
+__device__ __forceinline__ floatx16 mfma6(const Split &b, const Split &a, floatx16 c) {   // the small products first
+  c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b.p[0], a.p[2], c, 0, 0, 0);
+  c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b.p[2], a.p[0], c, 0, 0, 0);
+  c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b.p[1], a.p[1], c, 0, 0, 0);
+  c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b.p[0], a.p[1], c, 0, 0, 0);
+  c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b.p[1], a.p[0], c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(b.p[0], a.p[0], c, 0, 0, 0);
+}
+
 // ------------------------------------------------------------------------------------------------ kernel
 // WK groups of WM x WN wavefronts of (BM / WM) x (BN / WN) each; the groups take the slabs in turn and their sums are added in LDS in
 // group order (products with too few tiles to fill the chip: the chain of slabs is WK times shorter).
@@ -277,17 +316,15 @@ __device__ __forceinline__ void product_tile(const ProductArgs &a, const Epi &ep
   };
 
   floatx16 acc[TM][TN];
-#pragma unroll
-  for (int i = 0; i < TM; ++i)
-#pragma unroll
-    for (int j = 0; j < TN; ++j) acc[i][j] = floatx16{};
   const typename Epi::Ahead ahead = epi.ahead(m0 + wm, M, lane);   // what the epilogue wants on its way during the products
   const FragReader<T, BM, AKC> ra(lane);
   const FragReader<T, BN, BKC> rb(lane);
-  // Fragments are read one step ahead of the products that take them.  The one barrier of a slab stands before its last
-  // step: by then every wavefront holds its last fragments of this slab, so its place can take the slab STAGES turns on, and has
-  // seen its part of the next slab land, whose first fragments are read behind the barrier while the last step multiplies.
-  typename Elem<T>::Frag fa[2][TM], fb[2][TN];
+  // Fragments are read ahead of the products that take them: of one of a slab's four steps, or of half a slab where single
+  // precision is split.  The one barrier of a slab stands before its last products: by then every wavefront holds its last
+  // fragments of this slab, so its place can take the slab STAGES turns on, and has seen its part of the next slab land, whose
+  // first fragments are read behind the barrier while the last products run.
+  constexpr bool kSplits = sizeof(T) == 4 && TM * TN > 1;
+  typename Elem<T>::Frag fa[kSplits ? 4 : 2][TM], fb[kSplits ? 4 : 2][TN];
   const auto read = [&](int set, const char *lds, int s) {
 #pragma unroll
     for (int j = 0; j < TN; ++j) fb[set][j] = rb(lds + kA, wn + 32 * j, s);
@@ -302,30 +339,89 @@ __device__ __forceinline__ void product_tile(const ProductArgs &a, const Epi &ep
       for (int j = 0; j < TN; ++j) acc[i][j] = mfma(fb[set][j], fa[set][i], acc[i][j]);
     __builtin_amdgcn_sched_barrier(0);
   };
-  if (turns > 0) {
+  const auto multiply_split = [&](int set) {
+    if constexpr (sizeof(T) == 4) {
+      Split b[TN];
+#pragma unroll
+      for (int j = 0; j < TN; ++j) b[j] = split3(fb[set][j], fb[set + 1][j]);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        const Split x = split3(fa[set][i], fa[set + 1][i]);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = mfma6(b[j], x, acc[i][j]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  const auto products = [&](auto split) {
+    constexpr bool kSplit = decltype(split)::value;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = floatx16{};
+    if (turns == 0) return;
 #pragma unroll
     for (int p = 0; p < STAGES; ++p) load(p, p);
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads * (STAGES - 1)) : "memory");
     barrier();
     read(0, mine, 0);
+    if (kSplit) read(1, mine, 1);
     int stage = 0;
     for (int turn = 0; turn < turns; ++turn) {
       const int next = STAGES == 2 ? stage ^ 1 : stage + 1 == STAGES ? 0 : stage + 1;
       const char *now = mine + stage * kStage;
-      read(1, now, 1);
-      multiply(0);
-      read(0, now, 2);
-      multiply(1);
-      read(1, now, 3);
-      multiply(0);
+      if constexpr (kSplit) {
+        read(2, now, 2);
+        read(3, now, 3);
+        multiply_split(0);
+      } else {
+        read(1, now, 1);
+        multiply(0);
+        read(0, now, 2);
+        multiply(1);
+        read(1, now, 3);
+        multiply(0);
+      }
       asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLoads * (STAGES - 2)) : "memory");
       barrier();
       load(turn + STAGES, stage);
       read(0, mine + next * kStage, 0);
-      multiply(1);
+      if constexpr (kSplit) {
+        read(1, mine + next * kStage, 1);
+        multiply_split(2);
+      } else {
+        multiply(1);
+      }
       stage = next;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // of the slabs of zeros too
+  };
+  // Single precision is split where a fragment is used twice at least (4096 x 8192 x 1024 in tiles of 128 x 128: 187 TFLOP/s against
+  // 123 as it is, and an error of 3.4e-7 against 4.1e-7).  A number beyond bfloat16's range, an infinity or a NaN leaves sums that
+  // are not finite: such a tile is taken again as it is.  Numbers below 2^-110 lose digits, as their parts fall below 2^-126.
+  if constexpr (kSplits) {
+    products(std::true_type{});
+    bool finite = true;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) finite = finite && fabsf(acc[i][j][r]) < INFINITY;
+    unsigned *flag = reinterpret_cast<unsigned *>(smem);   // one a wavefront, in the slabs' place
+    __syncthreads();
+    if (lane == 0) flag[all] = 0u;
+    if (!finite) flag[all] = 1u;
+    __syncthreads();
+    unsigned again = 0u;
+#pragma unroll
+    for (int w = 0; w < WM * WN * WK; ++w) again |= flag[w];
+    if (__builtin_amdgcn_readfirstlane((int)again)) {
+      __syncthreads();   // everyone has read the flags
+      products(std::false_type{});
+    }
+  } else {
+    products(std::false_type{});
   }
   __syncthreads();   // the slabs' place becomes the epilogue's
   constexpr int kPiece = 32 * kStageLd;
@@ -577,13 +673,13 @@ struct ProductPlan { int tiling = TILE_128, splits = 1; };
 // products, what a workgroup takes besides its turns, and how many a unit holds.
 struct TilingCost { int bm, bn, groups, resident; double share[2], chain[2], besides[2]; };   // [fp32, bf16]
 constexpr TilingCost kTilings[TILINGS] = {
-    {256, 256, 1, 1, {7.8, 1.62}, {7.4, 1.5}, {6.0, 8.0}},
-    {128, 128, 1, 2, {2.08, 0.55}, {2.05, 1.0}, {4.0, 4.0}},
-    {128, 128, 1, 1, {2.1, 0.78}, {2.1, 0.78}, {3.5, 3.0}},
-    {64, 64, 2, 2, {1.07, 0.45}, {1.15, 0.88}, {3.0, 2.5}},
+    {256, 256, 1, 1, {0, 1.62}, {0, 1.5}, {0, 8.0}},   // bfloat16 alone: a split's fragments would not fit beside 128 sums
+    {128, 128, 1, 2, {1.4, 0.55}, {1.45, 1.0}, {4.0, 4.0}},
+    {128, 128, 1, 1, {1.6, 0.78}, {1.48, 0.78}, {3.5, 3.0}},
+    {64, 64, 2, 2, {0.9, 0.45}, {1.08, 0.88}, {3.0, 2.5}},
     {64, 64, 2, 1, {1.12, 0.62}, {1.12, 0.62}, {3.0, 2.5}},
-    {32, 64, 4, 1, {1.3, 0.9}, {1.3, 0.9}, {3.5, 2.5}},
-    {32, 32, 8, 1, {1.1, 0.9}, {1.1, 0.9}, {3.5, 3.0}},   // 32 columns a wavefront
+    {32, 64, 4, 1, {1.35, 0.9}, {1.35, 0.9}, {3.5, 2.5}},
+    {32, 32, 8, 1, {1.35, 0.9}, {1.35, 0.9}, {3.5, 3.0}},   // 32 columns a wavefront
 };
 
 // The tiling and the number of parts of k with the least estimated time.  Parts of k cost their sums' way to memory and back and
@@ -592,7 +688,7 @@ inline ProductPlan plan_product(int dtype, int M, int N, long slabs, int problem
   ProductPlan best;
   double least = 1e30;
   const int type = dtype == TYPE_BF16 ? 1 : 0, cus = chip().cus;
-  for (int i = 0; i < TILINGS; ++i) {
+  for (int i = type ? TILE_256 : TILE_128; i < TILINGS; ++i) {
     const TilingCost &c = kTilings[i];
     const long nn = pair ? 2L * N : N, tiles = (long)((M + c.bm - 1) / c.bm) * ((nn + c.bn - 1) / c.bn) * problems;
     for (int s = 1; s <= (may_split ? 32 : 1); s *= 2) {
@@ -642,7 +738,9 @@ template <class T, bool AKC, bool BKC, bool PAIR, class Epi>
 hipError_t launch_product(const ProductArgs &a, const Epi &epi, int tiling, hipStream_t stream) {
   if (a.M <= 0 || a.N <= 0) return hipSuccess;
   switch (tiling) {
-    case TILE_256: return launch_tiling<T, 256, 256, 2, 4, 1, 2, AKC, BKC, PAIR, Epi>(a, epi, stream);
+    case TILE_256:
+      if constexpr (sizeof(T) == 2) return launch_tiling<T, 256, 256, 2, 4, 1, 2, AKC, BKC, PAIR, Epi>(a, epi, stream);
+      [[fallthrough]];   // not planned for single precision
     case TILE_128: return launch_tiling<T, 128, 128, 2, 2, 1, 2, AKC, BKC, PAIR, Epi>(a, epi, stream);
     case TILE_128_DEEP: return launch_tiling<T, 128, 128, 2, 2, 1, 4, AKC, BKC, PAIR, Epi>(a, epi, stream);
     case TILE_64_K2: return launch_tiling<T, 64, 64, 2, 1, 2, 2, AKC, BKC, PAIR, Epi>(a, epi, stream);
@@ -727,7 +825,7 @@ inline ProductPlan plan_gradients(int dtype, const GradientShape *shape, int n) 
   ProductPlan best;
   double least = 1e30;
   const int type = dtype == TYPE_BF16 ? 1 : 0, cus = chip().cus;
-  for (int i = 0; i < TILINGS; ++i) {
+  for (int i = type ? TILE_256 : TILE_128; i < TILINGS; ++i) {
     const TilingCost &c = kTilings[i];
     for (int s = 1; s <= 32; s *= 2) {
       double all = 0, longest = 0, shortest = 1e30, extra = 0;
@@ -806,7 +904,9 @@ template <class T>
 hipError_t launch_gradients(const GradientJobs<T> &g, hipStream_t stream) {
   if (g.n == 0) return hipSuccess;
   switch (g.plan.tiling) {
-    case TILE_256: return launch_gradients_as<T, 256, 256, 2, 4, 1, 2>(g, stream);
+    case TILE_256:
+      if constexpr (sizeof(T) == 2) return launch_gradients_as<T, 256, 256, 2, 4, 1, 2>(g, stream);
+      [[fallthrough]];   // not planned for single precision
     case TILE_128: return launch_gradients_as<T, 128, 128, 2, 2, 1, 2>(g, stream);
     case TILE_128_DEEP: return launch_gradients_as<T, 128, 128, 2, 2, 1, 4>(g, stream);
     case TILE_64_K2: return launch_gradients_as<T, 64, 64, 2, 1, 2, 2>(g, stream);

@@ -4,6 +4,9 @@ an operand type may take a result from them.
 Bounds are elementwise and follow the computation.  A product of K terms summed in 32 bits in any order is off by at most
 K * 2^-24 * sum |a||b| (first order); a rounding to type t by half a step, eps(t) / 2 relative; errors of operands pass
 through products with the other operand's magnitude and through a function with the bound of its derivative.
+Single precision may be multiplied as three bfloat16 parts, x = hi + mid + lo + r with |mid| <= 2^-8 |x|, |lo| <= 2^-16 |x|,
+|r| <= 2^-24 |x|: the six products kept leave out mid lo + lo mid + r y + x r', at most 4 * 2^-24 |x||y|, and each term is six
+numbers to add, of which five are at most 2^-8 of it: five roundings of the first sums more.  Hence K + 12 for K + 4.
 """
 import math
 
@@ -18,7 +21,7 @@ def unit(dtype):
 
 
 def gamma(k):
-    return (k + 4) * U32
+    return (k + 12) * U32
 
 
 def act(name, a):

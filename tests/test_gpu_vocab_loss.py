@@ -151,11 +151,15 @@ def test_rows_without_a_finite_logit_and_nan_stay_in_their_rows():
     T, D, V = 20, 16, 130
     spec = VocabSpec(T, D, V, "float32")
     i = inputs(T, D, V, "float32", True, seed=3)
-    good = run_fwd(spec, i)
+    want = ref.vocab(*i.values())
     i["x"][5, 3] = float("nan")
     bad = run_fwd(spec, i)
     rest = torch.arange(T, device="cuda") != 5
-    assert torch.equal(good["row_loss"][rest], bad["row_loss"][rest]) and torch.isnan(bad["row_loss"][5]) and torch.isnan(bad["loss"]).all()
+    # a tile with a sum that is not finite is multiplied again in single precision as it is, so the other rows' last digits may
+    # differ from a run without the NaN; both are within the bounds of the same 64-bit result
+    for k in ("row_loss", "row_lse"):
+        ref.check(bad[k][rest], tuple(v[rest] for v in want[k]), k)
+    assert torch.isnan(bad["row_loss"][5]) and torch.isnan(bad["loss"]).all()
     i["bias"].fill_(float("-inf"))
     assert torch.isnan(run_fwd(spec, i)["row_loss"]).all()
 
