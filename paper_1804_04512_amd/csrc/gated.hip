@@ -70,8 +70,8 @@ __device__ __forceinline__ float gate_value(int gate, float a) {
 // padded rows
 template <class T>
 struct GateEpi : NothingAhead {
-  GateEpi(int gate_, int vec_kept_, T *h_, long ldh_, T *a_, T *b_) : gate(gate_), vec_kept(vec_kept_), h(h_), ldh(ldh_), kept_a(a_), kept_b(b_) {}
-  int gate, vec_kept;
+  GateEpi(int gate_, T *h_, long ldh_, T *a_, T *b_) : gate(gate_), h(h_), ldh(ldh_), kept_a(a_), kept_b(b_) {}
+  int gate;
   T *h;
   long ldh;
   T *kept_a, *kept_b;   // nullable, [T][H]
@@ -89,21 +89,11 @@ struct GateEpi : NothingAhead {
       const int left = H - n - col;
 #pragma unroll
       for (int j = 0; j < 8; ++j) vh[j] = j < left ? gate_value<T>(gate, va[j]) * vb[j] : 0.0f;
-      store8<T>(h + (long)(m + row) * ldh + n + col, vh, true, 8);
-      if (kept_a && vec_kept) {
+      store8<T>(h + (long)(m + row) * ldh + n + col, vh, 8);
+      if (kept_a) {
         const long o = (long)(m + row) * H + n + col;
-        store8<T>(kept_a + o, va, left >= 8, left);
-        store8<T>(kept_b + o, vb, left >= 8, left);
-      }
-    }
-    if (kept_a && !vec_kept) {   // rows that start anywhere: a column a lane
-      const int lane = threadIdx.x & 63, at = lane % (WC / 2);
-      T *const kept = lane % WC < WC / 2 ? kept_a : kept_b;
-      if (n + at >= H) return;
-#pragma unroll 8
-      for (int row = lane / WC; row < 32; row += 64 / WC) {
-        if (m + row >= M) break;
-        kept[(long)(m + row) * H + n + at] = (T)stage[row * kStageLd + lane % WC];
+        store8<T>(kept_a + o, va, left);
+        store8<T>(kept_b + o, vb, left);
       }
     }
   }
@@ -137,40 +127,23 @@ struct SkinnyGate {
 // da, db and h from dh and the kept a and b, all three in padded rows
 template <class T>
 struct GateBackEpi : NothingAhead {
-  GateBackEpi(int gate_, int vec_kept_, const T *a_, const T *b_, T *da_, T *db_, T *h_, long ld_)
-      : gate(gate_), vec_kept(vec_kept_), a(a_), b(b_), da(da_), db(db_), h(h_), ld(ld_) {}
-  int gate, vec_kept;
+  GateBackEpi(int gate_, const T *a_, const T *b_, T *da_, T *db_, T *h_, long ld_)
+      : gate(gate_), a(a_), b(b_), da(da_), db(db_), h(h_), ld(ld_) {}
+  int gate;
   const T *a, *b;
   T *da, *db, *h;
   long ld;
   template <int WC>
   __device__ __forceinline__ void piece(const float *stage, int m, int n, int M, int H, int, int, int, Nothing) const {
-    if (!vec_kept) {   // rows that start anywhere: a column a lane, zeros up to the next whole run of eight
-      const int lane = threadIdx.x & 63, at = n + lane % WC;
-      if (at >= ((H + 7) & ~7)) return;
-#pragma unroll 8
-      for (int row = lane / WC; row < 32; row += 64 / WC) {
-        if (m + row >= M) break;
-        const long from = (long)(m + row) * H + at, to = (long)(m + row) * ld + at;
-        const float va = at < H ? to_float(a[from]) : 0.0f, vb = at < H ? to_float(b[from]) : 0.0f, dh = at < H ? stage[row * kStageLd + lane % WC] : 0.0f;
-        float f, d;
-        gate_both<T>(gate, va, &f, &d);
-        da[to] = (T)(dh * vb * d);
-        db[to] = (T)(dh * f);
-        h[to] = (T)(f * vb);
-      }
-      return;
-    }
     const Lanes<WC> l;
     const int col = l.col, left = H - n - col;
     if (left <= 0) return;
-    const bool whole = left >= 8;
     Eight<T> va[l.kPasses], vb[l.kPasses];   // all loads of the piece go out together
 #pragma unroll
     for (int p = 0; p < l.kPasses; ++p) {
       const int row = min(m + l.kRows * p + l.row, M - 1);
-      va[p].load(a + (long)row * H + n + col, whole, left);
-      vb[p].load(b + (long)row * H + n + col, whole, left);
+      va[p].load(a + (long)row * H + n + col, left);
+      vb[p].load(b + (long)row * H + n + col, left);
     }
 #pragma unroll
     for (int p = 0; p < l.kPasses; ++p) {
@@ -188,9 +161,9 @@ struct GateBackEpi : NothingAhead {
         oh[j] = j < left ? f * vb_ : 0.0f;
       }
       const long o = (long)(m + row) * ld + n + col;
-      store8<T>(da + o, oa, true, 8);
-      store8<T>(db + o, ob, true, 8);
-      store8<T>(h + o, oh, true, 8);
+      store8<T>(da + o, oa, 8);
+      store8<T>(db + o, ob, 8);
+      store8<T>(h + o, oh, 8);
     }
   }
 };
@@ -235,8 +208,8 @@ struct FwdPlan {
       bytes = take.used;
       return;
     }
-    if (!whole_groups(D, dtype)) x = take((size_t)T * ldd * e), wg = take((size_t)H * ldd * e), wu = take((size_t)H * ldd * e);
-    if (!whole_groups(H, dtype)) wd = take((size_t)D * ldh * e);
+    if (!loadable(D, dtype)) x = take((size_t)T * ldd * e), wg = take((size_t)H * ldd * e), wu = take((size_t)H * ldd * e);
+    if (!loadable(H, dtype)) wd = take((size_t)D * ldh * e);
     up = plan_product(dtype, T, H, slabs_of(D, dtype), 1, true, false);
     down = plan_product(dtype, T, D, slabs_of(H, dtype), 1, false, true);
     part = (float *)take(partial_bytes(down.splits, T, D));
@@ -259,8 +232,8 @@ struct BwdPlan {
     db = take((size_t)T * ldh * e);
     h = take((size_t)T * ldh * e);
     x = wg = wu = wd = dy = nullptr;
-    if (!whole_groups(D, dtype)) x = take((size_t)T * ldd * e), dy = take((size_t)T * ldd * e), wg = take((size_t)H * ldd * e), wu = take((size_t)H * ldd * e);
-    if (!whole_groups(H, dtype)) wd = take((size_t)D * ldh * e);
+    if (!loadable(D, dtype)) x = take((size_t)T * ldd * e), dy = take((size_t)T * ldd * e), wg = take((size_t)H * ldd * e), wu = take((size_t)H * ldd * e);
+    if (!loadable(H, dtype)) wd = take((size_t)D * ldh * e);
     dh = plan_product(dtype, T, H, slabs_of(D, dtype), 1, false, false);
     const long tokens = slabs_of(T, dtype);
     const GradientShape shape[3] = {{T, D, 2 * slabs_of(H, dtype), 1, true}, {H, D, tokens, 2, false}, {D, H, tokens, 1, false}};
@@ -307,7 +280,7 @@ hipError_t gated_fwd(const GatedArgs &a, char *scratch, hipStream_t stream) {
   g.B[0] = {wg, ldx};
   g.B[1] = {wu, ldx};
   g.K[0] = a.D;
-  const GateEpi<T> ge(a.gate, rows16<T>(a.gate_pre, a.H) && rows16<T>(a.up_pre, a.H), (T *)p.h, p.ldh, (T *)a.gate_pre, (T *)a.up_pre);
+  const GateEpi<T> ge(a.gate, (T *)p.h, p.ldh, (T *)a.gate_pre, (T *)a.up_pre);
   DLL_TRY((launch_product<T, true, true, true>(g, ge, p.up.tiling, stream)));
   ProductArgs y;
   y.M = a.T;
@@ -315,7 +288,7 @@ hipError_t gated_fwd(const GatedArgs &a, char *scratch, hipStream_t stream) {
   y.A[0] = {p.h, p.ldh};
   y.B[0] = {wd, ldd};
   y.K[0] = a.H;
-  StoreEpi<T> out((T *)a.y, nullptr, a.D, rows16<T>(a.y, a.D), nullptr, 0);
+  StoreEpi<T> out((T *)a.y, nullptr, a.D, nullptr, 0);
   return product_to<T, true, true>(y, out, p.down, p.part, stream);
 }
 
@@ -346,7 +319,7 @@ hipError_t gated_bwd(const GatedArgs &a, char *scratch, hipStream_t stream) {
   g.A[0] = {dy, ldx};
   g.B[0] = {wd, ldd};
   g.K[0] = a.D;   // Wd lies across k; where D is no multiple of a 16-byte group, dy's copy has zeros behind it
-  const GateBackEpi<T> ge(a.gate, rows16<T>(a.gate_pre, a.H) && rows16<T>(a.up_pre, a.H), (const T *)a.gate_pre, (const T *)a.up_pre,
+  const GateBackEpi<T> ge(a.gate, (const T *)a.gate_pre, (const T *)a.up_pre,
                     (T *)p.da, (T *)p.db, (T *)p.h, p.ldh);
   DLL_TRY((launch_product<T, true, false, false>(g, ge, p.dh.tiling, stream)));
   GradientJobs<T> jobs;
@@ -361,7 +334,7 @@ hipError_t gated_bwd(const GatedArgs &a, char *scratch, hipStream_t stream) {
     w.B[0] = {wg, ldx};
     w.B[1] = {wu, ldx};
     w.K[0] = w.K[1] = a.H;
-    jobs.add(w, StoreEpi<T>((T *)a.dx, nullptr, a.D, rows16<T>(a.dx, a.D), nullptr, 0), true);
+    jobs.add(w, StoreEpi<T>((T *)a.dx, nullptr, a.D, nullptr, 0), true);
   }
   if (a.dw_gate || a.dw_up) {
     ProductArgs w;
@@ -375,7 +348,7 @@ hipError_t gated_bwd(const GatedArgs &a, char *scratch, hipStream_t stream) {
     w.A[1] = {d[1], p.ldh};
     w.B[0] = w.B[1] = {x, ldx};
     w.K[0] = a.T;
-    jobs.add(w, StoreEpi<T>(o[first], o[1], a.D, rows16<T>(o[first], a.D) && rows16<T>(o[w.problems - 1], a.D), nullptr, 0), false);
+    jobs.add(w, StoreEpi<T>(o[first], o[1], a.D, nullptr, 0), false);
   }
   if (a.dw_down) {
     ProductArgs w;
@@ -384,7 +357,7 @@ hipError_t gated_bwd(const GatedArgs &a, char *scratch, hipStream_t stream) {
     w.A[0] = {dy, ldx};
     w.B[0] = {p.h, p.ldh};
     w.K[0] = a.T;
-    jobs.add(w, StoreEpi<T>((T *)a.dw_down, nullptr, a.H, rows16<T>(a.dw_down, a.H), nullptr, 0), false);
+    jobs.add(w, StoreEpi<T>((T *)a.dw_down, nullptr, a.H, nullptr, 0), false);
   }
   return launch_gradients<T>(jobs, stream);
 }

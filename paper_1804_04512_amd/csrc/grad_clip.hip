@@ -26,7 +26,7 @@ struct NormTable {
   const void *g[kTable];
   long count[kTable];
   int first[kTable + 1];            // chunk at which each tensor starts
-  unsigned char type[kTable], vec[kTable];
+  unsigned char type[kTable];
 };
 struct ClipTable {
   NormTable t;
@@ -61,23 +61,15 @@ __device__ __forceinline__ double group_sum(double s) {
 }
 
 template <class T>
-__device__ __forceinline__ double squares(const T *g, long begin, long end, bool vec) {
+__device__ __forceinline__ double squares(const T *g, long begin, long end) {
   double s = 0.0;
-  if (vec) {
 #pragma unroll 4
-    for (long i = begin + 8 * threadIdx.x; i < end; i += 8 * 256) {
-      float v[8];
-      const long left = end - i;
-      load8<T>(g + i, v, left >= 8, (int)(left < 8 ? left : 8));
+  for (long i = begin + 8 * threadIdx.x; i < end; i += 8 * 256) {
+    float v[8];
+    const long left = end - i;
+    load8<T>(g + i, v, (int)(left < 8 ? left : 8));
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s += (double)v[j] * (double)v[j];
-    }
-  } else {
-#pragma unroll 8
-    for (long i = begin + threadIdx.x; i < end; i += 256) {
-      const double v = (double)to_float(g[i]);
-      s += v * v;
-    }
+    for (int j = 0; j < 8; ++j) s += (double)v[j] * (double)v[j];
   }
   return s;
 }
@@ -87,7 +79,7 @@ __global__ __launch_bounds__(256) void grad_squares_kernel(const NormTable t, do
   for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
     const int i = tensor_of(t, c);
     const long begin = (long)(c - t.first[i]) * kChunk, end = min(t.count[i], begin + kChunk);
-    s += t.type[i] == TYPE_BF16 ? squares<bf16>((const bf16 *)t.g[i], begin, end, t.vec[i]) : squares<float>((const float *)t.g[i], begin, end, t.vec[i]);
+    s += t.type[i] == TYPE_BF16 ? squares<bf16>((const bf16 *)t.g[i], begin, end) : squares<float>((const float *)t.g[i], begin, end);
   }
   s = group_sum(s);
   if (threadIdx.x == 0) partial[blockIdx.x] = s;
@@ -101,19 +93,18 @@ __device__ __forceinline__ void few_apply(const ClipTable &a, int i, long at, in
   if (c == 1.0f && a.out[i] == a.t.g[i]) return;
 #pragma unroll
   for (int j = 0; j < 8; ++j) g[j] *= c;
-  if (a.t.type[i] == TYPE_BF16) store8<bf16>((bf16 *)a.out[i] + at, g, a.t.vec[i] && left == 8, left);
-  else store8<float>((float *)a.out[i] + at, g, a.t.vec[i] && left == 8, left);
+  if (a.t.type[i] == TYPE_BF16) store8<bf16>((bf16 *)a.out[i] + at, g, left);
+  else store8<float>((float *)a.out[i] + at, g, left);
 }
 __device__ __forceinline__ void few_apply(const StepTable &a, int i, long at, int left, float (&g)[8], float c, float step, float mu) {
-  const bool whole = a.t.vec[i] && left == 8;
   float p[8], v[8];
-  load8<float>(a.p[i] + at, p, whole, left);
-  load8<float>(a.v[i] + at, v, whole, left);
+  load8<float>(a.p[i] + at, p, left);
+  load8<float>(a.v[i] + at, v, left);
 #pragma unroll
   for (int j = 0; j < 8; ++j) update_param(&p[j], &v[j], g[j] * c, step, mu, a.decay[i]);
-  store8<float>(a.p[i] + at, p, whole, left);
-  store8<float>(a.v[i] + at, v, whole, left);
-  if (a.copy[i]) store8<bf16>(a.copy[i] + at, p, whole, left);
+  store8<float>(a.p[i] + at, p, left);
+  store8<float>(a.v[i] + at, v, left);
+  if (a.copy[i]) store8<bf16>(a.copy[i] + at, p, left);
 }
 
 // the norm from the partial sums, the same in every workgroup
@@ -138,20 +129,15 @@ __global__ __launch_bounds__(256) void norm_kernel(const double *partial, int n,
 }
 
 template <class T>
-__device__ __forceinline__ void scale_chunk(const T *g, T *out, long begin, long end, bool vec, float c) {
-  if (vec) {
+__device__ __forceinline__ void scale_chunk(const T *g, T *out, long begin, long end, float c) {
 #pragma unroll 4
-    for (long i = begin + 8 * threadIdx.x; i < end; i += 8 * 256) {
-      float v[8];
-      const int left = (int)(end - i < 8 ? end - i : 8);
-      load8<T>(g + i, v, left == 8, left);
+  for (long i = begin + 8 * threadIdx.x; i < end; i += 8 * 256) {
+    float v[8];
+    const int left = (int)(end - i < 8 ? end - i : 8);
+    load8<T>(g + i, v, left);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] *= c;
-      store8<T>(out + i, v, left == 8, left);
-    }
-  } else {
-#pragma unroll 8
-    for (long i = begin + threadIdx.x; i < end; i += 256) out[i] = (T)(to_float(g[i]) * c);
+    for (int j = 0; j < 8; ++j) v[j] *= c;
+    store8<T>(out + i, v, left);
   }
 }
 
@@ -164,36 +150,25 @@ __global__ __launch_bounds__(256) void grad_scale_kernel(const ClipTable a, cons
     const int i = tensor_of(t, k);
     if (c == 1.0f && a.out[i] == t.g[i]) continue;   // in place, and nothing to scale
     const long begin = (long)(k - t.first[i]) * kChunk, end = min(t.count[i], begin + kChunk);
-    if (t.type[i] == TYPE_BF16) scale_chunk<bf16>((const bf16 *)t.g[i], (bf16 *)a.out[i], begin, end, t.vec[i], c);
-    else scale_chunk<float>((const float *)t.g[i], (float *)a.out[i], begin, end, t.vec[i], c);
+    if (t.type[i] == TYPE_BF16) scale_chunk<bf16>((const bf16 *)t.g[i], (bf16 *)a.out[i], begin, end, c);
+    else scale_chunk<float>((const float *)t.g[i], (float *)a.out[i], begin, end, c);
   }
 }
 
 template <class T>
-__device__ __forceinline__ void step_chunk(const T *g, float *p, float *v, bf16 *copy, long begin, long end, bool vec, float c, float step, float mu, float decay) {
-  if (vec) {
+__device__ __forceinline__ void step_chunk(const T *g, float *p, float *v, bf16 *copy, long begin, long end, float c, float step, float mu, float decay) {
 #pragma unroll 2
-    for (long i = begin + 8 * threadIdx.x; i < end; i += 8 * 256) {
-      float vg[8], vp[8], vv[8];
-      const int left = (int)(end - i < 8 ? end - i : 8);
-      load8<T>(g + i, vg, left == 8, left);
-      load8<float>(p + i, vp, left == 8, left);
-      load8<float>(v + i, vv, left == 8, left);
+  for (long i = begin + 8 * threadIdx.x; i < end; i += 8 * 256) {
+    float vg[8], vp[8], vv[8];
+    const int left = (int)(end - i < 8 ? end - i : 8);
+    load8<T>(g + i, vg, left);
+    load8<float>(p + i, vp, left);
+    load8<float>(v + i, vv, left);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) update_param(&vp[j], &vv[j], vg[j] * c, step, mu, decay);
-      store8<float>(p + i, vp, left == 8, left);
-      store8<float>(v + i, vv, left == 8, left);
-      if (copy) store8<bf16>(copy + i, vp, left == 8, left);
-    }
-  } else {
-#pragma unroll 4
-    for (long i = begin + threadIdx.x; i < end; i += 256) {
-      float q = p[i], w = v[i];
-      update_param(&q, &w, to_float(g[i]) * c, step, mu, decay);
-      p[i] = q;
-      v[i] = w;
-      if (copy) copy[i] = (bf16)q;
-    }
+    for (int j = 0; j < 8; ++j) update_param(&vp[j], &vv[j], vg[j] * c, step, mu, decay);
+    store8<float>(p + i, vp, left);
+    store8<float>(v + i, vv, left);
+    if (copy) store8<bf16>(copy + i, vp, left);
   }
 }
 
@@ -206,8 +181,8 @@ __global__ __launch_bounds__(256) void momentum_step_kernel(const StepTable a, c
   for (int k = blockIdx.x; k < t.chunks; k += gridDim.x) {
     const int i = tensor_of(t, k);
     const long begin = (long)(k - t.first[i]) * kChunk, end = min(t.count[i], begin + kChunk);
-    if (t.type[i] == TYPE_BF16) step_chunk<bf16>((const bf16 *)t.g[i], a.p[i], a.v[i], a.copy[i], begin, end, t.vec[i], c, step, mu, a.decay[i]);
-    else step_chunk<float>((const float *)t.g[i], a.p[i], a.v[i], a.copy[i], begin, end, t.vec[i], c, step, mu, a.decay[i]);
+    if (t.type[i] == TYPE_BF16) step_chunk<bf16>((const bf16 *)t.g[i], a.p[i], a.v[i], a.copy[i], begin, end, c, step, mu, a.decay[i]);
+    else step_chunk<float>((const float *)t.g[i], a.p[i], a.v[i], a.copy[i], begin, end, c, step, mu, a.decay[i]);
   }
 }
 
@@ -229,8 +204,8 @@ __global__ __launch_bounds__(1024) void few_kernel(const Table a, float max_norm
       const int i = tensor[k];
       const long at = (long)(run - t.first[i]) * 8;
       const int left = (int)min(8L, t.count[i] - at);
-      if (t.type[i] == TYPE_BF16) load8<bf16>((const bf16 *)t.g[i] + at, g[k], t.vec[i] && left == 8, left);
-      else load8<float>((const float *)t.g[i] + at, g[k], t.vec[i] && left == 8, left);
+      if (t.type[i] == TYPE_BF16) load8<bf16>((const bf16 *)t.g[i] + at, g[k], left);
+      else load8<float>((const float *)t.g[i] + at, g[k], left);
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j) g[k][j] = 0.0f;
@@ -261,8 +236,6 @@ __global__ __launch_bounds__(1024) void few_kernel(const Table a, float max_norm
   }
 }
 
-bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
-
 // Tensors [at, at + kTable) of the list that hold anything; returns where the next table starts
 int fill(NormTable &t, const GradList &l, const void *const *grads, int at, int *which, int chunk = kChunk) {
   t.n = t.chunks = 0;
@@ -274,7 +247,6 @@ int fill(NormTable &t, const GradList &l, const void *const *grads, int at, int 
     t.g[t.n] = grads[at];
     t.count[t.n] = (long)l.counts[at];
     t.type[t.n] = (unsigned char)l.dtypes[at];
-    t.vec[t.n] = aligned16(grads[at]);
     t.first[t.n] = t.chunks;
     t.chunks += (int)chunks;
     ++t.n;
@@ -347,10 +319,7 @@ hipError_t launch_grad_clip(const GradList &l, const void *const *grads, void *c
   do {
     ClipTable a;
     at = fill(a.t, l, grads, at, which, few ? 8 : kChunk);
-    for (int i = 0; i < a.t.n; ++i) {
-      a.out[i] = out[which[i]];
-      a.t.vec[i] = a.t.vec[i] && aligned16(a.out[i]);
-    }
+    for (int i = 0; i < a.t.n; ++i) a.out[i] = out[which[i]];
     if (few) few_kernel<kFewClip, ClipTable><<<dim3(1), dim3(1024), 0, stream>>>(a, max_norm, 0.0f, 0.0f, norm);
     else grad_scale_kernel<<<dim3(apply_blocks(a.t.chunks)), dim3(256), 0, stream>>>(a, partial, used, max_norm, norm);
     DLL_TRY(hipGetLastError());
@@ -373,7 +342,6 @@ hipError_t launch_momentum_clipped(const GradList &l, float *const *params, floa
       a.v[i] = velocity[k];
       a.copy[i] = copies ? (bf16 *)copies[k] : nullptr;
       a.decay[i] = decay ? decay[k] : 0.0f;
-      a.t.vec[i] = a.t.vec[i] && aligned16(a.p[i]) && aligned16(a.v[i]) && aligned16(a.copy[i]);
     }
     if (few) few_kernel<kFewStep, StepTable><<<dim3(1), dim3(1024), 0, stream>>>(a, max_norm, -lr, mu, norm);
     else momentum_step_kernel<<<dim3(apply_blocks(a.t.chunks)), dim3(256), 0, stream>>>(a, partial, used, max_norm, -lr, mu, norm);

@@ -6,9 +6,10 @@
 // forms of a layer's products (forward KC KC, data gradient KC KS, weight gradient KS KS) need no transposed copies.
 //
 // A workgroup owns a BM x BN tile of C and walks k in slabs of 128 bytes a row (64 bf16, 32 fp32).  Slabs go from global
-// memory straight into LDS (16 bytes a lane, no registers in between), the next one on its way while the current one is
-// multiplied.  Every access is range checked by the buffer descriptor: rows behind the end read as zeros, and columns
-// behind K are sent out of range where the last slab is not whole, so no operand needs padding to the tile.
+// memory straight into LDS (16 bytes a lane from any multiple of four, no registers in between), the next ones on their way while
+// the current one is multiplied.  Every access is range checked by the buffer descriptor: rows behind the end read as zeros,
+// columns behind K are sent out of range where the last slab is not whole, and where K ends inside a 16-byte group what follows
+// it is cleared in LDS, so no operand needs padding.
 //
 // LDS layouts.  The hardware writes a wavefront's 64 x 16 bytes in lane order, so a swizzle is made by permuting which
 // global bytes a lane fetches.  KC: rows of 128 bytes, 16-byte group c of row r at place c ^ ((r >> 1) & 7), so that the
@@ -49,7 +50,7 @@ template <> struct Elem<float> { static constexpr int kSlab = 32; typedef floatx
 
 struct Operand {
   const void *p = nullptr;
-  long ld = 0;   // elements; rows start at multiples of 16 bytes
+  long ld = 0;   // elements; rows start at multiples of 4 bytes
 };
 
 struct ProductArgs {
@@ -57,7 +58,7 @@ struct ProductArgs {
   // segment 0 and, where K[1] > 0, a second pair of operands whose products are added to the first's;
   // or two products of one shape side by side (problems == 2), each with its own operands and outputs
   Operand A[2], B[2];
-  int K[2] = {0, 0};          // KC operands: multiples of a 16-byte group (padded with zeros by whoever wrote them)
+  int K[2] = {0, 0};
   int problems = 1;
   // Rows that exist as the device counts them: M (m_rows) and K[0] (k_rows) become what *p leaves behind `first`.
   const int *m_rows = nullptr, *k_rows = nullptr;
@@ -353,6 +354,33 @@ __device__ __forceinline__ void product_tile(const ProductArgs &a, const Epi &ep
       __builtin_amdgcn_sched_barrier(0);
     }
   };
+  // A slab in which K ends inside a 16-byte group holds what lies behind the row's end there: cleared before anyone reads it.
+  // Called behind the barrier that the turn's slabs have landed at, by everyone.
+  constexpr int kG = 16 / (int)sizeof(T);
+  const int ragged0 = AKC || BKC ? K0 % kG : 0, ragged1 = AKC || BKC ? a.K[1] % kG : 0;
+  const auto clear_tail = [&](int turn, int stage) {
+    if (ragged0 == 0 && ragged1 == 0) return;
+    const int from = t0 + turn * WK, mine_t = from + group;
+    const auto ends_in = [&](int t) {   // the k's of slab t's cut group that exist, 0: it is whole or has none
+      return t >= t1 ? 0 : t == slabs0 - 1 ? ragged0 : t == slabs - 1 ? ragged1 : 0;
+    };
+    int any = 0;
+#pragma unroll
+    for (int g = 0; g < WK; ++g) any |= ends_in(from + g);
+    if (any == 0) return;
+    const int keep = ends_in(mine_t);
+    if (keep) {
+      const int K = mine_t == slabs0 - 1 ? K0 : a.K[1], cut = K % kK / kG;
+      char *slab = mine + stage * kStage;
+      for (int row = threadIdx.x % kThreads; row < (AKC ? BM : 0) + (BKC ? BN : 0); row += kThreads) {
+        const int r = AKC && row < BM ? row : row - (AKC ? BM : 0);
+        T *p = reinterpret_cast<T *>(slab + (AKC && row < BM ? 0 : kA) + r * kSlabBytes + ((cut ^ ((r >> 1) & 7)) << 4));
+        for (int k = keep; k < kG; ++k) p[k] = (T)0.0f;
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    barrier();
+  };
   const auto products = [&](auto split) {
     constexpr bool kSplit = decltype(split)::value;
 #pragma unroll
@@ -364,6 +392,7 @@ __device__ __forceinline__ void product_tile(const ProductArgs &a, const Epi &ep
     for (int p = 0; p < STAGES; ++p) load(p, p);
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads * (STAGES - 1)) : "memory");
     barrier();
+    clear_tail(0, 0);
     read(0, mine, 0);
     if (kSplit) read(1, mine, 1);
     int stage = 0;
@@ -385,6 +414,7 @@ __device__ __forceinline__ void product_tile(const ProductArgs &a, const Epi &ep
       asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLoads * (STAGES - 2)) : "memory");
       barrier();
       load(turn + STAGES, stage);
+      clear_tail(turn + 1, next);
       read(0, mine + next * kStage, 0);
       if constexpr (kSplit) {
         read(1, mine + next * kStage, 1);
@@ -472,73 +502,46 @@ __global__ __launch_bounds__(64 * WM *WN *WK, 2) void product_kernel(const Produ
 __device__ __forceinline__ float to_float(bf16 v) { return (float)v; }
 __device__ __forceinline__ float to_float(float v) { return v; }
 
-// eight neighbours of a row; `whole`: 16-byte aligned and all eight exist
-template <class T> __device__ __forceinline__ void store8(T *p, const float (&v)[8], bool whole, int n);
-template <> __device__ __forceinline__ void store8<bf16>(bf16 *p, const float (&v)[8], bool whole, int n) {
-  if (whole) {
-    bf16x8 o;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) o[j] = (bf16)v[j];   // to nearest, ties to even
-    *reinterpret_cast<bf16x8 *>(p) = o;
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (j < n) p[j] = (bf16)v[j];
-  }
-}
-template <> __device__ __forceinline__ void store8<float>(float *p, const float (&v)[8], bool whole, int n) {
-  if (whole) {
-    reinterpret_cast<floatx4 *>(p)[0] = floatx4{v[0], v[1], v[2], v[3]};
-    reinterpret_cast<floatx4 *>(p)[1] = floatx4{v[4], v[5], v[6], v[7]};
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (j < n) p[j] = v[j];
-  }
-}
-template <class T> __device__ __forceinline__ void load8(const T *p, float (&v)[8], bool whole, int n);
-template <> __device__ __forceinline__ void load8<bf16>(const bf16 *p, float (&v)[8], bool whole, int n) {
-  if (whole) {
-    const bf16x8 o = *reinterpret_cast<const bf16x8 *>(p);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = (float)o[j];
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = j < n ? (float)p[j] : 0.f;
-  }
-}
-template <> __device__ __forceinline__ void load8<float>(const float *p, float (&v)[8], bool whole, int n) {
-  if (whole) {
-    const floatx4 a = reinterpret_cast<const floatx4 *>(p)[0], b = reinterpret_cast<const floatx4 *>(p)[1];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = a[j], v[4 + j] = b[j];
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = j < n ? p[j] : 0.f;
-  }
-}
-__device__ __forceinline__ void stage8(const float *stage, int row, int col, float (&v)[8]) {
-  const floatx4 a = *reinterpret_cast<const floatx4 *>(stage + row * kStageLd + col), b = *reinterpret_cast<const floatx4 *>(stage + row * kStageLd + col + 4);
-#pragma unroll
-  for (int j = 0; j < 4; ++j) v[j] = a[j], v[4 + j] = b[j];
-}
-// eight neighbours of a row as they lie in memory
+// Eight neighbours of a row from any element on: accesses of 16 bytes ask for no more than an element's alignment (a column a
+// lane instead made the backward epilogue of 1000 x 1337 rows 14 us slower than that of 1000 x 1336).
 template <class T> struct Eight {
   typedef T V __attribute__((ext_vector_type(8)));
+  typedef V Any __attribute__((aligned(sizeof(T))));
   V v;
-  __device__ __forceinline__ void load(const T *p, bool whole, int n) {
-    if (whole) {
-      typedef V At16 __attribute__((aligned(16)));
-      v = *reinterpret_cast<const At16 *>(p);
+  __device__ __forceinline__ void load(const T *p, int n) {   // the first n exist
+    if (n >= 8) {
+      v = *reinterpret_cast<const Any *>(p);
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = j < n ? p[j] : (T)0.0f;
     }
   }
+  __device__ __forceinline__ void store(T *p, int n) const {
+    if (n >= 8) {
+      *reinterpret_cast<Any *>(p) = v;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j < n) p[j] = v[j];
+    }
+  }
 };
-// rows of ld elements may be accessed 16 bytes at a time
-template <class T> __host__ __device__ __forceinline__ bool rows16(const void *p, long ld) {
-  return ((uintptr_t)p & 15) == 0 && ld * (long)sizeof(T) % 16 == 0;
+template <class T> __device__ __forceinline__ void store8(T *p, const float (&v)[8], int n) {
+  Eight<T> e;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) e.v[j] = (T)v[j];   // to nearest, ties to even
+  e.store(p, n);
+}
+template <class T> __device__ __forceinline__ void load8(const T *p, float (&v)[8], int n) {
+  Eight<T> e;
+  e.load(p, n);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = (float)e.v[j];
+}
+__device__ __forceinline__ void stage8(const float *stage, int row, int col, float (&v)[8]) {
+  const floatx4 a = *reinterpret_cast<const floatx4 *>(stage + row * kStageLd + col), b = *reinterpret_cast<const floatx4 *>(stage + row * kStageLd + col + 4);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = a[j], v[4 + j] = b[j];
 }
 
 // How a wavefront's lanes take a piece of 32 rows x WC columns: eight columns a lane, whole rows side by side, so that outputs leave
@@ -558,26 +561,13 @@ struct NothingAhead {
 // C[problem][m][n] in T, rows optionally through a map; or += to what a former piece left (fp32 sums)
 template <class T>
 struct StoreEpi : NothingAhead {
-  StoreEpi(T *c0, T *c1, long ld_, int vec_, const int *rows_, int add_) : c{c0, c1}, ld(ld_), vec(vec_), rows(rows_), add(add_) {}
+  StoreEpi(T *c0, T *c1, long ld_, const int *rows_, int add_) : c{c0, c1}, ld(ld_), rows(rows_), add(add_) {}
   T *c[2];
   long ld;
-  int vec;                 // rows16 of both
   const int *rows;         // nullable: row m of the product goes to row rows[m]
   int add;                 // T = float only: add to what is there
   template <int WC>
   __device__ __forceinline__ void piece(const float *stage, int m, int n, int M, int N, int problem, int, int, Nothing) const {
-    if (!vec) {   // rows that start anywhere: a column a lane
-      const int lane = threadIdx.x & 63, col = lane % WC;
-      if (n + col >= N) return;
-#pragma unroll 8
-      for (int row = lane / WC; row < 32; row += 64 / WC) {
-        if (m + row >= M) break;
-        T *d = c[problem] + (long)(rows ? rows[m + row] : m + row) * ld + n + col;
-        const float v = stage[row * kStageLd + col];
-        *d = (T)(add ? to_float(*d) + v : v);
-      }
-      return;
-    }
     const Lanes<WC> l;
     const int col = l.col;
 #pragma unroll
@@ -588,14 +578,13 @@ struct StoreEpi : NothingAhead {
       stage8(stage, row, col, v);
       T *d = c[problem] + (long)(rows ? rows[m + row] : m + row) * ld + n + col;
       const int left = N - n - col;
-      const bool whole = vec && left >= 8;
       if (add) {
         float o[8];
-        load8<T>(d, o, whole, left);
+        load8<T>(d, o, left);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] += o[j];
       }
-      store8<T>(d, v, whole, left);
+      store8<T>(d, v, left);
     }
   }
 };
@@ -616,7 +605,7 @@ struct PartialEpi : NothingAhead {
       if (m + row >= M || n + col >= N) continue;
       float v[8];
       stage8(stage, row, col, v);
-      store8<float>(part + ((long)split * rows + m + row) * n8 + n + col, v, true, 8);
+      store8<float>(part + ((long)split * rows + m + row) * n8 + n + col, v, 8);
     }
   }
 };
@@ -626,37 +615,25 @@ template <class T>
 __global__ __launch_bounds__(256) void sum_splits_kernel(const float *part, int splits, int M, int N, const int *m_rows, int first, StoreEpi<T> out) {
   const long n8 = (N + 7) & ~7;
   const int rows = rows_left(m_rows, first, M), g = (int)(n8 >> 3);
-  if (!out.vec) {
-    for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < (long)rows * N; i += (long)gridDim.x * 256) {
-      const int m = (int)(i / N), n = (int)(i - (long)m * N);
-      float v = 0.0f;
-#pragma unroll 4
-      for (int s = 0; s < splits; ++s) v += part[((long)s * M + m) * n8 + n];
-      T *d = out.c[0] + (long)(out.rows ? out.rows[m] : m) * out.ld + n;
-      *d = (T)(out.add ? to_float(*d) + v : v);
-    }
-    return;
-  }
   for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < (long)rows * g; i += (long)gridDim.x * 256) {
     const int m = (int)(i / g), n = (int)(i % g) * 8;
     float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll 4
     for (int s = 0; s < splits; ++s) {
       float o[8];
-      load8<float>(part + ((long)s * M + m) * n8 + n, o, true, 8);
+      load8<float>(part + ((long)s * M + m) * n8 + n, o, 8);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] += o[j];
     }
     T *d = out.c[0] + (long)(out.rows ? out.rows[m] : m) * out.ld + n;
     const int left = N - n;
-    const bool whole = out.vec && left >= 8;
     if (out.add) {
       float o[8];
-      load8<T>(d, o, whole, left);
+      load8<T>(d, o, left);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] += o[j];
     }
-    store8<T>(d, v, whole, left);
+    store8<T>(d, v, left);
   }
 }
 
@@ -762,7 +739,7 @@ struct Take {
 
 template <class T>
 hipError_t launch_sum_splits(const ProductArgs &p, const StoreEpi<T> &out, int splits, const float *part, hipStream_t stream) {
-  const long groups = (long)p.M * (out.vec ? (p.N + 7) / 8 : p.N), blocks = (groups + 255) / 256;
+  const long groups = (long)p.M * ((p.N + 7) / 8), blocks = (groups + 255) / 256;
   sum_splits_kernel<T><<<dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, stream>>>(part, splits, p.M, p.N, p.m_rows, p.first, out);
   return hipGetLastError();
 }
@@ -785,7 +762,7 @@ hipError_t product_to(ProductArgs p, StoreEpi<T> out, const ProductPlan &plan, f
 // others fill the compute units that these leave.
 template <class T>
 struct GradientEpi : NothingAhead {
-  GradientEpi() : store(nullptr, nullptr, 0, 0, nullptr, 0), part(nullptr, 0), partial(0) {}
+  GradientEpi() : store(nullptr, nullptr, 0, nullptr, 0), part(nullptr, 0), partial(0) {}
   StoreEpi<T> store;
   PartialEpi part;
   int partial;

@@ -68,7 +68,7 @@ struct LogitEpi {
     const int col = l.col;
     if (n >= V) return;
     float b[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (bias) load8<T>(bias + n + col, b, false, V - n - col);
+    if (bias) load8<T>(bias + n + col, b, V - n - col);
 #pragma unroll
     for (int p = 0; p < l.kPasses; ++p) {
       const int at_row = l.kRows * p + l.row, row = m + at_row;
@@ -98,7 +98,7 @@ struct LogitEpi {
         for (int j = 1; j < 8; ++j) z_at = at == j ? z[j] : z_at;
         hit[row] = z_at;
       }
-      if (KEEP && n + col < ld) store8<T>(e + (long)row * ld + n + col, e8, true, 8);
+      if (KEEP && n + col < ld) store8<T>(e + (long)row * ld + n + col, e8, 8);
     }
   }
 };
@@ -178,7 +178,7 @@ __global__ __launch_bounds__(1024) void gather_list_kernel(const int *labels, in
 // by itself.
 template <class T>
 __global__ __launch_bounds__(256) void gather_kernel(const int *labels, int T_, int V, const T *x, int D, T *xc, long ld, int *rows, int *row_labels, int *count,
-                                                      float *row_loss, float *row_lse, T *dx, int vec_x, int vec_dx) {
+                                                      float *row_loss, float *row_lse, T *dx) {
   __shared__ int before_[4], all_[4], to[kGatherRows];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, r0 = blockIdx.x * kGatherRows;
   int before = 0, all = 0;
@@ -220,29 +220,29 @@ __global__ __launch_bounds__(256) void gather_kernel(const int *labels, int T_, 
     if (r >= T_) break;
     if (to[k] >= 0) {
       float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-      if (left > 0) load8<T>(x + (long)r * D + c, v, vec_x && left >= 8, left);
-      store8<T>(xc + (long)to[k] * ld + c, v, true, 8);
+      if (left > 0) load8<T>(x + (long)r * D + c, v, left);
+      store8<T>(xc + (long)to[k] * ld + c, v, 8);
     } else if (dx && left > 0) {
-      store8<T>(dx + (long)r * D + c, zero, vec_dx && left >= 8, left);
+      store8<T>(dx + (long)r * D + c, zero, left);
     }
   }
   for (int r = all + (int)blockIdx.x; r < whole; r += (int)gridDim.x)
-    for (int c = t; c < groups; c += 256) store8<T>(xc + (long)r * ld + 8 * c, zero, true, 8);
+    for (int c = t; c < groups; c += 256) store8<T>(xc + (long)r * ld + 8 * c, zero, 8);
 }
 
 // xc = the counted rows of x in padded rows, zeros up to the next whole slab of rows; rows of dx that do not count become zeros.
 template <class T>
 __global__ __launch_bounds__(256) void gather_rows_kernel(const T *x, T *xc, long ld, int T_, int D, const int *rows, const int *count, const int *labels, int V,
-                                                           T *dx, int vec_x, int vec_dx) {
+                                                           T *dx) {
   const int n = *count, groups = (int)(ld / 8), whole = (n + 63) & ~63;
   for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < (long)(T_ + 63) * groups; i += (long)gridDim.x * 256) {
     const int r = (int)(i / groups), c = (int)(i % groups) * 8, left = D - c;
     float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (r < n && left > 0) load8<T>(x + (long)rows[r] * D + c, v, vec_x && left >= 8, left);
-    if (r < whole) store8<T>(xc + (long)r * ld + c, v, true, 8);
+    if (r < n && left > 0) load8<T>(x + (long)rows[r] * D + c, v, left);
+    if (r < whole) store8<T>(xc + (long)r * ld + c, v, 8);
     if (dx && left > 0 && r < T_ && (labels[r] < 0 || labels[r] >= V)) {
       const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-      store8<T>(dx + (long)r * D + c, zero, vec_dx && left >= 8, left);
+      store8<T>(dx + (long)r * D + c, zero, left);
     }
   }
 }
@@ -347,7 +347,7 @@ __global__ __launch_bounds__(256) void exp_to_gradient_kernel(T *e, long ld, int
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int row = r0 + 16 * i + sub;
-      if (row < n) load8<T>(e + (long)row * ld + col, v[i], true, 8);
+      if (row < n) load8<T>(e + (long)row * ld + col, v[i], 8);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -366,7 +366,7 @@ __global__ __launch_bounds__(256) void exp_to_gradient_kernel(T *e, long ld, int
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;   // up to the next whole slab of rows
       }
-      store8<T>(e + (long)row * ld + col, v[i], true, 8);
+      store8<T>(e + (long)row * ld + col, v[i], 8);
     }
   }
   if (!sums) return;
@@ -432,7 +432,7 @@ struct Plan {
     rows = (int *)take((size_t)T * sizeof(int));
     labels = (int *)take((size_t)T * sizeof(int));
     x = take((size_t)(T + 63) * ldd * b);
-    w = whole_groups(D, dtype) ? nullptr : take((size_t)V * ldd * b);
+    w = loadable(D, dtype) ? nullptr : take((size_t)V * ldd * b);
     stats = (float2 *)take((size_t)piece * groups * sizeof(float2));
     hit = (float *)take((size_t)piece * sizeof(float));
     loss = (float *)take((size_t)T * sizeof(float));
@@ -463,15 +463,14 @@ hipError_t begin(const VocabArgs &a, const Plan &p, const void **w, long *ldw, h
   }
   if (a.T <= kOneGather) {
     gather_kernel<T><<<dim3((unsigned)((a.T + kGatherRows - 1) / kGatherRows)), dim3(256), 0, stream>>>(a.labels, a.T, a.V, (const T *)a.x, a.D, (T *)p.x, p.ldd, p.rows, p.labels,
-                                                                                      p.count, a.row_loss, a.row_lse, (T *)a.dx, rows16<T>(a.x, a.D),
-                                                                                      rows16<T>(a.dx, a.D));
+                                                                                      p.count, a.row_loss, a.row_lse, (T *)a.dx);
     return hipGetLastError();
   }
   gather_list_kernel<<<dim3(1), dim3(1024), 0, stream>>>(a.labels, a.T, a.V, p.rows, p.labels, p.count, a.row_loss, a.row_lse);
   DLL_TRY(hipGetLastError());
   const long blocks = ((long)(a.T + 63) * (p.ldd / 8) + 255) / 256;
   gather_rows_kernel<T><<<dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, stream>>>(
-      (const T *)a.x, (T *)p.x, p.ldd, a.T, a.D, p.rows, p.count, a.labels, a.V, (T *)a.dx, rows16<T>(a.x, a.D), rows16<T>(a.dx, a.D));
+      (const T *)a.x, (T *)p.x, p.ldd, a.T, a.D, p.rows, p.count, a.labels, a.V, (T *)a.dx);
   return hipGetLastError();
 }
 
@@ -572,7 +571,7 @@ hipError_t vocab_grad(const VocabArgs &a, char *scratch, hipStream_t stream) {
       g.K[0] = a.V;
       g.m_rows = p.count;
       g.first = first;
-      jobs.add(g, StoreEpi<T>((T *)a.dx, nullptr, a.D, rows16<T>(a.dx, a.D), p.rows + first, 0), true);
+      jobs.add(g, StoreEpi<T>((T *)a.dx, nullptr, a.D, p.rows + first, 0), true);
     }
     ProductArgs g;
     g.M = a.V;
@@ -582,10 +581,10 @@ hipError_t vocab_grad(const VocabArgs &a, char *scratch, hipStream_t stream) {
     g.K[0] = M;
     g.k_rows = p.count;
     g.first = first;
-    if (a.dw && !p.dw_sum) jobs.add(g, StoreEpi<T>((T *)a.dw, nullptr, a.D, rows16<T>(a.dw, a.D), nullptr, first > 0), false);
+    if (a.dw && !p.dw_sum) jobs.add(g, StoreEpi<T>((T *)a.dw, nullptr, a.D, nullptr, first > 0), false);
     DLL_TRY(launch_gradients<T>(jobs, stream));
     if (a.dw && p.dw_sum) {   // pieces of bfloat16 products add up in 32 bits
-      const StoreEpi<float> out(p.dw_sum, nullptr, a.D, rows16<float>(p.dw_sum, a.D), nullptr, first > 0);
+      const StoreEpi<float> out(p.dw_sum, nullptr, a.D, nullptr, first > 0);
       DLL_TRY((launch_product<T, false, false, false>(g, out, p.gradients.tiling, stream)));
       if (last) {
         const long n = (long)a.V * a.D, blocks = (n + 255) / 256;
