@@ -275,9 +275,13 @@ dll_status dll_cnn_forward(const dll_net_desc *net, const float *const *params, 
  * taken in 32 bits or more; with DLL_BF16 what one product hands to the next is rounded to
  * bfloat16 once (to nearest), and results are rounded once.  At most 2^24 tokens and 2^20
  * features, hidden units or classes; a tensor of 2^31 or more elements -> DLL_ERR_UNSUPPORTED.
- * Results are bit-identical from run to run.  Nothing is allocated or copied from the host, so
- * every call can be captured into a graph (calls that overlap in time need workspaces of their
- * own).  Rows of sizes that are no multiple of 16 bytes are copied into the workspace first.
+ * The same call gives the same bits on every run.  Nothing is allocated on the device or copied
+ * from the host, so every call can be captured into a graph (calls that overlap in time need
+ * workspaces of their own).  bfloat16 rows of odd length are copied into the workspace first,
+ * unless there are few of them to multiply with.  Products of DLL_FP32 tensors may be taken on
+ * three bfloat16 parts of each number: errors are those of single precision, but numbers below
+ * 2^-110 lose digits; where a tile's sums are not finite it is taken again without the parts,
+ * so an infinity or a NaN in one row may change its neighbours' last digits, and nothing more.
  * ------------------------------------------------------------------------------------- */
 typedef enum { DLL_FP32 = 0, DLL_BF16 = 1 } dll_dtype;
 
@@ -354,7 +358,8 @@ dll_status dll_grad_norm(const dll_tensor_list *list, const void *const *grads, 
                          size_t ws_bytes, void *stream);
 
 /* Clipping by the global norm: out = c * grad with c = min(1, max_norm / norm), max_norm > 0 (infinity:
- * c = 1), out in the gradients' types; out[i] may be grads[i].  Where the norm is not finite c is 1.
+ * c = 1), out in the gradients' types; out[i] may be grads[i], but no other gradient, output or norm
+ * (-> DLL_ERR_SHAPE).  Where the norm is not finite c is 1.
  * Workspace as for dll_grad_norm. */
 dll_status dll_grad_clip(const dll_tensor_list *list, const void *const *grads, void *const *out,
                          float max_norm, float *norm, void *ws, size_t ws_bytes, void *stream);
@@ -363,7 +368,8 @@ dll_status dll_grad_clip(const dll_tensor_list *list, const void *const *grads, 
  *   v <- momentum * v - lr * (c * g + weight_decay * theta);   theta <- theta + v
  * params and velocity are host arrays of n fp32 device pointers; weight_decay a host array of n factors,
  * or NULL (none).  copies, or NULL, is a host array of n device pointers (each may be NULL) that receive
- * the new parameters in bfloat16.  Where the norm is not finite no step is taken: only *norm is written. */
+ * the new parameters in bfloat16.  No tensor may be listed twice among the three, nor be a gradient or
+ * norm (-> DLL_ERR_SHAPE).  Where the norm is not finite no step is taken: only *norm is written. */
 dll_status dll_momentum_update_clipped(const dll_tensor_list *list, float *const *params,
                                        float *const *velocity, const void *const *grads, float lr,
                                        float momentum, const float *weight_decay, float max_norm,

@@ -5,6 +5,9 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <algorithm>
+#include <new>
+
 using namespace dllk;
 
 namespace {
@@ -68,6 +71,39 @@ dll_status check_list(const dll_tensor_list *l, const void *const *grads, bool w
     if (reinterpret_cast<uintptr_t>(grads[i]) % type_bytes(l->dtypes[i])) return DLL_ERR_SHAPE;
   }
   return DLL_OK;
+}
+
+// One address of a list: of tensor `tensor`, or of the norm (-1)
+struct Place {
+  uintptr_t at;
+  int tensor, output;
+};
+// Whether an output of a list of tensors is another output or any tensor's gradient; with in_place it may be its own.  The kernels
+// take all tensors at once, so a tensor listed twice would be stepped by two workgroups that race.
+dll_status check_places(const dll_tensor_list *l, const void *const *grads, const void *const *const *outs, int n_outs, const float *norm, bool in_place) {
+  constexpr int kHere = 256;
+  Place here[kHere];
+  const size_t most = (size_t)l->n * (n_outs + 1) + 1;
+  Place *const p = most <= kHere ? here : new (std::nothrow) Place[most];
+  if (!p) return DLL_ERR_DEVICE;
+  size_t n = 0;
+  p[n++] = Place{reinterpret_cast<uintptr_t>(norm), -1, 1};
+  for (int i = 0; i < l->n; ++i) {
+    if (l->counts[i] == 0) continue;
+    p[n++] = Place{reinterpret_cast<uintptr_t>(grads[i]), i, 0};
+    for (int k = 0; k < n_outs; ++k)
+      if (outs[k] && outs[k][i]) p[n++] = Place{reinterpret_cast<uintptr_t>(outs[k][i]), i, 1};
+  }
+  std::sort(p, p + n, [](const Place &a, const Place &b) { return a.at < b.at; });
+  bool clash = false;
+  for (size_t i = 0, j; i < n && !clash; i = j) {
+    int outputs = 0;
+    for (j = i; j < n && p[j].at == p[i].at; ++j) outputs += p[j].output;
+    const bool own = in_place && j - i == 2 && outputs == 1 && p[i].tensor == p[i + 1].tensor;
+    clash = j - i > 1 && outputs > 0 && !own;
+  }
+  if (p != here) delete[] p;
+  return clash ? DLL_ERR_SHAPE : DLL_OK;
 }
 
 GradList list_of(const dll_tensor_list *l) {
@@ -195,6 +231,8 @@ dll_status dll_grad_clip(const dll_tensor_list *list, const void *const *grads, 
     if (!out[i]) return DLL_ERR_NULL;
     if (reinterpret_cast<uintptr_t>(out[i]) % type_bytes(list->dtypes[i])) return DLL_ERR_SHAPE;
   }
+  const void *const *outs[] = {out};
+  if ((st = check_places(list, grads, outs, 1, norm, true)) != DLL_OK) return st;
   if ((st = check_ws(ws, ws_bytes, dll_grad_norm_workspace_bytes(list))) != DLL_OK) return st;
   return dev(launch_grad_clip(list_of(list), grads, out, max_norm, norm, static_cast<char *>(ws), static_cast<hipStream_t>(stream)));
 }
@@ -210,10 +248,10 @@ dll_status dll_momentum_update_clipped(const dll_tensor_list *list, float *const
     if (list->counts[i] == 0) continue;
     if (!params[i] || !velocity[i]) return DLL_ERR_NULL;
     const void *copy = copies ? copies[i] : nullptr;
-    const void *in[] = {grads[i]}, *out[] = {params[i], velocity[i], copy};
-    if (aliased(in, 1, out, 3)) return DLL_ERR_SHAPE;
     if ((reinterpret_cast<uintptr_t>(params[i]) | reinterpret_cast<uintptr_t>(velocity[i])) % 4 || reinterpret_cast<uintptr_t>(copy) % 2) return DLL_ERR_SHAPE;
   }
+  const void *const *outs[] = {reinterpret_cast<const void *const *>(params), reinterpret_cast<const void *const *>(velocity), copies};
+  if ((st = check_places(list, grads, outs, 3, norm, false)) != DLL_OK) return st;
   if ((st = check_ws(ws, ws_bytes, dll_grad_norm_workspace_bytes(list))) != DLL_OK) return st;
   return dev(launch_momentum_clipped(list_of(list), params, velocity, grads, weight_decay, lr, momentum, max_norm, norm, copies, static_cast<char *>(ws),
                                      static_cast<hipStream_t>(stream)));

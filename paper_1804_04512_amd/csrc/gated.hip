@@ -318,7 +318,7 @@ hipError_t gated_bwd(const GatedArgs &a, char *scratch, hipStream_t stream) {
   g.N = a.H;
   g.A[0] = {dy, ldx};
   g.B[0] = {wd, ldd};
-  g.K[0] = a.D;   // Wd lies across k; where D is no multiple of a 16-byte group, dy's copy has zeros behind it
+  g.K[0] = a.D;   // Wd lies across k
   const GateBackEpi<T> ge(a.gate, (const T *)a.gate_pre, (const T *)a.up_pre,
                     (T *)p.da, (T *)p.db, (T *)p.h, p.ldh);
   DLL_TRY((launch_product<T, true, false, false>(g, ge, p.dh.tiling, stream)));

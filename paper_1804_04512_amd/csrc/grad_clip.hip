@@ -242,7 +242,7 @@ int fill(NormTable &t, const GradList &l, const void *const *grads, int at, int 
   for (; at < l.n && t.n < kTable; ++at) {
     if (l.counts[at] == 0) continue;
     const long chunks = ((long)l.counts[at] + chunk - 1) / chunk;
-    if (t.chunks + chunks > 0x40000000L) break;   // of one launch; a tensor has 2^31 elements at most
+    if (t.chunks + chunks > 0x40000000L) break;   // of one launch; a tensor has 2^27 at most
     which[t.n] = at;
     t.g[t.n] = grads[at];
     t.count[t.n] = (long)l.counts[at];

@@ -73,6 +73,34 @@ def test_large_tiles(dtype):
         ref.check(got[k], want[k], k)
 
 
+@pytest.mark.parametrize("size", [(4095, 138, 4098), (138, 4098, 4096)], ids=lambda s: "x".join(map(str, s)))
+def test_each_product_on_the_largest_tiles(size):
+    """The forward products of the first size and the gradients of the second have 256 tiles of 256 x 256 and few slabs, the last
+    slab with k ending inside 16 bytes."""
+    spec = GatedSpec(*size, "silu", "bfloat16")
+    i, dy = inputs(*size, "bfloat16", seed=10)
+    got, want = run(spec, i, dy), ref.gated(*i.values(), "silu", dy)
+    for k in got:
+        ref.check(got[k], want[k], k)
+
+
+@pytest.mark.parametrize("size", [(70, 33, 35), (70, 34, 38), (40, 1030, 1026), (300, 66, 37)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_what_lies_behind_a_row_is_not_multiplied(size, dtype):
+    """Rows end inside 16 bytes, and the next row, which is another token's, holds NaN: it stays in that token's outputs."""
+    T, D, H = size
+    spec = GatedSpec(T, D, H, "silu", dtype)
+    i, dy = inputs(T, D, H, dtype, seed=11)
+    want = ref.gated(*i.values(), "silu", dy)
+    odd = torch.arange(T, device="cuda") % 2 == 1
+    i["x"][odd] = float("nan")
+    dy[odd] = float("nan")
+    got = run(spec, i, dy, ("dx",))
+    for k in ("y", "gate_pre", "up_pre", "dx"):
+        assert torch.isnan(got[k][odd]).all(), k
+        ref.check(got[k][~odd], tuple(v[~odd] for v in want[k]), k)
+
+
 @pytest.mark.parametrize("grads", [("dx",), ("dw_gate",), ("dw_up",), ("dw_down",), ("dw_gate", "dw_down"), ("dx", "dw_up")], ids="+".join)
 def test_some_gradients(grads):
     spec = GatedSpec(40, 72, 56, "silu", "bfloat16")

@@ -68,6 +68,17 @@ def test_large_tiles(dtype):
     compare(run_grad(spec, i), ref.vocab(*i.values()))
 
 
+@pytest.mark.parametrize("size", [(4094, 134, 4096), (4300, 24, 70), (9001, 40, 33)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_many_tokens(size, dtype):
+    """Logits on tiles of 256 x 256 (bfloat16); rows gathered by more than one launch, from 4097 tokens on."""
+    spec = VocabSpec(*size, dtype)
+    i = inputs(*size, dtype, True, 0.0 if size[0] < 4097 else 0.3, seed=6)
+    want = ref.vocab(*i.values())
+    compare(run_grad(spec, i), want)
+    compare(run_fwd(spec, i), want)
+
+
 @pytest.mark.parametrize("dtype,tokens", [("bfloat16", 700), ("float32", 300)])
 def test_pieces(dtype, tokens):
     """More exponentials than are kept at a time: two pieces of tokens, the second not whole and partly not counted."""

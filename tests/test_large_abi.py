@@ -143,6 +143,31 @@ def test_tensor_lists():
     assert L.dll_momentum_update_clipped(l, p, v, g, 0.1, 0.9, None, 1.0, norm, None, None, BIG, None) == WORKSPACE
 
 
+def test_no_tensor_is_written_twice():
+    """Every list is refused for an output that is another output, another tensor's gradient or the norm."""
+    L, ws = B.lib(), P[1]
+    for n in (2, 3, 150):   # addresses on the stack, and more than fit there
+        l = C.byref(B.dll_tensor_list(n, (C.c_size_t * n)(*[4] * n), (C.c_int * n)(*[0] * n)))
+        at = lambda base, **over: pointers(*[over.get(f"k{k}", base + 64 * k) for k in range(n)])
+        g, p, v, c = 0x100000, 0x200000, 0x300000, 0x400000
+        last = f"k{n - 1}"
+        clip = lambda out, norm=P[0]: L.dll_grad_clip(l, at(g), out, 1.0, norm, ws, 0, None)
+        assert clip(at(g)) == clip(at(p)) == WORKSPACE   # nothing else to refuse
+        assert clip(at(p, **{last: p})) == SHAPE         # two outputs
+        assert clip(at(p, **{last: g})) == SHAPE         # another tensor's gradient
+        assert clip(at(g, **{last: g})) == SHAPE
+        assert clip(at(p), C.c_void_p(p)) == clip(at(p), C.c_void_p(g)) == SHAPE
+        twice = at(g, **{last: g})
+        assert L.dll_grad_clip(l, twice, twice, 1.0, P[0], ws, 0, None) == SHAPE      # the same tensor twice, in place
+        assert L.dll_grad_clip(l, twice, at(p), 1.0, P[0], ws, 0, None) == WORKSPACE  # read twice, written apart
+        step = lambda params, vel, copies=None, grads=None, norm=P[0]: L.dll_momentum_update_clipped(
+            l, params, vel, grads or at(g), 0.1, 0.9, None, 1.0, norm, copies, ws, 0, None)
+        assert step(at(p), at(v)) == step(at(p), at(v), at(c)) == step(at(p), at(v), pointers(*[None] * n)) == WORKSPACE
+        assert step(at(p, **{last: p}), at(v)) == step(at(p), at(v, **{last: v})) == step(at(p), at(v), at(c, **{last: c})) == SHAPE
+        assert step(at(p), at(v, **{last: p})) == step(at(p), at(v), at(c, k0=p)) == step(at(p, **{last: g}), at(v)) == SHAPE
+        assert step(at(p), at(v), at(c, **{last: g})) == step(at(p), at(v), norm=C.c_void_p(v)) == SHAPE
+
+
 def test_binding_checks_what_an_address_cannot_say():
     cpu = torch.device("cpu")
     t = torch.zeros(4, 6)
