@@ -10,6 +10,11 @@
 // to their own group keep all the type's digits, which rounded logits would not (bfloat16 logits of size 10 are 2 % off
 // after exp).  This takes three products of T D V; forming the logits again for the gradients would take four.
 // The exponentials are kept for a piece of the tokens at a time, 1 GiB at most.
+//
+// With gradients the matrix pipe bounds it: 4096 x 2048 x 50257 bf16, 3690 rows counted, 2.40 ms = 950 TFLOP/s (logits 908 us, both
+// gradients 1410, the pass over the exponentials 137 = 5.4 TB/s).  Without them a few tokens are bound by the weights' bytes:
+// 16 x 1024 x 32000 bf16 19.8 us, 15.4 of which read 66 MB at 4.2 TB/s; the rest joins the groups.  A small layer is a chain of short
+// launches: 128 x 2048 x 1000 in single precision 51 us in seven.
 #include "large_ops.h"
 #include "skinny_product.h"
 
@@ -400,9 +405,11 @@ __global__ __launch_bounds__(256) void convert_kernel(const float *src, T *dst, 
   for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) dst[i] = (T)src[i];
 }
 
-// Weights in rows of odd sizes, which the tiles would have copied first (16 x 1024 x 32000 in whole rows: 15 us on either way, and
-// half as many groups to join on the tiles').
-bool skinny(int T, int D, int dtype) { return T <= kSkinnyRows && D >= kSkinnyLeastK && !whole_groups(D, dtype); }
+// Up to 16 tokens: weights in rows that are no whole 16-byte groups (16 x 1001 x 5000: 12.8 us against the tiles' 21.4 in bfloat16, whose
+// odd rows the tiles have copied first, 12.5 against 16.2 in single precision; 16 x 1002 x 5000 in bfloat16: 8.7 against 11.0; in whole
+// groups either way takes as long, and the tiles' leaves half as many groups to join).  Up to 32 only odd rows in bfloat16 (32 x 1001 x
+// 32000: 45.9 against 48.1; in single precision 57.3 against the tiles' 43.8, and 32 x 1002 x 32000 in bfloat16 25.7 against 22.1).
+bool skinny(int T, int D, int dtype) { return D >= kSkinnyLeastK && (T <= 16 ? !whole_groups(D, dtype) : T <= kSkinnyRows && !loadable(D, dtype)); }
 
 struct Plan {
   long ldd, lde;
