@@ -184,6 +184,36 @@ def test_some_gradients(grads):
         assert torch.equal(all_[k], some[k]), k
 
 
+@pytest.mark.parametrize("size", [(20, 64, 90), (20, 65, 90), (200, 72, 1000)], ids=lambda s: "x".join(map(str, s)))
+def test_any_label(size):
+    """The ends of the integers' range and of the classes."""
+    spec = VocabSpec(*size, "bfloat16")
+    i = inputs(*size, "bfloat16", True, seed=12)
+    i["labels"][:6] = torch.tensor([-2 ** 31, 2 ** 31 - 1, size[2], -1, 0, size[2] - 1], dtype=torch.int32)
+    want = ref.vocab(*i.values())
+    compare(run_grad(spec, i), want)
+    compare(run_fwd(spec, i), want)
+
+
+def test_two_calls_at_once():
+    """On two streams with a workspace each: the same bits as one after the other."""
+    spec = VocabSpec(600, 256, 5003, "bfloat16")
+    i = [inputs(600, 256, 5003, "bfloat16", True, 0.2, seed=k) for k in (1, 2)]
+    alone = [run_grad(spec, j) for j in i]
+    t = torch.bfloat16
+    out = [dict(row_loss=nan(600), row_lse=nan(600), loss=nan(1), dx=nan(600, 256, dtype=t), dw=nan(5003, 256, dtype=t), dbias=nan(5003, dtype=t)) for _ in i]
+    ws = [B.workspace(B.dll_vocab_loss_grad_workspace_bytes(spec)) for _ in i]
+    streams = [torch.cuda.Stream() for _ in i]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for k in (0, 1):
+            B.dll_vocab_loss_grad(spec, **i[k], scale=1.0, **out[k], ws=ws[k], stream=streams[k])
+    torch.cuda.synchronize()
+    for k in (0, 1):
+        for n in out[k]:
+            assert torch.equal(out[k][n], alone[k][n]), n
+
+
 def test_gradients_against_differences():
     T, D, V = 7, 12, 90
     spec = VocabSpec(T, D, V, "float32")
