@@ -818,14 +818,14 @@ __global__ __launch_bounds__(64 * WM *WN *WK, 2) void gradient_kernel(const Grad
 
 struct GradientShape { int M, N; long slabs; int problems; bool data; };
 
-// When `n` kinds of units, count[k] of time[k] each, the longest first, are all done on `slots` places, each unit taken by the place
+// When `n` kinds (at most three) of units, count[k] of time[k] each, the longest first, are all done on `slots` places, each unit taken by the place
 // that is free first.  Places that are free at the same time are counted together; what would be more than a few rounds is taken as
 // spread evenly with half a unit's tail.
 inline double makespan(const double *count, const double *time, int n, int slots) {
   double all = 0, units = 0;
   for (int k = 0; k < n; ++k) all += count[k] * time[k], units += count[k];
   if (units > 4.0 * slots) return all / slots + 0.5 * time[n - 1];
-  struct Level { double at; int places; } level[16];
+  struct Level { double at; int places; } level[4];   // each kind leaves one more at most
   int levels = 1;
   level[0] = Level{0.0, slots};
   double end = 0;
@@ -842,7 +842,7 @@ inline double makespan(const double *count, const double *time, int n, int slots
         level[low].at = at;
       } else {
         level[low].places -= take;
-        if (levels < 16) level[levels++] = Level{at, take};
+        level[levels++] = Level{at, take};
       }
     }
   return end;
@@ -855,8 +855,6 @@ inline ProductPlan plan_gradients(int dtype, const GradientShape *shape, int n) 
   double least = 1e30;
   const int type = dtype == TYPE_BF16 ? 1 : 0, cus = chip().cus;
   constexpr int kParts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
-  bool data = false;
-  for (int k = 0; k < n; ++k) data = data || shape[k].data;
   for (int i = type ? TILE_256 : TILE_128; i < TILINGS; ++i) {
     const TilingCost &c = kTilings[i];
     for (const int s : kParts) {
@@ -896,7 +894,6 @@ inline ProductPlan plan_gradients(int dtype, const GradientShape *shape, int n) 
         best.tiling = i;
         best.splits = s;
       }
-      if (!data) break;
     }
   }
   return best;
