@@ -63,9 +63,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void skinny_kernel(const SkinnyArgs 
   __shared__ __attribute__((aligned(16))) floatx4 part[WAVES][TOKENS * R][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i16 = lane & 15, kq = (lane >> 4) * Step<T>::kGroup;
   const int n0 = blockIdx.x * (PAIR ? kSkinnyColumns : R * kSkinnyColumns);
+  const int m0 = 16 * TOKENS * blockIdx.y;
   const T *x[TOKENS], *w[R];  // rows of x and W that do not exist stand in as the last one: their sums are not stored
 #pragma unroll
-  for (int t = 0; t < TOKENS; ++t) x[t] = (const T *)a.x + (long)min(16 * t + i16, a.M - 1) * a.K;
+  for (int t = 0; t < TOKENS; ++t) x[t] = (const T *)a.x + (long)min(m0 + 16 * t + i16, a.M - 1) * a.K;
 #pragma unroll
   for (int r = 0; r < R; ++r) w[r] = (const T *)a.w[PAIR ? r : 0] + (long)min(n0 + i16 + (PAIR ? 0 : kSkinnyColumns * r), a.N - 1) * a.K;
   // A wavefront takes 128 bytes of each row at a time, 32 of them a lane in two loads (the order of k is the same for both
@@ -138,24 +139,26 @@ __global__ __launch_bounds__(64 * WAVES, 2) void skinny_kernel(const SkinnyArgs 
 #pragma unroll
     for (int v = 1; v < WAVES; ++v) sum[r] += part[v][wave * R + r][lane];
   }
-  epi.template tile<R>(sum, 16 * wave + i16, n0 + 4 * (lane >> 4), a.M, a.N);
+  epi.template tile<R>(sum, m0 + 16 * wave + i16, n0 + 4 * (lane >> 4), a.M, a.N);
 }
 
 template <class T, int TOKENS, int R, bool PAIR, class Epi>
-hipError_t launch_skinny_tokens(const SkinnyArgs &a, const Epi &epi, hipStream_t stream) {
-  const int each = PAIR ? kSkinnyColumns : R * kSkinnyColumns;
-  const unsigned blocks = (unsigned)((a.N + each - 1) / each);
+hipError_t launch_skinny_tokens(const SkinnyArgs &a, const Epi &epi, unsigned blocks, hipStream_t stream) {
+  const unsigned tiles = (unsigned)((a.M + 16 * TOKENS - 1) / (16 * TOKENS));
   // few columns: sixteen wavefronts share a workgroup's k (eight with two tiles of tokens, whose registers allow no more);
   // short rows: four, so that each has a set and one ahead
   constexpr int kMost = TOKENS == 1 ? 16 : 8;
-  if ((long)a.K * (int)sizeof(T) <= 2048) skinny_kernel<T, TOKENS, R, PAIR, 4, Epi><<<dim3(blocks), dim3(256), 0, stream>>>(a, epi);
-  else if ((int)blocks < chip().cus) skinny_kernel<T, TOKENS, R, PAIR, kMost, Epi><<<dim3(blocks), dim3(64 * kMost), 0, stream>>>(a, epi);
-  else skinny_kernel<T, TOKENS, R, PAIR, 8, Epi><<<dim3(blocks), dim3(512), 0, stream>>>(a, epi);
+  if ((long)a.K * (int)sizeof(T) <= 2048) skinny_kernel<T, TOKENS, R, PAIR, 4, Epi><<<dim3(blocks, tiles), dim3(256), 0, stream>>>(a, epi);
+  else if ((int)(blocks * tiles) < chip().cus) skinny_kernel<T, TOKENS, R, PAIR, kMost, Epi><<<dim3(blocks, tiles), dim3(64 * kMost), 0, stream>>>(a, epi);
+  else skinny_kernel<T, TOKENS, R, PAIR, 8, Epi><<<dim3(blocks, tiles), dim3(512), 0, stream>>>(a, epi);
   return hipGetLastError();
 }
 template <class T, int R, bool PAIR, class Epi>
 hipError_t launch_skinny(const SkinnyArgs &a, const Epi &epi, hipStream_t stream) {
-  return a.M <= 16 ? launch_skinny_tokens<T, 1, R, PAIR>(a, epi, stream) : launch_skinny_tokens<T, 2, R, PAIR>(a, epi, stream);
+  constexpr int kEach = PAIR ? kSkinnyColumns : R * kSkinnyColumns;
+  const unsigned blocks = (unsigned)((a.N + kEach - 1) / kEach);
+  return a.M <= 16 || 2 * (int)blocks <= chip().cus ? launch_skinny_tokens<T, 1, R, PAIR>(a, epi, blocks, stream)
+                                                    : launch_skinny_tokens<T, 2, R, PAIR>(a, epi, blocks, stream);
 }
 
 // four neighbours of a row
