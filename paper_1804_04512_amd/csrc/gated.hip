@@ -189,13 +189,16 @@ __global__ __launch_bounds__(256) void pad_rows_kernel(const T *src, T *dst, int
   }
 }
 
-// A few tokens: the weights straight from memory.  Up to 16 always (2048 x 8192 bf16, one token: 25.6 us against 30 on tiles with k
-// in parts); up to 32 where the weights are small (24 x 1000 x 2730: 12.6 against 21), as every workgroup reads the tokens again
-// (24 x 2048 x 8192: 39 against the tiles' 28; 24 x 2047 x 8191, which the tiles have copied first in bfloat16: 115 against 69, in
-// single precision 85 against 50).
-bool skinny(int T, int D, int H) {
+// A few tokens: the weights straight from memory, up to 16 where the second product's rows of H are at most 16 KB, as one compute
+// unit reads sixteen of them (one token, 2048 x 8192 bf16: 25.6 us against 30 on tiles with k in parts; 16 tokens, 2048 x 16000: 58
+// against 40, 512 x 8000 in single precision 40 against 25), or where the tiles would have rows of odd bfloat16 length copied first.
+// Up to 32 where the weights are small as well (24 x 1000 x 2730 bf16: 11.7 against 17), as the tokens are read by every workgroup
+// (24 x 2048 x 8192: 39 against 28; 24 x 2047 x 8191, copied first: 115 against 69).
+bool skinny(int T, int D, int H, int dtype) {
   if (T > kSkinnyRows || D < kSkinnyLeastK || H < kSkinnyLeastK) return false;
-  return T <= 16 || (long)D * H <= (1L << 22);
+  const bool short_rows = (size_t)H * type_bytes(dtype) <= 16384;
+  if (T <= 16) return short_rows || !loadable(D, dtype) || !loadable(H, dtype);
+  return short_rows && (long)D * H <= (1L << 22);
 }
 
 // The workspace's parts, the same walk for the query and the call
@@ -213,7 +216,7 @@ struct FwdPlan {
     h = take((size_t)T * ldh * e);
     x = wg = wu = wd = nullptr;
     part = nullptr;
-    if (skinny(T, D, H)) {   // nothing else
+    if (skinny(T, D, H, dtype)) {   // nothing else
       bytes = take.used;
       return;
     }
@@ -255,7 +258,7 @@ struct BwdPlan {
 template <class T>
 hipError_t gated_fwd(const GatedArgs &a, char *scratch, hipStream_t stream) {
   const FwdPlan p(a.T, a.D, a.H, a.dtype, scratch);
-  if (skinny(a.T, a.D, a.H)) {
+  if (skinny(a.T, a.D, a.H, a.dtype)) {
     SkinnyArgs s;
     s.M = a.T;
     s.N = a.H;

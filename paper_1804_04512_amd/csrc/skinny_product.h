@@ -145,7 +145,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void skinny_kernel(const SkinnyArgs 
 template <class T, int TOKENS, int R, bool PAIR, class Epi>
 hipError_t launch_skinny_tokens(const SkinnyArgs &a, const Epi &epi, unsigned blocks, hipStream_t stream) {
   const unsigned tiles = (unsigned)((a.M + 16 * TOKENS - 1) / (16 * TOKENS));
-  // few columns: sixteen wavefronts share a workgroup's k (eight with two tiles of tokens, whose registers allow no more);
+  // few workgroups: sixteen wavefronts share a workgroup's k (eight with two tiles of tokens, whose registers allow no more);
   // short rows: four, so that each has a set and one ahead
   constexpr int kMost = TOKENS == 1 ? 16 : 8;
   if ((long)a.K * (int)sizeof(T) <= 2048) skinny_kernel<T, TOKENS, R, PAIR, 4, Epi><<<dim3(blocks, tiles), dim3(256), 0, stream>>>(a, epi);
@@ -155,6 +155,8 @@ hipError_t launch_skinny_tokens(const SkinnyArgs &a, const Epi &epi, unsigned bl
 }
 template <class T, int R, bool PAIR, class Epi>
 hipError_t launch_skinny(const SkinnyArgs &a, const Epi &epi, hipStream_t stream) {
+  // The second sixteen tokens share their weights' loads, or take workgroups of their own where the columns leave half the compute
+  // units empty (24 x 784 x 500 in single precision: 15.3 us shared, 11.6 apart; 24 x 1000 x 2730 bf16: 11.7 against 13.2).
   constexpr int kEach = PAIR ? kSkinnyColumns : R * kSkinnyColumns;
   const unsigned blocks = (unsigned)((a.N + kEach - 1) / kEach);
   return a.M <= 16 || 2 * (int)blocks <= chip().cus ? launch_skinny_tokens<T, 1, R, PAIR>(a, epi, blocks, stream)

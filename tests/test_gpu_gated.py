@@ -84,6 +84,17 @@ def test_each_product_on_the_largest_tiles(size):
         ref.check(got[k], want[k], k)
 
 
+@pytest.mark.parametrize("size", [(3, 40, 8250), (16, 33, 4100), (16, 32, 4098), (5, 40, 8251), (32, 24, 8250), (20, 1000, 2500), (32, 9, 4100)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_few_tokens(size, dtype):
+    """On either side of where a few tokens' products change hands: rows of 16 KB, columns that fill half the compute units."""
+    spec = GatedSpec(*size, "silu", dtype)
+    i, dy = inputs(*size, dtype, seed=13)
+    got, want = run(spec, i, dy), ref.gated(*i.values(), "silu", dy)
+    for k in got:
+        ref.check(got[k], want[k], k)
+
+
 @pytest.mark.parametrize("size", [(70, 33, 35), (70, 34, 38), (40, 1030, 1026), (300, 66, 37)], ids=lambda s: "x".join(map(str, s)))
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 def test_what_lies_behind_a_row_is_not_multiplied(size, dtype):
