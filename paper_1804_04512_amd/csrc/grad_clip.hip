@@ -238,11 +238,13 @@ __global__ __launch_bounds__(1024) void few_kernel(const Table a, float max_norm
   }
 }
 
-// Tensors [at, at + kTable) of the list that hold anything; returns where the next table starts
+// The next kTable tensors from `at` on that hold anything; returns where the table behind it starts, l.n if none that does is left
+// (a launch with an empty table would leave a norm of its own)
 int fill(NormTable &t, const GradList &l, const void *const *grads, int at, int *which, int chunk = kChunk) {
   t.n = t.chunks = 0;
-  for (; at < l.n && t.n < kTable; ++at) {
+  for (; at < l.n; ++at) {
     if (l.counts[at] == 0) continue;
+    if (t.n == kTable) break;
     const long chunks = ((long)l.counts[at] + chunk - 1) / chunk;
     if (t.chunks + chunks > 0x40000000L) break;   // of one launch; a tensor has 2^27 at most
     which[t.n] = at;
@@ -264,7 +266,6 @@ hipError_t launch_squares(const GradList &l, const void *const *grads, double **
   for (int at = 0; at < l.n;) {
     NormTable t;
     at = fill(t, l, grads, at, which);
-    if (t.n == 0) break;
     const int blocks = t.chunks < kPartials ? t.chunks : kPartials;
     grad_squares_kernel<<<dim3((unsigned)blocks), dim3(256), 0, stream>>>(t, *partial + *used);
     DLL_TRY(hipGetLastError());
@@ -292,7 +293,7 @@ bool is_few(const GradList &l) {
   return true;
 }
 
-unsigned apply_blocks(int chunks) { return (unsigned)(chunks < 1 ? 1 : chunks < 8 * chip().cus ? chunks : 8 * chip().cus); }
+unsigned apply_blocks(int chunks) { return (unsigned)(chunks < 8 * chip().cus ? chunks : 8 * chip().cus); }
 
 }  // namespace
 

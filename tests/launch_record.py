@@ -34,9 +34,18 @@ class _Pointers:
 def _make(B, L, what, *args):
     """One call by name: 'fwd' / 'bwd' / 'wgrad' / 'fft' / 'fft_less' / 'crbm' (ConvSpec fields), 'rbm' (batch, n_vis, n_hid),
     'infer' / 'train' (conv layers, dense layers, classes, batch); 'rbm_in_place' writes v1 over h0_sample_in,
-    'infer_in_place' the probabilities over x."""
+    'infer_in_place' the probabilities over x; 'norm' / 'clip' / 'step' (numbers of elements of a list of fp32 gradients)."""
     from paper_1804_04512_amd.workloads import ConvSpec, DenseSpec
     p, ws = _Pointers(), C.c_void_p(1 << 20)
+    if what in ("norm", "clip", "step"):
+        n = len(args[0])
+        l = C.byref(B.dll_tensor_list(n, (C.c_size_t * n)(*args[0]), (C.c_int * n)(*[0] * n)))
+        many = lambda: (C.c_void_p * n)(*[p() for _ in range(n)])
+        if what == "norm":
+            return L.dll_grad_norm(l, many(), p(), ws, WORKSPACE, None)
+        if what == "clip":
+            return L.dll_grad_clip(l, many(), many(), 1.0, p(), ws, WORKSPACE, None)
+        return L.dll_momentum_update_clipped(l, many(), many(), many(), 0.1, 0.9, None, 1.0, p(), None, ws, WORKSPACE, None)
     if what in ("fwd", "bwd", "wgrad", "fft", "fft_less", "crbm"):
         d = B.conv_desc(ConvSpec(*args))
         ref, idx = C.byref(d), p() if d.pool == 2 else None
