@@ -459,6 +459,21 @@ __device__ __forceinline__ void product_tile(const ProductArgs &a, const Epi &ep
       for (int j = 0; j < TN; ++j)
 #pragma unroll
         for (int r = 0; r < 16; ++r) finite = finite && fabsf(acc[i][j][r]) < INFINITY;
+    // Only sums that exist count: an operand across k may hold anything behind its last row or column (a workspace's rows are written
+    // up to their last whole group of eight), and what a former call left there must change neither digits nor time.  Looked at only
+    // where there is something: for every tile it would cost 2.5 % of 1000 x 500 x 1337 both ways.
+    if (!finite) {
+      const int left = PAIR ? WC : a.N - n0 - wn - 4 * (lane >> 5);   // a pair's rows behind the last one are zeros
+      finite = true;
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        const bool row = m0 + wm + 32 * i + (lane & 31) < M;
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) finite = finite && (fabsf(acc[i][j][r]) < INFINITY || !row || 32 * j + 8 * (r >> 2) + (r & 3) >= left);
+      }
+    }
     unsigned *flag = reinterpret_cast<unsigned *>(smem);   // one a wavefront, in the slabs' place
     __syncthreads();
     if (lane == 0) flag[all] = 0u;

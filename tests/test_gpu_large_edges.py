@@ -39,3 +39,118 @@ def test_empty_tensors_behind_a_full_table(counts):
         ref.check(a, (half, bound), "clipped")
         ref.check(b, (-half, bound + U32 * half.abs()), "v")
         ref.check(c, (1 - half, bound + U32 * half.abs() + U32 * (1 - half).abs()), "theta")
+
+
+def gated_inputs(T, D, H, dtype, seed=0):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    n = lambda *s, std=1.0: (torch.randn(s, generator=gen, device="cuda") * std).to(TYPES[dtype])
+    return dict(x=n(T, D), w_gate=n(H, D, std=D ** -0.5), w_up=n(H, D, std=D ** -0.5), w_down=n(D, H, std=H ** -0.5)), n(T, D)
+
+
+def block(spec, i, dy, fill):
+    """Forward and backward pass with workspaces that hold `fill` in every byte."""
+    e = lambda *s: torch.empty(s, dtype=TYPES[spec.dtype], device="cuda")
+    T, D, H = spec.tokens, spec.width, spec.hidden
+    out = dict(y=e(T, D), gate_pre=e(T, H), up_pre=e(T, H))
+    B.dll_gated_fwd(spec, **i, **out, ws=B.workspace(B.dll_gated_fwd_workspace_bytes(spec)).fill_(fill))
+    g = dict(dx=e(T, D), dw_gate=e(H, D), dw_up=e(H, D), dw_down=e(D, H))
+    B.dll_gated_bwd(spec, **i, gate_pre=out["gate_pre"], up_pre=out["up_pre"], dy=dy, **g,
+                    ws=B.workspace(B.dll_gated_bwd_workspace_bytes(spec)).fill_(fill))
+    return {**out, **g}
+
+
+def vocab_inputs(T, D, V, dtype, seed=0, ignored=0.2):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    n = lambda *s, std=1.0: (torch.randn(s, generator=gen, device="cuda") * std).to(TYPES[dtype])
+    labels = torch.randint(0, V, (T,), generator=gen, device="cuda", dtype=torch.int32)
+    out = torch.rand(T, generator=gen, device="cuda") < ignored
+    return dict(x=n(T, D), w=n(V, D, std=2 * D ** -0.5), bias=n(V), labels=torch.where(out, torch.full_like(labels, -100), labels))
+
+
+def head(spec, i, fill):
+    """Loss, then loss with gradients, with workspaces that hold `fill` in every byte."""
+    e = lambda *s, d=TYPES[spec.dtype]: torch.empty(s, dtype=d, device="cuda")
+    T, D, V = spec.tokens, spec.width, spec.classes
+    losses = lambda: dict(row_loss=e(T, d=torch.float32), row_lse=e(T, d=torch.float32), loss=e(1, d=torch.float32))
+    fwd, out = losses(), dict(**losses(), dx=e(T, D), dw=e(V, D), dbias=e(V))
+    B.dll_vocab_loss_fwd(spec, **i, **fwd, ws=B.workspace(B.dll_vocab_loss_fwd_workspace_bytes(spec)).fill_(fill))
+    B.dll_vocab_loss_grad(spec, **i, scale=1.0, **out, ws=B.workspace(B.dll_vocab_loss_grad_workspace_bytes(spec)).fill_(fill))
+    return {**{"fwd " + k: v for k, v in fwd.items()}, **out}
+
+
+# bytes of NaN, of the largest finite numbers' neighbourhood (beyond bfloat16's range in single precision: 3.39e38), of 1.7e38
+FILLS = (0, 255, 0x7F, 0x7E)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("size", [(200, 72, 1000), (300, 260, 970), (1000, 500, 1337), (40, 1030, 1026), (130, 259, 77)], ids=lambda s: "x".join(map(str, s)))
+def test_block_whatever_the_workspace_holds(size, dtype):
+    """The same bits, and within the bounds, from every former content."""
+    spec = GatedSpec(*size, "silu", dtype)
+    i, dy = gated_inputs(*size, dtype, seed=sum(size))
+    want = ref.gated(*i.values(), "silu", dy)
+    first = block(spec, i, dy, FILLS[0])
+    for k in first:
+        ref.check(first[k], want[k], k)
+    for fill in FILLS[1:]:
+        got = block(spec, i, dy, fill)
+        for k in first:
+            assert torch.equal(got[k], first[k]), (k, fill)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("size", [(200, 72, 970), (128, 2048, 1000), (300, 40, 4099), (31, 260, 4099), (130, 50, 517)], ids=lambda s: "x".join(map(str, s)))
+def test_loss_whatever_the_workspace_holds(size, dtype):
+    spec = VocabSpec(*size, dtype)
+    i = vocab_inputs(*size, dtype, seed=sum(size))
+    want = ref.vocab(*i.values())
+    first = head(spec, i, FILLS[0])
+    for k in first:
+        ref.check(first[k], want[k.replace("fwd ", "")], k)
+    for fill in FILLS[1:]:
+        got = head(spec, i, fill)
+        for k in first:
+            assert torch.equal(got[k], first[k]), (k, fill)
+
+
+def test_single_precision_in_graphs_and_on_two_streams():
+    """Captured once, replayed on changed inputs with eager work between; two calls at once with a workspace each."""
+    gs, vs = GatedSpec(150, 72, 250, "gelu", "float32"), VocabSpec(150, 72, 970, "float32")
+    i, dy = gated_inputs(150, 72, 250, "float32")
+    j = vocab_inputs(150, 72, 970, "float32")
+    e = lambda *s: torch.empty(s, device="cuda")
+    kept = dict(gate_pre=e(150, 250), up_pre=e(150, 250))
+    g = dict(dx=e(150, 72), dw_gate=e(250, 72), dw_up=e(250, 72), dw_down=e(72, 250))
+    o = dict(row_loss=e(150), row_lse=e(150), loss=e(1), dx=e(150, 72), dw=e(970, 72), dbias=e(970))
+    y = e(150, 72)
+    ws = [B.workspace(max(B.dll_gated_fwd_workspace_bytes(gs), B.dll_gated_bwd_workspace_bytes(gs))), B.workspace(B.dll_vocab_loss_grad_workspace_bytes(vs))]
+
+    def blocks(stream=None):
+        B.dll_gated_fwd(gs, **i, y=y, **kept, ws=ws[0], stream=stream)
+        B.dll_gated_bwd(gs, **i, **kept, dy=dy, **g, ws=ws[0], stream=stream)
+
+    def loss(stream=None):
+        B.dll_vocab_loss_grad(vs, **j, scale=1.0, **o, ws=ws[1], stream=stream)
+
+    blocks(), loss()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        blocks(), loss()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for seed in range(3):
+        i2, dy2 = gated_inputs(150, 72, 250, "float32", seed=90 + seed)
+        j2 = vocab_inputs(150, 72, 970, "float32", seed=90 + seed)
+        for a, b in list(zip(i.values(), i2.values())) + list(zip(j.values(), j2.values())) + [(dy, dy2)]:
+            a.copy_(b)
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = [t.clone() for t in [y, *kept.values(), *g.values(), *o.values()]]
+        eager = [*block(gs, i, dy, 255).values(), *(v for k, v in head(vs, j, 255).items() if "fwd" not in k)]
+        assert all(torch.equal(a, b) for a, b in zip(replayed, eager))
+        torch.cuda.synchronize()
+        blocks(streams[0]), loss(streams[1])
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip([y, *kept.values(), *g.values(), *o.values()], eager))
