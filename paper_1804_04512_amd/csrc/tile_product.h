@@ -280,7 +280,8 @@ __device__ __forceinline__ floatx16 mfma6(const Split &b, const Split &a, floatx
 // WK groups of WM x WN wavefronts of (BM / WM) x (BN / WN) each; the groups take the slabs in turn and their sums are added in LDS in
 // group order (products with too few tiles to fill the chip: the chain of slabs is WK times shorter).
 // Epi: `piece<WC>(stage, m, n, M, N, problem, split, q, ahead)` takes 32 x WC sums (WC = 64 or 32) from the wavefront's LDS area
-// (row stride kStageLd floats), first element C(m, n), the wavefront's q-th piece along m; `ahead(m, M, lane)` is called before the products.
+// (row stride kStageLd floats), first element C(m, n), the wavefront's q-th piece along m; `ahead(m, M, lane)` is called before the products;
+// `counts(ahead, q, lane, N)`, called by whole wavefronts, says whether row lane % 32 of the q-th piece is used.
 // PAIR: B[0] and B[1] are the gate and up projections (KC), N counts hidden units, a tile covers BN / 2 of them.
 template <class T, int BM, int BN, int WM, int WN, int WK, int STAGES, bool AKC, bool BKC, bool PAIR, class Epi>
 __device__ __forceinline__ void product_tile(const ProductArgs &a, const Epi &epi, int id, char *smem) {
@@ -459,15 +460,15 @@ __device__ __forceinline__ void product_tile(const ProductArgs &a, const Epi &ep
       for (int j = 0; j < TN; ++j)
 #pragma unroll
         for (int r = 0; r < 16; ++r) finite = finite && fabsf(acc[i][j][r]) < INFINITY;
-    // Only sums that exist count: an operand across k may hold anything behind its last row or column (a workspace's rows are written
+    // Only sums that exist and whose rows count for the epilogue do: an operand across k may hold anything behind its last row or column (a workspace's rows are written
     // up to their last whole group of eight), and what a former call left there must change neither digits nor time.  Looked at only
     // where there is something: for every tile it would cost 2.5 % of 1000 x 500 x 1337 both ways.
-    if (!finite) {
+    if (__any(!finite)) {
       const int left = PAIR ? WC : a.N - n0 - wn - 4 * (lane >> 5);   // a pair's rows behind the last one are zeros
       finite = true;
 #pragma unroll
       for (int i = 0; i < TM; ++i) {
-        const bool row = m0 + wm + 32 * i + (lane & 31) < M;
+        const bool counts = epi.counts(ahead, i, lane, a.N), row = m0 + wm + 32 * i + (lane & 31) < M && counts;
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
@@ -592,6 +593,7 @@ struct Nothing {};
 struct NothingAhead {
   typedef Nothing Ahead;
   __device__ __forceinline__ Nothing ahead(int, int, int) const { return Nothing{}; }
+  __device__ __forceinline__ bool counts(Nothing, int, int, int) const { return true; }
 };
 
 // C[problem][m][n] in T, rows optionally through a map; or += to what a former piece left (fp32 sums)

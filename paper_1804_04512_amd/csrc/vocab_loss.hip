@@ -67,6 +67,10 @@ struct LogitEpi {
   __device__ __forceinline__ Ahead ahead(int m, int M, int lane) const {
     return Ahead{{labels[min(m + lane, M - 1)], labels[min(m + 64 + lane, M - 1)]}};
   }
+  // rows that were not gathered may hold anything where their label is none
+  __device__ __forceinline__ bool counts(Ahead of, int q, int lane, int V) const {
+    return (unsigned)__shfl(q & 2 ? of.label[1] : of.label[0], (q & 1) * 32 + (lane & 31)) < (unsigned)V;
+  }
   template <int WC>
   __device__ __forceinline__ void piece(const float *stage, int m, int n, int M, int V, int, int, int q, Ahead of) const {
     const Lanes<WC> l;

@@ -154,3 +154,29 @@ def test_single_precision_in_graphs_and_on_two_streams():
         blocks(streams[0]), loss(streams[1])
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip([y, *kept.values(), *g.values(), *o.values()], eager))
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("size", [(20, 64, 600), (31, 260, 4099), (32, 33, 9000), (5, 40, 300), (24, 72, 65), (32, 512, 33000)], ids=lambda s: "x".join(map(str, s)))
+def test_few_rows_that_do_not_count_reach_nothing(size, dtype):
+    """A forward pass of few rows, which are not gathered: NaN, infinities and the largest numbers in rows that do not count leave
+    the others' bits as they are."""
+    spec = VocabSpec(*size, dtype)
+    i = vocab_inputs(*size, dtype, seed=sum(size), ignored=0.5)
+    i["labels"][0], i["labels"][1] = 3, -1
+    e = lambda *s: torch.full(s, float("nan"), device="cuda")
+    T, out = size[0], i["labels"] < 0
+
+    def fwd():
+        o = dict(row_loss=e(T), row_lse=e(T), loss=e(1))
+        B.dll_vocab_loss_fwd(spec, **i, **o, ws=B.workspace(B.dll_vocab_loss_fwd_workspace_bytes(spec)).fill_(255))
+        return o
+
+    clean, want = fwd(), ref.vocab(*i.values())
+    for k in clean:
+        ref.check(clean[k], want[k], k)
+    for bad in (float("nan"), float("inf"), torch.finfo(torch.float32).max):
+        i["x"][out] = bad
+        dirty = fwd()
+        for k in clean:
+            assert torch.equal(clean[k], dirty[k]), (k, bad)
