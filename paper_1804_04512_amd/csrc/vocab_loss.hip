@@ -256,7 +256,7 @@ __global__ __launch_bounds__(256) void gather_rows_kernel(const T *x, T *xc, lon
   }
 }
 
-// lse = M + ln sum_g s_g exp(m_g - M).  A workgroup takes 16 rows at a time, 64 threads each.  Rows that were not gathered
+// lse = M + ln sum_g s_g exp(m_g - M), loss = (M - z_label) + the same logarithm.  A workgroup takes 16 rows at a time, 64 threads each.  Rows that were not gathered
 // (all_labels given) are taken by one workgroup, which passes over those that do not count and leaves the mean as well.
 __global__ __launch_bounds__(1024) void join_groups_kernel(const float2 *stats, int groups, long rows_ld, const float *hit, int M, const int *count, int first,
                                                             const int *rows, float *lse, float *piece_loss, float *row_loss, float *row_lse, const int *all_labels, int V, float *loss) {
@@ -298,7 +298,9 @@ __global__ __launch_bounds__(1024) void join_groups_kernel(const float2 *stats, 
 #pragma unroll
       for (int w = 0; w < 16; ++w) join(part[w][r].x, part[w][r].y);
       const bool in = !all_labels || (all_labels[row] >= 0 && all_labels[row] < V);
-      const float l = in ? top + logf(sum) : 0.0f, each = in ? l - hit[row] : 0.0f;
+      // The loss from the two logits' difference: where the label has nearly all the probability it is the small logarithm alone, which
+      // top + logf(sum) would round to a last digit of top.
+      const float tail = logf(sum), l = in ? top + tail : 0.0f, each = in ? (top - hit[row]) + tail : 0.0f;
       const int to = all_labels ? row : rows[row];
       if (lse) lse[row] = l;
       if (piece_loss) piece_loss[row] = each;

@@ -180,3 +180,45 @@ def test_few_rows_that_do_not_count_reach_nothing(size, dtype):
         dirty = fwd()
         for k in clean:
             assert torch.equal(clean[k], dirty[k]), (k, bad)
+
+
+def sure_rows(T, V, D, dtype):
+    """Logits that every way of multiplying gives exactly: row t of x is the t-th unit vector, so that z[t][v] = w[v][t], whole
+    numbers of 8 bits.  The label's is 1024 (or in every third row 1008), the others' are at most 1008."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(T + V)
+    x = torch.zeros(T, D, dtype=TYPES[dtype], device="cuda")
+    x[torch.arange(T), torch.arange(T)] = 1
+    w = (1008 - 16 * torch.randint(0, 8, (V, D), generator=gen, device="cuda")).to(TYPES[dtype])
+    labels = torch.randint(0, V, (T,), generator=gen, device="cuda", dtype=torch.int32)
+    w[labels.long(), torch.arange(T, device="cuda")] = 1024
+    labels[2::3] = (labels[2::3] + 1) % V   # the label of another row is not there: rows are columns of w
+    return x, w, labels
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("size", [(1, 900, 8), (20, 1000, 33), (20, 4000, 40), (100, 1000, 128), (300, 3001, 300)], ids=lambda s: "x".join(map(str, s)))
+def test_loss_of_rows_that_are_nearly_sure(size, dtype):
+    """The label has all but about 1e-5 of the probability at logits of 1024, whose last digit in 32 bits is 1.2e-4.
+    Bound: the terms are at most 1.002 together, each with the error of its exponential (EXP, of the terms below the largest, which is
+    exact); a row's sum has 8 terms a lane, 3 steps among lanes, ceil(groups / 64) <= 2 groups a thread, 2 and 16 steps: 31 roundings of
+    2^-24 of the sum; logf two last digits; then the difference and its sum with the logarithm, 2^-24 of the loss each."""
+    T, V, D = size
+    x, w, labels = sure_rows(T, V, D, dtype)
+    spec = VocabSpec(T, D, V, dtype)
+    e = lambda *s, d=torch.float32: torch.full(s, float("nan"), dtype=d, device="cuda")
+    z = w.double().t()[:T]
+    top = z.amax(1)
+    rest = torch.exp(z - top[:, None]).sum(1) - 1
+    loss = torch.log1p(rest) + (top - z[torch.arange(T), labels.long()])
+    bound = rest * ref.EXP + 31 * U32 * (1 + rest) + 4 * U32 * torch.log1p(rest) + 2 * U32 * loss
+    assert float(loss.min()) < 2e-3 and float(bound[loss.argmin()]) < 8e-6   # below the last digit of 1024
+    for call in ("fwd", "grad"):
+        o = dict(row_loss=e(T), row_lse=e(T), loss=e(1))
+        if call == "fwd":
+            B.dll_vocab_loss_fwd(spec, x, w, None, labels, **o, ws=B.workspace(B.dll_vocab_loss_fwd_workspace_bytes(spec)).fill_(255))
+        else:
+            B.dll_vocab_loss_grad(spec, x, w, None, labels, 1.0, **o, dx=e(T, D, d=x.dtype), ws=B.workspace(B.dll_vocab_loss_grad_workspace_bytes(spec)).fill_(255))
+        ref.check(o["row_loss"], (loss, bound), call)
+        ref.check(o["loss"], (loss.mean().reshape(1), bound.mean().reshape(1) + U32 * loss.mean()), call)
+        ref.check(o["row_lse"], (top + torch.log1p(rest), bound + U32 * (top + 1)), call)
