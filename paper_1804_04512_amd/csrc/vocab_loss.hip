@@ -6,7 +6,8 @@
 //
 // The product's epilogue takes each row's maximum m_g and sum of exp(z - m_g) over groups of 64 or 32 columns; one kernel joins
 // the groups to lse.  For the gradients the epilogue also leaves e = exp(z - m_g) in the operands' type, and a second pass
-// turns it in place into dz = e * exp(m_g - lse) * scale / count (minus the label's share): exponentials in (0, 1] relative
+// turns it in place into dz = e * exp((M - lse) + (m_g - M)) * scale / count (minus the label's share; M the row's maximum, whose
+// distance to lse is kept, as their difference afterwards would have lost it): exponentials in (0, 1] relative
 // to their own group keep all the type's digits, which rounded logits would not (bfloat16 logits of size 10 are 2 % off
 // after exp).  This takes three products of T D V; forming the logits again for the gradients would take four.
 // The exponentials are kept for a piece of the tokens at a time, 1 GiB at most.
@@ -259,7 +260,7 @@ __global__ __launch_bounds__(256) void gather_rows_kernel(const T *x, T *xc, lon
 // lse = M + ln sum_g s_g exp(m_g - M), loss = (M - z_label) + the same logarithm.  A workgroup takes 16 rows at a time, 64 threads each.  Rows that were not gathered
 // (all_labels given) are taken by one workgroup, which passes over those that do not count and leaves the mean as well.
 __global__ __launch_bounds__(1024) void join_groups_kernel(const float2 *stats, int groups, long rows_ld, const float *hit, int M, const int *count, int first,
-                                                            const int *rows, float *lse, float *piece_loss, float *row_loss, float *row_lse, const int *all_labels, int V, float *loss) {
+                                                            const int *rows, float2 *lse, float *piece_loss, float *row_loss, float *row_lse, const int *all_labels, int V, float *loss) {
   __shared__ float2 part[16][17];
   __shared__ double mean[16];
   __shared__ int counts[16];
@@ -302,7 +303,7 @@ __global__ __launch_bounds__(1024) void join_groups_kernel(const float2 *stats, 
       // top + logf(sum) would round to a last digit of top.
       const float tail = logf(sum), l = in ? top + tail : 0.0f, each = in ? (top - hit[row]) + tail : 0.0f;
       const int to = all_labels ? row : rows[row];
-      if (lse) lse[row] = l;
+      if (lse) lse[row] = make_float2(top, tail);
       if (piece_loss) piece_loss[row] = each;
       if (row_loss) row_loss[to] = each;
       if (row_lse) row_lse[to] = l;
@@ -343,7 +344,7 @@ __global__ __launch_bounds__(1024) void mean_loss_kernel(const float *row, const
 // last piece one workgroup more (the last column's) leaves the mean loss.
 template <class T>
 __global__ __launch_bounds__(256) void exp_to_gradient_kernel(T *e, long ld, int V, int M, const int *count, int first, const float2 *stats, long rows_ld,
-                                                               const float *lse, const int *labels, int group, float scale, float *sums, const float *row_loss, float *loss) {
+                                                               const float2 *lse, const int *labels, int group, float scale, float *sums, const float *row_loss, float *loss) {
   __shared__ float part[16][128 + 4];
   const int n = rows_left(count, first, M), t = threadIdx.x, r0 = blockIdx.y * 64, sub = t >> 4, col = blockIdx.x * 128 + (t & 15) * 8;
   if (loss && blockIdx.x == gridDim.x - 1) {
@@ -364,8 +365,9 @@ __global__ __launch_bounds__(256) void exp_to_gradient_kernel(T *e, long ld, int
     for (int i = 0; i < 4; ++i) {
       const int row = r0 + 16 * i + sub;
       if (row < n) {
-        const float m = stats[(long)(col / group) * rows_ld + row].x, l = lse[row];
-        const float f = m == -INFINITY ? 0.0f * l : exp_below(m - l) * share;   // 0 unless the row's sum is not finite
+        const float m = stats[(long)(col / group) * rows_ld + row].x;
+        const float2 l = lse[row];   // lse = l.x + l.y
+        const float f = m == -INFINITY ? 0.0f * (l.x + l.y) : exp_below((m - l.x) - l.y) * share;   // 0 unless the row's sum is not finite
         const int at = labels[row] - col;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -424,7 +426,8 @@ struct Plan {
   int *count, *rows, *labels;
   void *x, *w, *e;
   float2 *stats;
-  float *hit, *lse, *loss, *sums, *bias_sum, *dw_sum, *part;
+  float2 *lse;    // the row's maximum, and the logarithm of its sum
+  float *hit, *loss, *sums, *bias_sum, *dw_sum, *part;
   size_t bytes;
   Plan(int T, int D, int V, int dtype, bool grad, char *base) {
     Take take{base};
@@ -451,7 +454,7 @@ struct Plan {
     loss = (float *)take((size_t)T * sizeof(float));
     lse = nullptr, e = nullptr, sums = bias_sum = dw_sum = part = nullptr;
     if (grad) {
-      lse = (float *)take((size_t)piece * sizeof(float));
+      lse = (float2 *)take((size_t)piece * sizeof(float2));
       e = take(slab_rows * lde * b);
       sums = (float *)take(slab_rows / 64 * lde * sizeof(float));
       bias_sum = (float *)take((size_t)V * sizeof(float));

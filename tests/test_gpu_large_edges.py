@@ -222,3 +222,36 @@ def test_loss_of_rows_that_are_nearly_sure(size, dtype):
         ref.check(o["row_loss"], (loss, bound), call)
         ref.check(o["loss"], (loss.mean().reshape(1), bound.mean().reshape(1) + U32 * loss.mean()), call)
         ref.check(o["row_lse"], (top + torch.log1p(rest), bound + U32 * (top + 1)), call)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("size", [(1, 900, 8), (20, 1000, 33), (100, 1000, 128), (300, 3001, 300)], ids=lambda s: "x".join(map(str, s)))
+def test_gradients_of_rows_that_are_nearly_sure(size, dtype):
+    """dw[v][t] is dz[t][v] alone, as row t of x is the t-th unit vector.  Of a label with all but 1e-5 of the probability it is
+    -1e-5 / count; p itself is off by the bound of the logarithm of the sum (31 roundings of a sum of about 1, and logf's
+    last digits), by that of its exponential (EXP / 64: x is below 1e-3 there, so two last digits of 1) and, elsewhere, by EXP and
+    the type's rounding of e; dz by the type's rounding and 4 of 32 bits."""
+    T, V, D = size
+    x, w, labels = sure_rows(T, V, D, dtype)
+    spec = VocabSpec(T, D, V, dtype)
+    e = lambda *s, d=torch.float32: torch.full(s, float("nan"), dtype=d, device="cuda")
+    z = w.double().t()[:T]
+    top = z.amax(1, keepdim=True)
+    terms = torch.exp(z - top)
+    at = torch.arange(T, device="cuda"), labels.long()
+    best = z == top
+    rest = torch.where(best, 0.0, terms).sum(1, keepdim=True) + (best.sum(1, keepdim=True) - 1)
+    p = terms / (1 + rest)
+    dz = p.clone()
+    sure = torch.zeros_like(dz, dtype=torch.bool).index_put(at, torch.tensor(True, device="cuda")) & best
+    dz[at] -= 1
+    dz = torch.where(sure, (-rest / (1 + rest)).expand_as(dz), dz)
+    u = ref.unit(x.dtype)
+    log = 31 * U32 + 4 * U32 * torch.log1p(rest)
+    edz = p * log + torch.where(best, p * 4 * U32, p * (ref.EXP + u)) + (u + 4 * U32) * dz.abs() + 2 * U32 + 2 * 2.0 ** -126
+    o = dict(row_loss=e(T), row_lse=e(T), loss=e(1), dx=e(T, D, d=x.dtype), dw=e(V, D, d=x.dtype))
+    B.dll_vocab_loss_grad(spec, x, w, None, labels, float(T), **o, ws=B.workspace(B.dll_vocab_loss_grad_workspace_bytes(spec)).fill_(255))
+    assert float(dz[sure].abs().min()) < 2.0 ** -14   # half a last digit of 1024 (scale / count = 1)
+    want, bound = torch.zeros(V, D, dtype=torch.float64, device="cuda"), torch.zeros(V, D, dtype=torch.float64, device="cuda")
+    want[:, :T], bound[:, :T] = dz.t(), (edz + (ref.gamma(T) + u) * dz.abs()).t()
+    ref.check(o["dw"], (want, bound), "dw")
