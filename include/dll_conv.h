@@ -351,8 +351,8 @@ typedef struct {
 } dll_tensor_list;
 
 /* The 2-norm over all elements of all gradients, *norm a device scalar.  grads is a host array of n
- * device pointers (aligned to their elements; NULL only where the count is 0).  Squares are added
- * in 64 bits in a fixed order. */
+ * device pointers (aligned to their elements; NULL only where the count is 0); none of them may be norm
+ * (-> DLL_ERR_SHAPE).  Squares are added in 64 bits in a fixed order. */
 size_t dll_grad_norm_workspace_bytes(const dll_tensor_list *list);
 dll_status dll_grad_norm(const dll_tensor_list *list, const void *const *grads, float *norm, void *ws,
                          size_t ws_bytes, void *stream);

@@ -73,21 +73,24 @@ dll_status check_list(const dll_tensor_list *l, const void *const *grads, bool w
   return DLL_OK;
 }
 
-// One address of a list: of tensor `tensor`, or of the norm (-1)
+// One address of a list: of tensor `tensor`, or of the norm or the workspace (-1)
 struct Place {
   uintptr_t at;
   int tensor, output;
 };
-// Whether an output of a list of tensors is another output or any tensor's gradient; with in_place it may be its own.  The kernels
+// Whether an output of a list of tensors, the norm or the workspace is another of these or any tensor's gradient; with in_place an
+// output may be its own.  The kernels
 // take all tensors at once, so a tensor listed twice would be stepped by two workgroups that race.
-dll_status check_places(const dll_tensor_list *l, const void *const *grads, const void *const *const *outs, int n_outs, const float *norm, bool in_place) {
+dll_status check_places(const dll_tensor_list *l, const void *const *grads, const void *const *const *outs, int n_outs, const float *norm, const void *ws,
+                        bool in_place) {
   constexpr int kHere = 256;
   Place here[kHere];
-  const size_t most = (size_t)l->n * (n_outs + 1) + 1;
+  const size_t most = (size_t)l->n * (n_outs + 1) + 2;
   Place *const p = most <= kHere ? here : new (std::nothrow) Place[most];
   if (!p) return DLL_ERR_DEVICE;
   size_t n = 0;
   p[n++] = Place{reinterpret_cast<uintptr_t>(norm), -1, 1};
+  p[n++] = Place{reinterpret_cast<uintptr_t>(ws), -1, 1};
   for (int i = 0; i < l->n; ++i) {
     if (l->counts[i] == 0) continue;
     p[n++] = Place{reinterpret_cast<uintptr_t>(grads[i]), i, 0};
@@ -216,6 +219,7 @@ dll_status dll_grad_norm(const dll_tensor_list *list, const void *const *grads, 
   dll_status st = check_list(list, grads, true);
   if (st != DLL_OK) return st;
   if (!norm) return DLL_ERR_NULL;
+  if ((st = check_places(list, grads, nullptr, 0, norm, ws, false)) != DLL_OK) return st;
   if ((st = check_ws(ws, ws_bytes, dll_grad_norm_workspace_bytes(list))) != DLL_OK) return st;
   return dev(launch_grad_norm(list_of(list), grads, norm, static_cast<char *>(ws), static_cast<hipStream_t>(stream)));
 }
@@ -232,7 +236,7 @@ dll_status dll_grad_clip(const dll_tensor_list *list, const void *const *grads, 
     if (reinterpret_cast<uintptr_t>(out[i]) % type_bytes(list->dtypes[i])) return DLL_ERR_SHAPE;
   }
   const void *const *outs[] = {out};
-  if ((st = check_places(list, grads, outs, 1, norm, true)) != DLL_OK) return st;
+  if ((st = check_places(list, grads, outs, 1, norm, ws, true)) != DLL_OK) return st;
   if ((st = check_ws(ws, ws_bytes, dll_grad_norm_workspace_bytes(list))) != DLL_OK) return st;
   return dev(launch_grad_clip(list_of(list), grads, out, max_norm, norm, static_cast<char *>(ws), static_cast<hipStream_t>(stream)));
 }
@@ -251,7 +255,7 @@ dll_status dll_momentum_update_clipped(const dll_tensor_list *list, float *const
     if ((reinterpret_cast<uintptr_t>(params[i]) | reinterpret_cast<uintptr_t>(velocity[i])) % 4 || reinterpret_cast<uintptr_t>(copy) % 2) return DLL_ERR_SHAPE;
   }
   const void *const *outs[] = {reinterpret_cast<const void *const *>(params), reinterpret_cast<const void *const *>(velocity), copies};
-  if ((st = check_places(list, grads, outs, 3, norm, false)) != DLL_OK) return st;
+  if ((st = check_places(list, grads, outs, 3, norm, ws, false)) != DLL_OK) return st;
   if ((st = check_ws(ws, ws_bytes, dll_grad_norm_workspace_bytes(list))) != DLL_OK) return st;
   return dev(launch_momentum_clipped(list_of(list), params, velocity, grads, weight_decay, lr, momentum, max_norm, norm, copies, static_cast<char *>(ws),
                                      static_cast<hipStream_t>(stream)));

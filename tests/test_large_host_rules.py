@@ -1,8 +1,12 @@
 """What the large-model operators settle on the host: which kernels a call launches (launches are noted instead of run: no
 GPU needed)."""
-import pytest
+import ctypes as C
+
+from paper_1804_04512_amd import binding as B
 
 from launch_record import record
+
+OK, NULL, SHAPE, UNSUPPORTED, WORKSPACE = 0, 1, 2, 3, 4
 
 
 def test_no_launch_behind_the_last_tensor(tmp_path):
@@ -15,3 +19,20 @@ def test_no_launch_behind_the_last_tensor(tmp_path):
             assert status == 0
             small = sum(counts) <= 64 * 8
             assert len(launches) == (1 if small else n + 1 if what == "norm" else 2 * n), (what, counts, launches)
+
+
+def test_norm_and_workspace_are_no_tensor_of_the_list():
+    """The norm of a list is refused where it lies on one of its gradients, as clipping and the step refuse it, and so is a workspace
+    there or on the norm.  A gradient that is listed twice may be read twice."""
+    L = B.lib()
+    for n in (2, 150):   # addresses on the stack, and more than fit there
+        l = C.byref(B.dll_tensor_list(n, (C.c_size_t * n)(*[4] * n), (C.c_int * n)(*[0] * n)))
+        at = lambda base, step=256: (C.c_void_p * n)(*[base + step * k for k in range(n)])
+        g, p, v = at(0x100000), at(0x200000), at(0x300000)
+        norm, ws, first, last = (C.c_void_p(a) for a in (0x10000, 0x20000, 0x100000, 0x100000 + 256 * (n - 1)))
+        calls = (lambda norm, ws, g=g: L.dll_grad_norm(l, g, norm, ws, 0, None), lambda norm, ws, g=g: L.dll_grad_clip(l, g, p, 1.0, norm, ws, 0, None),
+                 lambda norm, ws, g=g: L.dll_momentum_update_clipped(l, p, v, g, 0.1, 0.9, None, 1.0, norm, None, ws, 0, None))
+        for call in calls:
+            assert call(norm, ws) == call(norm, ws, at(0x100000, 0)) == WORKSPACE   # nothing else to refuse
+            assert call(first, ws) == call(last, ws) == call(norm, last) == call(norm, norm) == SHAPE
+        assert L.dll_grad_clip(l, g, g, 1.0, norm, ws, 0, None) == WORKSPACE and L.dll_grad_clip(l, g, p, 1.0, norm, C.c_void_p(0x200000), 0, None) == SHAPE
