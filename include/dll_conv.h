@@ -270,7 +270,8 @@ dll_status dll_cnn_forward(const dll_net_desc *net, const float *const *params, 
  * network steps above: a gated feed-forward block, softmax cross entropy over a large
  * vocabulary, and clipping by the global gradient norm with the momentum step behind it.
  * The conventions at the top hold: device pointers, row-major and contiguous, 16-byte aligned
- * (else DLL_ERR_SHAPE) unless stated, caller-owned workspaces, errors before any launch.
+ * (else DLL_ERR_SHAPE) unless stated (labels, row_loss, row_lse, loss and norm: to 4 bytes),
+ * caller-owned workspaces, errors before any launch.
  * Tensors typed `void *` hold the descriptor's dtype.  Sums, softmax statistics and norms are
  * taken in 32 bits or more; with DLL_BF16 what one product hands to the next is rounded to
  * bfloat16 once (to nearest), and results are rounded once.  At most 2^24 tokens and 2^20

@@ -15,6 +15,8 @@ namespace {
 constexpr size_t kAlign = 256;
 inline size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
 inline bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+// labels, losses and norms: 32-bit values at any place of theirs
+inline bool off_element(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
 inline dll_status dev(hipError_t e) { return e == hipSuccess ? DLL_OK : DLL_ERR_DEVICE; }
 
 dll_status check_ws(const void *ws, size_t have, size_t need) {
@@ -78,11 +80,12 @@ struct Place {
   uintptr_t at;
   int tensor, output;
 };
-// Whether an output of a list of tensors, the norm or the workspace is another of these or any tensor's gradient; with in_place an
+// Whether the norm is no place of a 32-bit value, or an output of a list of tensors, the norm or the workspace is another of these or any tensor's gradient; with in_place an
 // output may be its own.  The kernels
 // take all tensors at once, so a tensor listed twice would be stepped by two workgroups that race.
 dll_status check_places(const dll_tensor_list *l, const void *const *grads, const void *const *const *outs, int n_outs, const float *norm, const void *ws,
                         bool in_place) {
+  if (off_element(norm)) return DLL_ERR_SHAPE;
   constexpr int kHere = 256;
   Place here[kHere];
   const size_t most = (size_t)l->n * (n_outs + 1) + 2;
@@ -182,6 +185,7 @@ dll_status dll_vocab_loss_fwd(const dll_vocab_desc *d, const void *x, const void
   if (!x || !w || !labels || !loss) return DLL_ERR_NULL;
   const void *in[] = {x, w, bias, labels}, *out[] = {row_loss, row_lse, loss, ws};
   if (aliased(in, 4, out, 4) || misaligned(x) || misaligned(w) || misaligned(bias)) return DLL_ERR_SHAPE;
+  if (off_element(labels) || off_element(row_loss) || off_element(row_lse) || off_element(loss)) return DLL_ERR_SHAPE;
   if ((st = check_ws(ws, ws_bytes, dll_vocab_loss_fwd_workspace_bytes(d))) != DLL_OK) return st;
   VocabArgs a;
   a.T = d->tokens; a.D = d->width; a.V = d->classes; a.dtype = d->dtype;
@@ -202,6 +206,7 @@ dll_status dll_vocab_loss_grad(const dll_vocab_desc *d, const void *x, const voi
   const void *in[] = {x, w, bias, labels}, *out[] = {row_loss, row_lse, loss, dx, dw, dbias, ws};
   if (aliased(in, 4, out, 7) || misaligned(x) || misaligned(w) || misaligned(bias) || misaligned(dx) || misaligned(dw) || misaligned(dbias))
     return DLL_ERR_SHAPE;
+  if (off_element(labels) || off_element(row_loss) || off_element(row_lse) || off_element(loss)) return DLL_ERR_SHAPE;
   if ((st = check_ws(ws, ws_bytes, dll_vocab_loss_grad_workspace_bytes(d))) != DLL_OK) return st;
   VocabArgs a;
   a.T = d->tokens; a.D = d->width; a.V = d->classes; a.dtype = d->dtype;

@@ -3,6 +3,7 @@ GPU needed)."""
 import ctypes as C
 
 from paper_1804_04512_amd import binding as B
+from paper_1804_04512_amd.workloads import VocabSpec
 
 from launch_record import record
 
@@ -36,3 +37,21 @@ def test_norm_and_workspace_are_no_tensor_of_the_list():
             assert call(norm, ws) == call(norm, ws, at(0x100000, 0)) == WORKSPACE   # nothing else to refuse
             assert call(first, ws) == call(last, ws) == call(norm, last) == call(norm, norm) == SHAPE
         assert L.dll_grad_clip(l, g, g, 1.0, norm, ws, 0, None) == WORKSPACE and L.dll_grad_clip(l, g, p, 1.0, norm, C.c_void_p(0x200000), 0, None) == SHAPE
+
+
+def test_labels_losses_and_norms_lie_at_their_elements():
+    """At any multiple of four bytes; refused elsewhere, before any launch."""
+    L = B.lib()
+    d = C.byref(B.vocab_desc(VocabSpec(16, 24, 40, "float32")))
+    at = lambda k, off=0: C.c_void_p(0x10000 * (k + 1) + off)
+    ws, out = at(9), [at(10), at(11), at(12)]
+    for k in range(4):   # labels, row_loss, row_lse, loss
+        for off, status in ((0, WORKSPACE), (4, WORKSPACE), (1, SHAPE), (2, SHAPE)):
+            labels, *losses = [at(4 + i, off if i == k else 0) for i in range(4)]
+            assert L.dll_vocab_loss_fwd(d, at(0), at(1), at(2), labels, *losses, ws, 0, None) == status
+            assert L.dll_vocab_loss_grad(d, at(0), at(1), at(2), labels, 1.0, *losses, *out, ws, 0, None) == status
+    l, one = C.byref(B.dll_tensor_list(1, (C.c_size_t * 1)(4), (C.c_int * 1)(0))), lambda k: (C.c_void_p * 1)(at(k).value)
+    for off, status in ((0, WORKSPACE), (4, WORKSPACE), (2, SHAPE)):
+        norm = at(5, off)
+        assert L.dll_grad_norm(l, one(0), norm, ws, 0, None) == L.dll_grad_clip(l, one(0), one(1), 1.0, norm, ws, 0, None) == status
+        assert L.dll_momentum_update_clipped(l, one(1), one(2), one(0), 0.1, 0.9, None, 1.0, norm, None, ws, 0, None) == status
