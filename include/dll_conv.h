@@ -358,9 +358,9 @@ size_t dll_grad_norm_workspace_bytes(const dll_tensor_list *list);
 dll_status dll_grad_norm(const dll_tensor_list *list, const void *const *grads, float *norm, void *ws,
                          size_t ws_bytes, void *stream);
 
-/* Clipping by the global norm: out = c * grad with c = min(1, max_norm / norm), max_norm > 0 (infinity:
+/* Clipping by the global norm: out = c * grad with c = min(1, max_norm / norm) in 32 bits, max_norm > 0 (infinity:
  * c = 1), out in the gradients' types; out[i] may be grads[i], but no other gradient, output or norm
- * (-> DLL_ERR_SHAPE).  Where the norm is not finite c is 1.
+ * (-> DLL_ERR_SHAPE).  Where *norm is not finite (more than 32 bits hold, too) c is 1.
  * Workspace as for dll_grad_norm. */
 dll_status dll_grad_clip(const dll_tensor_list *list, const void *const *grads, void *const *out,
                          float max_norm, float *norm, void *ws, size_t ws_bytes, void *stream);
@@ -370,7 +370,7 @@ dll_status dll_grad_clip(const dll_tensor_list *list, const void *const *grads, 
  * params and velocity are host arrays of n fp32 device pointers; weight_decay a host array of n factors,
  * or NULL (none).  copies, or NULL, is a host array of n device pointers (each may be NULL) that receive
  * the new parameters in bfloat16.  No tensor may be listed twice among the three, nor be a gradient or
- * norm (-> DLL_ERR_SHAPE).  Where the norm is not finite no step is taken: only *norm is written. */
+ * norm (-> DLL_ERR_SHAPE).  Where *norm is not finite no step is taken: only *norm is written. */
 dll_status dll_momentum_update_clipped(const dll_tensor_list *list, float *const *params,
                                        float *const *velocity, const void *const *grads, float lr,
                                        float momentum, const float *weight_decay, float max_norm,

@@ -117,6 +117,14 @@ __device__ __forceinline__ double norm_of(const double *partial, int n) {
   return sqrt(group_sum(s));
 }
 
+// Whether the norm as it is written is finite: sums of 64 bits reach further than the 32 bits that the caller sees, and a caller
+// who reads infinity is promised gradients and parameters that were left alone.
+__device__ __forceinline__ bool finite_norm(double x) { return isfinite((float)x); }
+// c = min(1, max_norm / norm), rounded to 32 bits once; 1 where the norm is not finite
+__device__ __forceinline__ float clip_factor(double x, float max_norm) {
+  return finite_norm(x) && x > (double)max_norm ? (float)((double)max_norm / x) : 1.0f;
+}
+
 __global__ __launch_bounds__(256) void join_squares_kernel(const double *partial, int n, double *sum) {
   double s = 0.0;
 #pragma unroll 8
@@ -146,7 +154,7 @@ __device__ __forceinline__ void scale_chunk(const T *g, T *out, long begin, long
 __global__ __launch_bounds__(256) void grad_scale_kernel(const ClipTable a, const double *partial, int n, float max_norm, float *norm) {
   const double x = norm_of(partial, n);
   if (blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)x;
-  const float c = x > (double)max_norm && isfinite(x) ? (float)((double)max_norm / x) : 1.0f;
+  const float c = clip_factor(x, max_norm);
   const NormTable &t = a.t;
   for (int k = blockIdx.x; k < t.chunks; k += gridDim.x) {
     const int i = tensor_of(t, k);
@@ -177,8 +185,8 @@ __device__ __forceinline__ void step_chunk(const T *g, float *p, float *v, bf16 
 __global__ __launch_bounds__(256) void momentum_step_kernel(const StepTable a, const double *partial, int n, float max_norm, float step, float mu, float *norm) {
   const double x = norm_of(partial, n);
   if (blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)x;
-  if (!isfinite(x)) return;   // a gradient that overflowed: no step
-  const float c = x > (double)max_norm ? (float)((double)max_norm / x) : 1.0f;
+  if (!finite_norm(x)) return;   // a gradient that overflowed: no step
+  const float c = clip_factor(x, max_norm);
   const NormTable &t = a.t;
   for (int k = blockIdx.x; k < t.chunks; k += gridDim.x) {
     const int i = tensor_of(t, k);
@@ -226,8 +234,8 @@ __global__ __launch_bounds__(1024) void few_kernel(const Table a, float max_norm
   for (int w = 0; w < 16; ++w) s += part[w];
   const double x = sqrt(s);
   if (threadIdx.x == 0) *norm = (float)x;
-  if (WHAT == kFewNorm || (WHAT == kFewStep && !isfinite(x))) return;
-  const float c = x > (double)max_norm && isfinite(x) ? (float)((double)max_norm / x) : 1.0f;
+  if (WHAT == kFewNorm || (WHAT == kFewStep && !finite_norm(x))) return;
+  const float c = clip_factor(x, max_norm);
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     const int i = tensor[k];

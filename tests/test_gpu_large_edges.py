@@ -255,3 +255,25 @@ def test_gradients_of_rows_that_are_nearly_sure(size, dtype):
     want, bound = torch.zeros(V, D, dtype=torch.float64, device="cuda"), torch.zeros(V, D, dtype=torch.float64, device="cuda")
     want[:, :T], bound[:, :T] = dz.t(), (edz + (ref.gamma(T) + u) * dz.abs()).t()
     ref.check(o["dw"], (want, bound), "dw")
+
+
+@pytest.mark.parametrize("counts", [[8, 3], [40000, 9]], ids=["one workgroup", "many"])
+def test_a_norm_beyond_32_bits_is_not_finite(counts):
+    """Finite gradients whose norm 32 bits do not hold: the caller reads infinity, and then nothing was scaled and no step taken."""
+    g = [torch.full((n,), 3e38, device="cuda") for n in counts]
+    l, norm = B.tensor_list(g), torch.zeros(1, device="cuda")
+    ws = B.workspace(B.dll_grad_norm_workspace_bytes(l)).fill_(255)
+    B.dll_grad_norm(l, g, norm, ws)
+    assert math.isinf(float(norm))
+    out = [torch.zeros_like(t) for t in g]
+    B.dll_grad_clip(l, g, out, 1.0, norm, ws)
+    assert math.isinf(float(norm)) and all(torch.equal(a, b) for a, b in zip(out, g))
+    p, v = [torch.ones_like(t) for t in g], [torch.full_like(t, 2) for t in g]
+    B.dll_momentum_update_clipped(l, p, v, g, 0.1, 0.9, None, 1.0, norm, ws=ws)
+    assert math.isinf(float(norm)) and all(bool((t == 1).all()) for t in p) and all(bool((t == 2).all()) for t in v)
+    g = [t / 1e10 for t in g]   # and in reach again
+    B.dll_grad_clip(l, g, out, 1.0, norm, ws)
+    want = math.sqrt(sum(float(t.double().square().sum()) for t in g))
+    assert abs(float(norm) - want) <= 2 * U32 * want
+    for a, b in zip(out, g):
+        ref.check(a, (b.double() / want, 3 * U32 * b.double() / want), "clipped")
