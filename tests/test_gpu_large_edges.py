@@ -277,3 +277,37 @@ def test_a_norm_beyond_32_bits_is_not_finite(counts):
     assert abs(float(norm) - want) <= 2 * U32 * want
     for a, b in zip(out, g):
         ref.check(a, (b.double() / want, 3 * U32 * b.double() / want), "clipped")
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("tokens", [1, 40])
+def test_gelu_keeps_its_digits_in_the_tail(tokens, dtype):
+    """a Phi(a) and its derivative one by one, relative to themselves: x is a unit vector, w_down a unit matrix, w_up ones, so that
+    y[h] = gelu(a_h) and dw_gate[h][0] = tokens * gelu'(a_h).
+    Single precision: the argument a / sqrt 2 is off by 1.5 * 2^-24 relative (its factor, the product), which erfc multiplies by
+    x d/dx ln erfc <= a^2 + 2; 16 * 2^-24 for the library's function (a few last digits), 4 for the products; the density's exponent
+    a^2 / 2 log2 e has three roundings and the hardware's 2^x a last digit.  Bfloat16: the handbook's formula with 64 bits shows what it
+    leaves out; roundings on the way as in single precision, and the type's own (da and dw_gate, h and y: two each)."""
+    a = torch.arange(-64 if dtype == "bfloat16" else -88, 65, device="cuda", dtype=torch.float64) / 8
+    n = len(a)
+    unit, low = ref.unit(TYPES[dtype]), TYPES[dtype]
+    spec = GatedSpec(tokens, n, n, "gelu", dtype)
+    x, wg, wu = (torch.zeros(s, device="cuda", dtype=torch.float64) for s in ((tokens, n), (n, n), (n, n)))
+    x[:, 0], wg[:, 0], wu[:, 0] = 1, a, 1
+    i = dict(x=x.to(low), w_gate=wg.to(low), w_up=wu.to(low), w_down=torch.eye(n, device="cuda", dtype=low))
+    assert torch.equal(i["w_gate"][:, 0].double(), a)
+    got = block(spec, i, torch.ones(tokens, n, device="cuda", dtype=low), 255)
+    cdf, pdf = 0.5 * torch.special.erfc(-a * math.sqrt(0.5)), torch.exp(-a * a / 2) / math.sqrt(2 * math.pi)
+    ecdf = (1.5 * (a * a + 2) + 20) * U32 * cdf
+    if dtype == "bfloat16":
+        t = 1 / (1 + 0.3275911 * a.abs() * math.sqrt(0.5))
+        half = 0.5 * t * (0.254829592 + t * (-0.284496736 + t * (1.421413741 + t * (-1.453152027 + t * 1.061405429)))) * torch.exp(-a * a / 2)
+        form = torch.where(a < 0, half, 1 - half)
+        ecdf = (form - cdf).abs() + (1.5 * (a * a + 2) + 40) * U32 * (half + (a > 0))   # the polynomial's terms are up to 6 times its value
+    f, d = a * cdf, cdf + a * pdf
+    ef = a.abs() * ecdf + U32 * f.abs()
+    ed = ecdf + (2 * a * a + 20) * U32 * a.abs() * pdf + U32 * d.abs()
+    roundings = 2 * unit if dtype == "bfloat16" else 2 * U32
+    for row in got["y"]:
+        ref.check(row, (f, ef + roundings * f.abs() * 1.01), "y")
+    ref.check(got["dw_gate"][:, 0], (tokens * d, tokens * (ed + (roundings * 1.01 + ref.gamma(tokens)) * d.abs())), "dw_gate")
