@@ -177,16 +177,15 @@ struct GateBackEpi : NothingAhead {
   }
 };
 
-template <class T>
-__global__ __launch_bounds__(256) void pad_rows_kernel(const T *src, T *dst, int rows, int cols, long ld) {
+__global__ __launch_bounds__(256) void pad_rows_kernel(const bf16 *src, bf16 *dst, int rows, int cols, long ld) {
   const int c0 = blockIdx.x * 512 + (threadIdx.x & 63);
   for (long r = blockIdx.y * 4 + (threadIdx.x >> 6); r < rows; r += gridDim.y * 4) {
-    T v[8];
+    bf16 v[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = src[r * cols + min(c0 + 64 * j, cols - 1)];   // all on their way before the first is stored
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      if (c0 + 64 * j < ld) dst[r * ld + c0 + 64 * j] = c0 + 64 * j < cols ? v[j] : (T)0.0f;
+      if (c0 + 64 * j < ld) dst[r * ld + c0 + 64 * j] = c0 + 64 * j < cols ? v[j] : (bf16)0.0f;
   }
 }
 
@@ -223,8 +222,8 @@ struct FwdPlan {
     }
     if (!loadable(D, dtype)) x = take((size_t)T * ldd * e), wg = take((size_t)H * ldd * e), wu = take((size_t)H * ldd * e);
     if (!loadable(H, dtype)) wd = take((size_t)D * ldh * e);
-    up = plan_product(dtype, T, H, slabs_of(D, dtype), 1, true, false);
-    down = plan_product(dtype, T, D, slabs_of(H, dtype), 1, false, true);
+    up = plan_product(dtype, T, H, slabs_of(D, dtype), true, false);
+    down = plan_product(dtype, T, D, slabs_of(H, dtype), false, true);
     part = (float *)take(partial_bytes(down.splits, T, D));
     bytes = take.used;
   }
@@ -247,7 +246,7 @@ struct BwdPlan {
     x = wg = wu = wd = dy = nullptr;
     if (!loadable(D, dtype)) x = take((size_t)T * ldd * e), dy = take((size_t)T * ldd * e), wg = take((size_t)H * ldd * e), wu = take((size_t)H * ldd * e);
     if (!loadable(H, dtype)) wd = take((size_t)D * ldh * e);
-    dh = plan_product(dtype, T, H, slabs_of(D, dtype), 1, false, false);
+    dh = plan_product(dtype, T, H, slabs_of(D, dtype), false, false);
     const long tokens = slabs_of(T, dtype);
     const GradientShape shape[3] = {{T, D, 2 * slabs_of(H, dtype), 1, true}, {H, D, tokens, 2, false}, {D, H, tokens, 1, false}};
     gradients = plan_gradients(dtype, shape, 3);
@@ -276,13 +275,13 @@ hipError_t gated_fwd(const GatedArgs &a, char *scratch, hipStream_t stream) {
   }
   const void *x = a.x, *wg = a.w_gate, *wu = a.w_up, *wd = a.w_down;
   if (p.x) {
-    DLL_TRY(launch_pad_rows(x, p.x, a.T, a.D, a.dtype, stream));
-    DLL_TRY(launch_pad_rows(wg, p.wg, a.H, a.D, a.dtype, stream));
-    DLL_TRY(launch_pad_rows(wu, p.wu, a.H, a.D, a.dtype, stream));
+    DLL_TRY(launch_pad_rows(x, p.x, a.T, a.D, stream));
+    DLL_TRY(launch_pad_rows(wg, p.wg, a.H, a.D, stream));
+    DLL_TRY(launch_pad_rows(wu, p.wu, a.H, a.D, stream));
     x = p.x, wg = p.wg, wu = p.wu;
   }
   if (p.wd) {
-    DLL_TRY(launch_pad_rows(wd, p.wd, a.D, a.H, a.dtype, stream));
+    DLL_TRY(launch_pad_rows(wd, p.wd, a.D, a.H, stream));
     wd = p.wd;
   }
   const long ldx = p.x ? p.ldd : a.D, ldd = p.wd ? p.ldh : a.H;
@@ -310,18 +309,18 @@ hipError_t gated_bwd(const GatedArgs &a, char *scratch, hipStream_t stream) {
   const BwdPlan p(a.T, a.D, a.H, a.dtype, scratch);
   const void *x = a.x, *wg = a.w_gate, *wu = a.w_up, *wd = a.w_down, *dy = a.dy;
   if (p.x) {
-    DLL_TRY(launch_pad_rows(dy, p.dy, a.T, a.D, a.dtype, stream));
+    DLL_TRY(launch_pad_rows(dy, p.dy, a.T, a.D, stream));
     dy = p.dy;
-    if (a.dw_gate || a.dw_up) DLL_TRY(launch_pad_rows(x, p.x, a.T, a.D, a.dtype, stream));
+    if (a.dw_gate || a.dw_up) DLL_TRY(launch_pad_rows(x, p.x, a.T, a.D, stream));
     x = p.x;
     if (a.dx) {
-      DLL_TRY(launch_pad_rows(wg, p.wg, a.H, a.D, a.dtype, stream));
-      DLL_TRY(launch_pad_rows(wu, p.wu, a.H, a.D, a.dtype, stream));
+      DLL_TRY(launch_pad_rows(wg, p.wg, a.H, a.D, stream));
+      DLL_TRY(launch_pad_rows(wu, p.wu, a.H, a.D, stream));
       wg = p.wg, wu = p.wu;
     }
   }
   if (p.wd) {
-    DLL_TRY(launch_pad_rows(wd, p.wd, a.D, a.H, a.dtype, stream));
+    DLL_TRY(launch_pad_rows(wd, p.wd, a.D, a.H, stream));
     wd = p.wd;
   }
   const long ldx = p.x ? p.ldd : a.D, ldd = p.wd ? p.ldh : a.H;
@@ -377,11 +376,10 @@ hipError_t gated_bwd(const GatedArgs &a, char *scratch, hipStream_t stream) {
 
 }  // namespace
 
-hipError_t launch_pad_rows(const void *src, void *dst, long rows, long cols, int dtype, hipStream_t stream) {
+hipError_t launch_pad_rows(const void *src, void *dst, long rows, long cols, hipStream_t stream) {
   const long ld = padded(cols), fours = (rows + 3) / 4;
   const dim3 grid((unsigned)((ld + 511) / 512), (unsigned)(fours < 32768 ? fours : 32768));
-  if (dtype == TYPE_BF16) pad_rows_kernel<bf16><<<grid, dim3(256), 0, stream>>>((const bf16 *)src, (bf16 *)dst, (int)rows, (int)cols, ld);
-  else pad_rows_kernel<float><<<grid, dim3(256), 0, stream>>>((const float *)src, (float *)dst, (int)rows, (int)cols, ld);
+  pad_rows_kernel<<<grid, dim3(256), 0, stream>>>((const bf16 *)src, (bf16 *)dst, (int)rows, (int)cols, ld);
   return hipGetLastError();
 }
 

@@ -60,7 +60,7 @@ hipError_t launch_momentum_clipped(const GradList &l, float *const *params, floa
                                    float lr, float mu, float max_norm, float *norm, void *const *copies, char *scratch, hipStream_t stream);
 
 // ---- shared: rows copied into padded rows -------------------------------------------------------------------------------
-// dst [rows][padded(cols)] = src [rows][cols], zeros behind
-hipError_t launch_pad_rows(const void *src, void *dst, long rows, long cols, int dtype, hipStream_t stream);
+// dst [rows][padded(cols)] = src [rows][cols], zeros behind; bfloat16, as single precision's rows are loadable whatever their length
+hipError_t launch_pad_rows(const void *src, void *dst, long rows, long cols, hipStream_t stream);
 
 }  // namespace dllk

@@ -616,7 +616,7 @@ struct StoreEpi : NothingAhead {
       stage8(stage, row, col, v);
       T *d = c[problem] + (long)(rows ? rows[m + row] : m + row) * ld + n + col;
       const int left = N - n - col;
-      if (add) {
+      if (sizeof(T) == 4 && add) {
         float o[8];
         load8<T>(d, o, left);
 #pragma unroll
@@ -648,7 +648,8 @@ struct PartialEpi : NothingAhead {
   }
 };
 
-// The splits added up in order, as a StoreEpi of one problem would have stored them
+// The splits added up in order, as a StoreEpi of one problem would have stored them (products that add to a former piece's have no
+// split k)
 template <class T>
 __global__ __launch_bounds__(256) void sum_splits_kernel(const float *part, int splits, int M, int N, const int *m_rows, int first, StoreEpi<T> out) {
   const long n8 = (N + 7) & ~7;
@@ -663,15 +664,7 @@ __global__ __launch_bounds__(256) void sum_splits_kernel(const float *part, int 
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] += o[j];
     }
-    T *d = out.c[0] + (long)(out.rows ? out.rows[m] : m) * out.ld + n;
-    const int left = N - n;
-    if (out.add) {
-      float o[8];
-      load8<T>(d, o, left);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] += o[j];
-    }
-    store8<T>(d, v, left);
+    store8<T>(out.c[0] + (long)(out.rows ? out.rows[m] : m) * out.ld + n, v, N - n);
   }
 }
 
@@ -699,13 +692,13 @@ constexpr TilingCost kTilings[TILINGS] = {
 
 // The tiling and the number of parts of k with the least estimated time.  Parts of k cost their sums' way to memory and back and
 // a second launch.
-inline ProductPlan plan_product(int dtype, int M, int N, long slabs, int problems, bool pair, bool may_split) {
+inline ProductPlan plan_product(int dtype, int M, int N, long slabs, bool pair, bool may_split) {
   ProductPlan best;
   double least = 1e30;
   const int type = dtype == TYPE_BF16 ? 1 : 0, cus = chip().cus;
   for (int i = type ? TILE_256 : TILE_128; i < TILINGS; ++i) {
     const TilingCost &c = kTilings[i];
-    const long nn = pair ? 2L * N : N, tiles = (long)((M + c.bm - 1) / c.bm) * ((nn + c.bn - 1) / c.bn) * problems;
+    const long nn = pair ? 2L * N : N, tiles = (long)((M + c.bm - 1) / c.bm) * ((nn + c.bn - 1) / c.bn);
     for (int s = 1; s <= (may_split ? 32 : 1); s *= 2) {
       if (s > 1 && (slabs < 4L * s || tiles * s > 4L * cus * c.resident)) break;
       const long each = ((slabs + s - 1) / s + c.groups - 1) / c.groups, n = (tiles * s + cus - 1) / cus, full = n / c.resident, rest = n % c.resident;
@@ -751,7 +744,6 @@ hipError_t launch_tiling(ProductArgs a, const Epi &epi, hipStream_t stream) {
 
 template <class T, bool AKC, bool BKC, bool PAIR, class Epi>
 hipError_t launch_product(const ProductArgs &a, const Epi &epi, int tiling, hipStream_t stream) {
-  if (a.M <= 0 || a.N <= 0) return hipSuccess;
   switch (tiling) {
     case TILE_256:
       if constexpr (sizeof(T) == 2) return launch_tiling<T, 256, 256, 2, 4, 1, 2, AKC, BKC, PAIR, Epi>(a, epi, stream);
@@ -787,7 +779,7 @@ inline size_t partial_bytes(int splits, int M, int N) { return splits > 1 ? (siz
 template <class T, bool AKC, bool BKC>
 hipError_t product_to(ProductArgs p, StoreEpi<T> out, const ProductPlan &plan, float *part, hipStream_t stream) {
   if (plan.splits <= 1) return launch_product<T, AKC, BKC, false>(p, out, plan.tiling, stream);
-  const int slab = Elem<T>::kSlab, slabs = (p.K[0] + slab - 1) / slab + (p.K[1] + slab - 1) / slab;
+  const int slabs = (p.K[0] + Elem<T>::kSlab - 1) / Elem<T>::kSlab;   // one segment
   p.slabs_per_split = (slabs + plan.splits - 1) / plan.splits;
   p.splits = plan.splits;
   hipError_t e = launch_product<T, AKC, BKC, false>(p, PartialEpi(part, p.M), plan.tiling, stream);

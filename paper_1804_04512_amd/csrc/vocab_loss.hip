@@ -440,7 +440,7 @@ struct Plan {
     if (most > (1u << 20)) most = 1u << 20;   // 64 rows a workgroup along the grid's second axis
     piece = (size_t)T < most ? T : (int)most;
     pieces = (T + piece - 1) / piece;
-    z = plan_product(dtype, piece, V, slabs_of(D, dtype), 1, false, false);
+    z = plan_product(dtype, piece, V, slabs_of(D, dtype), false, false);
     group = !grad && skinny(T, D, dtype) ? 2 * kSkinnyColumns : piece_columns(z.tiling);
     groups = (V + group - 1) / group;
     const size_t slab_rows = (size_t)(piece + 63) / 64 * 64;
@@ -473,7 +473,7 @@ hipError_t begin(const VocabArgs &a, const Plan &p, const void **w, long *ldw, h
   *w = a.w;
   *ldw = a.D;
   if (p.w) {
-    DLL_TRY(launch_pad_rows(a.w, p.w, a.V, a.D, a.dtype, stream));
+    DLL_TRY(launch_pad_rows(a.w, p.w, a.V, a.D, stream));
     *w = p.w;
     *ldw = p.ldd;
   }
@@ -526,8 +526,8 @@ hipError_t few_rows_fwd(const VocabArgs &a, const Plan &p, hipStream_t stream) {
     return hipGetLastError();
   }
   if (p.w) {
-    DLL_TRY(launch_pad_rows(a.x, p.x, a.T, a.D, a.dtype, stream));
-    DLL_TRY(launch_pad_rows(a.w, p.w, a.V, a.D, a.dtype, stream));
+    DLL_TRY(launch_pad_rows(a.x, p.x, a.T, a.D, stream));
+    DLL_TRY(launch_pad_rows(a.w, p.w, a.V, a.D, stream));
     x = p.x;
     w = p.w;
   }
