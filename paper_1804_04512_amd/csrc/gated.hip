@@ -266,12 +266,12 @@ hipError_t gated_fwd(const GatedArgs &a, char *scratch, hipStream_t stream) {
     s.x = a.x;
     s.w[0] = a.w_gate;
     s.w[1] = a.w_up;
-    DLL_TRY((launch_skinny<T, 2, true>(s, SkinnyGate<T>{a.gate, (T *)p.h, (T *)a.gate_pre, (T *)a.up_pre}, stream)));
+    DLL_TRY((launch_skinny<T, 2, true, kSkinnyRows>(s, SkinnyGate<T>{a.gate, (T *)p.h, (T *)a.gate_pre, (T *)a.up_pre}, stream)));
     s.N = a.D;
     s.K = a.H;
     s.x = p.h;
     s.w[0] = a.w_down;
-    return launch_skinny<T, 1, false>(s, SkinnyStore<T>{(T *)a.y}, stream);
+    return launch_skinny<T, 1, false, kSkinnyRows>(s, SkinnyStore<T>{(T *)a.y}, stream);
   }
   const void *x = a.x, *wg = a.w_gate, *wu = a.w_up, *wd = a.w_down;
   if (p.x) {

@@ -153,14 +153,17 @@ hipError_t launch_skinny_tokens(const SkinnyArgs &a, const Epi &epi, unsigned bl
   else skinny_kernel<T, TOKENS, R, PAIR, 8, Epi><<<dim3(blocks, tiles), dim3(512), 0, stream>>>(a, epi);
   return hipGetLastError();
 }
-template <class T, int R, bool PAIR, class Epi>
+// MOST: rows at most that the caller sends here
+template <class T, int R, bool PAIR, int MOST, class Epi>
 hipError_t launch_skinny(const SkinnyArgs &a, const Epi &epi, hipStream_t stream) {
   // The second sixteen tokens share their weights' loads, or take workgroups of their own where the columns leave half the compute
   // units empty (24 x 784 x 500 in single precision: 15.3 us shared, 11.6 apart; 24 x 1000 x 2730 bf16: 11.7 against 13.2).
   constexpr int kEach = PAIR ? kSkinnyColumns : R * kSkinnyColumns;
   const unsigned blocks = (unsigned)((a.N + kEach - 1) / kEach);
-  return a.M <= 16 || 2 * (int)blocks <= chip().cus ? launch_skinny_tokens<T, 1, R, PAIR>(a, epi, blocks, stream)
-                                                    : launch_skinny_tokens<T, 2, R, PAIR>(a, epi, blocks, stream);
+  if constexpr (MOST > 16) {
+    if (a.M > 16 && 2 * (int)blocks > chip().cus) return launch_skinny_tokens<T, 2, R, PAIR>(a, epi, blocks, stream);
+  }
+  return launch_skinny_tokens<T, 1, R, PAIR>(a, epi, blocks, stream);
 }
 
 // four neighbours of a row

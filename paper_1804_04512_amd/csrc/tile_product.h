@@ -697,6 +697,7 @@ inline ProductPlan plan_product(int dtype, int M, int N, long slabs, bool pair, 
   double least = 1e30;
   const int type = dtype == TYPE_BF16 ? 1 : 0, cus = chip().cus;
   for (int i = type ? TILE_256 : TILE_128; i < TILINGS; ++i) {
+    if (i == TILE_64_K2_DEEP && !type) continue;   // as long as with two slabs for a lone workgroup, longer with two a unit
     const TilingCost &c = kTilings[i];
     const long nn = pair ? 2L * N : N, tiles = (long)((M + c.bm - 1) / c.bm) * ((nn + c.bn - 1) / c.bn);
     for (int s = 1; s <= (may_split ? 32 : 1); s *= 2) {
@@ -751,7 +752,9 @@ hipError_t launch_product(const ProductArgs &a, const Epi &epi, int tiling, hipS
     case TILE_128: return launch_tiling<T, 128, 128, 2, 2, 1, 2, AKC, BKC, PAIR, Epi>(a, epi, stream);
     case TILE_128_DEEP: return launch_tiling<T, 128, 128, 2, 2, 1, 4, AKC, BKC, PAIR, Epi>(a, epi, stream);
     case TILE_64_K2: return launch_tiling<T, 64, 64, 2, 1, 2, 2, AKC, BKC, PAIR, Epi>(a, epi, stream);
-    case TILE_64_K2_DEEP: return launch_tiling<T, 64, 64, 2, 1, 2, 4, AKC, BKC, PAIR, Epi>(a, epi, stream);
+    case TILE_64_K2_DEEP:
+      if constexpr (sizeof(T) == 2) return launch_tiling<T, 64, 64, 2, 1, 2, 4, AKC, BKC, PAIR, Epi>(a, epi, stream);
+      [[fallthrough]];   // nor this one
     case TILE_32_K4: return launch_tiling<T, 32, 64, 1, 1, 4, 3, AKC, BKC, PAIR, Epi>(a, epi, stream);
     default: return launch_tiling<T, 32, 32, 1, 1, 8, 2, AKC, BKC, PAIR, Epi>(a, epi, stream);
   }

@@ -408,9 +408,8 @@ __global__ __launch_bounds__(256) void sum_columns_kernel(const float *sums, lon
   else acc[v] = s;
 }
 
-template <class T>
-__global__ __launch_bounds__(256) void convert_kernel(const float *src, T *dst, long n) {
-  for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) dst[i] = (T)src[i];
+__global__ __launch_bounds__(256) void convert_kernel(const float *src, bf16 *dst, long n) {
+  for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) dst[i] = (bf16)src[i];
 }
 
 // Up to 16 tokens: weights in rows that are no whole 16-byte groups (16 x 1001 x 5000: 12.8 us against the tiles' 21.4 in bfloat16, whose
@@ -520,7 +519,7 @@ hipError_t few_rows_fwd(const VocabArgs &a, const Plan &p, hipStream_t stream) {
     s.K = a.D;
     s.x = x;
     s.w[0] = w;
-    DLL_TRY((launch_skinny<T, 2, false>(s, SkinnyLogits<T>{(const T *)a.bias, a.labels, p.stats, p.piece, p.hit}, stream)));
+    DLL_TRY((launch_skinny<T, 2, false, sizeof(T) == 4 ? 16 : kSkinnyRows>(s, SkinnyLogits<T>{(const T *)a.bias, a.labels, p.stats, p.piece, p.hit}, stream)));
     join_groups_kernel<<<dim3(1), dim3(1024), 0, stream>>>(p.stats, p.groups, p.piece, p.hit, a.T, nullptr, 0, nullptr, nullptr, nullptr, a.row_loss, a.row_lse,
                                                                a.labels, a.V, a.loss);
     return hipGetLastError();
@@ -599,13 +598,15 @@ hipError_t vocab_grad(const VocabArgs &a, char *scratch, hipStream_t stream) {
     g.first = first;
     if (a.dw && !p.dw_sum) jobs.add(g, StoreEpi<T>((T *)a.dw, nullptr, a.D, nullptr, first > 0), false);
     DLL_TRY(launch_gradients<T>(jobs, stream));
-    if (a.dw && p.dw_sum) {   // pieces of bfloat16 products add up in 32 bits
-      const StoreEpi<float> out(p.dw_sum, nullptr, a.D, nullptr, first > 0);
-      DLL_TRY((launch_product<T, false, false, false>(g, out, p.gradients.tiling, stream)));
-      if (last) {
-        const long n = (long)a.V * a.D, blocks = (n + 255) / 256;
-        convert_kernel<T><<<dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, stream>>>(p.dw_sum, (T *)a.dw, n);
-        DLL_TRY(hipGetLastError());
+    if constexpr (sizeof(T) == 2) {   // pieces of bfloat16 products add up in 32 bits; single precision's in dw itself
+      if (a.dw && p.dw_sum) {
+        const StoreEpi<float> out(p.dw_sum, nullptr, a.D, nullptr, first > 0);
+        DLL_TRY((launch_product<T, false, false, false>(g, out, p.gradients.tiling, stream)));
+        if (last) {
+          const long n = (long)a.V * a.D, blocks = (n + 255) / 256;
+          convert_kernel<<<dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, stream>>>(p.dw_sum, (bf16 *)a.dw, n);
+          DLL_TRY(hipGetLastError());
+        }
       }
     }
   }

@@ -34,9 +34,20 @@ class _Pointers:
 def _make(B, L, what, *args):
     """One call by name: 'fwd' / 'bwd' / 'wgrad' / 'fft' / 'fft_less' / 'crbm' (ConvSpec fields), 'rbm' (batch, n_vis, n_hid),
     'infer' / 'train' (conv layers, dense layers, classes, batch); 'rbm_in_place' writes v1 over h0_sample_in,
-    'infer_in_place' the probabilities over x; 'norm' / 'clip' / 'step' (numbers of elements of a list of fp32 gradients)."""
-    from paper_1804_04512_amd.workloads import ConvSpec, DenseSpec
+    'infer_in_place' the probabilities over x; 'norm' / 'clip' / 'step' (numbers of elements of a list of fp32 gradients);
+    'gated_fwd' / 'gated_bwd' (GatedSpec fields), 'loss_fwd' / 'loss_grad' (VocabSpec fields)."""
+    from paper_1804_04512_amd.workloads import ConvSpec, DenseSpec, GatedSpec, VocabSpec
     p, ws = _Pointers(), C.c_void_p(1 << 20)
+    if what in ("gated_fwd", "gated_bwd"):
+        d = C.byref(B.gated_desc(GatedSpec(*args)))
+        if what == "gated_fwd":
+            return L.dll_gated_fwd(d, *[p() for _ in range(7)], ws, WORKSPACE, None)
+        return L.dll_gated_bwd(d, *[p() for _ in range(11)], ws, WORKSPACE, None)
+    if what in ("loss_fwd", "loss_grad"):
+        d = C.byref(B.vocab_desc(VocabSpec(*args)))
+        if what == "loss_fwd":
+            return L.dll_vocab_loss_fwd(d, *[p() for _ in range(7)], ws, WORKSPACE, None)
+        return L.dll_vocab_loss_grad(d, *[p() for _ in range(4)], 1.0, *[p() for _ in range(6)], ws, WORKSPACE, None)
     if what in ("norm", "clip", "step"):
         n = len(args[0])
         l = C.byref(B.dll_tensor_list(n, (C.c_size_t * n)(*args[0]), (C.c_int * n)(*[0] * n)))
