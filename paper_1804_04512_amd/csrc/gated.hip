@@ -189,16 +189,20 @@ __global__ __launch_bounds__(256) void pad_rows_kernel(const bf16 *src, bf16 *ds
   }
 }
 
-// A few tokens: the weights straight from memory, up to 16 where the second product's rows of H are at most 16 KB, as one compute
-// unit reads sixteen of them (one token, 2048 x 8192 bf16: 25.6 us against 30 on tiles with k in parts; 16 tokens, 2048 x 16000: 58
-// against 40, 512 x 8000 in single precision 40 against 25), or where the tiles would have rows of odd bfloat16 length copied first.
-// Up to 32 where the weights are small as well (24 x 1000 x 2730 bf16: 11.7 against 17), as the tokens are read by every workgroup
-// (24 x 2048 x 8192: 39 against 28; 24 x 2047 x 8191, copied first: 115 against 69).
+// A few tokens: the weights straight from memory, or tiles with k in parts.  Straight from memory y has a workgroup for 16 of its D
+// columns, which reads 16 rows of Wd and every token's h: with long rows of H and few columns some compute units read much and
+// the others nothing, and each token adds a row (of h in single precision two rows' time).  With many columns all units read.  The
+// constants leave least time over 1386 measured calls of 1 to 32 tokens, widths of 63 to 8192 and 256 to 22016 hidden units with weights
+// from memory, odd sizes too (rows of odd bfloat16 length are copied before the tiles): against the faster of both 1.1 % on
+// average in bfloat16 and 1.3 % in single precision, 29 % at most.  Microseconds, straight / tiles:
+//   1 x 2048 x 8192 27.4 / 30.1, x 11008 37.3 / 39.8, x 14336 45.3 / 44.1; fp32 51.0 / 53.8, 69.6 / 84.7, 86.4 / 88.3
+//   4 x 2048 x 8192 28.5 / 30.0, x 11008 39.1 / 40.0, x 14336 47.9 / 44.3; fp32 53.2 / 54.4, 73.2 / 85.0, 90.7 / 88.7
+//   16 x 2048 x 8192 33.3 / 30.7, x 4096 18.9 / 23.7; fp32 64.0 / 54.9, 34.8 / 36.9; 16 x 4096 x 8192 47.4 / 48.2; fp32 93.3 / 95.4
+//   16 x 63 x 22015 146 / 37; 1 x 512 x 14336 26.5 / 22.4; 32 x 2048 x 8192 37.2 / 32.7; 24 x 1000 x 2730 14.5 / 21.8
 bool skinny(int T, int D, int H, int dtype) {
   if (T > kSkinnyRows || D < kSkinnyLeastK || H < kSkinnyLeastK) return false;
-  const bool short_rows = (size_t)H * type_bytes(dtype) <= 16384;
-  if (T <= 16) return short_rows || !loadable(D, dtype) || !loadable(H, dtype);
-  return short_rows && (long)D * H <= (1L << 22);
+  const long row = (long)H * (long)type_bytes(dtype), columns = D < 4096 ? D : 4096;
+  return dtype == TYPE_BF16 ? (16 + T) * row <= 192 * (columns > 1536 ? columns : 1536) : (8 + T) * row <= 288 * (columns > 640 ? columns : 640);
 }
 
 // The workspace's parts, the same walk for the query and the call

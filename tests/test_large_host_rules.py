@@ -55,3 +55,18 @@ def test_labels_losses_and_norms_lie_at_their_elements():
         norm = at(5, off)
         assert L.dll_grad_norm(l, one(0), norm, ws, 0, None) == L.dll_grad_clip(l, one(0), one(1), 1.0, norm, ws, 0, None) == status
         assert L.dll_momentum_update_clipped(l, one(1), one(2), one(0), 0.1, 0.9, None, 1.0, norm, None, ws, 0, None) == status
+
+
+# tokens, width, hidden units, type, whether the weights go straight from memory: either side of the line, where the other way was
+# measured slower
+FEW = [(1, 2048, 8192, "bfloat16", True), (1, 2048, 11008, "bfloat16", True), (1, 512, 14336, "bfloat16", False), (16, 2048, 4096, "bfloat16", True),
+       (16, 2048, 8192, "bfloat16", False), (16, 63, 22015, "bfloat16", False), (1, 4095, 22015, "bfloat16", True), (4, 255, 8191, "bfloat16", False),
+       (24, 1000, 2730, "bfloat16", True), (24, 2047, 8191, "bfloat16", False), (32, 2048, 2730, "bfloat16", True), (33, 1000, 2730, "bfloat16", False),
+       (1, 2048, 8192, "float32", True), (1, 2048, 11008, "float32", True), (1, 512, 8192, "float32", False), (16, 4096, 8192, "float32", True), (16, 2048, 8192, "float32", False),
+       (4, 4096, 14336, "float32", True), (16, 64, 4096, "float32", False), (24, 784, 500, "float32", True), (1, 7, 100, "float32", False)]
+
+
+def test_blocks_of_few_tokens_take_the_faster_way(tmp_path):
+    calls = [["gated_fwd", T, D, H, "silu", dtype] for T, D, H, dtype, _ in FEW]
+    for call, case, (status, launches) in zip(calls, FEW, record(calls, tmp_path)):
+        assert status == 0 and ("skinny_kernel" in launches[0][0]) == case[-1], (call, launches)
