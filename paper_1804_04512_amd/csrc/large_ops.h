@@ -13,9 +13,8 @@ inline size_t type_bytes(int dtype) { return dtype == TYPE_BF16 ? 2 : 4; }
 // Elements of a row that is kept in the workspace: whole 128-byte lines (of either type), so that no slab's row takes two.
 inline long padded(long n) { return (n + 63) & ~63L; }
 // Rows of n elements that a product can load as they are (they start at multiples of four bytes); others are copied into padded rows
-// first.  And rows that are whole 16-byte groups.
+// first.
 inline bool loadable(long n, int dtype) { return n * (long)type_bytes(dtype) % 4 == 0; }
-inline bool whole_groups(long n, int dtype) { return n * (long)type_bytes(dtype) % 16 == 0; }
 
 // ---- gated feed-forward block -------------------------------------------------------------------------------------
 struct GatedArgs {

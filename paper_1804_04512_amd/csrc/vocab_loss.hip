@@ -412,11 +412,20 @@ __global__ __launch_bounds__(256) void convert_kernel(const float *src, bf16 *ds
   for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) dst[i] = (bf16)src[i];
 }
 
-// Up to 16 tokens: weights in rows that are no whole 16-byte groups (16 x 1001 x 5000: 12.8 us against the tiles' 21.4 in bfloat16, whose
-// odd rows the tiles have copied first, 12.5 against 16.2 in single precision; 16 x 1002 x 5000 in bfloat16: 8.7 against 11.0; in whole
-// groups either way takes as long, and the tiles' leaves half as many groups to join).  Up to 32 only odd rows in bfloat16 (32 x 1001 x
-// 32000: 45.9 against 48.1; in single precision 57.3 against the tiles' 43.8, and 32 x 1002 x 32000 in bfloat16 25.7 against 22.1).
-bool skinny(int T, int D, int dtype) { return D >= kSkinnyLeastK && (T <= 16 ? !whole_groups(D, dtype) : T <= kSkinnyRows && !loadable(D, dtype)); }
+// A few tokens straight from memory, where a workgroup reads every token for its 32 classes: up to 16, or 32 where the tiles would have
+// rows of odd bfloat16 length copied first, as long as the tokens' rows are not too long.  Odd rows are read twice as slowly, and
+// with few classes their copies cost little.  The constants leave least time over 1057 measured calls of 1 to 32 tokens, widths of 64 to
+// 16001 and 500 to 100000 classes with weights from memory: against the faster way 2.1 % on average, 31 % at most, with odd rows 3.0 %
+// (32 x 255 x 100000 is 74 % off).  Microseconds, straight / tiles:
+//   1 x 1024 x 5000 9.8 / 11.6, x 100000 49.6 / 59.3; fp32 12.8 / 16.4, 83.5 / 112.8; 16 x 1024 x 32000 21.0 / 22.3; fp32 36.1 / 42.1
+//   16 x 4098 x 32000 78.6 / 75.0; fp32 149.6 / 118.4; 1 x 8192 x 100000 354.8 / 289.2; 4 x 2048 x 12000 19.2 / 18.6
+//   odd: 16 x 1001 x 32000 34.5 / 49.9; 32 x 513 x 8000 18.4 / 26.5; 16 x 16001 x 500 151.7 / 50.7; 32 x 4095 x 32000 217 / 163
+bool skinny(int T, int D, int V, int dtype) {
+  const bool odd = !loadable(D, dtype);
+  if (D < kSkinnyLeastK || T > (odd ? kSkinnyRows : 16)) return false;
+  const long classes = !odd || V > 8192 ? 8192 : V < 1024 ? 1024 : V;
+  return (4 + T) * (long)D * (long)type_bytes(dtype) <= 24 * classes;
+}
 
 struct Plan {
   long ldd, lde;
@@ -440,7 +449,7 @@ struct Plan {
     piece = (size_t)T < most ? T : (int)most;
     pieces = (T + piece - 1) / piece;
     z = plan_product(dtype, piece, V, slabs_of(D, dtype), false, false);
-    group = !grad && skinny(T, D, dtype) ? 2 * kSkinnyColumns : piece_columns(z.tiling);
+    group = !grad && skinny(T, D, V, dtype) ? 2 * kSkinnyColumns : piece_columns(z.tiling);
     groups = (V + group - 1) / group;
     const size_t slab_rows = (size_t)(piece + 63) / 64 * 64;
     count = (int *)take(sizeof(int));
@@ -512,7 +521,7 @@ hipError_t logits(const VocabArgs &a, const Plan &p, int first, const void *w, l
 template <class T>
 hipError_t few_rows_fwd(const VocabArgs &a, const Plan &p, hipStream_t stream) {
   const void *x = a.x, *w = a.w;
-  if (skinny(a.T, a.D, a.dtype)) {
+  if (skinny(a.T, a.D, a.V, a.dtype)) {
     SkinnyArgs s;
     s.M = a.T;
     s.N = a.V;

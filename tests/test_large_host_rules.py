@@ -70,3 +70,16 @@ def test_blocks_of_few_tokens_take_the_faster_way(tmp_path):
     calls = [["gated_fwd", T, D, H, "silu", dtype] for T, D, H, dtype, _ in FEW]
     for call, case, (status, launches) in zip(calls, FEW, record(calls, tmp_path)):
         assert status == 0 and ("skinny_kernel" in launches[0][0]) == case[-1], (call, launches)
+
+
+# tokens, width, classes, type, whether the weights go straight from memory
+SCORED = [(1, 1024, 5000, "bfloat16", True), (16, 1024, 32000, "bfloat16", True), (17, 1024, 32000, "bfloat16", False), (1, 1024, 100000, "float32", True),
+          (16, 4098, 32000, "bfloat16", True), (16, 4098, 32000, "float32", False), (1, 8192, 100000, "bfloat16", True), (16, 8194, 500, "bfloat16", False),
+          (4, 8191, 5000, "float32", False), (16, 1001, 32000, "bfloat16", True), (32, 513, 8000, "bfloat16", True), (16, 16001, 500, "bfloat16", False),
+          (32, 4095, 32000, "bfloat16", False), (1, 4095, 500, "bfloat16", False), (1, 4095, 32000, "bfloat16", True), (3, 7, 50, "bfloat16", False)]
+
+
+def test_losses_of_few_tokens_take_the_faster_way(tmp_path):
+    calls = [["loss_fwd", T, D, V, dtype] for T, D, V, dtype, _ in SCORED]
+    for call, case, (status, launches) in zip(calls, SCORED, record(calls, tmp_path)):
+        assert status == 0 and ("skinny_kernel" in launches[0][0]) == case[-1], (call, launches)
