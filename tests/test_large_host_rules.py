@@ -1,10 +1,13 @@
 """What the large-model operators settle on the host: which kernels a call launches (launches are noted instead of run: no
 GPU needed)."""
 import ctypes as C
+import math
+import random
 
 from paper_1804_04512_amd import binding as B
 from paper_1804_04512_amd.workloads import VocabSpec
 
+import large_sizes
 from launch_record import record
 
 OK, NULL, SHAPE, UNSUPPORTED, WORKSPACE = 0, 1, 2, 3, 4
@@ -83,3 +86,39 @@ def test_losses_of_few_tokens_take_the_faster_way(tmp_path):
     calls = [["loss_fwd", T, D, V, dtype] for T, D, V, dtype, _ in SCORED]
     for call, case, (status, launches) in zip(calls, SCORED, record(calls, tmp_path)):
         assert status == 0 and ("skinny_kernel" in launches[0][0]) == case[-1], (call, launches)
+
+
+def products(launches):
+    """The product kernels among a call's launches; gradients also by whether their k is split."""
+    names = [l[0] for l in launches]
+    split = any("sum_splits" in n for n in names)
+    return {(n, "gradient_kernel" in n and split) for n in names if n.startswith("_ZN4dllk4tile") and "sum_splits" not in n}
+
+
+def sweep(seed, n):
+    """Calls over the operators' ranges, sizes even over their logarithms, and losses of more exponentials than are kept at a time."""
+    rng = random.Random(seed)
+    spread = lambda low, high: int(round(math.exp(rng.uniform(math.log(low), math.log(high)))))
+    calls = []
+    for _ in range(n):
+        what, dtype = rng.choice(["gated_fwd", "gated_bwd", "loss_fwd", "loss_grad"]), rng.choice(["bfloat16", "float32"])
+        calls.append([what, spread(1, 8192), spread(1, 8192), spread(1, 16384), "silu", dtype] if what.startswith("gated") else
+                     [what, spread(1, 8192), spread(1, 8192), spread(1, 110000), dtype])
+    for _ in range(n // 20):
+        pieces = ((1 << 20) + spread(1, 400000), spread(3, 40), spread(3, 40)) if rng.random() < 0.5 else (spread(257, 1500), spread(8, 40), (1 << 20) - rng.randint(0, 9))
+        calls.append(["loss_grad", *pieces, rng.choice(["bfloat16", "float32"])])
+    return calls
+
+
+def test_every_kernel_that_the_plans_choose_is_tested(tmp_path):
+    """What a sweep of calls launches, the sizes of the GPU tests launch too: a change of the plans' constants that leaves a kernel without
+    a test shows here."""
+    covered = set().union(*[products(launches) for _, launches in record(large_sizes.calls(), tmp_path)])
+    calls = sweep(3, 16000)
+    for call, (status, launches) in zip(calls, record(calls, tmp_path)):
+        assert status == 0
+        assert products(launches) <= covered, (call, products(launches) - covered)
+    largest = {(what, split) for name, split in covered if "Li256ELi256E" in name
+               for what in ("7GateEpi", "11GateBackEpi", "8StoreEpiIDF16b", "10PartialEpi", "Lb0EEE", "Lb1EEE", "gradient_kernel") if what in name}
+    assert {("7GateEpi", False), ("11GateBackEpi", False), ("8StoreEpiIDF16b", False), ("10PartialEpi", False), ("gradient_kernel", False), ("gradient_kernel", True)} <= largest
+    assert sum("LogitEpi" in name and "Li256ELi256E" in name for name, _ in covered) == 2   # with and without the exponentials
