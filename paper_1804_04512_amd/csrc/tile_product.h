@@ -596,24 +596,35 @@ struct NothingAhead {
   __device__ __forceinline__ bool counts(Nothing, int, int, int) const { return true; }
 };
 
-// C[problem][m][n] in T, rows optionally through a map; or += to what a former piece left (fp32 sums)
+// C[problem][m][n] in T, rows optionally through a map, times scale / *count; or += to what a former piece left (fp32 sums)
 template <class T>
 struct StoreEpi : NothingAhead {
-  StoreEpi(T *c0, T *c1, long ld_, const int *rows_, int add_) : c{c0, c1}, ld(ld_), rows(rows_), add(add_) {}
+  StoreEpi(T *c0, T *c1, long ld_, const int *rows_, int add_, const int *count_ = nullptr, float scale_ = 1.0f)
+      : c{c0, c1}, ld(ld_), rows(rows_), add(add_), count(count_), scale(scale_) {}
   T *c[2];
   long ld;
   const int *rows;         // nullable: row m of the product goes to row rows[m]
   int add;                 // T = float only: add to what is there
+  const int *count;        // nullable: no factor
+  float scale;
+  __device__ __forceinline__ float factor() const {   // of no rows: the sums are zeros
+    const int n = *count;
+    return n > 0 ? scale / (float)n : 0.0f;
+  }
   template <int WC>
   __device__ __forceinline__ void piece(const float *stage, int m, int n, int M, int N, int problem, int, int, Nothing) const {
     const Lanes<WC> l;
     const int col = l.col;
+    const float f = count ? factor() : 1.0f;
 #pragma unroll
     for (int p = 0; p < l.kPasses; ++p) {
       const int row = l.kRows * p + l.row;
       if (m + row >= M || n + col >= N) continue;
       float v[8];
       stage8(stage, row, col, v);
+      if (count)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] *= f;
       T *d = c[problem] + (long)(rows ? rows[m + row] : m + row) * ld + n + col;
       const int left = N - n - col;
       if (sizeof(T) == 4 && add) {
@@ -654,6 +665,7 @@ template <class T>
 __global__ __launch_bounds__(256) void sum_splits_kernel(const float *part, int splits, int M, int N, const int *m_rows, int first, StoreEpi<T> out) {
   const long n8 = (N + 7) & ~7;
   const int rows = rows_left(m_rows, first, M), g = (int)(n8 >> 3);
+  const float f = out.count ? out.factor() : 1.0f;
   for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < (long)rows * g; i += (long)gridDim.x * 256) {
     const int m = (int)(i / g), n = (int)(i % g) * 8;
     float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
@@ -664,6 +676,9 @@ __global__ __launch_bounds__(256) void sum_splits_kernel(const float *part, int 
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] += o[j];
     }
+    if (out.count)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] *= f;
     store8<T>(out.c[0] + (long)(out.rows ? out.rows[m] : m) * out.ld + n, v, N - n);
   }
 }

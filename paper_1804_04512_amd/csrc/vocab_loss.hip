@@ -6,10 +6,11 @@
 //
 // The product's epilogue takes each row's maximum m_g and sum of exp(z - m_g) over groups of 64 or 32 columns; one kernel joins
 // the groups to lse.  For the gradients the epilogue also leaves e = exp(z - m_g) in the operands' type, and a second pass
-// turns it in place into dz = e * exp((M - lse) + (m_g - M)) * scale / count (minus the label's share; M the row's maximum, whose
-// distance to lse is kept, as their difference afterwards would have lost it): exponentials in (0, 1] relative
-// to their own group keep all the type's digits, which rounded logits would not (bfloat16 logits of size 10 are 2 % off
-// after exp).  This takes three products of T D V; forming the logits again for the gradients would take four.
+// turns it in place into p - onehot, p = e * exp((M - lse) + (m_g - M)) with the row's maximum M (whose distance to lse is kept, as the
+// difference of the two afterwards would have lost it).  Exponentials in (0, 1] relative to their own group keep all the type's digits,
+// which rounded logits would not (bfloat16 logits of size 10 are 2 % off after exp); e and p - onehot are rounded to the type once
+// each.  scale / count multiplies the products' sums: inside dz its rounding to bfloat16, up to 0.4 %, would be the same for all
+// gradients.  This takes three products of T D V; forming the logits again for the gradients would take four.
 // The exponentials are kept for a piece of the tokens at a time, 1 GiB at most.
 //
 // With gradients the matrix pipe bounds it: 4096 x 2048 x 50257 bf16, 3690 rows counted, 2.40 ms = 950 TFLOP/s (logits 908 us, both
@@ -340,7 +341,7 @@ __device__ __forceinline__ void mean_loss(const float *row, const int *count, fl
 }
 __global__ __launch_bounds__(1024) void mean_loss_kernel(const float *row, const int *count, float *loss) { mean_loss(row, count, loss); }
 
-// dz from the exponentials, in place; a workgroup takes 64 rows x 128 columns and leaves the column sums of its rows.  With the
+// p - onehot from the exponentials, in place; a workgroup takes 64 rows x 128 columns and leaves its rows' column sums of dz.  With the
 // last piece one workgroup more (the last column's) leaves the mean loss.
 template <class T>
 __global__ __launch_bounds__(256) void exp_to_gradient_kernel(T *e, long ld, int V, int M, const int *count, int first, const float2 *stats, long rows_ld,
@@ -352,7 +353,6 @@ __global__ __launch_bounds__(256) void exp_to_gradient_kernel(T *e, long ld, int
     return;
   }
   if (r0 >= n) return;
-  const float share = scale / (float)*count;
   float total[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   if (col < V) {
     float v[4][8];
@@ -367,12 +367,12 @@ __global__ __launch_bounds__(256) void exp_to_gradient_kernel(T *e, long ld, int
       if (row < n) {
         const float m = stats[(long)(col / group) * rows_ld + row].x;
         const float2 l = lse[row];   // lse = l.x + l.y
-        const float f = m == -INFINITY ? 0.0f * (l.x + l.y) : exp_below((m - l.x) - l.y) * share;   // 0 unless the row's sum is not finite
+        const float f = m == -INFINITY ? 0.0f * (l.x + l.y) : exp_below((m - l.x) - l.y);   // 0 unless the row's sum is not finite
         const int at = labels[row] - col;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           v[i][j] *= f;
-          if (j == at) v[i][j] -= share;
+          if (j == at) v[i][j] -= 1.0f;
           total[j] += v[i][j];
         }
       } else {
@@ -390,7 +390,7 @@ __global__ __launch_bounds__(256) void exp_to_gradient_kernel(T *e, long ld, int
     float s = 0.0f;
 #pragma unroll
     for (int w = 0; w < 16; ++w) s += part[w][t];
-    sums[(long)blockIdx.y * ld + blockIdx.x * 128 + t] = s;
+    sums[(long)blockIdx.y * ld + blockIdx.x * 128 + t] = s * (scale / (float)*count);
   }
 }
 
@@ -595,7 +595,7 @@ hipError_t vocab_grad(const VocabArgs &a, char *scratch, hipStream_t stream) {
       g.K[0] = a.V;
       g.m_rows = p.count;
       g.first = first;
-      jobs.add(g, StoreEpi<T>((T *)a.dx, nullptr, a.D, p.rows + first, 0), true);
+      jobs.add(g, StoreEpi<T>((T *)a.dx, nullptr, a.D, p.rows + first, 0, p.count, a.scale), true);
     }
     ProductArgs g;
     g.M = a.V;
@@ -605,11 +605,11 @@ hipError_t vocab_grad(const VocabArgs &a, char *scratch, hipStream_t stream) {
     g.K[0] = M;
     g.k_rows = p.count;
     g.first = first;
-    if (a.dw && !p.dw_sum) jobs.add(g, StoreEpi<T>((T *)a.dw, nullptr, a.D, nullptr, first > 0), false);
+    if (a.dw && !p.dw_sum) jobs.add(g, StoreEpi<T>((T *)a.dw, nullptr, a.D, nullptr, first > 0, p.count, a.scale), false);
     DLL_TRY(launch_gradients<T>(jobs, stream));
     if constexpr (sizeof(T) == 2) {   // pieces of bfloat16 products add up in 32 bits; single precision's in dw itself
       if (a.dw && p.dw_sum) {
-        const StoreEpi<float> out(p.dw_sum, nullptr, a.D, nullptr, first > 0);
+        const StoreEpi<float> out(p.dw_sum, nullptr, a.D, nullptr, first > 0, p.count, a.scale);
         DLL_TRY((launch_product<T, false, false, false>(g, out, p.gradients.tiling, stream)));
         if (last) {
           const long n = (long)a.V * a.D, blocks = (n + 255) / 256;

@@ -311,3 +311,24 @@ def test_gelu_keeps_its_digits_in_the_tail(tokens, dtype):
     for row in got["y"]:
         ref.check(row, (f, ef + roundings * f.abs() * 1.01), "y")
     ref.check(got["dw_gate"][:, 0], (tokens * d, tokens * (ed + (roundings * 1.01 + ref.gamma(tokens)) * d.abs())), "dw_gate")
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("tokens,scale", [(7, 1.0), (3680, 1.0), (3682, 1.0), (3699, 1.0), (4800, 1.0), (3682, 65536.0), (3682, 2.0 ** -120)])
+def test_the_factor_of_the_loss_is_rounded_with_the_results_alone(tokens, scale, dtype):
+    """Every row's label is a class of nearly no probability, so that dz is -scale / count there: its sum over all rows is -scale, and
+    a row's dx 40 scale / count.  Single precision is off by the factor's rounding, the sums' and the product's; what is rounded to
+    bfloat16 is rounded from there once (dz with scale / count in it would be off by the same 0.3 % in every row at 3682)."""
+    t, V, D = TYPES[dtype], 10, 8
+    spec = VocabSpec(tokens, D, V, dtype)
+    x, w = torch.zeros(tokens, D, dtype=t, device="cuda"), torch.zeros(V, D, dtype=t, device="cuda")
+    x[:, 0], w[3, 0] = 1, -40
+    e = lambda *s, d=t: torch.full(s, float("nan"), dtype=d, device="cuda")
+    o = dict(row_loss=e(tokens, d=torch.float32), row_lse=e(tokens, d=torch.float32), loss=e(1, d=torch.float32), dx=e(tokens, D), dw=e(V, D), dbias=e(V))
+    labels = torch.full((tokens,), 3, dtype=torch.int32, device="cuda")
+    B.dll_vocab_loss_grad(spec, x, w, torch.zeros(V, dtype=t, device="cuda"), labels, scale, **o,
+                          ws=B.workspace(B.dll_vocab_loss_grad_workspace_bytes(spec)).fill_(255))
+    bound = ref.gamma(tokens) if dtype == "float32" else 0.0
+    for got, want in ((o["dw"][3, 0], -scale), (o["dbias"][3], -scale), (o["dx"][0, 0], 40 * scale / tokens), (o["dx"][tokens - 1, 0], 40 * scale / tokens)):
+        rounded = float(torch.tensor(want, dtype=torch.float64).float().to(t))
+        assert abs(float(got) - rounded) <= bound * abs(want), (float(got), want)
