@@ -8,10 +8,10 @@
 //
 // Forward: a and b in one product, whose wavefronts hold both factors of a hidden unit, so that h leaves from its epilogue; then y.
 // Backward: dh, whose epilogue leaves da, db and h; then every gradient in one launch.  A few tokens are bound by the weights' bytes:
-// 2048 x 8192 bf16, one token, 25.5 us for 101 MB = 3.9 TB/s.  Many are bound by the matrix pipe: 4096 tokens, training pass 1.19 ms,
-// 1040 TFLOP/s of 18 T D H (a and b 303 us, y 156, dh 199, of which 70 are what its epilogue reads and writes, gradients 630).
+// 2048 x 8192 bf16, one token, 25.8 us for 101 MB = 3.9 TB/s.  Many are bound by the matrix pipe: 4096 tokens, training pass 1.19 ms,
+// 1040 TFLOP/s of 18 T D H (a and b 279 us, y 147, dh 183, a third of it what its epilogue reads and writes, gradients 586).
 // In between workgroups are few and short: 777 x 1000 x 2730 bf16 41 us, 310 TFLOP/s, 301 tiles of 16 slabs; 1000 x 500 x 1337 in single
-// precision 144 us with its backward pass.
+// precision 145 us with its backward pass.
 #include "large_ops.h"
 #include "skinny_product.h"
 

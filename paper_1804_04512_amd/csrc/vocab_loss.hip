@@ -13,9 +13,9 @@
 // gradients.  This takes three products of T D V; forming the logits again for the gradients would take four.
 // The exponentials are kept for a piece of the tokens at a time, 1 GiB at most.
 //
-// With gradients the matrix pipe bounds it: 4096 x 2048 x 50257 bf16, 3690 rows counted, 2.40 ms = 950 TFLOP/s (logits 908 us, both
-// gradients 1410, the pass over the exponentials 137 = 5.4 TB/s).  Without them a few tokens are bound by the weights' bytes:
-// 16 x 1024 x 32000 bf16 19.8 us, 15.4 of which read 66 MB at 4.2 TB/s; the rest joins the groups.  A small layer is a chain of short
+// With gradients the matrix pipe bounds it: 4096 x 2048 x 50257 bf16, 3690 rows counted, 2.39 ms = 950 TFLOP/s (logits 868 us, both
+// gradients 1371, the pass over the exponentials 140 = 5.3 TB/s).  Without them a few tokens are bound by the weights' bytes:
+// 16 x 1024 x 32000 bf16 20.3 us, 14.7 of which read 66 MB at 4.5 TB/s; the rest joins the groups.  A small layer is a chain of short
 // launches: 128 x 2048 x 1000 in single precision 51 us in seven.
 #include "large_ops.h"
 #include "skinny_product.h"
