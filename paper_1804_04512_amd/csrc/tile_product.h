@@ -460,9 +460,9 @@ __device__ __forceinline__ void product_tile(const ProductArgs &a, const Epi &ep
       for (int j = 0; j < TN; ++j)
 #pragma unroll
         for (int r = 0; r < 16; ++r) finite = finite && fabsf(acc[i][j][r]) < INFINITY;
-    // Only sums that exist and whose rows count for the epilogue do: an operand across k may hold anything behind its last row or column (a workspace's rows are written
-    // up to their last whole group of eight), and what a former call left there must change neither digits nor time.  Looked at only
-    // where there is something: for every tile it would cost 2.5 % of 1000 x 500 x 1337 both ways.
+    // Only sums that exist and whose rows count for the epilogue do: an operand across k may hold anything behind its last row or
+    // column (a workspace's rows are written up to their last whole group of eight), and what a former call left there must change
+    // neither digits nor time.  Looked at only where there is something: for every tile it would cost 2.5 % of 1000 x 500 x 1337 both ways.
     if (__any(!finite)) {
       const int left = PAIR ? WC : a.N - n0 - wn - 4 * (lane >> 5);   // a pair's rows behind the last one are zeros
       finite = true;

@@ -258,8 +258,9 @@ __global__ __launch_bounds__(256) void gather_rows_kernel(const T *x, T *xc, lon
   }
 }
 
-// lse = M + ln sum_g s_g exp(m_g - M), loss = (M - z_label) + the same logarithm.  A workgroup takes 16 rows at a time, 64 threads each.  Rows that were not gathered
-// (all_labels given) are taken by one workgroup, which passes over those that do not count and leaves the mean as well.
+// lse = M + ln sum_g s_g exp(m_g - M), loss = (M - z_label) + the same logarithm.  A workgroup takes 16 rows at a time, 64 threads
+// each.  Rows that were not gathered (all_labels given) are taken by one workgroup, which passes over those that do not count and
+// leaves the mean as well.
 __global__ __launch_bounds__(1024) void join_groups_kernel(const float2 *stats, int groups, long rows_ld, const float *hit, int M, const int *count, int first,
                                                             const int *rows, float2 *lse, float *piece_loss, float *row_loss, float *row_lse, const int *all_labels, int V, float *loss) {
   __shared__ float2 part[16][17];
