@@ -267,7 +267,7 @@ dll_status dll_cnn_forward(const dll_net_desc *net, const float *const *params, 
 
 /* ---------------------------------------------------------------------------------------
  * Operators of large language models, beside the dense layers, the loss and the update of the
- * network steps above: a gated feed-forward block, softmax cross entropy over a large
+ * network steps above: a gated feed-forward block, attention, softmax cross entropy over a large
  * vocabulary, and clipping by the global gradient norm with the momentum step behind it.
  * The conventions at the top hold: device pointers, row-major and contiguous, 16-byte aligned
  * (else DLL_ERR_SHAPE) unless stated (labels, row_loss, row_lse, loss and norm: to 4 bytes),
@@ -378,6 +378,43 @@ dll_status dll_momentum_update_clipped(const dll_tensor_list *list, float *const
                                        float momentum, const float *weight_decay, float max_norm,
                                        float *norm, void *const *copies, void *ws, size_t ws_bytes,
                                        void *stream);
+
+typedef struct {
+  int q_tokens, kv_tokens;       /* rows of q and o; of k and v */
+  int sequences;                 /* packed into them */
+  int heads, kv_heads, head_dim; /* heads a multiple of kv_heads; head_dim at most 256 */
+  int causal;                    /* 0 or 1 */
+  int dtype;                     /* dll_dtype of all tensors but lse */
+  int q_row, kv_row;             /* elements from a token's row to the next; 0: heads * head_dim, kv_heads * head_dim */
+} dll_attention_desc;
+
+/* Attention of packed sequences.  Sequence s has the tokens q_starts[s] to q_starts[s + 1] of q and kv_starts[s] to
+ * kv_starts[s + 1] of k and v, n_q and n_k of them (either may be 0; both arrays [sequences + 1] int32 on the device, not
+ * decreasing; they may be the same one).  Head h reads the keys and values of head h / (heads / kv_heads):
+ *   s_ij = scale q_i . k_j for the keys that query i may see: all of its sequence, with causal those with j <= i + n_k - n_q
+ *   lse_i = ln sum_j exp s_ij,  p_ij = exp(s_ij - lse_i),  o_i = sum_j p_ij v_j
+ *   q [q_tokens][heads][head_dim] in rows of q_row elements, k and v [kv_tokens][kv_heads][head_dim] in rows of kv_row
+ *   (so that one projection's output may hold all three), at any multiple of their elements
+ *   o [q_tokens][heads][head_dim] contiguous;  lse [heads][q_tokens] fp32, may be NULL
+ * A query that may see no key has o = 0 and lse = -infinity.  Rows outside the sequences are neither read nor written.  What other
+ * sequences hold does not matter; a NaN or an infinity in a sequence may reach all of its own outputs.  scale is finite
+ * (else DLL_ERR_SHAPE).  Starts outside [0, tokens] are taken as the nearest of these.  With DLL_BF16 p is rounded, relative to its row's
+ * maximum, before it meets v. */
+size_t dll_attention_fwd_workspace_bytes(const dll_attention_desc *d);
+dll_status dll_attention_fwd(const dll_attention_desc *d, const void *q, const void *k, const void *v,
+                             const int *q_starts, const int *kv_starts, float scale, void *o, float *lse,
+                             void *ws, size_t ws_bytes, void *stream);
+
+/* Its backward pass, d_o [q_tokens][heads][head_dim] the gradient w.r.t. o, from o and lse as the forward pass left them:
+ *   delta_i = d_o_i . o_i,  ds_ij = p_ij (d_o_i . v_j - delta_i)
+ *   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij d_o_i   (over the heads that read j, too)
+ * dq in rows like q's, dk and dv in rows like k's; each may be NULL (that gradient is not taken), not all three.  A key that no
+ * query may see has gradients of 0.  With DLL_BF16 p and ds are rounded before the sums, and delta takes o as it was rounded. */
+size_t dll_attention_bwd_workspace_bytes(const dll_attention_desc *d);
+dll_status dll_attention_bwd(const dll_attention_desc *d, const void *q, const void *k, const void *v,
+                             const int *q_starts, const int *kv_starts, float scale, const void *o,
+                             const float *lse, const void *d_o, void *dq, void *dk, void *dv, void *ws,
+                             size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

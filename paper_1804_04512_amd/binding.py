@@ -14,7 +14,7 @@ from typing import List, Optional, Sequence
 
 import torch
 
-from .workloads import ConvSpec, DenseSpec, GatedSpec, VocabSpec
+from .workloads import AttentionSpec, ConvSpec, DenseSpec, GatedSpec, VocabSpec
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libdll_conv.so")
@@ -28,7 +28,8 @@ SYMBOLS = ["dll_status_string", "dll_conv_workspace_bytes", "dll_conv_valid_fwd"
            "dll_conv_valid_wgrad_partial", "dll_conv_valid_wgrad_finish",
            "dll_gated_fwd_workspace_bytes", "dll_gated_fwd", "dll_gated_bwd_workspace_bytes", "dll_gated_bwd",
            "dll_vocab_loss_fwd_workspace_bytes", "dll_vocab_loss_fwd", "dll_vocab_loss_grad_workspace_bytes",
-           "dll_vocab_loss_grad", "dll_grad_norm_workspace_bytes", "dll_grad_norm", "dll_grad_clip",
+           "dll_vocab_loss_grad", "dll_attention_fwd_workspace_bytes", "dll_attention_fwd", "dll_attention_bwd_workspace_bytes",
+           "dll_attention_bwd", "dll_grad_norm_workspace_bytes", "dll_grad_norm", "dll_grad_clip",
            "dll_momentum_update_clipped"]
 NOALLOC_SCRATCH_BYTES = 8 << 20   # DLL_NOALLOC_SCRATCH_BYTES of include/dll_conv.h
 VISIBLE = {"binary": 0, "gaussian": 1}
@@ -58,6 +59,11 @@ class dll_gated_desc(C.Structure):
 
 class dll_vocab_desc(C.Structure):
     _fields_ = [(n, C.c_int) for n in ("tokens", "width", "classes", "dtype")]
+
+
+class dll_attention_desc(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("q_tokens", "kv_tokens", "sequences", "heads", "kv_heads", "head_dim", "causal", "dtype",
+                                       "q_row", "kv_row")]
 
 
 class dll_tensor_list(C.Structure):
@@ -110,12 +116,15 @@ def lib() -> C.CDLL:
         L.dll_cnn_forward_workspace_bytes.argtypes = [C.POINTER(dll_net_desc)]
         L.dll_cnn_forward.argtypes = [C.POINTER(dll_net_desc), vp, vp, vp, vp, vp, sz, vp]
         pg, pv, pl = C.POINTER(dll_gated_desc), C.POINTER(dll_vocab_desc), C.POINTER(dll_tensor_list)
+        pa = C.POINTER(dll_attention_desc)
         for name, arg in (("dll_gated_fwd", pg), ("dll_gated_bwd", pg), ("dll_vocab_loss_fwd", pv), ("dll_vocab_loss_grad", pv),
-                          ("dll_grad_norm", pl)):
+                          ("dll_attention_fwd", pa), ("dll_attention_bwd", pa), ("dll_grad_norm", pl)):
             query = getattr(L, name + "_workspace_bytes")
             query.restype, query.argtypes = sz, [arg]
         L.dll_gated_fwd.argtypes = [pg] + [vp] * 8 + [sz, vp]
         L.dll_gated_bwd.argtypes = [pg] + [vp] * 12 + [sz, vp]
+        L.dll_attention_fwd.argtypes = [pa] + [vp] * 5 + [C.c_float] + [vp] * 3 + [sz, vp]
+        L.dll_attention_bwd.argtypes = [pa] + [vp] * 5 + [C.c_float] + [vp] * 7 + [sz, vp]
         L.dll_vocab_loss_fwd.argtypes = [pv] + [vp] * 8 + [sz, vp]
         L.dll_vocab_loss_grad.argtypes = [pv] + [vp] * 4 + [C.c_float] + [vp] * 7 + [sz, vp]
         L.dll_grad_norm.argtypes = [pl, vp, vp, vp, sz, vp]
@@ -403,6 +412,59 @@ def dll_vocab_loss_grad(v: VocabSpec, x, w, bias, labels, scale, row_loss, row_l
                                   _tensor(dw, (v.classes, v.width), t, "dw", dev, True),
                                   _tensor(dbias, (v.classes,), t, "dbias", dev, True), *_ws(ws, dev), s.cuda_stream),
         "dll_vocab_loss_grad")
+
+
+def attention_desc(a: AttentionSpec) -> dll_attention_desc:
+    return dll_attention_desc(a.q_tokens, a.kv_tokens, a.sequences, a.heads, a.kv_heads, a.head_dim, int(a.causal), DTYPE[a.dtype],
+                              a.q_row, a.kv_row)
+
+
+def _head_rows(t: Optional[torch.Tensor], shape, row: int, dtype: torch.dtype, what: str, device, optional: bool = False):
+    """The address of a tensor [tokens][heads][head_dim] whose tokens lie `row` elements apart (0: contiguous)."""
+    if t is None:
+        return _tensor(t, shape, dtype, what, device, optional)
+    if t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{what}: {dtype} of shape {tuple(shape)} expected, got {t.dtype} of shape {tuple(t.shape)}")
+    strides = (row or shape[1] * shape[2], shape[2], 1)
+    if t.device != device or any(n > 1 and s != want for n, s, want in zip(shape, t.stride(), strides)):
+        raise ValueError(f"{what}: strides {strides} and on {device} (the device of the call's stream) expected")
+    return t.data_ptr()
+
+
+def _attention_inputs(a: AttentionSpec, q, k, v, q_starts, kv_starts, dev):
+    t, kv = _TORCH_TYPE[a.dtype], (a.kv_tokens, a.kv_heads, a.head_dim)
+    return (_head_rows(q, (a.q_tokens, a.heads, a.head_dim), a.q_row, t, "q", dev), _head_rows(k, kv, a.kv_row, t, "k", dev),
+            _head_rows(v, kv, a.kv_row, t, "v", dev), _tensor(q_starts, (a.sequences + 1,), torch.int32, "q_starts", dev),
+            _tensor(kv_starts, (a.sequences + 1,), torch.int32, "kv_starts", dev))
+
+
+def dll_attention_fwd_workspace_bytes(a: AttentionSpec) -> int:
+    return int(lib().dll_attention_fwd_workspace_bytes(C.byref(attention_desc(a))))
+
+
+def dll_attention_fwd(a: AttentionSpec, q, k, v, q_starts, kv_starts, scale, o, lse=None, ws=None, stream=None) -> None:
+    s = _call_stream(stream)
+    t, dev = _TORCH_TYPE[a.dtype], s.device
+    _ok(lib().dll_attention_fwd(C.byref(attention_desc(a)), *_attention_inputs(a, q, k, v, q_starts, kv_starts, dev), C.c_float(scale),
+                                _tensor(o, (a.q_tokens, a.heads, a.head_dim), t, "o", dev),
+                                _tensor(lse, (a.heads, a.q_tokens), torch.float32, "lse", dev, True), *_ws(ws, dev), s.cuda_stream),
+        "dll_attention_fwd")
+
+
+def dll_attention_bwd_workspace_bytes(a: AttentionSpec) -> int:
+    return int(lib().dll_attention_bwd_workspace_bytes(C.byref(attention_desc(a))))
+
+
+def dll_attention_bwd(a: AttentionSpec, q, k, v, q_starts, kv_starts, scale, o, lse, d_o, dq=None, dk=None, dv=None, ws=None,
+                      stream=None) -> None:
+    s = _call_stream(stream)
+    t, dev = _TORCH_TYPE[a.dtype], s.device
+    qs, kvs = (a.q_tokens, a.heads, a.head_dim), (a.kv_tokens, a.kv_heads, a.head_dim)
+    _ok(lib().dll_attention_bwd(C.byref(attention_desc(a)), *_attention_inputs(a, q, k, v, q_starts, kv_starts, dev), C.c_float(scale),
+                                _tensor(o, qs, t, "o", dev), _tensor(lse, (a.heads, a.q_tokens), torch.float32, "lse", dev),
+                                _tensor(d_o, qs, t, "d_o", dev), _head_rows(dq, qs, a.q_row, t, "dq", dev, True),
+                                _head_rows(dk, kvs, a.kv_row, t, "dk", dev, True), _head_rows(dv, kvs, a.kv_row, t, "dv", dev, True),
+                                *_ws(ws, dev), s.cuda_stream), "dll_attention_bwd")
 
 
 _DTYPE_OF = operator.attrgetter("dtype")

@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <cmath>
 #include <new>
 
 using namespace dllk;
@@ -59,6 +60,43 @@ dll_status check_vocab(const dll_vocab_desc *d) {
   if (!d) return DLL_ERR_NULL;
   return check_sizes(d->tokens, d->width, d->classes, d->dtype);
 }
+
+// rows of `heads` heads: contiguous where `row` is 0
+inline long row_of(int row, int heads, int dim) { return row ? row : (long)heads * dim; }
+constexpr int kMaxHeads = 1 << 12, kMaxDim = 256;
+
+dll_status check_heads(int heads, int kv_heads, int dim, int dtype) {
+  if (heads <= 0 || kv_heads <= 0 || dim <= 0 || heads % kv_heads) return DLL_ERR_SHAPE;
+  if (dtype != DLL_FP32 && dtype != DLL_BF16) return DLL_ERR_UNSUPPORTED;
+  return heads > kMaxHeads || dim > kMaxDim ? DLL_ERR_UNSUPPORTED : DLL_OK;
+}
+
+dll_status check_attention(const dll_attention_desc *d) {
+  if (!d) return DLL_ERR_NULL;
+  if (d->q_tokens <= 0 || d->kv_tokens <= 0 || d->sequences <= 0) return DLL_ERR_SHAPE;
+  const dll_status st = check_heads(d->heads, d->kv_heads, d->head_dim, d->dtype);
+  if (st != DLL_OK) return st;
+  if (d->causal != 0 && d->causal != 1) return DLL_ERR_UNSUPPORTED;
+  const long q_least = (long)d->heads * d->head_dim, kv_least = (long)d->kv_heads * d->head_dim;
+  const long q_row = row_of(d->q_row, d->heads, d->head_dim), kv_row = row_of(d->kv_row, d->kv_heads, d->head_dim);
+  if (q_row < q_least || kv_row < kv_least) return DLL_ERR_SHAPE;
+  if (d->q_tokens > kMaxTokens || d->kv_tokens > kMaxTokens || d->sequences > kMaxFeatures || q_row > kMaxFeatures || kv_row > kMaxFeatures)
+    return DLL_ERR_UNSUPPORTED;
+  if ((size_t)d->q_tokens * q_row >= kMaxElements || (size_t)d->kv_tokens * kv_row >= kMaxElements) return DLL_ERR_UNSUPPORTED;
+  return attention_fits(d->q_tokens, d->kv_tokens, d->sequences, d->heads) ? DLL_OK : DLL_ERR_UNSUPPORTED;
+}
+
+AttentionArgs attention_args(const dll_attention_desc *d) {
+  AttentionArgs a;
+  a.Tq = d->q_tokens; a.Tk = d->kv_tokens; a.S = d->sequences; a.H = d->heads; a.KV = d->kv_heads; a.D = d->head_dim;
+  a.causal = d->causal; a.dtype = d->dtype;
+  a.q_row = row_of(d->q_row, d->heads, d->head_dim);
+  a.kv_row = row_of(d->kv_row, d->kv_heads, d->head_dim);
+  return a;
+}
+
+// q, k, v and their gradients stand at any multiple of their elements; o and its gradient at 16 bytes
+bool off_type(const void *p, int dtype) { return reinterpret_cast<uintptr_t>(p) % type_bytes(dtype) != 0; }
 
 // counts and types, the gradients behind them
 dll_status check_list(const dll_tensor_list *l, const void *const *grads, bool with_grads) {
@@ -214,6 +252,45 @@ dll_status dll_vocab_loss_grad(const dll_vocab_desc *d, const void *x, const voi
   a.row_loss = row_loss; a.row_lse = row_lse; a.loss = loss;
   a.dx = dx; a.dw = dw; a.dbias = dbias;
   return dev(launch_vocab_grad(a, static_cast<char *>(ws), static_cast<hipStream_t>(stream)));
+}
+
+size_t dll_attention_fwd_workspace_bytes(const dll_attention_desc *d) {
+  return check_attention(d) == DLL_OK ? align_up(attention_fwd_scratch(attention_args(d))) : 0;
+}
+
+dll_status dll_attention_fwd(const dll_attention_desc *d, const void *q, const void *k, const void *v, const int *q_starts, const int *kv_starts, float scale,
+                             void *o, float *lse, void *ws, size_t ws_bytes, void *stream) {
+  dll_status st = check_attention(d);
+  if (st != DLL_OK) return st;
+  if (!q || !k || !v || !q_starts || !kv_starts || !o) return DLL_ERR_NULL;
+  const void *in[] = {q, k, v, q_starts, kv_starts}, *out[] = {o, lse, ws};
+  if (aliased(in, 5, out, 3) || misaligned(o) || off_element(lse) || off_element(q_starts) || off_element(kv_starts)) return DLL_ERR_SHAPE;
+  if (off_type(q, d->dtype) || off_type(k, d->dtype) || off_type(v, d->dtype) || !std::isfinite(scale)) return DLL_ERR_SHAPE;
+  if ((st = check_ws(ws, ws_bytes, dll_attention_fwd_workspace_bytes(d))) != DLL_OK) return st;
+  AttentionArgs a = attention_args(d);
+  a.q = q; a.k = k; a.v = v; a.q_starts = q_starts; a.kv_starts = kv_starts; a.scale = scale; a.o = o; a.lse = lse;
+  return dev(launch_attention_fwd(a, static_cast<char *>(ws), static_cast<hipStream_t>(stream)));
+}
+
+size_t dll_attention_bwd_workspace_bytes(const dll_attention_desc *d) {
+  return check_attention(d) == DLL_OK ? align_up(attention_bwd_scratch(attention_args(d))) : 0;
+}
+
+dll_status dll_attention_bwd(const dll_attention_desc *d, const void *q, const void *k, const void *v, const int *q_starts, const int *kv_starts, float scale,
+                             const void *o, const float *lse, const void *d_o, void *dq, void *dk, void *dv, void *ws, size_t ws_bytes, void *stream) {
+  dll_status st = check_attention(d);
+  if (st != DLL_OK) return st;
+  if (!q || !k || !v || !q_starts || !kv_starts || !o || !lse || !d_o || (!dq && !dk && !dv)) return DLL_ERR_NULL;
+  const void *in[] = {q, k, v, q_starts, kv_starts, o, lse, d_o}, *out[] = {dq, dk, dv, ws};
+  if (aliased(in, 8, out, 4) || misaligned(o) || misaligned(d_o) || off_element(lse) || off_element(q_starts) || off_element(kv_starts)) return DLL_ERR_SHAPE;
+  for (const void *p : {q, k, v, (const void *)dq, (const void *)dk, (const void *)dv})
+    if (off_type(p, d->dtype)) return DLL_ERR_SHAPE;
+  if (!std::isfinite(scale)) return DLL_ERR_SHAPE;
+  if ((st = check_ws(ws, ws_bytes, dll_attention_bwd_workspace_bytes(d))) != DLL_OK) return st;
+  AttentionArgs a = attention_args(d);
+  a.q = q; a.k = k; a.v = v; a.q_starts = q_starts; a.kv_starts = kv_starts; a.scale = scale;
+  a.o = const_cast<void *>(o); a.lse = const_cast<float *>(lse); a.d_o = d_o; a.dq = dq; a.dk = dk; a.dv = dv;
+  return dev(launch_attention_bwd(a, static_cast<char *>(ws), static_cast<hipStream_t>(stream)));
 }
 
 size_t dll_grad_norm_workspace_bytes(const dll_tensor_list *list) {

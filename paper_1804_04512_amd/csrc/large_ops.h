@@ -1,4 +1,4 @@
-// Internal launch interfaces of the large-model operators: gated feed-forward block, vocabulary loss, gradient clipping.
+// Internal launch interfaces of the large-model operators: gated feed-forward block, vocabulary loss, attention, gradient clipping.
 // Every pointer is a device pointer unless it says host.
 #pragma once
 
@@ -57,6 +57,25 @@ hipError_t launch_grad_norm(const GradList &l, const void *const *grads, float *
 hipError_t launch_grad_clip(const GradList &l, const void *const *grads, void *const *out, float max_norm, float *norm, char *scratch, hipStream_t stream);
 hipError_t launch_momentum_clipped(const GradList &l, float *const *params, float *const *velocity, const void *const *grads, const float *decay,
                                    float lr, float mu, float max_norm, float *norm, void *const *copies, char *scratch, hipStream_t stream);
+
+// ---- attention over packed sequences ------------------------------------------------------------------------------------
+struct AttentionArgs {
+  int Tq = 0, Tk = 0, S = 0, H = 0, KV = 0, D = 0, causal = 0, dtype = 0;
+  long q_row = 0, kv_row = 0;      // elements between tokens of q and dq; of k, v, dk and dv
+  float scale = 1.0f;
+  const void *q = nullptr, *k = nullptr, *v = nullptr;
+  const int *q_starts = nullptr, *kv_starts = nullptr;
+  void *o = nullptr;               // forward: output; backward: input.  [Tq][H][D]
+  float *lse = nullptr;            // [H][Tq]; forward: nullable output; backward: input
+  const void *d_o = nullptr;       // [Tq][H][D]
+  void *dq = nullptr, *dk = nullptr, *dv = nullptr;   // each nullable
+};
+// whether the launches' grids hold so many tiles
+bool attention_fits(int q_tokens, int kv_tokens, int sequences, int heads);
+size_t attention_fwd_scratch(const AttentionArgs &a);
+size_t attention_bwd_scratch(const AttentionArgs &a);
+hipError_t launch_attention_fwd(const AttentionArgs &a, char *scratch, hipStream_t stream);
+hipError_t launch_attention_bwd(const AttentionArgs &a, char *scratch, hipStream_t stream);
 
 // ---- shared: rows copied into padded rows -------------------------------------------------------------------------------
 // dst [rows][padded(cols)] = src [rows][cols], zeros behind; bfloat16, as single precision's rows are loadable whatever their length

@@ -93,6 +93,22 @@ class VocabSpec:
     dtype: str = "bfloat16"
 
 
+@dataclass(frozen=True)
+class AttentionSpec:
+    """Attention of `sequences` packed sequences, `q_tokens` queries over `kv_tokens` keys in all; rows of `q_row` and `kv_row`
+    elements (0: contiguous)."""
+    q_tokens: int
+    kv_tokens: int
+    sequences: int
+    heads: int
+    kv_heads: int
+    head_dim: int
+    causal: bool = True
+    dtype: str = "bfloat16"
+    q_row: int = 0
+    kv_row: int = 0
+
+
 @dataclass
 class ConvWorkload:
     cfg: int
