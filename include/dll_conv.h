@@ -416,6 +416,50 @@ dll_status dll_attention_bwd(const dll_attention_desc *d, const void *q, const v
                              const float *lse, const void *d_o, void *dq, void *dk, void *dv, void *ws,
                              size_t ws_bytes, void *stream);
 
+/* A cache of keys and values in pages that requests take as they grow.  k_cache and v_cache [pages][kv_heads][page_tokens][head_dim],
+ * 16-byte aligned, may have 2^31 or more elements; token t of request r is place t % page_tokens of page
+ * table[r][t / page_tokens].  At most 2^16 requests; fewer than 2^31 tokens in all pages, 2^30 in a row of the table. */
+typedef struct {
+  int requests;
+  int heads, kv_heads, head_dim; /* heads a multiple of kv_heads; head_dim at most 256 */
+  int pages, page_tokens;        /* of the cache */
+  int table_pages;               /* columns of the table */
+  int dtype;                     /* dll_dtype of all tensors but lse */
+} dll_cache_desc;
+
+/* Pages and slots for a step's new tokens, all int32:
+ *   lengths [requests]  tokens of each request, the new ones among them;  added [requests]  how many of these are new (below 0
+ *           counts as 0, more than lengths as lengths)
+ *   free_pages [n_free] pages that nobody has, taken from entry *free_at on (NULL: 0; n_free = 0: free_pages may be NULL) in the requests' order
+ *   table   [requests][table_pages]  entries of the pages that the requests had before are read, those of the new pages are written,
+ *           the others left as they are
+ *   starts  [requests + 1]  receives where each request's new tokens lie when they are packed (q_starts of dll_attention_fwd)
+ *   slots   [tokens]  receives page * page_tokens + place for each new token; -1 where it has no page.  tokens, at least 1, is the array's room:
+ *           new tokens behind it get neither slot nor table entry; what lies behind the new tokens is left as it is
+ *   state   [2]  receives the first entry of free_pages that is still free, and how many pages were missing, as the list was too short (their
+ *           entries are -1) or the table too narrow
+ * Calls may be repeated: they change none of what they read. */
+dll_status dll_cache_plan(const dll_cache_desc *d, const int *lengths, const int *added, const int *free_pages,
+                          int n_free, const int *free_at, int *table, int *starts, int *slots, int tokens,
+                          int *state, void *stream);
+
+/* Rows of new tokens into the cache: k and v [tokens][kv_heads][head_dim] in rows of `row` elements (0: contiguous), at any multiple of their
+ * elements; slots [tokens] int32 as dll_cache_plan leaves them.  Tokens whose slot lies outside [0, pages * page_tokens) are left out.
+ * Slots that are not -1 have to differ. */
+dll_status dll_cache_write(const dll_cache_desc *d, int tokens, int row, const void *k, const void *v,
+                           const int *slots, void *k_cache, void *v_cache, void *stream);
+
+/* Attention of one new token a request over its keys and values in the cache, its own among them:
+ *   o[r][h] = sum_t p_t v_t,  p = softmax_t(scale q[r][h] . k_t),  t < lengths[r], keys and values of head h / (heads / kv_heads)
+ *   q, o [requests][heads][head_dim];  table [requests][table_pages], lengths [requests] int32;  lse [requests][heads] fp32, may be NULL
+ * A length below 0 counts as 0, one that the table has no room for as that room.  Keys whose table entry lies outside [0, pages)
+ * are left out, and nothing that pages hold behind a request's last token is used.  A request without keys has o = 0 and lse = -infinity.
+ * scale is finite (else DLL_ERR_SHAPE).  With DLL_BF16 p is rounded, relative to its maximum, before it meets v. */
+size_t dll_paged_attention_workspace_bytes(const dll_cache_desc *d);
+dll_status dll_paged_attention(const dll_cache_desc *d, const void *q, const void *k_cache, const void *v_cache,
+                               const int *table, const int *lengths, float scale, void *o, float *lse, void *ws,
+                               size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -14,7 +14,7 @@ from typing import List, Optional, Sequence
 
 import torch
 
-from .workloads import AttentionSpec, ConvSpec, DenseSpec, GatedSpec, VocabSpec
+from .workloads import AttentionSpec, CacheSpec, ConvSpec, DenseSpec, GatedSpec, VocabSpec
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libdll_conv.so")
@@ -29,7 +29,8 @@ SYMBOLS = ["dll_status_string", "dll_conv_workspace_bytes", "dll_conv_valid_fwd"
            "dll_gated_fwd_workspace_bytes", "dll_gated_fwd", "dll_gated_bwd_workspace_bytes", "dll_gated_bwd",
            "dll_vocab_loss_fwd_workspace_bytes", "dll_vocab_loss_fwd", "dll_vocab_loss_grad_workspace_bytes",
            "dll_vocab_loss_grad", "dll_attention_fwd_workspace_bytes", "dll_attention_fwd", "dll_attention_bwd_workspace_bytes",
-           "dll_attention_bwd", "dll_grad_norm_workspace_bytes", "dll_grad_norm", "dll_grad_clip",
+           "dll_attention_bwd", "dll_cache_plan", "dll_cache_write", "dll_paged_attention_workspace_bytes", "dll_paged_attention",
+           "dll_grad_norm_workspace_bytes", "dll_grad_norm", "dll_grad_clip",
            "dll_momentum_update_clipped"]
 NOALLOC_SCRATCH_BYTES = 8 << 20   # DLL_NOALLOC_SCRATCH_BYTES of include/dll_conv.h
 VISIBLE = {"binary": 0, "gaussian": 1}
@@ -64,6 +65,10 @@ class dll_vocab_desc(C.Structure):
 class dll_attention_desc(C.Structure):
     _fields_ = [(n, C.c_int) for n in ("q_tokens", "kv_tokens", "sequences", "heads", "kv_heads", "head_dim", "causal", "dtype",
                                        "q_row", "kv_row")]
+
+
+class dll_cache_desc(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("requests", "heads", "kv_heads", "head_dim", "pages", "page_tokens", "table_pages", "dtype")]
 
 
 class dll_tensor_list(C.Structure):
@@ -116,15 +121,18 @@ def lib() -> C.CDLL:
         L.dll_cnn_forward_workspace_bytes.argtypes = [C.POINTER(dll_net_desc)]
         L.dll_cnn_forward.argtypes = [C.POINTER(dll_net_desc), vp, vp, vp, vp, vp, sz, vp]
         pg, pv, pl = C.POINTER(dll_gated_desc), C.POINTER(dll_vocab_desc), C.POINTER(dll_tensor_list)
-        pa = C.POINTER(dll_attention_desc)
+        pa, pc = C.POINTER(dll_attention_desc), C.POINTER(dll_cache_desc)
         for name, arg in (("dll_gated_fwd", pg), ("dll_gated_bwd", pg), ("dll_vocab_loss_fwd", pv), ("dll_vocab_loss_grad", pv),
-                          ("dll_attention_fwd", pa), ("dll_attention_bwd", pa), ("dll_grad_norm", pl)):
+                          ("dll_attention_fwd", pa), ("dll_attention_bwd", pa), ("dll_paged_attention", pc), ("dll_grad_norm", pl)):
             query = getattr(L, name + "_workspace_bytes")
             query.restype, query.argtypes = sz, [arg]
         L.dll_gated_fwd.argtypes = [pg] + [vp] * 8 + [sz, vp]
         L.dll_gated_bwd.argtypes = [pg] + [vp] * 12 + [sz, vp]
         L.dll_attention_fwd.argtypes = [pa] + [vp] * 5 + [C.c_float] + [vp] * 3 + [sz, vp]
         L.dll_attention_bwd.argtypes = [pa] + [vp] * 5 + [C.c_float] + [vp] * 7 + [sz, vp]
+        L.dll_cache_plan.argtypes = [pc, vp, vp, vp, C.c_int] + [vp] * 4 + [C.c_int, vp, vp]
+        L.dll_cache_write.argtypes = [pc, C.c_int, C.c_int] + [vp] * 6
+        L.dll_paged_attention.argtypes = [pc] + [vp] * 5 + [C.c_float] + [vp] * 3 + [sz, vp]
         L.dll_vocab_loss_fwd.argtypes = [pv] + [vp] * 8 + [sz, vp]
         L.dll_vocab_loss_grad.argtypes = [pv] + [vp] * 4 + [C.c_float] + [vp] * 7 + [sz, vp]
         L.dll_grad_norm.argtypes = [pl, vp, vp, vp, sz, vp]
@@ -465,6 +473,56 @@ def dll_attention_bwd(a: AttentionSpec, q, k, v, q_starts, kv_starts, scale, o, 
                                 _tensor(d_o, qs, t, "d_o", dev), _head_rows(dq, qs, a.q_row, t, "dq", dev, True),
                                 _head_rows(dk, kvs, a.kv_row, t, "dk", dev, True), _head_rows(dv, kvs, a.kv_row, t, "dv", dev, True),
                                 *_ws(ws, dev), s.cuda_stream), "dll_attention_bwd")
+
+
+def cache_desc(c: CacheSpec) -> dll_cache_desc:
+    return dll_cache_desc(c.requests, c.heads, c.kv_heads, c.head_dim, c.pages, c.page_tokens, c.table_pages, DTYPE[c.dtype])
+
+
+def _ints(t, n, what: str, dev, optional: bool = False):
+    """The address of a vector of whole numbers; n: its length, or None (any), or a shape."""
+    if t is not None and n is None:
+        n = t.numel()
+    return _tensor(t, n if isinstance(n, tuple) else (n,), torch.int32, what, dev, optional)
+
+
+def dll_cache_plan(c: CacheSpec, lengths, added, free_pages, table, starts, slots, state, free_at=None, stream=None) -> None:
+    """free_pages and slots: of any length."""
+    s = _call_stream(stream)
+    dev, n = s.device, c.requests
+    _ok(lib().dll_cache_plan(C.byref(cache_desc(c)), _ints(lengths, n, "lengths", dev), _ints(added, n, "added", dev),
+                             _ints(free_pages, None, "free_pages", dev), free_pages.numel(), _ints(free_at, 1, "free_at", dev, True),
+                             _ints(table, (n, c.table_pages), "table", dev), _ints(starts, n + 1, "starts", dev),
+                             _ints(slots, None, "slots", dev), slots.numel(), _ints(state, 2, "state", dev), s.cuda_stream), "dll_cache_plan")
+
+
+def _caches(c: CacheSpec, k_cache, v_cache, dev):
+    shape, t = (c.pages, c.kv_heads, c.page_tokens, c.head_dim), _TORCH_TYPE[c.dtype]
+    return _tensor(k_cache, shape, t, "k_cache", dev), _tensor(v_cache, shape, t, "v_cache", dev)
+
+
+def dll_cache_write(c: CacheSpec, k, v, slots, k_cache, v_cache, stream=None) -> None:
+    """k, v: [tokens][kv_heads][head_dim], their tokens equally far apart in both."""
+    s = _call_stream(stream)
+    dev, t = s.device, _TORCH_TYPE[c.dtype]
+    tokens, row = slots.numel(), k.stride(0) if k.shape[0] > 1 else 0
+    shape = (tokens, c.kv_heads, c.head_dim)
+    _ok(lib().dll_cache_write(C.byref(cache_desc(c)), tokens, row, _head_rows(k, shape, row, t, "k", dev), _head_rows(v, shape, row, t, "v", dev),
+                              _ints(slots, None, "slots", dev), *_caches(c, k_cache, v_cache, dev), s.cuda_stream), "dll_cache_write")
+
+
+def dll_paged_attention_workspace_bytes(c: CacheSpec) -> int:
+    return int(lib().dll_paged_attention_workspace_bytes(C.byref(cache_desc(c))))
+
+
+def dll_paged_attention(c: CacheSpec, q, k_cache, v_cache, table, lengths, scale, o, lse=None, ws=None, stream=None) -> None:
+    s = _call_stream(stream)
+    dev, t, rows = s.device, _TORCH_TYPE[c.dtype], (c.requests, c.heads, c.head_dim)
+    _ok(lib().dll_paged_attention(C.byref(cache_desc(c)), _tensor(q, rows, t, "q", dev), *_caches(c, k_cache, v_cache, dev),
+                                  _ints(table, (c.requests, c.table_pages), "table", dev), _ints(lengths, c.requests, "lengths", dev),
+                                  C.c_float(scale), _tensor(o, rows, t, "o", dev),
+                                  _tensor(lse, (c.requests, c.heads), torch.float32, "lse", dev, True), *_ws(ws, dev), s.cuda_stream),
+        "dll_paged_attention")
 
 
 _DTYPE_OF = operator.attrgetter("dtype")

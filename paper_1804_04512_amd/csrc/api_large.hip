@@ -95,6 +95,23 @@ AttentionArgs attention_args(const dll_attention_desc *d) {
   return a;
 }
 
+dll_status check_cache(const dll_cache_desc *d) {
+  if (!d) return DLL_ERR_NULL;
+  if (d->requests <= 0 || d->pages <= 0 || d->page_tokens <= 0 || d->table_pages <= 0) return DLL_ERR_SHAPE;
+  const dll_status st = check_heads(d->heads, d->kv_heads, d->head_dim, d->dtype);
+  if (st != DLL_OK) return st;
+  if (d->requests > 1 << 16 || (long)d->requests * d->heads > kMaxGrid || (size_t)d->requests * d->table_pages >= kMaxElements) return DLL_ERR_UNSUPPORTED;
+  if ((size_t)d->pages * d->page_tokens >= kMaxElements || (size_t)d->table_pages * d->page_tokens > (size_t)1 << 30) return DLL_ERR_UNSUPPORTED;
+  return DLL_OK;
+}
+
+CacheArgs cache_args(const dll_cache_desc *d) {
+  CacheArgs a;
+  a.R = d->requests; a.H = d->heads; a.KV = d->kv_heads; a.D = d->head_dim;
+  a.pages = d->pages; a.page = d->page_tokens; a.columns = d->table_pages; a.dtype = d->dtype;
+  return a;
+}
+
 // q, k, v and their gradients stand at any multiple of their elements; o and its gradient at 16 bytes
 bool off_type(const void *p, int dtype) { return reinterpret_cast<uintptr_t>(p) % type_bytes(dtype) != 0; }
 
@@ -291,6 +308,58 @@ dll_status dll_attention_bwd(const dll_attention_desc *d, const void *q, const v
   a.q = q; a.k = k; a.v = v; a.q_starts = q_starts; a.kv_starts = kv_starts; a.scale = scale;
   a.o = const_cast<void *>(o); a.lse = const_cast<float *>(lse); a.d_o = d_o; a.dq = dq; a.dk = dk; a.dv = dv;
   return dev(launch_attention_bwd(a, static_cast<char *>(ws), static_cast<hipStream_t>(stream)));
+}
+
+dll_status dll_cache_plan(const dll_cache_desc *d, const int *lengths, const int *added, const int *free_pages, int n_free, const int *free_at, int *table,
+                          int *starts, int *slots, int tokens, int *state, void *stream) {
+  const dll_status st = check_cache(d);
+  if (st != DLL_OK) return st;
+  if (!lengths || !added || (!free_pages && n_free > 0) || !table || !starts || !slots || !state) return DLL_ERR_NULL;
+  if (n_free < 0 || tokens <= 0) return DLL_ERR_SHAPE;
+  if (tokens > kMaxTokens) return DLL_ERR_UNSUPPORTED;
+  const void *in[] = {lengths, added, free_pages, free_at}, *out[] = {table, starts, slots, state};
+  if (aliased(in, 4, out, 4)) return DLL_ERR_SHAPE;
+  for (int i = 0; i < 4; ++i)
+    if (off_element(in[i]) || off_element(out[i])) return DLL_ERR_SHAPE;
+  CacheArgs a = cache_args(d);
+  a.lengths = lengths; a.added = added; a.free_pages = free_pages; a.n_free = n_free; a.free_at = free_at;
+  a.table = table; a.starts = starts; a.slots = slots; a.tokens = tokens; a.state = state;
+  return dev(launch_cache_plan(a, static_cast<hipStream_t>(stream)));
+}
+
+dll_status dll_cache_write(const dll_cache_desc *d, int tokens, int row, const void *k, const void *v, const int *slots, void *k_cache, void *v_cache,
+                           void *stream) {
+  const dll_status st = check_cache(d);
+  if (st != DLL_OK) return st;
+  if (!k || !v || !slots || !k_cache || !v_cache) return DLL_ERR_NULL;
+  const long least = (long)d->kv_heads * d->head_dim, between = row_of(row, d->kv_heads, d->head_dim);
+  if (tokens <= 0 || between < least) return DLL_ERR_SHAPE;
+  if (tokens > kMaxTokens || between > kMaxFeatures || (size_t)tokens * between >= kMaxElements) return DLL_ERR_UNSUPPORTED;
+  const void *in[] = {k, v, slots}, *out[] = {k_cache, v_cache};
+  if (aliased(in, 3, out, 2) || misaligned(k_cache) || misaligned(v_cache) || off_type(k, d->dtype) || off_type(v, d->dtype) || off_element(slots))
+    return DLL_ERR_SHAPE;
+  CacheArgs a = cache_args(d);
+  a.tokens = tokens; a.row = between; a.k = k; a.v = v; a.slots = const_cast<int *>(slots); a.k_cache = k_cache; a.v_cache = v_cache;
+  return dev(launch_cache_write(a, static_cast<hipStream_t>(stream)));
+}
+
+size_t dll_paged_attention_workspace_bytes(const dll_cache_desc *d) {
+  return check_cache(d) == DLL_OK ? align_up(paged_attention_scratch(cache_args(d))) : 0;
+}
+
+dll_status dll_paged_attention(const dll_cache_desc *d, const void *q, const void *k_cache, const void *v_cache, const int *table, const int *lengths,
+                               float scale, void *o, float *lse, void *ws, size_t ws_bytes, void *stream) {
+  dll_status st = check_cache(d);
+  if (st != DLL_OK) return st;
+  if (!q || !k_cache || !v_cache || !table || !lengths || !o) return DLL_ERR_NULL;
+  const void *in[] = {q, k_cache, v_cache, table, lengths}, *out[] = {o, lse, ws};
+  if (aliased(in, 5, out, 3) || misaligned(q) || misaligned(k_cache) || misaligned(v_cache) || misaligned(o)) return DLL_ERR_SHAPE;
+  if (off_element(table) || off_element(lengths) || off_element(lse) || !std::isfinite(scale)) return DLL_ERR_SHAPE;
+  if ((st = check_ws(ws, ws_bytes, dll_paged_attention_workspace_bytes(d))) != DLL_OK) return st;
+  CacheArgs a = cache_args(d);
+  a.q = q; a.k_cache = const_cast<void *>(k_cache); a.v_cache = const_cast<void *>(v_cache); a.table = const_cast<int *>(table); a.lengths = lengths;
+  a.scale = scale; a.o = o; a.lse = lse;
+  return dev(launch_paged_attention(a, static_cast<char *>(ws), static_cast<hipStream_t>(stream)));
 }
 
 size_t dll_grad_norm_workspace_bytes(const dll_tensor_list *list) {

@@ -77,6 +77,31 @@ size_t attention_bwd_scratch(const AttentionArgs &a);
 hipError_t launch_attention_fwd(const AttentionArgs &a, char *scratch, hipStream_t stream);
 hipError_t launch_attention_bwd(const AttentionArgs &a, char *scratch, hipStream_t stream);
 
+// ---- paged cache of keys and values ---------------------------------------------------------------------------------------
+struct CacheArgs {
+  int R = 0, H = 0, KV = 0, D = 0, pages = 0, page = 0, columns = 0, dtype = 0;
+  const int *lengths = nullptr;
+  // plan
+  const int *added = nullptr, *free_pages = nullptr, *free_at = nullptr;   // free_at: nullable
+  int n_free = 0;
+  int *table = nullptr, *starts = nullptr, *state = nullptr;
+  int *slots = nullptr;            // plan: output; store: input
+  int tokens = 0;                  // of slots
+  // store
+  const void *k = nullptr, *v = nullptr;
+  long row = 0;                    // elements between tokens of k and v
+  void *k_cache = nullptr, *v_cache = nullptr;   // [pages][KV][page][D]
+  // attention
+  const void *q = nullptr;
+  float scale = 1.0f;
+  void *o = nullptr;
+  float *lse = nullptr;            // nullable, [R][H]
+};
+hipError_t launch_cache_plan(const CacheArgs &a, hipStream_t stream);
+hipError_t launch_cache_write(const CacheArgs &a, hipStream_t stream);
+size_t paged_attention_scratch(const CacheArgs &a);
+hipError_t launch_paged_attention(const CacheArgs &a, char *scratch, hipStream_t stream);
+
 // ---- shared: rows copied into padded rows -------------------------------------------------------------------------------
 // dst [rows][padded(cols)] = src [rows][cols], zeros behind; bfloat16, as single precision's rows are loadable whatever their length
 hipError_t launch_pad_rows(const void *src, void *dst, long rows, long cols, hipStream_t stream);

@@ -1,0 +1,401 @@
+// Attention of one new token a request over a paged cache: o = softmax(scale q k^T) v over the request's keys, which the block table finds.
+//
+// Bound by memory: each request's keys and values are read once, for all heads that share them.  Those are the columns of 16 x 16 x 32
+// products (scores transposed: keys are registers, the head is the lane), up to sixteen at a time.
+//
+// The work is units of kUnit keys of one request and key head, dealt to the workgroups in equal runs whatever the lengths are: each
+// workgroup finds its run by adding the lengths up.  Where a run holds all of a request's head the result is written; where it
+// begins or ends inside one, sums, maximum and un-normalised outputs go to the workspace (two places a workgroup) and a second
+// launch joins them, in the order of the keys.
+//
+// Inside a workgroup the wavefronts take tiles of 32 keys in turn, each with its own running maximum and sums.  A lane holds eight elements of
+// two keys a step, straight from memory into the operand's registers; values have the same addresses, and go through the
+// wavefront's own LDS to be read across keys, in the order in which the scores' registers hold them: register r of quarter c is key 4 c + r of
+// its sixteen, so eight registers of two results are keys 4 c + j and 16 + 4 c + j.
+#include "attention_tile.h"
+
+namespace dllk {
+
+using namespace attn;
+
+namespace {
+
+constexpr int kThreads = 256, kWaves = 4, kTile = 32, kUnit = 128, kHeads = 16;
+constexpr int kGroups = 1024;   // workgroups of a launch: four a compute unit
+
+__device__ __forceinline__ floatx4 mma16(bf16x8 a, bf16x8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ floatx4 mma16(floatx8 a, floatx8 b, floatx4 c) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+  return c;
+}
+// over the four quarters of the lanes
+__device__ __forceinline__ float most4(float v) { v = fmaxf(v, __shfl_xor(v, 16)); return fmaxf(v, __shfl_xor(v, 32)); }
+__device__ __forceinline__ float sum4(float v) { v += __shfl_xor(v, 16); return v + __shfl_xor(v, 32); }
+
+// keys of a request: what its table has room for at most
+__device__ __forceinline__ int keys_of(const CacheArgs &a, int r) { return (int)max(0L, min((long)a.lengths[r], (long)a.columns * a.page)); }
+__device__ __forceinline__ int units_of(int keys) { return (keys + kUnit - 1) / kUnit; }
+
+struct Parts {
+  float *o;    // [2 kGroups][kHeads][D], relative to the maximum
+  float *ml;   // [2 kGroups][kHeads][2]: maximum in the exponent's base, sum
+  int blocks;  // of at most kHeads heads that share a key head
+};
+
+// Units before request r and in all, by the whole workgroup
+__device__ __forceinline__ void add_units(const CacheArgs &a, int r, long *before, long *all, long *scratch) {
+  long b = 0, s = 0;
+  for (int i = threadIdx.x; i < a.R; i += kThreads) {
+    const int u = units_of(keys_of(a, i));
+    s += u;
+    if (i < r) b += u;
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) b += __shfl_xor(b, d), s += __shfl_xor(s, d);
+  if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = b, scratch[kWaves + (threadIdx.x >> 6)] = s;
+  __syncthreads();
+  b = s = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) b += scratch[w], s += scratch[kWaves + w];
+  *before = b;
+  *all = s;
+}
+// runs of units: workgroup w of n has those from w * all / n on, and where there are fewer units than workgroups one each
+__device__ __forceinline__ int working(long all, int n) { return (int)min((long)n, all); }
+__device__ __forceinline__ long run_of(long w, long all, int n) { return w * all / n; }
+__device__ __forceinline__ int owner_of(long unit, long all, int n) { return (int)(((unit + 1) * n - 1) / all); }
+
+// behind the wavefronts' areas in LDS
+struct Shared {
+  long scratch[kWaves + 1];
+  int found;
+  float ml[kWaves][kHeads][2];
+};
+
+template <class T, int DP>
+__global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DP <= 128 : DP <= 96) ? 2 : 1) void paged_attention_kernel(const CacheArgs a, const Parts parts) {
+  typedef Tile<T, DP> G;
+  constexpr int kSteps = DP / 32, kArea = kTile * G::kRowBytes;   // LDS of a wavefront: its values, or at the end its sums [16][DP] fp32
+  static_assert(kArea >= kHeads * DP * 4, "");
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  Shared &shared = *reinterpret_cast<Shared *>(smem + kWaves * kArea);
+  long (&scratch)[kWaves + 1] = shared.scratch;
+  auto &ml = shared.ml;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4, col = lane & 15;
+  char *area = smem + wave * kArea;
+  const int group = a.H / a.KV, blocks = parts.blocks, VH = a.KV * blocks;
+  const bool whole = a.D % 8 == 0;
+  const float c = fmaxf(fabsf(a.scale) * kLog2e, 0x1p-126f);
+
+  // requests without keys
+  for (int r = blockIdx.x; r < a.R; r += gridDim.x)
+    if (keys_of(a, r) == 0)
+      for (int i = threadIdx.x; i < a.H * a.D; i += kThreads) {
+        ((T *)a.o)[(long)r * a.H * a.D + i] = (T)0.0f;
+        if (a.lse && i < a.H) a.lse[(long)r * a.H + i] = -INFINITY;
+      }
+
+  // this workgroup's units, and the request that the first of them belongs to
+  const int each = (a.R + kThreads - 1) / kThreads, r0 = min((int)threadIdx.x * each, a.R), r1 = min(r0 + each, a.R);
+  long mine = 0;
+  for (int r = r0; r < r1; ++r) mine += units_of(keys_of(a, r));
+  long up = mine;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const long o = __shfl_up(up, d);
+    if (lane >= d) up += o;
+  }
+  if (lane == 63) scratch[wave] = up;
+  __syncthreads();
+  long before = up - mine, all = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave) before += scratch[w];
+    all += scratch[w];
+  }
+  all *= VH;
+  const int n = working(all, gridDim.x);
+  if ((int)blockIdx.x >= n) return;
+  const long first = run_of(blockIdx.x, all, n), end = run_of(blockIdx.x + 1, all, n);
+  if (before * VH <= first && first < (before + mine) * VH) {
+    long base = before * VH;
+    for (int r = r0; r < r1; ++r) {
+      const long n = (long)units_of(keys_of(a, r)) * VH;
+      if (first < base + n) {
+        shared.found = r;
+        scratch[kWaves] = base;
+        break;
+      }
+      base += n;
+    }
+  }
+  __syncthreads();
+  int r = __builtin_amdgcn_readfirstlane(shared.found);
+  long base = scratch[kWaves];
+
+  for (long u = first; u < end;) {
+    const int keys = __builtin_amdgcn_readfirstlane(keys_of(a, r)), per = units_of(keys);
+    if (per == 0) {   // r stays in range: units before `end` are somebody's
+      ++r;
+      continue;
+    }
+    const long rel = u - base;
+    const int vh = (int)(rel / per), unit0 = (int)(rel % per), units = (int)min((long)(per - unit0), end - u);
+    const int kv = vh / blocks, block = vh % blocks, heads = min(kHeads, group - block * kHeads), head0 = kv * group + block * kHeads;
+    const int key_begin = unit0 * kUnit, key_end = min(keys, (unit0 + units) * kUnit);
+    const int *table = a.table + (long)r * a.columns;
+
+    Frag<T> q[kSteps];
+    {
+      const T *row = (const T *)a.q + ((long)r * a.H + head0 + min(col, heads - 1)) * a.D;
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        Eight<T> e;
+        const int at = 32 * s + 8 * quarter;
+        e.load(row + at, a.D - at);
+        q[s] = a.scale < 0.0f ? -e.v : e.v;
+      }
+    }
+    // Where a lane's two keys of a tile lie: -1 without a page
+    const auto place = [&](int key0, long (&at)[2]) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int key = key0 + 16 * h + col;
+        at[h] = -1;
+        if (key < key_end) {
+          const int column = key / a.page, id = table[column];
+          if (id >= 0 && id < a.pages) at[h] = (((long)id * a.KV + kv) * a.page + (key - column * a.page)) * a.D;
+        }
+      }
+    };
+    const auto load = [&](Frag<T> (&f)[2][kSteps], const void *cache, const long (&at)[2]) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+          const int d = 32 * s + 8 * quarter, n = at[h] < 0 ? 0 : a.D - d;
+          const T *p = (const T *)cache + at[h] + d;
+          Eight<T> e;
+          if (whole) {
+            e.v = Frag<T>{};
+            if (n > 0) e.load(p, 8);
+          } else {
+            e.load(p, n);
+          }
+          f[h][s] = e.v;
+        }
+    };
+
+    floatx4 o[DP / 16];
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i) o[i] = floatx4{};
+    float m = -INFINITY, l = 0.0f;
+    long at[2], next[2];
+    Frag<T> k[2][kSteps], v[2][kSteps];
+    int key0 = key_begin + wave * kTile;
+    place(key0, at);
+    load(k, a.k_cache, at);
+    load(v, a.v_cache, at);
+    place(key0 + kWaves * kTile, next);
+    for (; key0 < key_end; key0 += kWaves * kTile) {
+      // values into LDS, row by row; the rows' same groups of sixteen lanes land in different banks
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+          const int row = 16 * h + col;
+          char *p = area + row * G::kRowBytes;
+          if constexpr (sizeof(T) == 2) {
+            *reinterpret_cast<bf16x8 *>(p + (((4 * s + quarter) ^ G::flip(row)) << 4)) = v[h][s];
+          } else {
+            const int g = (8 * s + 2 * quarter) ^ G::flip(row);
+            *reinterpret_cast<floatx4 *>(p + (g << 4)) = floatx4{v[h][s][0], v[h][s][1], v[h][s][2], v[h][s][3]};
+            *reinterpret_cast<floatx4 *>(p + ((g ^ 1) << 4)) = floatx4{v[h][s][4], v[h][s][5], v[h][s][6], v[h][s][7]};
+          }
+        }
+      load(v, a.v_cache, next);
+      floatx4 z[2] = {};
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) z[h] = mma16(k[h][s], q[s], z[h]);
+      const unsigned long seen0 = __ballot(at[0] >= 0), seen1 = __ballot(at[1] >= 0);   // bits of the first quarter: keys
+      load(k, a.k_cache, next);
+      at[0] = next[0];
+      at[1] = next[1];
+      place(key0 + 2 * kWaves * kTile, next);
+      if ((seen0 & seen1) != ~0ul)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (!(seen0 >> (4 * quarter + j) & 1)) z[0][j] = -INFINITY;
+          if (!(seen1 >> (4 * quarter + j) & 1)) z[1][j] = -INFINITY;
+        }
+      float top = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) top = fmaxf(top, fmaxf(z[0][j], z[1][j]));
+      top = most4(top) * c;
+      if (__any(top > m + 8.0f)) {
+        const float grown = fmaxf(m, top), shrink = grown == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - grown);
+        m = grown;
+        l *= shrink;
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i) o[i] *= shrink;
+      }
+      const float from = m == -INFINITY ? 0.0f : m;
+      Frag<T> p;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j >> 2][j & 3], c, -from));
+        l += e;
+        p[j] = (T)e;
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+      for (int i = 0; i < DP / 16; ++i) {
+        Frag<T> w;
+        if constexpr (sizeof(T) == 2) {
+          typedef __attribute__((address_space(3))) shortx4 *Lp;
+          const int row = 4 * quarter + (col >> 2);
+          const char *at0 = area + row * G::kRowBytes + (((2 * i + ((col & 3) >> 1)) ^ G::flip(row)) << 4) + 8 * (col & 1);
+          const shortx4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lp)at0), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lp)(at0 + 16 * G::kRowBytes));
+          const shortx8 b = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+          w = __builtin_bit_cast(bf16x8, b);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int row = 16 * (j >> 2) + 4 * quarter + (j & 3);
+            w[j] = *reinterpret_cast<const float *>(area + row * G::kRowBytes + (((4 * i + (col >> 2)) ^ G::flip(row)) << 4) + 4 * (col & 3));
+          }
+        }
+        o[i] = mma16(w, p, o[i]);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+    l = sum4(l);
+
+    // the wavefronts' sums joined: o and l relative to the largest maximum
+    if (quarter == 0) ml[wave][col][0] = m, ml[wave][col][1] = l;
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i) *reinterpret_cast<floatx4 *>(area + (col * DP + 16 * i + 4 * quarter) * 4) = o[i];
+    __syncthreads();
+    const bool full = units == per;
+    const int slot = 2 * (int)blockIdx.x + (u == first ? 0 : 1);
+    for (int i = threadIdx.x; i < heads * DP; i += kThreads) {
+      const int h = i / DP, d = i % DP;
+      float top = -INFINITY, sum = 0.0f, out = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[w][h][0]);
+      const float from = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float f = __builtin_amdgcn_exp2f(ml[w][h][0] - from);
+        sum += f * ml[w][h][1];
+        out += f * *reinterpret_cast<const float *>(smem + w * kArea + i * 4);
+      }
+      if (d >= a.D) continue;
+      if (full) {
+        const long to = (long)r * a.H + head0 + h;
+        ((T *)a.o)[to * a.D + d] = (T)(sum == 0.0f ? 0.0f : out / sum);
+        if (a.lse && d == 0) a.lse[to] = sum == 0.0f ? -INFINITY : top * kLn2 + logf(sum);
+      } else {
+        parts.o[((long)slot * kHeads + h) * a.D + d] = out;
+        if (d == 0) parts.ml[(slot * kHeads + h) * 2] = top, parts.ml[(slot * kHeads + h) * 2 + 1] = sum;
+      }
+    }
+    __syncthreads();
+    u += units;
+    if (rel + units == (long)per * VH) {
+      base += (long)per * VH;
+      ++r;
+    }
+  }
+}
+
+// One request's head, where more than one workgroup had a part of it
+template <class T>
+__global__ __launch_bounds__(kThreads) void paged_join_kernel(const CacheArgs a, const Parts parts, int groups) {
+  __shared__ long scratch[2 * kWaves];
+  const int r = blockIdx.x / a.H, head = blockIdx.x % a.H, group = a.H / a.KV, VH = a.KV * parts.blocks;
+  const int per = units_of(keys_of(a, r));
+  long before, all;
+  add_units(a, r, &before, &all, scratch);
+  if (per <= 1) return;
+  all *= VH;
+  groups = working(all, groups);
+  const int in = head % group, h = in % kHeads;
+  const long unit = before * VH + (long)((head / group) * parts.blocks + in / kHeads) * per;
+  const int w0 = owner_of(unit, all, groups), w1 = owner_of(unit + per - 1, all, groups);
+  if (w0 == w1) return;
+  const int slot0 = 2 * w0 + (unit == run_of(w0, all, groups) ? 0 : 1);
+  const auto slot_of = [&](int w) { return w == w0 ? slot0 : 2 * w; };
+  float top = -INFINITY;
+  for (int w = w0; w <= w1; ++w) top = fmaxf(top, parts.ml[(slot_of(w) * kHeads + h) * 2]);
+  const float from = top == -INFINITY ? 0.0f : top;
+  for (int d = threadIdx.x; d < a.D; d += kThreads) {
+    float sum = 0.0f, out = 0.0f;
+    for (int w = w0; w <= w1; ++w) {
+      const int s = slot_of(w) * kHeads + h;
+      const float f = __builtin_amdgcn_exp2f(parts.ml[s * 2] - from);
+      sum += f * parts.ml[s * 2 + 1];
+      out += f * parts.o[(long)s * a.D + d];
+    }
+    const long to = (long)r * a.H + head;
+    ((T *)a.o)[to * a.D + d] = (T)(sum == 0.0f ? 0.0f : out / sum);
+    if (a.lse && d == 0) a.lse[to] = sum == 0.0f ? -INFINITY : top * kLn2 + logf(sum);
+  }
+}
+
+// Workgroups: no more than units that there may be
+int groups_of(const CacheArgs &a) {
+  const long room = (long)a.columns * a.page, blocks = (a.H / a.KV + kHeads - 1) / kHeads;
+  const long units = ((room + kUnit - 1) / kUnit) * a.R * a.KV * blocks;
+  return (int)(units < kGroups ? units : kGroups);
+}
+
+// The workspace's parts, the same walk for the query and the call
+struct PagedParts {
+  Parts parts;
+  size_t bytes;
+  PagedParts(const CacheArgs &a, char *base) {
+    Take take{base};
+    const int groups = groups_of(a);
+    parts.blocks = (a.H / a.KV + kHeads - 1) / kHeads;
+    parts.o = (float *)take((size_t)2 * groups * kHeads * a.D * sizeof(float));
+    parts.ml = (float *)take((size_t)2 * groups * kHeads * 2 * sizeof(float));
+    bytes = take.used;
+  }
+};
+
+template <class T, int DP>
+hipError_t paged_as(const CacheArgs &a, const Parts &parts, hipStream_t stream) {
+  constexpr size_t lds = kWaves * kTile * Tile<T, DP>::kRowBytes + sizeof(Shared);
+  const auto kernel = paged_attention_kernel<T, DP>;
+  DLL_TRY(allow_large_lds(reinterpret_cast<const void *>(kernel), lds));
+  const int groups = groups_of(a);
+  kernel<<<dim3((unsigned)groups), dim3(kThreads), lds, stream>>>(a, parts);
+  DLL_TRY(hipGetLastError());
+  if ((long)a.columns * a.page <= kUnit) return hipSuccess;   // one unit a request and head
+  paged_join_kernel<T><<<dim3((unsigned)(a.R * a.H)), dim3(kThreads), 0, stream>>>(a, parts, groups);
+  return hipGetLastError();
+}
+
+template <class T>
+hipError_t paged(const CacheArgs &a, const Parts &parts, hipStream_t stream) {
+  if (a.D <= 32) return paged_as<T, 32>(a, parts, stream);
+  if (a.D <= 64) return paged_as<T, 64>(a, parts, stream);
+  if (a.D <= 96) return paged_as<T, 96>(a, parts, stream);
+  if (a.D <= 128) return paged_as<T, 128>(a, parts, stream);
+  return paged_as<T, 256>(a, parts, stream);
+}
+
+}  // namespace
+
+size_t paged_attention_scratch(const CacheArgs &a) { return PagedParts(a, nullptr).bytes; }
+
+hipError_t launch_paged_attention(const CacheArgs &a, char *scratch, hipStream_t stream) {
+  const PagedParts p(a, scratch);
+  return a.dtype == TYPE_BF16 ? paged<bf16>(a, p.parts, stream) : paged<float>(a, p.parts, stream);
+}
+
+}  // namespace dllk

@@ -109,6 +109,19 @@ class AttentionSpec:
     kv_row: int = 0
 
 
+@dataclass(frozen=True)
+class CacheSpec:
+    """A cache of keys and values of `pages` pages of `page_tokens` tokens each, and a table of `table_pages` pages a request."""
+    requests: int
+    heads: int
+    kv_heads: int
+    head_dim: int
+    pages: int
+    page_tokens: int
+    table_pages: int
+    dtype: str = "bfloat16"
+
+
 @dataclass
 class ConvWorkload:
     cfg: int

@@ -6,7 +6,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from paper_1804_04512_amd import binding as B
-from paper_1804_04512_amd.workloads import AttentionSpec
+from paper_1804_04512_amd.workloads import AttentionSpec, CacheSpec
 
 OK, NULL, SHAPE, UNSUPPORTED, WORKSPACE = 0, 1, 2, 3, 4
 P = [C.c_void_p(0x10000 * k) for k in range(1, 20)]   # never dereferenced: every call below is refused
@@ -90,3 +90,65 @@ def test_binding_checks_rows():
             B._head_rows(bad, (5, 2 if bad is k else 4, 16), row, torch.float32, "k", cpu)
     with pytest.raises(KeyError):
         B.attention_desc(AttentionSpec(1, 1, 1, 1, 1, 1, True, "float16"))
+
+
+def cache(**over):
+    d = B.cache_desc(CacheSpec(4, 8, 2, 64, 100, 16, 10, "float32"))
+    for k, v in over.items():
+        setattr(d, k, v)
+    return C.byref(d)
+
+
+def plan(L, d, p=P, n_free=5, free_at=P[17], tokens=9):
+    return L.dll_cache_plan(d, p[0], p[1], p[2], n_free, free_at, *p[3:6], tokens, p[6], None)
+
+
+def store(L, d, p=P, tokens=9, row=0):
+    return L.dll_cache_write(d, tokens, row, *p[:5], None)
+
+
+def paged(L, d, p=P, scale=1.0, lse=P[12], ws=P[14], room=BIG):
+    return L.dll_paged_attention(d, *p[:5], scale, p[5], lse, ws, room, None)
+
+
+@pytest.mark.parametrize("over,status", [
+    (dict(requests=0), SHAPE), (dict(heads=0), SHAPE), (dict(heads=7), SHAPE), (dict(kv_heads=-2), SHAPE), (dict(head_dim=0), SHAPE), (dict(pages=0), SHAPE),
+    (dict(page_tokens=0), SHAPE), (dict(table_pages=-1), SHAPE), (dict(dtype=5), UNSUPPORTED), (dict(head_dim=257), UNSUPPORTED),
+    (dict(requests=(1 << 16) + 1), UNSUPPORTED), (dict(requests=1 << 14, heads=1 << 11), UNSUPPORTED), (dict(pages=1 << 28), UNSUPPORTED),
+    (dict(table_pages=(1 << 26) + 1), UNSUPPORTED), (dict(requests=1 << 12, table_pages=1 << 19), UNSUPPORTED)], ids=str)
+def test_cache_descriptors(over, status):
+    L = B.lib()
+    d = cache(**over)
+    assert L.dll_paged_attention_workspace_bytes(d) == 0
+    assert plan(L, d) == store(L, d) == paged(L, d) == status
+
+
+def test_cache_pointers():
+    L = B.lib()
+    d = cache()
+    swap = lambda k, v: [*P[:k], v, *P[k + 1:]]
+    at = lambda k, off: C.c_void_p(P[k].value + off)
+    for k in range(7):
+        assert plan(L, d, swap(k, None)) == NULL and plan(L, d, swap(k, at(k, 2))) == SHAPE
+    assert plan(L, None) == store(L, None) == paged(L, None) == NULL
+    assert plan(L, d, n_free=-1) == SHAPE and plan(L, d, tokens=0) == SHAPE and plan(L, d, tokens=(1 << 24) + 1) == UNSUPPORTED
+    assert plan(L, d, free_at=P[6]) == SHAPE and plan(L, d, free_at=at(17, 2)) == SHAPE   # other workgroups still read it
+    assert plan(L, d, swap(3, P[2])) == SHAPE and plan(L, d, swap(4, P[0])) == SHAPE and plan(L, d, swap(5, P[4])) == SHAPE
+    for k in range(5):
+        assert store(L, d, swap(k, None)) == NULL
+    for k, off in ((0, 2), (1, 1), (2, 2), (3, 8), (4, 4)):
+        assert store(L, d, swap(k, at(k, off))) == SHAPE
+    assert store(L, d, tokens=0) == SHAPE and store(L, d, row=127) == SHAPE and store(L, d, row=-1) == SHAPE
+    assert store(L, d, tokens=(1 << 24) + 1) == store(L, d, row=(1 << 20) + 1) == store(L, d, tokens=1 << 20, row=1 << 11) == UNSUPPORTED
+    assert store(L, d, swap(3, P[0])) == SHAPE and store(L, d, swap(4, P[3])) == SHAPE
+    need = L.dll_paged_attention_workspace_bytes(d)
+    assert need > 0 and need % 256 == 0
+    for k in range(6):
+        assert paged(L, d, swap(k, None)) == NULL
+    for k, off in ((0, 8), (1, 8), (2, 8), (3, 2), (4, 2), (5, 8)):
+        assert paged(L, d, swap(k, at(k, off))) == SHAPE
+    assert paged(L, d, lse=at(12, 2)) == SHAPE and paged(L, d, lse=P[5]) == SHAPE and paged(L, d, swap(5, P[0])) == SHAPE
+    for bad in (INF, NAN):
+        assert paged(L, d, scale=bad) == SHAPE
+    assert paged(L, d, room=need - 1) == paged(L, d, ws=None) == paged(L, d, ws=at(14, 16)) == WORKSPACE
+    assert paged(L, d, lse=None, room=0) == WORKSPACE
