@@ -21,7 +21,20 @@ using namespace attn;
 namespace {
 
 constexpr int kThreads = 256, kWaves = 4, kTile = 32, kUnit = 128, kHeads = 16;
-constexpr int kGroups = 1024;   // workgroups of a launch: four a compute unit
+constexpr int kMaxGroups = 1024;   // workgroups of a launch
+
+// n / d for n below 2^30: n * (floor(2^(30 + shift) / d) + 1) / 2^(30 + shift), off by less than 1 / d where 2^shift >= d
+struct Divisor {
+  unsigned factor, shift;
+  explicit Divisor(int d) : shift(0) {
+    while (1L << shift < d) ++shift;
+    factor = (unsigned)((1L << (30 + shift)) / d + 1);
+  }
+  __device__ __forceinline__ int of(int n) const { return (int)(__umulhi((unsigned)n << 2, factor) >> shift); }
+};
+
+// workgroups that a compute unit holds, by their registers
+template <class T, int DP> constexpr int residents() { return (sizeof(T) == 2 ? DP <= 128 : DP <= 96) ? 2 : 1; }
 
 __device__ __forceinline__ floatx4 mma16(bf16x8 a, bf16x8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ floatx4 mma16(floatx8 a, floatx8 b, floatx4 c) {
@@ -38,8 +51,9 @@ __device__ __forceinline__ int keys_of(const CacheArgs &a, int r) { return (int)
 __device__ __forceinline__ int units_of(int keys) { return (keys + kUnit - 1) / kUnit; }
 
 struct Parts {
-  float *o;    // [2 kGroups][kHeads][D], relative to the maximum
-  float *ml;   // [2 kGroups][kHeads][2]: maximum in the exponent's base, sum
+  float *o;    // [2 groups][kHeads][ld], relative to the maximum
+  float *ml;   // [2 groups][kHeads][2]: maximum in the exponent's base, sum
+  int ld;      // head_dim in whole fours
   int blocks;  // of at most kHeads heads that share a key head
 };
 
@@ -73,8 +87,10 @@ struct Shared {
   float ml[kWaves][kHeads][2];
 };
 
-template <class T, int DP>
-__global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DP <= 128 : DP <= 96) ? 2 : 1) void paged_attention_kernel(const CacheArgs a, const Parts parts) {
+// WHOLE: a head's rows are whole runs of eight elements, so every load is 16 bytes or more from a place that exists and no branch stands
+// between the loads; what a lane has no run for it takes from its row's last one, against zeros of q.
+template <class T, int DP, bool WHOLE>
+__global__ __launch_bounds__(kThreads, (residents<T, DP>())) void paged_attention_kernel(const CacheArgs a, const Parts parts, const Divisor page) {
   typedef Tile<T, DP> G;
   constexpr int kSteps = DP / 32, kArea = kTile * G::kRowBytes;   // LDS of a wavefront: its values, or at the end its sums [16][DP] fp32
   static_assert(kArea >= kHeads * DP * 4, "");
@@ -85,7 +101,6 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DP <= 128 : DP <= 96) ?
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4, col = lane & 15;
   char *area = smem + wave * kArea;
   const int group = a.H / a.KV, blocks = parts.blocks, VH = a.KV * blocks;
-  const bool whole = a.D % 8 == 0;
   const float c = fmaxf(fabsf(a.scale) * kLog2e, 0x1p-126f);
 
   // requests without keys
@@ -134,6 +149,11 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DP <= 128 : DP <= 96) ?
   int r = __builtin_amdgcn_readfirstlane(shared.found);
   long base = scratch[kWaves];
 
+  int off[kSteps];   // a lane's run of each step in its row, in bytes
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) off[s] = min(32 * s + 8 * quarter, a.D - 8) * (int)sizeof(T);
+  const long row_bytes = (long)a.D * (int)sizeof(T), head_bytes = a.page * row_bytes, page_bytes = a.KV * head_bytes;
+
   for (long u = first; u < end;) {
     const int keys = __builtin_amdgcn_readfirstlane(keys_of(a, r)), per = units_of(keys);
     if (per == 0) {   // r stays in range: units before `end` are somebody's
@@ -145,6 +165,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DP <= 128 : DP <= 96) ?
     const int kv = vh / blocks, block = vh % blocks, heads = min(kHeads, group - block * kHeads), head0 = kv * group + block * kHeads;
     const int key_begin = unit0 * kUnit, key_end = min(keys, (unit0 + units) * kUnit);
     const int *table = a.table + (long)r * a.columns;
+    const char *k_head = (const char *)a.k_cache + kv * head_bytes, *v_head = (const char *)a.v_cache + kv * head_bytes;
 
     Frag<T> q[kSteps];
     {
@@ -157,48 +178,69 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DP <= 128 : DP <= 96) ?
         q[s] = a.scale < 0.0f ? -e.v : e.v;
       }
     }
-    // Where a lane's two keys of a tile lie: -1 without a page
-    const auto place = [&](int key0, long (&at)[2]) {
+    // A lane's two keys of a tile: their pages (-1: none), and where their rows lie.  A key without a page gets a row of page 0, which
+    // exists.
+    const auto pages = [&](int key0, int (&id)[2]) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int key = key0 + 16 * h + col;
-        at[h] = -1;
-        if (key < key_end) {
-          const int column = key / a.page, id = table[column];
-          if (id >= 0 && id < a.pages) at[h] = (((long)id * a.KV + kv) * a.page + (key - column * a.page)) * a.D;
-        }
+        id[h] = table[page.of(min(key, key_end - 1))];
+        if (key >= key_end) id[h] = -1;
       }
     };
-    const auto load = [&](Frag<T> (&f)[2][kSteps], const void *cache, const long (&at)[2]) {
+    const auto places = [&](int key0, const int (&id)[2], long (&at)[2]) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < 2; ++h) {
+        const int key = key0 + 16 * h + col;
+        at[h] = (unsigned)id[h] < (unsigned)a.pages ? id[h] * page_bytes + (key - page.of(key) * a.page) * row_bytes : -1;
+      }
+    };
+    const auto load = [&](Frag<T> (&f)[2][kSteps], const char *head, const long (&at)[2]) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const char *row = head + max(at[h], 0L);
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
-          const int d = 32 * s + 8 * quarter, n = at[h] < 0 ? 0 : a.D - d;
-          const T *p = (const T *)cache + at[h] + d;
           Eight<T> e;
-          if (whole) {
-            e.v = Frag<T>{};
-            if (n > 0) e.load(p, 8);
+          if (WHOLE) {
+            e.load(reinterpret_cast<const T *>(row + off[s]), 8);
           } else {
-            e.load(p, n);
+            const int d = 32 * s + 8 * quarter;
+            e.load(reinterpret_cast<const T *>(row) + d, a.D - d);
           }
           f[h][s] = e.v;
         }
+      }
     };
 
     floatx4 o[DP / 16];
 #pragma unroll
     for (int i = 0; i < DP / 16; ++i) o[i] = floatx4{};
     float m = -INFINITY, l = 0.0f;
+    // On their way while a tile is worked on: the next one's values and keys, and the pages of the one behind it, which are asked
+    // for first: loads come back in order, and the next rows' addresses must not wait for rows.
+    int key0 = key_begin + wave * kTile, id[2], id_next[2];
     long at[2], next[2];
     Frag<T> k[2][kSteps], v[2][kSteps];
-    int key0 = key_begin + wave * kTile;
-    place(key0, at);
-    load(k, a.k_cache, at);
-    load(v, a.v_cache, at);
-    place(key0 + kWaves * kTile, next);
-    for (; key0 < key_end; key0 += kWaves * kTile) {
+    constexpr int kNext = kWaves * kTile;
+    pages(key0, id);
+    pages(key0 + kNext, id_next);
+    places(key0, id, at);
+    load(v, v_head, at);
+    __builtin_amdgcn_sched_barrier(0);
+    load(k, k_head, at);
+    __builtin_amdgcn_sched_barrier(0);
+    for (; key0 < key_end; key0 += kNext) {
+      places(key0 + kNext, id_next, next);
+      pages(key0 + 2 * kNext, id_next);
+      __builtin_amdgcn_sched_barrier(0);
+      const unsigned long seen0 = __ballot(at[0] >= 0), seen1 = __ballot(at[1] >= 0);   // bits of the first quarter: keys
+      if ((seen0 & seen1) != ~0ul)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int s = 0; s < kSteps; ++s)
+            if (at[h] < 0) v[h][s] = Frag<T>{};
       // values into LDS, row by row; the rows' same groups of sixteen lanes land in different banks
 #pragma unroll
       for (int h = 0; h < 2; ++h)
@@ -214,17 +256,19 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DP <= 128 : DP <= 96) ?
             *reinterpret_cast<floatx4 *>(p + ((g ^ 1) << 4)) = floatx4{v[h][s][4], v[h][s][5], v[h][s][6], v[h][s][7]};
           }
         }
-      load(v, a.v_cache, next);
+      __builtin_amdgcn_sched_barrier(0);
+      load(v, v_head, next);
+      __builtin_amdgcn_sched_barrier(0);
       floatx4 z[2] = {};
 #pragma unroll
       for (int s = 0; s < kSteps; ++s)
 #pragma unroll
         for (int h = 0; h < 2; ++h) z[h] = mma16(k[h][s], q[s], z[h]);
-      const unsigned long seen0 = __ballot(at[0] >= 0), seen1 = __ballot(at[1] >= 0);   // bits of the first quarter: keys
-      load(k, a.k_cache, next);
+      __builtin_amdgcn_sched_barrier(0);
+      load(k, k_head, next);
+      __builtin_amdgcn_sched_barrier(0);
       at[0] = next[0];
       at[1] = next[1];
-      place(key0 + 2 * kWaves * kTile, next);
       if ((seen0 & seen1) != ~0ul)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -251,24 +295,29 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DP <= 128 : DP <= 96) ?
         p[j] = (T)e;
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      constexpr int kAhead = DP * (int)sizeof(T) <= 256 ? DP / 16 : DP % 64 ? 3 : 4;   // fragments read at a time
+      static_assert(DP / 16 % kAhead == 0, "");
+      Frag<T> w[kAhead];
 #pragma unroll
       for (int i = 0; i < DP / 16; ++i) {
-        Frag<T> w;
         if constexpr (sizeof(T) == 2) {
           typedef __attribute__((address_space(3))) shortx4 *Lp;
           const int row = 4 * quarter + (col >> 2);
           const char *at0 = area + row * G::kRowBytes + (((2 * i + ((col & 3) >> 1)) ^ G::flip(row)) << 4) + 8 * (col & 1);
           const shortx4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lp)at0), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lp)(at0 + 16 * G::kRowBytes));
           const shortx8 b = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-          w = __builtin_bit_cast(bf16x8, b);
+          w[i % kAhead] = __builtin_bit_cast(bf16x8, b);
         } else {
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             const int row = 16 * (j >> 2) + 4 * quarter + (j & 3);
-            w[j] = *reinterpret_cast<const float *>(area + row * G::kRowBytes + (((4 * i + (col >> 2)) ^ G::flip(row)) << 4) + 4 * (col & 3));
+            w[i % kAhead][j] = *reinterpret_cast<const float *>(area + row * G::kRowBytes + (((4 * i + (col >> 2)) ^ G::flip(row)) << 4) + 4 * (col & 3));
           }
         }
-        o[i] = mma16(w, p, o[i]);
+        if (i % kAhead < kAhead - 1) continue;
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int b = 0; b < kAhead; ++b) o[i - kAhead + 1 + b] = mma16(w[b], p, o[i - kAhead + 1 + b]);
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
@@ -299,7 +348,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DP <= 128 : DP <= 96) ?
         ((T *)a.o)[to * a.D + d] = (T)(sum == 0.0f ? 0.0f : out / sum);
         if (a.lse && d == 0) a.lse[to] = sum == 0.0f ? -INFINITY : top * kLn2 + logf(sum);
       } else {
-        parts.o[((long)slot * kHeads + h) * a.D + d] = out;
+        parts.o[((long)slot * kHeads + h) * parts.ld + d] = out;
         if (d == 0) parts.ml[(slot * kHeads + h) * 2] = top, parts.ml[(slot * kHeads + h) * 2 + 1] = sum;
       }
     }
@@ -312,45 +361,68 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DP <= 128 : DP <= 96) ?
   }
 }
 
-// One request's head, where more than one workgroup had a part of it
+// One request's head, where more than one workgroup had a part of it: the parts' factors first, then their outputs, four elements a thread
+// and as many parts side by side as there are threads
 template <class T>
 __global__ __launch_bounds__(kThreads) void paged_join_kernel(const CacheArgs a, const Parts parts, int groups) {
   __shared__ long scratch[2 * kWaves];
-  const int r = blockIdx.x / a.H, head = blockIdx.x % a.H, group = a.H / a.KV, VH = a.KV * parts.blocks;
+  __shared__ float factor[kMaxGroups], level[2][kWaves];
+  __shared__ floatx4 sums[kThreads];
+  const int r = blockIdx.x / a.H, head = blockIdx.x % a.H, group = a.H / a.KV, VH = a.KV * parts.blocks, t = threadIdx.x;
   const int per = units_of(keys_of(a, r));
+  if (per <= 1) return;
   long before, all;
   add_units(a, r, &before, &all, scratch);
-  if (per <= 1) return;
   all *= VH;
   groups = working(all, groups);
   const int in = head % group, h = in % kHeads;
   const long unit = before * VH + (long)((head / group) * parts.blocks + in / kHeads) * per;
-  const int w0 = owner_of(unit, all, groups), w1 = owner_of(unit + per - 1, all, groups);
-  if (w0 == w1) return;
+  const int w0 = owner_of(unit, all, groups), n = owner_of(unit + per - 1, all, groups) - w0 + 1;
+  if (n == 1) return;
   const int slot0 = 2 * w0 + (unit == run_of(w0, all, groups) ? 0 : 1);
-  const auto slot_of = [&](int w) { return w == w0 ? slot0 : 2 * w; };
+  const auto row_of = [&](int i) { return (i == 0 ? slot0 : 2 * (w0 + i)) * kHeads + h; };
   float top = -INFINITY;
-  for (int w = w0; w <= w1; ++w) top = fmaxf(top, parts.ml[(slot_of(w) * kHeads + h) * 2]);
+  for (int i = t; i < n; i += kThreads) top = fmaxf(top, parts.ml[row_of(i) * 2]);
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+  if ((t & 63) == 0) level[0][t >> 6] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, level[0][w]);
   const float from = top == -INFINITY ? 0.0f : top;
-  for (int d = threadIdx.x; d < a.D; d += kThreads) {
-    float sum = 0.0f, out = 0.0f;
-    for (int w = w0; w <= w1; ++w) {
-      const int s = slot_of(w) * kHeads + h;
-      const float f = __builtin_amdgcn_exp2f(parts.ml[s * 2] - from);
-      sum += f * parts.ml[s * 2 + 1];
-      out += f * parts.o[(long)s * a.D + d];
-    }
-    const long to = (long)r * a.H + head;
-    ((T *)a.o)[to * a.D + d] = (T)(sum == 0.0f ? 0.0f : out / sum);
-    if (a.lse && d == 0) a.lse[to] = sum == 0.0f ? -INFINITY : top * kLn2 + logf(sum);
+  float sum = 0.0f;
+  for (int i = t; i < n; i += kThreads) {
+    const float f = __builtin_amdgcn_exp2f(parts.ml[row_of(i) * 2] - from);
+    factor[i] = f;
+    sum += f * parts.ml[row_of(i) * 2 + 1];
   }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+  if ((t & 63) == 0) level[1][t >> 6] = sum;
+  __syncthreads();
+  sum = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) sum += level[1][w];
+  const int wide = parts.ld / 4, side = kThreads / wide, c = t % wide, p = t / wide;   // wide: 1 to 64
+  floatx4 out = {};
+  if (p < side)
+    for (int i = p; i < n; i += side) out += factor[i] * *reinterpret_cast<const floatx4 *>(parts.o + (long)row_of(i) * parts.ld + 4 * c);
+  sums[t] = out;
+  __syncthreads();
+  if (p > 0) return;
+  for (int i = 1; i < side; ++i) out += sums[i * wide + c];
+  const long to = (long)r * a.H + head;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (4 * c + j < a.D) ((T *)a.o)[to * a.D + 4 * c + j] = (T)(sum == 0.0f ? 0.0f : out[j] / sum);
+  if (a.lse && t == 0) a.lse[to] = sum == 0.0f ? -INFINITY : top * kLn2 + logf(sum);
 }
 
-// Workgroups: no more than units that there may be
-int groups_of(const CacheArgs &a) {
-  const long room = (long)a.columns * a.page, blocks = (a.H / a.KV + kHeads - 1) / kHeads;
-  const long units = ((room + kUnit - 1) / kUnit) * a.R * a.KV * blocks;
-  return (int)(units < kGroups ? units : kGroups);
+int blocks_of(const CacheArgs &a) { return (a.H / a.KV + kHeads - 1) / kHeads; }
+// Workgroups: as many as the chip holds, and no more than units that there may be
+int groups_of(const CacheArgs &a, int resident) {
+  const long room = (long)a.columns * a.page, units = ((room + kUnit - 1) / kUnit) * a.R * a.KV * blocks_of(a), most = (long)resident * chip().cus;
+  return (int)(units < most ? units : most < kMaxGroups ? most : kMaxGroups);
 }
 
 // The workspace's parts, the same walk for the query and the call
@@ -359,21 +431,22 @@ struct PagedParts {
   size_t bytes;
   PagedParts(const CacheArgs &a, char *base) {
     Take take{base};
-    const int groups = groups_of(a);
-    parts.blocks = (a.H / a.KV + kHeads - 1) / kHeads;
-    parts.o = (float *)take((size_t)2 * groups * kHeads * a.D * sizeof(float));
-    parts.ml = (float *)take((size_t)2 * groups * kHeads * 2 * sizeof(float));
+    const size_t rows = (size_t)2 * groups_of(a, 2) * kHeads;
+    parts.blocks = blocks_of(a);
+    parts.ld = (a.D + 3) & ~3;
+    parts.o = (float *)take(rows * parts.ld * sizeof(float));
+    parts.ml = (float *)take(rows * 2 * sizeof(float));
     bytes = take.used;
   }
 };
 
-template <class T, int DP>
+template <class T, int DP, bool WHOLE>
 hipError_t paged_as(const CacheArgs &a, const Parts &parts, hipStream_t stream) {
   constexpr size_t lds = kWaves * kTile * Tile<T, DP>::kRowBytes + sizeof(Shared);
-  const auto kernel = paged_attention_kernel<T, DP>;
+  const auto kernel = paged_attention_kernel<T, DP, WHOLE>;
   DLL_TRY(allow_large_lds(reinterpret_cast<const void *>(kernel), lds));
-  const int groups = groups_of(a);
-  kernel<<<dim3((unsigned)groups), dim3(kThreads), lds, stream>>>(a, parts);
+  const int groups = groups_of(a, residents<T, DP>());
+  kernel<<<dim3((unsigned)groups), dim3(kThreads), lds, stream>>>(a, parts, Divisor(a.page));
   DLL_TRY(hipGetLastError());
   if ((long)a.columns * a.page <= kUnit) return hipSuccess;   // one unit a request and head
   paged_join_kernel<T><<<dim3((unsigned)(a.R * a.H)), dim3(kThreads), 0, stream>>>(a, parts, groups);
@@ -382,11 +455,12 @@ hipError_t paged_as(const CacheArgs &a, const Parts &parts, hipStream_t stream) 
 
 template <class T>
 hipError_t paged(const CacheArgs &a, const Parts &parts, hipStream_t stream) {
-  if (a.D <= 32) return paged_as<T, 32>(a, parts, stream);
-  if (a.D <= 64) return paged_as<T, 64>(a, parts, stream);
-  if (a.D <= 96) return paged_as<T, 96>(a, parts, stream);
-  if (a.D <= 128) return paged_as<T, 128>(a, parts, stream);
-  return paged_as<T, 256>(a, parts, stream);
+  if (a.D % 8) return a.D <= 64 ? paged_as<T, 64, false>(a, parts, stream) : a.D <= 128 ? paged_as<T, 128, false>(a, parts, stream) : paged_as<T, 256, false>(a, parts, stream);
+  if (a.D <= 32) return paged_as<T, 32, true>(a, parts, stream);
+  if (a.D <= 64) return paged_as<T, 64, true>(a, parts, stream);
+  if (a.D <= 96) return paged_as<T, 96, true>(a, parts, stream);
+  if (a.D <= 128) return paged_as<T, 128, true>(a, parts, stream);
+  return paged_as<T, 256, true>(a, parts, stream);
 }
 
 }  // namespace
