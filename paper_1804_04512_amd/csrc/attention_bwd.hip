@@ -17,7 +17,7 @@ namespace {
 
 constexpr int kRows = 128, kThreads = 256;
 
-template <class T, int DP> constexpr int tile_rows() { return Tile<T, DP>::kRowBytes >= 512 ? 32 : 64; }
+template <class T, int DP> constexpr int tile_rows() { return DP > 128 || (sizeof(T) == 4 && DP > 64) ? 32 : 64; }
 
 // Four bytes a lane from the buffer to 256 bytes of LDS, as load_to_lds
 __device__ __forceinline__ void load_words_to_lds(const uintx4 &rs, unsigned off, unsigned lds) {
@@ -30,28 +30,34 @@ struct Rows {
   float *lse2, *minus_delta;
 };
 
+// The sum of two rows' products, over both lane halves
 template <class T, int DP>
-__device__ __forceinline__ float row_delta(const Frag<T> (&g)[DP / 16], const T *o, int dim, int half) {
+__device__ __forceinline__ float row_product(const T *x, const T *y, int dim, int half) {
   float sum = 0.0f;
 #pragma unroll
   for (int s = 0; s < DP / 16; ++s) {
-    Eight<T> e;
+    Eight<T> e, f;
     const int at = 16 * s + 8 * half;
-    e.load(o + at, dim - at);
+    e.load(x + at, dim - at);
+    f.load(y + at, dim - at);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum += to_float(g[s][j]) * to_float(e.v[j]);
+    for (int j = 0; j < 8; ++j) sum += to_float(e.v[j]) * to_float(f.v[j]);
   }
   return sum + other_half(sum);
 }
 
 // ------------------------------------------------------------------------------------------------ dq
+// workgroups that a compute unit holds, by their registers
+template <class T, int DP> constexpr int dq_residents() { return (sizeof(T) == 2 ? DP <= 128 : DP <= 64) ? 2 : 1; }
+
 // dq may be NULL: then the rows' figures are all that is wanted
 template <class T, int DP, int BN>
-__global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DP <= 96 : DP <= 64) ? 2 : 1) void attention_dq_kernel(const AttentionArgs a, const Rows rows, const int tiles) {
+__global__ __launch_bounds__(kThreads, (dq_residents<T, DP>())) void attention_dq_kernel(const AttentionArgs a, const Rows rows, const Parts parts, const int tiles) {
   typedef Stager<T, DP, BN, kThreads> S;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-  const int kv = blockIdx.x % a.KV, rest = blockIdx.x / a.KV, group = a.H / a.KV, head = kv * group + rest % group, tile = tiles - 1 - rest / group;
+  const int part = blockIdx.x % parts.n, id = blockIdx.x / parts.n, kv = id % a.KV, rest = id / a.KV, group = a.H / a.KV, head = kv * group + rest % group,
+            tile = tiles - 1 - rest / group;
   const Place pq = place_of(a.q_starts, a.S, a.Tq, tile, kRows);
   if (pq.at >= pq.count) return;
   const int kv_first = start_of(a.kv_starts, pq.sequence, a.Tk), keys = max(0, start_of(a.kv_starts, pq.sequence + 1, a.Tk) - kv_first);
@@ -61,40 +67,37 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DP <= 96 : DP <= 64) ? 
   const int seen_last = row0 >= pq.count ? 0 : a.causal ? max(0, min(keys, min(row0 + 32, pq.count) + shift)) : keys;
   const int seen_all = a.causal ? max(0, min(keys, min(pq.at + kRows, pq.count) + shift)) : keys;
 
-  Frag<T> g[DP / 16];
   const long at = pq.first + min(row, pq.count - 1);
-  load_row<T, DP>(g, (const T *)a.d_o + at * a.H * a.D + head * a.D, a.D, half);
-  const float minus_delta = -row_delta<T, DP>(g, (const T *)a.o + at * a.H * a.D + head * a.D, a.D, half);
+  const T *g_row = (const T *)a.d_o + at * a.H * a.D + head * a.D;
+  const float minus_delta = -row_product<T, DP>(g_row, (const T *)a.o + at * a.H * a.D + head * a.D, a.D, half);
   const float lse2 = a.lse[(long)head * a.Tq + at] * kLog2e;
-  if (half == 0 && row < pq.count) {
+  if (part == 0 && half == 0 && row < pq.count) {
     rows.lse2[(long)head * a.Tq + at] = lse2;
     rows.minus_delta[(long)head * a.Tq + at] = minus_delta;
   }
   if (!a.dq) return;
 
+  const T *k = (const T *)a.k + (long)kv_first * a.kv_row + kv * a.D, *v = (const T *)a.v + (long)kv_first * a.kv_row + kv * a.D;
   S sk, sv;
-  sk.init((const T *)a.k + (long)kv_first * a.kv_row + kv * a.D, a.kv_row, a.D, threadIdx.x);
-  sv.init((const T *)a.v + (long)kv_first * a.kv_row + kv * a.D, a.kv_row, a.D, threadIdx.x);
-  const auto load = [&](int stage, int key0) {
-    char *to = smem + stage * 2 * S::kBytes;
-    sk.load(to, wave, key0, keys);
-    sv.load(to + S::kBytes, wave, key0, keys);
-  };
-  load(0, 0);
-  Frag<T> q[DP / 16];
-  load_row<T, DP>(q, (const T *)a.q + at * a.q_row + head * a.D, a.D, half);
+  sk.init(smem, k, a.kv_row, a.D);
+  sv.init(smem + S::kBytes, v, a.kv_row, a.D);
+  const int turns = (seen_all + BN - 1) / BN, begin = turn_from(part, parts.n, turns) * BN, end = min(seen_all, turn_from(part + 1, parts.n, turns) * BN);
+  sk.start(wave, k, begin, keys);
+  sv.start(wave, v, begin, keys);
+  RowFrags<T, DP> q, g;
+  q.load((const T *)a.q + at * a.q_row + head * a.D, a.D, half);
+  g.load(g_row, a.D, half);
   const float c = a.scale * kLog2e;
 
   floatx16 dq[DP / 32];
 #pragma unroll
   for (int i = 0; i < DP / 32; ++i) dq[i] = floatx16{};
-  const Reader<T, DP> reader(lane);
-  int stage = 0;
-  for (int key0 = 0; key0 < seen_all; key0 += BN, stage ^= 1) {
-    load(stage ^ 1, key0 + BN);
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * S::kLoads) : "memory");
+  const Reader<T, DP, BN> reader(lane);
+  int odd = 1;
+  for (int key0 = begin; key0 < end; key0 += BN, odd ^= 1) {
+    const char *lk = sk.turn(wave, odd, k, key0 + BN, keys), *lv = sv.turn(wave, odd, v, key0 + BN, keys);
+    landed<T, 2 * S::kLoads>();
     barrier();
-    const char *lk = smem + stage * 2 * S::kBytes, *lv = lk + S::kBytes;
 #pragma unroll 1
     for (int b = 0; b < BN && key0 + b < seen_last; b += 32) {
       floatx16 z = {}, d;
@@ -125,19 +128,22 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DP <= 96 : DP <= 64) ? 
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   if (row >= pq.count) return;
+  if (parts.n > 1) return store_sums(parts.sums[0] + (((long)part * a.Tq + at) * a.H + head) * parts.ld, dq, parts.ld, half);
   store_row<T>((T *)a.dq + at * a.q_row + head * a.D, dq, a.scale, a.D, half);
 }
 
 // ------------------------------------------------------------------------------------------------ dk, dv
 // DK, DV: which of the two this instance takes (single precision with more than 128 elements a head takes them one after the other, as their
 // sums and both rows would not fit the registers)
+template <class T, int DP> constexpr int dkv_residents() { return (sizeof(T) == 2 ? DP <= 64 : DP <= 32) ? 2 : 1; }
+
 template <class T, int DP, int BN, bool DK, bool DV>
-__global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DP <= 64 : DP <= 32) ? 2 : 1) void attention_dkv_kernel(const AttentionArgs a, const Rows rows) {
+__global__ __launch_bounds__(kThreads, (dkv_residents<T, DP>())) void attention_dkv_kernel(const AttentionArgs a, const Rows rows, const Parts parts) {
   typedef Stager<T, DP, BN, kThreads> S;
-  constexpr int kStage = 2 * S::kBytes + 2 * 256, kWait = 2 * S::kLoads + 1;
+  constexpr int kFigures = 256;   // bytes of one kind of figures of a tile
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-  const int kv = blockIdx.x % a.KV, tile = blockIdx.x / a.KV, group = a.H / a.KV;
+  const int part = blockIdx.x % parts.n, id = blockIdx.x / parts.n, kv = id % a.KV, tile = id / a.KV, group = a.H / a.KV;
   const Place pk = place_of(a.kv_starts, a.S, a.Tk, tile, kRows);
   if (pk.at >= pk.count) return;
   const int q_first = start_of(a.q_starts, pk.sequence, a.Tq), queries = max(0, start_of(a.q_starts, pk.sequence + 1, a.Tq) - q_first);
@@ -147,9 +153,9 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DP <= 64 : DP <= 32) ? 
   const int sees_first = key0 - shift, sees_all = key0 + 31 - shift;
 
   const long at = pk.first + min(key, pk.count - 1);
-  Frag<T> k[DP / 16], v[DK ? DP / 16 : 1];
-  load_row<T, DP>(k, (const T *)a.k + at * a.kv_row + kv * a.D, a.D, half);
-  if constexpr (DK) load_row<T, DP>(v, (const T *)a.v + at * a.kv_row + kv * a.D, a.D, half);
+  RowFrags<T, DP> k, v;
+  k.load((const T *)a.k + at * a.kv_row + kv * a.D, a.D, half);
+  if (DK) v.load((const T *)a.v + at * a.kv_row + kv * a.D, a.D, half);
   const float c = a.scale * kLog2e;
   floatx16 dk[DK ? DP / 32 : 1], dv[DV ? DP / 32 : 1];
 #pragma unroll
@@ -157,32 +163,46 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DP <= 64 : DP <= 32) ? 
     if (DK) dk[i] = floatx16{};
     if (DV) dv[i] = floatx16{};
   }
-  const Reader<T, DP> reader(lane);
+  const Reader<T, DP, BN> reader(lane);
   S sq, sg;
-  sq.init(a.q, a.q_row, a.D, threadIdx.x);
-  sg.init(a.d_o, (long)a.H * a.D, a.D, threadIdx.x);
+  sq.init(smem, a.q, a.q_row, a.D);
+  sg.init(smem + S::kBytes, a.d_o, (long)a.H * a.D, a.D);
+  char *const figures = smem + 2 * S::kBytes;   // lse2 and minus_delta of a tile; twice
   // turns: the group's heads, each over the tiles of queries
   const int tiles = queries > from ? (queries - from + BN - 1) / BN : 0, turns = tiles * group;
-  const auto load = [&](int stage, int turn) {   // behind the last turn: zeros
-    const int h = kv * group + min(turn / max(tiles, 1), group - 1), i0 = turn < turns ? from + (turn % max(tiles, 1)) * BN : queries;
-    char *to = smem + stage * kStage;
-    sq.base = (const char *)((const T *)a.q + (long)q_first * a.q_row + h * a.D);
-    sg.base = (const char *)((const T *)a.d_o + ((long)q_first * a.H + h) * a.D);
-    sq.load(to, wave, i0, queries);
-    sg.load(to + S::kBytes, wave, i0, queries);
-    // two wavefronts bring the one, two the other: as many loads on their way in each
-    const float *figures = (wave & 1 ? rows.minus_delta : rows.lse2) + (long)h * a.Tq + q_first + i0;
-    const uintx4 rs = buffer_of((const char *)figures, (unsigned)max(0, min(queries - i0, BN)) * 4u);
-    load_words_to_lds(rs, lane * 4, (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)(to + 2 * S::kBytes + (wave & 1) * 256));
+  const int begin = turn_from(part, parts.n, turns), end = turn_from(part + 1, parts.n, turns);
+  struct Turn { const T *q, *g; const float *figures; int i0; };
+  const auto turn_of = [&](int turn) {   // behind the last one: no queries
+    const int h = kv * group + min(turn / max(tiles, 1), group - 1), i0 = turn < end ? from + (turn % max(tiles, 1)) * BN : queries;
+    return Turn{(const T *)a.q + (long)q_first * a.q_row + h * a.D, (const T *)a.d_o + ((long)q_first * a.H + h) * a.D,
+                (wave & 1 ? rows.minus_delta : rows.lse2) + (long)h * a.Tq + q_first + i0, i0};
   };
-  if (turns > 0) load(0, 0);
-  int stage = 0;
-  for (int turn = 0; turn < turns; ++turn, stage ^= 1) {
-    load(stage ^ 1, turn + 1);
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kWait) : "memory");
+  // two wavefronts bring the one kind of figures, two the other: as many loads on their way in each.  Like the rows, they go straight
+  // into LDS or come through a register.
+  float held = 0.0f;
+  const auto load_figures = [&](const Turn &t, int odd) {
+    if constexpr (sizeof(T) == 4) {
+      held = lane < min(queries - t.i0, BN) ? t.figures[lane] : 0.0f;
+      return;
+    }
+    const uintx4 rs = buffer_of((const char *)t.figures, (unsigned)max(0, min(queries - t.i0, BN)) * 4u);
+    load_words_to_lds(rs, lane * 4, (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)(figures + (2 * odd + (wave & 1)) * kFigures));
+  };
+  if (begin < end) {
+    const Turn t = turn_of(begin);
+    sq.start(wave, t.q, t.i0, queries);
+    sg.start(wave, t.g, t.i0, queries);
+    load_figures(t, 0);
+  }
+  int odd = 1;
+  for (int turn = begin; turn < end; ++turn, odd ^= 1) {
+    const Turn next = turn_of(turn + 1);
+    const char *lq = sq.turn(wave, odd, next.q, next.i0, queries), *lg = sg.turn(wave, odd, next.g, next.i0, queries);
+    if constexpr (sizeof(T) == 4) reinterpret_cast<float *>(figures)[(2 * (odd ^ 1) + (wave & 1)) * (kFigures / 4) + lane] = held;
+    load_figures(next, odd);
+    landed<T, 2 * S::kLoads + 1>();
     barrier();
-    const char *lq = smem + stage * kStage, *lg = lq + S::kBytes;
-    const float *lse2 = reinterpret_cast<const float *>(lg + S::kBytes), *minus_delta = lse2 + 64;
+    const float *lse2 = reinterpret_cast<const float *>(figures + 2 * (odd ^ 1) * kFigures), *minus_delta = lse2 + kFigures / 4;
     const int i0 = from + (turn % tiles) * BN;
 #pragma unroll 1
     for (int b = 0; b < BN && i0 + b < queries; b += 32) {
@@ -235,73 +255,126 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DP <= 64 : DP <= 32) ? 
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   if (key >= pk.count) return;
+  if (parts.n > 1) {
+    const long to = (((long)part * a.Tk + at) * a.KV + kv) * parts.ld;
+    if (DK && a.dk) store_sums(parts.sums[0] + to, dk, parts.ld, half);
+    if (DV && a.dv) store_sums(parts.sums[1] + to, dv, parts.ld, half);
+    return;
+  }
   if (DK && a.dk) store_row<T>((T *)a.dk + at * a.kv_row + kv * a.D, dk, a.scale, a.D, half);
   if (DV && a.dv) store_row<T>((T *)a.dv + at * a.kv_row + kv * a.D, dv, 1.0f, a.D, half);
 }
 
-// ------------------------------------------------------------------------------------------------ host
-template <class T, int DP>
-hipError_t dq_as(const AttentionArgs &a, const Rows &rows, hipStream_t stream) {
-  constexpr int BN = tile_rows<T, DP>();
-  constexpr size_t lds = 4 * Stager<T, DP, BN, kThreads>::kBytes;
-  const auto kernel = attention_dq_kernel<T, DP, BN>;
-  DLL_TRY(allow_large_lds(reinterpret_cast<const void *>(kernel), lds));
-  const long tiles = tiles_of(a.Tq, a.S, kRows), grid = tiles * a.H;
-  kernel<<<dim3((unsigned)grid), dim3(kThreads), lds, stream>>>(a, rows, (int)tiles);
-  return hipGetLastError();
-}
-
-template <class T, int DP, bool DK, bool DV>
-hipError_t dkv_as(const AttentionArgs &a, const Rows &rows, hipStream_t stream) {
-  constexpr int BN = tile_rows<T, DP>();
-  constexpr size_t lds = 2 * (2 * Stager<T, DP, BN, kThreads>::kBytes + 2 * 256);
-  const auto kernel = attention_dkv_kernel<T, DP, BN, DK, DV>;
-  DLL_TRY(allow_large_lds(reinterpret_cast<const void *>(kernel), lds));
-  const long grid = tiles_of(a.Tk, a.S, kRows) * a.KV;
-  kernel<<<dim3((unsigned)grid), dim3(kThreads), lds, stream>>>(a, rows);
-  return hipGetLastError();
-}
-
-template <class T, int DP>
-hipError_t bwd_as(const AttentionArgs &a, const Rows &rows, hipStream_t stream) {
-  DLL_TRY((dq_as<T, DP>(a, rows, stream)));
-  if (!a.dk && !a.dv) return hipSuccess;
-  if constexpr (sizeof(T) == 4 && DP > 128) {
-    if (a.dv) DLL_TRY((dkv_as<T, DP, false, true>(a, rows, stream)));
-    return a.dk ? dkv_as<T, DP, true, false>(a, rows, stream) : hipSuccess;
-  } else {
-    return dkv_as<T, DP, true, true>(a, rows, stream);
+// ------------------------------------------------------------------------------------------------ parts
+// One or two gradients' rows from their parts, four elements a thread
+struct Sums {
+  Parts parts;
+  const int *starts;
+  int sequences, tokens, heads, dim;
+  long row;
+  void *out[2];
+  float factor[2];
+};
+template <class T>
+__global__ __launch_bounds__(kThreads) void attention_sums_kernel(const Sums s, const long units) {
+  const int wide = s.parts.ld / 4, first = start_of(s.starts, 0, s.tokens), end = start_of(s.starts, s.sequences, s.tokens);
+  const long part = (long)s.tokens * s.heads * s.parts.ld;
+  for (long u = (long)blockIdx.x * kThreads + threadIdx.x; u < units; u += (long)gridDim.x * kThreads) {
+    const int d = (int)(u % wide) * 4;
+    const long row = u / wide, head = row % s.heads, at = row / s.heads;
+    if (at < first || at >= end) continue;   // nobody's
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      if (!s.out[k]) continue;
+      floatx4 v = {};
+#pragma unroll 4
+      for (int p = 0; p < s.parts.n; ++p) v += *reinterpret_cast<const floatx4 *>(s.parts.sums[k] + p * part + row * s.parts.ld + d);
+      T *to = (T *)s.out[k] + at * s.row + head * s.dim + d;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (d + j < s.dim) to[j] = (T)(v[j] * s.factor[k]);
+    }
   }
 }
-
 template <class T>
-hipError_t bwd(const AttentionArgs &a, const Rows &rows, hipStream_t stream) {
-  if (a.D <= 32) return bwd_as<T, 32>(a, rows, stream);
-  if (a.D <= 64) return bwd_as<T, 64>(a, rows, stream);
-  if (a.D <= 96) return bwd_as<T, 96>(a, rows, stream);
-  if (a.D <= 128) return bwd_as<T, 128>(a, rows, stream);
-  return bwd_as<T, 256>(a, rows, stream);
+hipError_t launch_sums(const Sums &s, hipStream_t stream) {
+  const long units = (long)s.tokens * s.heads * (s.parts.ld / 4), blocks = (units + kThreads - 1) / kThreads;
+  attention_sums_kernel<T><<<dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(kThreads), 0, stream>>>(s, units);
+  return hipGetLastError();
 }
 
+// ------------------------------------------------------------------------------------------------ host
 // The workspace's parts, the same walk for the query and the call
-struct BwdParts {
+struct BwdPlan {
   Rows rows;
+  Parts dq, dkv;
   size_t bytes;
-  BwdParts(const AttentionArgs &a, char *base) {
+  BwdPlan(const AttentionArgs &a, int tile, int dq_resident, int dkv_resident, char *base) {
     Take take{base};
     rows.lse2 = (float *)take((size_t)a.H * a.Tq * sizeof(float));
     rows.minus_delta = (float *)take((size_t)a.H * a.Tq * sizeof(float));
+    dq.n = parts_of((a.Tq + kRows - 1) / kRows * (long)a.H, tiles_of(a.Tq, a.S, kRows) * a.H, (long)dq_resident * chip().cus, a.Tk / a.S / tile);
+    dkv.n = parts_of((a.Tk + kRows - 1) / kRows * (long)a.KV, tiles_of(a.Tk, a.S, kRows) * a.KV, (long)dkv_resident * chip().cus,
+                      (long)a.Tq / a.S * (a.H / a.KV) / tile);
+    dq.ld = dkv.ld = (a.D + 3) & ~3;
+    if (dq.n > 1) dq.sums[0] = (float *)take((size_t)dq.n * a.Tq * a.H * dq.ld * sizeof(float));
+    if (dkv.n > 1)
+      for (float *&s : dkv.sums) s = (float *)take((size_t)dkv.n * a.Tk * a.KV * dkv.ld * sizeof(float));
     bytes = take.used;
   }
 };
+template <class T, int DP>
+BwdPlan plan_of(const AttentionArgs &a, char *scratch) { return BwdPlan(a, tile_rows<T, DP>(), dq_residents<T, DP>(), dkv_residents<T, DP>(), scratch); }
+
+template <class T, int DP, bool DK, bool DV>
+hipError_t launch_dkv(const AttentionArgs &a, const BwdPlan &p, hipStream_t stream) {
+  constexpr int BN = tile_rows<T, DP>();
+  constexpr size_t lds = 2 * Stager<T, DP, BN, kThreads>::kBytes + 4 * 256;
+  const auto kernel = attention_dkv_kernel<T, DP, BN, DK, DV>;
+  DLL_TRY(allow_large_lds(reinterpret_cast<const void *>(kernel), lds));
+  kernel<<<dim3((unsigned)(tiles_of(a.Tk, a.S, kRows) * a.KV * p.dkv.n)), dim3(kThreads), lds, stream>>>(a, p.rows, p.dkv);
+  return hipGetLastError();
+}
+
+template <class T, int DP>
+hipError_t bwd_as(const AttentionArgs &a, char *scratch, hipStream_t stream) {
+  constexpr int BN = tile_rows<T, DP>();
+  constexpr size_t lds = 2 * Stager<T, DP, BN, kThreads>::kBytes;
+  const BwdPlan p = plan_of<T, DP>(a, scratch);
+  const auto kernel = attention_dq_kernel<T, DP, BN>;
+  DLL_TRY(allow_large_lds(reinterpret_cast<const void *>(kernel), lds));
+  const long tiles = tiles_of(a.Tq, a.S, kRows);
+  const Parts one;
+  const Parts &dq = a.dq ? p.dq : one;
+  kernel<<<dim3((unsigned)(tiles * a.H * dq.n)), dim3(kThreads), lds, stream>>>(a, p.rows, dq, (int)tiles);
+  DLL_TRY(hipGetLastError());
+  if (dq.n > 1) DLL_TRY(launch_sums<T>(Sums{dq, a.q_starts, a.S, a.Tq, a.H, a.D, a.q_row, {a.dq, nullptr}, {a.scale, 0.0f}}, stream));
+  if (!a.dk && !a.dv) return hipSuccess;
+  if constexpr (sizeof(T) == 4 && DP > 128) {
+    if (a.dv) DLL_TRY((launch_dkv<T, DP, false, true>(a, p, stream)));
+    if (a.dk) DLL_TRY((launch_dkv<T, DP, true, false>(a, p, stream)));
+  } else {
+    DLL_TRY((launch_dkv<T, DP, true, true>(a, p, stream)));
+  }
+  if (p.dkv.n == 1) return hipSuccess;
+  return launch_sums<T>(Sums{p.dkv, a.kv_starts, a.S, a.Tk, a.KV, a.D, a.kv_row, {a.dk, a.dv}, {a.scale, 1.0f}}, stream);
+}
+
+template <class T>
+hipError_t bwd(const AttentionArgs &a, char *scratch, hipStream_t stream) {
+  return instance(a.D, [&](auto dp) { return bwd_as<T, decltype(dp)::value>(a, scratch, stream); });
+}
+template <class T>
+size_t bwd_bytes(const AttentionArgs &a) {
+  return instance(a.D, [&](auto dp) { return plan_of<T, decltype(dp)::value>(a, nullptr).bytes; });
+}
 
 }  // namespace
 
-size_t attention_bwd_scratch(const AttentionArgs &a) { return BwdParts(a, nullptr).bytes; }
+size_t attention_bwd_scratch(const AttentionArgs &a) { return a.dtype == TYPE_BF16 ? bwd_bytes<bf16>(a) : bwd_bytes<float>(a); }
 
 hipError_t launch_attention_bwd(const AttentionArgs &a, char *scratch, hipStream_t stream) {
-  const BwdParts p(a, scratch);
-  return a.dtype == TYPE_BF16 ? bwd<bf16>(a, p.rows, stream) : bwd<float>(a, p.rows, stream);
+  return a.dtype == TYPE_BF16 ? bwd<bf16>(a, scratch, stream) : bwd<float>(a, scratch, stream);
 }
 
 }  // namespace dllk

@@ -17,15 +17,20 @@ namespace {
 
 constexpr int kQueries = 128, kThreads = 256;
 
-template <class T, int DP> constexpr int keys_of() { return Tile<T, DP>::kRowBytes >= 512 ? 32 : 64; }
+// keys of a tile: 64 KB of LDS at most for both halves of a workgroup's tiles of keys and values, or 96 for the three planes of the largest
+template <class T, int DP> constexpr int keys_of() { return DP > 128 || (sizeof(T) == 4 && DP > 64) ? 32 : 64; }
+
+// workgroups that a compute unit holds, by their registers
+template <class T, int DP> constexpr int residents() { return (sizeof(T) == 2 ? DP <= 128 : DP <= 96) ? 2 : 1; }
 
 template <class T, int DP, int BN>
-__global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DP <= 128 : DP <= 96) ? 2 : 1) void attention_fwd_kernel(const AttentionArgs a, const int tiles) {
+__global__ __launch_bounds__(kThreads, (residents<T, DP>())) void attention_fwd_kernel(const AttentionArgs a, const Parts parts, const int tiles) {
   typedef Stager<T, DP, BN, kThreads> S;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
   // heads of one key head side by side, on as few XCDs as may be; the last tiles, which see most keys, first
-  const int kv = blockIdx.x % a.KV, rest = blockIdx.x / a.KV, group = a.H / a.KV, head = kv * group + rest % group, tile = tiles - 1 - rest / group;
+  const int part = blockIdx.x % parts.n, id = blockIdx.x / parts.n, kv = id % a.KV, rest = id / a.KV, group = a.H / a.KV, head = kv * group + rest % group,
+            tile = tiles - 1 - rest / group;
   const Place pq = place_of(a.q_starts, a.S, a.Tq, tile, kQueries);
   if (pq.at >= pq.count) return;
   const int kv_first = start_of(a.kv_starts, pq.sequence, a.Tk), keys = max(0, start_of(a.kv_starts, pq.sequence + 1, a.Tk) - kv_first);
@@ -35,34 +40,28 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DP <= 128 : DP <= 96) ?
   const int seen_last = row0 >= pq.count ? 0 : a.causal ? max(0, min(keys, min(row0 + 32, pq.count) + shift)) : keys;   // by its last
   const int seen_all = a.causal ? max(0, min(keys, min(pq.at + kQueries, pq.count) + shift)) : keys;        // by the workgroup's last
 
+  const T *k = (const T *)a.k + (long)kv_first * a.kv_row + kv * a.D, *v = (const T *)a.v + (long)kv_first * a.kv_row + kv * a.D;
   S sk, sv;
-  sk.init((const T *)a.k + (long)kv_first * a.kv_row + kv * a.D, a.kv_row, a.D, threadIdx.x);
-  sv.init((const T *)a.v + (long)kv_first * a.kv_row + kv * a.D, a.kv_row, a.D, threadIdx.x);
-  const auto load = [&](int stage, int key0) {   // behind the last key: zeros
-    char *at = smem + stage * 2 * S::kBytes;
-    sk.load(at, wave, key0, keys);
-    sv.load(at + S::kBytes, wave, key0, keys);
-  };
-  load(0, 0);
-  Frag<T> q[DP / 16];
-  load_row<T, DP>(q, (const T *)a.q + (long)(pq.first + min(row, pq.count - 1)) * a.q_row + head * a.D, a.D, half);
-  if (a.scale < 0.0f)   // the maximum of the scores is then that of -q k
-#pragma unroll
-    for (int s = 0; s < DP / 16; ++s) q[s] = -q[s];
+  sk.init(smem, k, a.kv_row, a.D);
+  sv.init(smem + S::kBytes, v, a.kv_row, a.D);
+  const int turns = (seen_all + BN - 1) / BN, begin = turn_from(part, parts.n, turns) * BN, end = min(seen_all, turn_from(part + 1, parts.n, turns) * BN);
+  sk.start(wave, k, begin, keys);
+  sv.start(wave, v, begin, keys);
+  RowFrags<T, DP> q;   // with a scale below 0 the maximum of the scores is that of -q k
+  q.load((const T *)a.q + (long)(pq.first + min(row, pq.count - 1)) * a.q_row + head * a.D, a.D, half, a.scale < 0.0f);
   const float c = fmaxf(fabsf(a.scale) * kLog2e, 0x1p-126f);   // a masked score of -infinity stays one where the scale is 0
 
   floatx16 o[DP / 32];
 #pragma unroll
   for (int i = 0; i < DP / 32; ++i) o[i] = floatx16{};
   float m = -INFINITY, l = 0.0f;
-  const Reader<T, DP> reader(lane);
-  int stage = 0;
-  for (int key0 = 0; key0 < seen_all; key0 += BN, stage ^= 1) {
-    load(stage ^ 1, key0 + BN);
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * S::kLoads) : "memory");
+  const Reader<T, DP, BN> reader(lane);
+  int odd = 1;
+  for (int key0 = begin; key0 < end; key0 += BN, odd ^= 1) {
+    const char *lk = sk.turn(wave, odd, k, key0 + BN, keys), *lv = sv.turn(wave, odd, v, key0 + BN, keys);
+    landed<T, 2 * S::kLoads>();
     barrier();
     if (key0 < seen_last) {
-      const char *lk = smem + stage * 2 * S::kBytes, *lv = lk + S::kBytes;
       floatx16 z[BN / 32];
 #pragma unroll
       for (int b = 0; b < BN / 32; ++b) z[b] = floatx16{};
@@ -113,29 +112,85 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DP <= 128 : DP <= 96) ?
   if (row >= pq.count) return;
   l += other_half(l);
   const long at = pq.first + row;
+  if (parts.n > 1) {
+    const long to = (long)part * a.Tq + at;
+    store_sums(parts.sums[0] + (to * a.H + head) * parts.ld, o, parts.ld, half);
+    if (half == 0) {
+      float *ml = parts.ml + (((long)part * a.H + head) * a.Tq + at) * 2;
+      ml[0] = m;
+      ml[1] = l;
+    }
+    return;
+  }
   store_row<T>((T *)a.o + at * a.H * a.D + head * a.D, o, l == 0.0f ? 0.0f : 1.0f / l, a.D, half);
   if (a.lse && half == 0) a.lse[(long)head * a.Tq + at] = l == 0.0f ? -INFINITY : m * kLn2 + logf(l);
 }
 
+// A row's parts, each relative to its own maximum: four elements a thread
+template <class T>
+__global__ __launch_bounds__(kThreads) void attention_join_kernel(const AttentionArgs a, const Parts parts, const long units) {
+  const int wide = parts.ld / 4, first = start_of(a.q_starts, 0, a.Tq), end = start_of(a.q_starts, a.S, a.Tq);
+  for (long u = (long)blockIdx.x * kThreads + threadIdx.x; u < units; u += (long)gridDim.x * kThreads) {
+    const int d = (int)(u % wide) * 4;
+    const long row = u / wide, head = row % a.H, at = row / a.H;
+    if (at < first || at >= end) continue;   // nobody's
+    float top = -INFINITY, l = 0.0f;
+    for (int p = 0; p < parts.n; ++p) top = fmaxf(top, parts.ml[((p * (long)a.H + head) * a.Tq + at) * 2]);
+    const float from = top == -INFINITY ? 0.0f : top;
+    floatx4 o = {};
+    for (int p = 0; p < parts.n; ++p) {
+      const float *ml = parts.ml + ((p * (long)a.H + head) * a.Tq + at) * 2, f = __builtin_amdgcn_exp2f(ml[0] - from);
+      l += f * ml[1];
+      o += f * *reinterpret_cast<const floatx4 *>(parts.sums[0] + ((p * (long)a.Tq + at) * a.H + head) * parts.ld + d);
+    }
+    const float by = l == 0.0f ? 0.0f : 1.0f / l;
+    T *to = (T *)a.o + row * a.D + d;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (d + j < a.D) to[j] = (T)(o[j] * by);
+    if (a.lse && d == 0) a.lse[head * a.Tq + at] = l == 0.0f ? -INFINITY : top * kLn2 + logf(l);
+  }
+}
+
+// The workspace's parts, the same walk for the query and the call
+struct FwdPlan {
+  Parts parts;
+  size_t bytes;
+  FwdPlan(const AttentionArgs &a, int keys, int resident, char *base) {
+    Take take{base};
+    parts.n = parts_of((a.Tq + kQueries - 1) / kQueries * (long)a.H, tiles_of(a.Tq, a.S, kQueries) * a.H, (long)resident * chip().cus, a.Tk / a.S / keys);
+    parts.ld = (a.D + 3) & ~3;
+    if (parts.n > 1) {
+      parts.sums[0] = (float *)take((size_t)parts.n * a.Tq * a.H * parts.ld * sizeof(float));
+      parts.ml = (float *)take((size_t)parts.n * a.Tq * a.H * 2 * sizeof(float));
+    }
+    bytes = take.used;
+  }
+};
+
 template <class T, int DP>
-hipError_t fwd_as(const AttentionArgs &a, hipStream_t stream) {
+hipError_t fwd_as(const AttentionArgs &a, char *scratch, hipStream_t stream) {
   constexpr int BN = keys_of<T, DP>();
-  constexpr size_t lds = 4 * Stager<T, DP, BN, kThreads>::kBytes;
+  constexpr size_t lds = 2 * Stager<T, DP, BN, kThreads>::kBytes;
   const auto kernel = attention_fwd_kernel<T, DP, BN>;
-  const hipError_t e = allow_large_lds(reinterpret_cast<const void *>(kernel), lds);
-  if (e != hipSuccess) return e;
-  const long tiles = tiles_of(a.Tq, a.S, kQueries), grid = tiles * a.H;
-  kernel<<<dim3((unsigned)grid), dim3(kThreads), lds, stream>>>(a, (int)tiles);
+  DLL_TRY(allow_large_lds(reinterpret_cast<const void *>(kernel), lds));
+  const FwdPlan p(a, BN, residents<T, DP>(), scratch);
+  const long tiles = tiles_of(a.Tq, a.S, kQueries);
+  kernel<<<dim3((unsigned)(tiles * a.H * p.parts.n)), dim3(kThreads), lds, stream>>>(a, p.parts, (int)tiles);
+  DLL_TRY(hipGetLastError());
+  if (p.parts.n == 1) return hipSuccess;
+  const long units = (long)a.Tq * a.H * (p.parts.ld / 4), blocks = (units + kThreads - 1) / kThreads;
+  attention_join_kernel<T><<<dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(kThreads), 0, stream>>>(a, p.parts, units);
   return hipGetLastError();
 }
 
 template <class T>
-hipError_t fwd(const AttentionArgs &a, hipStream_t stream) {
-  if (a.D <= 32) return fwd_as<T, 32>(a, stream);
-  if (a.D <= 64) return fwd_as<T, 64>(a, stream);
-  if (a.D <= 96) return fwd_as<T, 96>(a, stream);
-  if (a.D <= 128) return fwd_as<T, 128>(a, stream);
-  return fwd_as<T, 256>(a, stream);
+hipError_t fwd(const AttentionArgs &a, char *scratch, hipStream_t stream) {
+  return instance(a.D, [&](auto dp) { return fwd_as<T, decltype(dp)::value>(a, scratch, stream); });
+}
+template <class T>
+size_t fwd_bytes(const AttentionArgs &a) {
+  return instance(a.D, [&](auto dp) { return FwdPlan(a, keys_of<T, decltype(dp)::value>(), residents<T, decltype(dp)::value>(), nullptr).bytes; });
 }
 
 }  // namespace
@@ -144,10 +199,10 @@ bool attention_fits(int q_tokens, int kv_tokens, int sequences, int heads) {
   return tiles_of(q_tokens > kv_tokens ? q_tokens : kv_tokens, sequences, kQueries) * heads <= kMaxGrid;
 }
 
-size_t attention_fwd_scratch(const AttentionArgs &) { return 256; }
+size_t attention_fwd_scratch(const AttentionArgs &a) { return (a.dtype == TYPE_BF16 ? fwd_bytes<bf16>(a) : fwd_bytes<float>(a)) + 1; }   // never nothing
 
-hipError_t launch_attention_fwd(const AttentionArgs &a, char *, hipStream_t stream) {
-  return a.dtype == TYPE_BF16 ? fwd<bf16>(a, stream) : fwd<float>(a, stream);
+hipError_t launch_attention_fwd(const AttentionArgs &a, char *scratch, hipStream_t stream) {
+  return a.dtype == TYPE_BF16 ? fwd<bf16>(a, scratch, stream) : fwd<float>(a, scratch, stream);
 }
 
 }  // namespace dllk

@@ -8,7 +8,7 @@
 // tokens may be taken in any order, so the other operand is read from LDS in that same order (two transposing reads) and the scores
 // never leave their registers.
 //
-// LDS: rows of a power of two of elements, each 16-byte group at place group ^ flip(row), chosen so that sixteen rows' same group
+// LDS: rows of a power of two of bfloat16 elements (single precision: three planes of them), each 16-byte group at place group ^ flip(row), chosen so that sixteen rows' same group
 // (scores) and four rows' same 64 bytes (the transposing read) lie in different banks.
 #pragma once
 
@@ -20,70 +20,85 @@ namespace attn {
 using namespace tile;
 
 typedef float floatx8 __attribute__((ext_vector_type(8)));
+// Eight elements as the 32 x 32 x 16 products take them.  Single precision is three bfloat16 parts of each number (split3): six products on
+// a pipe of sixteen times the rate.
 template <class T> struct FragOf;
 template <> struct FragOf<bf16> { typedef bf16x8 Type; };
-template <> struct FragOf<float> { typedef floatx8 Type; };
+template <> struct FragOf<float> { typedef Split Type; };
 template <class T> using Frag = typename FragOf<T>::Type;
+template <class T> constexpr int planes() { return sizeof(T) == 2 ? 1 : 3; }
 
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
 
 // c += a b over sixteen: a's 32 rows become c's registers, b's its lanes
 __device__ __forceinline__ floatx16 mma(bf16x8 a, bf16x8 b, floatx16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-__device__ __forceinline__ floatx16 mma(floatx8 a, floatx8 b, floatx16 c) {
-#pragma unroll
-  for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
-  return c;
-}
+__device__ __forceinline__ floatx16 mma(const Split &a, const Split &b, floatx16 c) { return mfma6(a, b, c); }
+
+__device__ __forceinline__ Split split_of(const floatx8 &v) { return split3(floatx4{v[0], v[1], v[2], v[3]}, floatx4{v[4], v[5], v[6], v[7]}); }
 
 // Registers 8 s to 8 s + 7 of a 32 x 32 result as a fragment; bfloat16 is rounded to nearest
 template <class T>
 __device__ __forceinline__ Frag<T> frag_of(const floatx16 &c, int s) {
-  Frag<T> f;
+  if constexpr (sizeof(T) == 2) {
+    bf16x8 f;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) f[j] = (T)c[8 * s + j];
-  return f;
+    for (int j = 0; j < 8; ++j) f[j] = (bf16)c[8 * s + j];
+    return f;
+  } else {
+    floatx8 f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = c[8 * s + j];
+    return split_of(f);
+  }
 }
 // the token of a 32 x 32 result's register, without the lane half's 4
 __device__ __forceinline__ constexpr int token_of(int r) { return 8 * (r >> 2) + (r & 3); }
 
-template <class T, int DP>
+// Rows of bfloat16 in LDS, of numbers or of one of their parts
+template <int DP>
 struct Tile {
   static constexpr int kPitch = DP <= 64 ? 64 : DP <= 128 ? 128 : 256;   // elements of a row
-  static constexpr int kRowBytes = kPitch * (int)sizeof(T), kGroups = kRowBytes / 16;
-  static constexpr int kSteps = DP / 16, kBlocks = DP / 32;
-  static_assert(DP % 32 == 0 && kRowBytes >= 128, "");
+  static constexpr int kRowBytes = kPitch * 2, kGroups = kRowBytes / 16;
+  static_assert(DP % 32 == 0, "");
   static __device__ __forceinline__ int flip(int row) {
     return kGroups == 8 ? (((row >> 1) & 1) << 2) | ((row >> 2) & 3) : ((row & 3) << 2) | ((row >> 2) & 3);
   }
 };
 
-// NR tokens' rows from memory into LDS
+// NR tokens' rows from memory into LDS, for a loop over tiles of them: `start` sends the first tile on its way; `turn` sees to it that tile
+// `now` is in LDS (behind the caller's barrier), sends `next` on its way and says where the tile lies.  What lies behind the last row, and behind a
+// row's dim elements, is zeros.
+//
+// bfloat16 goes straight into LDS, the next tile into the other half of the area.  Single precision comes through registers, where it is split once for
+// all wavefronts, and has one area, written between the caller's barriers.
 template <class T, int DP, int NR, int THREADS>
-struct Stager {
-  typedef Tile<T, DP> G;
-  static constexpr int kBytes = NR * G::kRowBytes, kIts = kBytes / (16 * THREADS), kLoads = kIts;
-  static_assert(kBytes % (16 * THREADS) == 0, "whole steps");
-  const char *base;
+struct Stager;
+
+template <int DP, int NR, int THREADS>
+struct Stager<bf16, DP, NR, THREADS> {
+  typedef Tile<DP> G;
+  static constexpr int kTile = NR * G::kRowBytes, kBytes = 2 * kTile, kIts = kTile / (16 * THREADS), kLoads = kIts;
+  static_assert(kTile % (16 * THREADS) == 0, "whole steps");
+  char *area;
   long ld;          // bytes from row to row
   int dim_bytes;
   bool whole;       // rows come in 16-byte groups from multiples of four bytes
   unsigned off[kIts];
 
-  __device__ __forceinline__ void init(const void *p, long ld_, int dim, int t) {
-    base = (const char *)p;
-    ld = ld_ * (long)sizeof(T);
-    dim_bytes = dim * (int)sizeof(T);
+  __device__ __forceinline__ void init(char *area_, const void *p, long ld_, int dim) {
+    area = area_;
+    ld = ld_ * 2;
+    dim_bytes = dim * 2;
     whole = ((ld | (long)(uintptr_t)p) & 3) == 0 && dim_bytes % 16 == 0;
 #pragma unroll
     for (int it = 0; it < kIts; ++it) {
-      const int at = it * THREADS + t, row = at / G::kGroups, group = (at % G::kGroups) ^ G::flip(row);
+      const int at = it * THREADS + (int)threadIdx.x, row = at / G::kGroups, group = (at % G::kGroups) ^ G::flip(row);
       off[it] = group * 16 < dim_bytes ? (unsigned)(row * ld) + 16u * group : kOutOfRange;
     }
   }
-  // rows row0 to row0 + NR of `rows`; what lies behind them, and behind a row's dim elements, is zeros
-  __device__ __forceinline__ void load(char *lds, int wave, int row0, int rows) const {
+  __device__ __forceinline__ void load(char *lds, int wave, const bf16 *base, int row0, int rows) const {
     const int left = max(0, min(rows - row0, NR));
-    const char *p = base + (long)row0 * ld;
+    const char *p = (const char *)base + (long)row0 * ld;
     if (whole) {
       const uintx4 rs = buffer_of(p, left > 0 ? (unsigned)((left - 1) * ld) + dim_bytes : 0u);
       const unsigned at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
@@ -91,24 +106,75 @@ struct Stager {
       for (int it = 0; it < kIts; ++it) load_to_lds(rs, off[it], at + (it * THREADS + wave * 64) * 16);
       return;
     }
-    constexpr int kE = 16 / (int)sizeof(T);
-    const int t = (int)(threadIdx.x % THREADS), dim = dim_bytes / (int)sizeof(T);
+    const int dim = dim_bytes / 2;
 #pragma unroll 1
     for (int it = 0; it < kIts; ++it) {
-      const int at = it * THREADS + t, row = at / G::kGroups, col = ((at % G::kGroups) ^ G::flip(row)) * kE;
-      const T *src = reinterpret_cast<const T *>(p + row * ld);
-      T *dst = reinterpret_cast<T *>(lds + at * 16);
+      const int at = it * THREADS + (int)threadIdx.x, row = at / G::kGroups, col = ((at % G::kGroups) ^ G::flip(row)) * 8;
+      const bf16 *src = reinterpret_cast<const bf16 *>(p + row * ld);
+      bf16 *dst = reinterpret_cast<bf16 *>(lds + at * 16);
 #pragma unroll
-      for (int j = 0; j < kE; ++j) dst[j] = row < left && col + j < dim ? src[col + j] : (T)0.0f;
+      for (int j = 0; j < 8; ++j) dst[j] = row < left && col + j < dim ? src[col + j] : (bf16)0.0f;
     }
+  }
+  __device__ __forceinline__ void start(int wave, const bf16 *base, int row0, int rows) { load(area, wave, base, row0, rows); }
+  // tiles alternate between the halves: `odd` is the next one's
+  __device__ __forceinline__ const char *turn(int wave, int odd, const bf16 *base, int next_row0, int rows) {
+    load(area + odd * kTile, wave, base, next_row0, rows);
+    return area + (odd ^ 1) * kTile;
   }
 };
 
-// Fragments of a tile in LDS for lane l: of scores, elements 16 s + 8 (l / 32) on of row x0 + l % 32; of sums over tokens, element
+template <int DP, int NR, int THREADS>
+struct Stager<float, DP, NR, THREADS> {
+  typedef Tile<DP> G;
+  static constexpr int kTile = NR * G::kRowBytes, kBytes = 3 * kTile, kIts = kTile / (16 * THREADS), kLoads = 0;
+  static_assert(kTile % (16 * THREADS) == 0, "whole steps");
+  char *area;
+  long ld;
+  int dim;
+  floatx8 held[kIts];
+
+  __device__ __forceinline__ void init(char *area_, const void *, long ld_, int dim_) {
+    area = area_;
+    ld = ld_;
+    dim = dim_;
+  }
+  static __device__ __forceinline__ int row_of(int it) { return (it * THREADS + (int)threadIdx.x) / G::kGroups; }
+  static __device__ __forceinline__ int col_of(int it) { return ((it * THREADS + (int)threadIdx.x) % G::kGroups ^ G::flip(row_of(it))) * 8; }
+  __device__ __forceinline__ void start(int, const float *base, int row0, int rows) {
+    const int left = rows - row0;
+#pragma unroll
+    for (int it = 0; it < kIts; ++it) {
+      Eight<float> e;
+      const int row = row_of(it), n = row < left ? dim - col_of(it) : 0;
+      e.load(base + (long)(row0 + row) * ld + col_of(it), n);
+      held[it] = e.v;
+    }
+  }
+  __device__ __forceinline__ const char *turn(int wave, int, const float *base, int next_row0, int rows) {
+#pragma unroll
+    for (int it = 0; it < kIts; ++it) {
+      const Split s = split_of(held[it]);
+#pragma unroll
+      for (int k = 0; k < 3; ++k) *reinterpret_cast<bf16x8 *>(area + k * kTile + (it * THREADS + (int)threadIdx.x) * 16) = s.p[k];
+    }
+    start(wave, base, next_row0, rows);
+    return area;
+  }
+};
+
+// What the caller's barrier of a turn stands behind: all loads straight into LDS but the LATER newest ones have landed, and LDS is written
+template <class T, int LATER>
+__device__ __forceinline__ void landed() {
+  if constexpr (sizeof(T) == 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LATER) : "memory");
+  else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+}
+
+// Fragments of a tile of NR rows in LDS for lane l: of scores, elements 16 s + 8 (l / 32) on of row x0 + l % 32; of sums over tokens, element
 // d0 + l % 32 of the sixteen tokens from x0 on, in the order of a result's registers.  x0 is a multiple of 32 and of 16.
-template <class T, int DP>
+template <class T, int DP, int NR>
 struct Reader {
-  typedef Tile<T, DP> G;
+  typedef Tile<DP> G;
   int row, half, low;     // scores
   int trow, tgroup, tlow, tbyte;   // sums over tokens
   __device__ __forceinline__ explicit Reader(int lane) {
@@ -116,61 +182,68 @@ struct Reader {
     half = lane >> 5;
     low = G::flip(lane & 31);
     const int i = lane & 15;
-    if (sizeof(T) == 2) {
-      trow = (4 * half + (i >> 2)) * G::kRowBytes;
-      tgroup = 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
-      tlow = G::flip(4 * half + (i >> 2));
-      tbyte = 8 * (i & 1);
-    } else {
-      trow = 4 * half * G::kRowBytes;
-      tgroup = (lane & 31) >> 2;
-      tlow = 0;
-      tbyte = 4 * (lane & 3);
-    }
+    trow = (4 * half + (i >> 2)) * G::kRowBytes;
+    tgroup = 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
+    tlow = G::flip(4 * half + (i >> 2));
+    tbyte = 8 * (i & 1);
+  }
+  __device__ __forceinline__ bf16x8 along_plane(const char *p, int s) const { return *reinterpret_cast<const bf16x8 *>(p + (((2 * s + half) ^ low) << 4)); }
+  __device__ __forceinline__ bf16x8 across_plane(const char *p, int d0) const {
+    typedef __attribute__((address_space(3))) shortx4 *Lp;
+    const int g = d0 / 8 + tgroup;
+    // eight rows on, flip differs in its second bit, whatever the row
+    const shortx4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lp)(p + ((g ^ tlow) << 4) + tbyte));
+    const shortx4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lp)(p + 8 * G::kRowBytes + ((g ^ tlow ^ 2) << 4) + tbyte));
+    const shortx8 v = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    return __builtin_bit_cast(bf16x8, v);
   }
   __device__ __forceinline__ Frag<T> along(const char *lds, int x0, int s) const {
     const char *p = lds + x0 * G::kRowBytes + row;
     if constexpr (sizeof(T) == 2) {
-      return *reinterpret_cast<const bf16x8 *>(p + (((2 * s + half) ^ low) << 4));
+      return along_plane(p, s);
     } else {
-      const int g = (4 * s + 2 * half) ^ low;
-      const floatx4 a = *reinterpret_cast<const floatx4 *>(p + (g << 4)), b = *reinterpret_cast<const floatx4 *>(p + ((g ^ 1) << 4));
-      return floatx8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+      Split f;
+#pragma unroll
+      for (int k = 0; k < 3; ++k) f.p[k] = along_plane(p + k * NR * G::kRowBytes, s);
+      return f;
     }
   }
   __device__ __forceinline__ Frag<T> across(const char *lds, int x0, int d0) const {
     const char *p = lds + x0 * G::kRowBytes + trow;
     if constexpr (sizeof(T) == 2) {
-      typedef __attribute__((address_space(3))) shortx4 *Lp;
-      const int g = d0 / 8 + tgroup;
-      // eight rows on, flip differs in its second bit, whatever the row
-      const shortx4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lp)(p + ((g ^ tlow) << 4) + tbyte));
-      const shortx4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lp)(p + 8 * G::kRowBytes + ((g ^ tlow ^ 2) << 4) + tbyte));
-      const shortx8 v = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-      return __builtin_bit_cast(bf16x8, v);
+      return across_plane(p, d0);
     } else {
-      floatx8 v;
+      Split f;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int r = 8 * (j >> 2) + (j & 3);   // of sixteen, and 4 * half more
-        v[j] = *reinterpret_cast<const float *>(p + r * G::kRowBytes + (((d0 / 4 + tgroup) ^ G::flip(r + 4 * half)) << 4) + tbyte);
-      }
-      return v;
+      for (int k = 0; k < 3; ++k) f.p[k] = across_plane(p + k * NR * G::kRowBytes, d0);
+      return f;
     }
   }
 };
 
-// A token's row straight from memory: the fragments of lane half `half`, zeros behind dim elements
+// A token's row straight from memory, kept as fragments of lane half `half`, zeros behind dim elements.  Single precision of more than 128
+// elements is split where it is used, as its parts would not fit the registers.
 template <class T, int DP>
-__device__ __forceinline__ void load_row(Frag<T> (&f)[DP / 16], const T *p, int dim, int half) {
+struct RowFrags {
+  static constexpr bool kLate = sizeof(T) == 4 && DP > 128;
+  typedef typename std::conditional<kLate, floatx8, Frag<T>>::type Kept;
+  Kept f[DP / 16];
+  __device__ __forceinline__ void load(const T *p, int dim, int half, bool negate = false) {
 #pragma unroll
-  for (int s = 0; s < DP / 16; ++s) {
-    Eight<T> e;
-    const int at = 16 * s + 8 * half;
-    e.load(p + at, dim - at);
-    f[s] = e.v;
+    for (int s = 0; s < DP / 16; ++s) {
+      Eight<T> e;
+      const int at = 16 * s + 8 * half;
+      e.load(p + at, dim - at);
+      if (negate) e.v = -e.v;
+      if constexpr (sizeof(T) == 2 || kLate) f[s] = e.v;
+      else f[s] = split_of(e.v);
+    }
   }
-}
+  __device__ __forceinline__ Frag<T> operator[](int s) const {
+    if constexpr (kLate) return split_of(f[s]);
+    else return f[s];
+  }
+};
 
 // A lane's part of a result's row (32 x 32 results over elements d0 = 0, 32, ..): element 32 i + 8 q + 4 half + j from register 4 q + j
 template <class T, int N>
@@ -193,6 +266,17 @@ __device__ __forceinline__ void store_row(T *p, const floatx16 (&c)[N], float fa
           if (at + j < dim) p[at + j] = v[j];
       }
     }
+}
+
+// The same unrounded, into a row of sums whose length is a multiple of four
+template <int N>
+__device__ __forceinline__ void store_sums(float *p, const floatx16 (&c)[N], int ld, int half) {
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (32 * i + 8 * q + 4 * half < ld)
+        *reinterpret_cast<floatx4 *>(p + 32 * i + 8 * q + 4 * half) = floatx4{c[i][4 * q], c[i][4 * q + 1], c[i][4 * q + 2], c[i][4 * q + 3]};
 }
 
 // What the other half of the wavefront's lanes holds for the same column
@@ -226,6 +310,34 @@ __device__ __forceinline__ Place place_of(const int *starts, int sequences, int 
   return p;
 }
 inline long tiles_of(int tokens, int sequences, int B) { return (long)tokens / B + sequences; }
+
+// Work split along the axis that a workgroup goes over: part k of n of a workgroup's `turns`, its sums left in 32 bits for a launch that adds them
+// up in order.  Taken where there are too few workgroups for the chip.
+struct Parts {
+  int n = 1;
+  float *sums[2] = {nullptr, nullptr};   // [n][tokens][heads][ld]: un-normalised outputs; or a gradient's, or both gradients'
+  float *ml = nullptr;                   // [n][heads][tokens][2]: maximum in the exponent's base, sum
+  int ld = 0;                            // head_dim in whole fours
+};
+__device__ __forceinline__ int turn_from(int part, int parts, int turns) { return (int)((long)part * turns / parts); }
+// The n that fills the chip's `slots` places for workgroups, with eight turns a part left on average; grid: workgroups of one part's launch,
+// empty ones too
+inline int parts_of(long workgroups, long grid, long slots, long turns) {
+  long n = (slots + workgroups - 1) / workgroups;
+  for (const long most : {turns / 8, kMaxGrid / grid, 16L}) n = n < most ? n : most;
+  return (int)(n > 1 ? n : 1);
+}
+
+
+// What `call` makes of the smallest instance that holds a head
+template <class F>
+auto instance(int dim, const F &call) {
+  if (dim <= 32) return call(std::integral_constant<int, 32>{});
+  if (dim <= 64) return call(std::integral_constant<int, 64>{});
+  if (dim <= 96) return call(std::integral_constant<int, 96>{});
+  if (dim <= 128) return call(std::integral_constant<int, 128>{});
+  return call(std::integral_constant<int, 256>{});
+}
 
 }  // namespace attn
 }  // namespace dllk

@@ -36,6 +36,20 @@ struct Divisor {
 // workgroups that a compute unit holds, by their registers
 template <class T, int DP> constexpr int residents() { return (sizeof(T) == 2 ? DP <= 128 : DP <= 96) ? 2 : 1; }
 
+// Eight numbers of an operand: single precision is multiplied as it is, as what bounds these kernels is memory
+template <class T> struct EightOf;
+template <> struct EightOf<bf16> { typedef bf16x8 Type; };
+template <> struct EightOf<float> { typedef floatx8 Type; };
+template <class T> using Numbers = typename EightOf<T>::Type;
+// Rows in LDS, places as in Tile
+template <class T, int DP>
+struct Rows {
+  static constexpr int kRowBytes = Tile<DP>::kPitch * (int)sizeof(T), kGroups = kRowBytes / 16;
+  static __device__ __forceinline__ int flip(int row) {
+    return kGroups == 8 ? (((row >> 1) & 1) << 2) | ((row >> 2) & 3) : ((row & 3) << 2) | ((row >> 2) & 3);
+  }
+};
+
 __device__ __forceinline__ floatx4 mma16(bf16x8 a, bf16x8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ floatx4 mma16(floatx8 a, floatx8 b, floatx4 c) {
 #pragma unroll
@@ -50,7 +64,7 @@ __device__ __forceinline__ float sum4(float v) { v += __shfl_xor(v, 16); return 
 __device__ __forceinline__ int keys_of(const CacheArgs &a, int r) { return (int)max(0L, min((long)a.lengths[r], (long)a.columns * a.page)); }
 __device__ __forceinline__ int units_of(int keys) { return (keys + kUnit - 1) / kUnit; }
 
-struct Parts {
+struct Runs {
   float *o;    // [2 groups][kHeads][ld], relative to the maximum
   float *ml;   // [2 groups][kHeads][2]: maximum in the exponent's base, sum
   int ld;      // head_dim in whole fours
@@ -90,8 +104,8 @@ struct Shared {
 // WHOLE: a head's rows are whole runs of eight elements, so every load is 16 bytes or more from a place that exists and no branch stands
 // between the loads; what a lane has no run for it takes from its row's last one, against zeros of q.
 template <class T, int DP, bool WHOLE>
-__global__ __launch_bounds__(kThreads, (residents<T, DP>())) void paged_attention_kernel(const CacheArgs a, const Parts parts, const Divisor page) {
-  typedef Tile<T, DP> G;
+__global__ __launch_bounds__(kThreads, (residents<T, DP>())) void paged_attention_kernel(const CacheArgs a, const Runs parts, const Divisor page) {
+  typedef Rows<T, DP> G;
   constexpr int kSteps = DP / 32, kArea = kTile * G::kRowBytes;   // LDS of a wavefront: its values, or at the end its sums [16][DP] fp32
   static_assert(kArea >= kHeads * DP * 4, "");
   extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -167,7 +181,7 @@ __global__ __launch_bounds__(kThreads, (residents<T, DP>())) void paged_attentio
     const int *table = a.table + (long)r * a.columns;
     const char *k_head = (const char *)a.k_cache + kv * head_bytes, *v_head = (const char *)a.v_cache + kv * head_bytes;
 
-    Frag<T> q[kSteps];
+    Numbers<T> q[kSteps];
     {
       const T *row = (const T *)a.q + ((long)r * a.H + head0 + min(col, heads - 1)) * a.D;
 #pragma unroll
@@ -195,7 +209,7 @@ __global__ __launch_bounds__(kThreads, (residents<T, DP>())) void paged_attentio
         at[h] = (unsigned)id[h] < (unsigned)a.pages ? id[h] * page_bytes + (key - page.of(key) * a.page) * row_bytes : -1;
       }
     };
-    const auto load = [&](Frag<T> (&f)[2][kSteps], const char *head, const long (&at)[2]) {
+    const auto load = [&](Numbers<T> (&f)[2][kSteps], const char *head, const long (&at)[2]) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const char *row = head + max(at[h], 0L);
@@ -221,7 +235,7 @@ __global__ __launch_bounds__(kThreads, (residents<T, DP>())) void paged_attentio
     // for first: loads come back in order, and the next rows' addresses must not wait for rows.
     int key0 = key_begin + wave * kTile, id[2], id_next[2];
     long at[2], next[2];
-    Frag<T> k[2][kSteps], v[2][kSteps];
+    Numbers<T> k[2][kSteps], v[2][kSteps];
     constexpr int kNext = kWaves * kTile;
     pages(key0, id);
     pages(key0 + kNext, id_next);
@@ -240,7 +254,7 @@ __global__ __launch_bounds__(kThreads, (residents<T, DP>())) void paged_attentio
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int s = 0; s < kSteps; ++s)
-            if (at[h] < 0) v[h][s] = Frag<T>{};
+            if (at[h] < 0) v[h][s] = Numbers<T>{};
       // values into LDS, row by row; the rows' same groups of sixteen lanes land in different banks
 #pragma unroll
       for (int h = 0; h < 2; ++h)
@@ -287,7 +301,7 @@ __global__ __launch_bounds__(kThreads, (residents<T, DP>())) void paged_attentio
         for (int i = 0; i < DP / 16; ++i) o[i] *= shrink;
       }
       const float from = m == -INFINITY ? 0.0f : m;
-      Frag<T> p;
+      Numbers<T> p;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j >> 2][j & 3], c, -from));
@@ -297,7 +311,7 @@ __global__ __launch_bounds__(kThreads, (residents<T, DP>())) void paged_attentio
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       constexpr int kAhead = DP * (int)sizeof(T) <= 256 ? DP / 16 : DP % 64 ? 3 : 4;   // fragments read at a time
       static_assert(DP / 16 % kAhead == 0, "");
-      Frag<T> w[kAhead];
+      Numbers<T> w[kAhead];
 #pragma unroll
       for (int i = 0; i < DP / 16; ++i) {
         if constexpr (sizeof(T) == 2) {
@@ -364,7 +378,7 @@ __global__ __launch_bounds__(kThreads, (residents<T, DP>())) void paged_attentio
 // One request's head, where more than one workgroup had a part of it: the parts' factors first, then their outputs, four elements a thread
 // and as many parts side by side as there are threads
 template <class T>
-__global__ __launch_bounds__(kThreads) void paged_join_kernel(const CacheArgs a, const Parts parts, int groups) {
+__global__ __launch_bounds__(kThreads) void paged_join_kernel(const CacheArgs a, const Runs parts, int groups) {
   __shared__ long scratch[2 * kWaves];
   __shared__ float factor[kMaxGroups], level[2][kWaves];
   __shared__ floatx4 sums[kThreads];
@@ -427,7 +441,7 @@ int groups_of(const CacheArgs &a, int resident) {
 
 // The workspace's parts, the same walk for the query and the call
 struct PagedParts {
-  Parts parts;
+  Runs parts;
   size_t bytes;
   PagedParts(const CacheArgs &a, char *base) {
     Take take{base};
@@ -441,8 +455,8 @@ struct PagedParts {
 };
 
 template <class T, int DP, bool WHOLE>
-hipError_t paged_as(const CacheArgs &a, const Parts &parts, hipStream_t stream) {
-  constexpr size_t lds = kWaves * kTile * Tile<T, DP>::kRowBytes + sizeof(Shared);
+hipError_t paged_as(const CacheArgs &a, const Runs &parts, hipStream_t stream) {
+  constexpr size_t lds = kWaves * kTile * Rows<T, DP>::kRowBytes + sizeof(Shared);
   const auto kernel = paged_attention_kernel<T, DP, WHOLE>;
   DLL_TRY(allow_large_lds(reinterpret_cast<const void *>(kernel), lds));
   const int groups = groups_of(a, residents<T, DP>());
@@ -454,7 +468,7 @@ hipError_t paged_as(const CacheArgs &a, const Parts &parts, hipStream_t stream) 
 }
 
 template <class T>
-hipError_t paged(const CacheArgs &a, const Parts &parts, hipStream_t stream) {
+hipError_t paged(const CacheArgs &a, const Runs &parts, hipStream_t stream) {
   if (a.D % 8) return a.D <= 64 ? paged_as<T, 64, false>(a, parts, stream) : a.D <= 128 ? paged_as<T, 128, false>(a, parts, stream) : paged_as<T, 256, false>(a, parts, stream);
   if (a.D <= 32) return paged_as<T, 32, true>(a, parts, stream);
   if (a.D <= 64) return paged_as<T, 64, true>(a, parts, stream);
