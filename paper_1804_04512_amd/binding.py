@@ -10,7 +10,7 @@ import ctypes as C
 import operator
 import os
 from dataclasses import dataclass
-from typing import List, Optional, Sequence
+from typing import List, NamedTuple, Optional, Sequence
 
 import torch
 
@@ -316,6 +316,8 @@ def dll_cnn_train_step_momentum(net: NetHandle, params: List[torch.Tensor], velo
 # ---------------------------------------------------------------------------------------
 def _tensor(t: Optional[torch.Tensor], shape, dtype: torch.dtype, what: str, device, optional: bool = False):
     """The address of a tensor that has to have this shape and type and lie on this device."""
+    if t is not None and t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous():
+        return t.data_ptr()
     if t is None:
         if optional:
             return None
@@ -327,9 +329,16 @@ def _tensor(t: Optional[torch.Tensor], shape, dtype: torch.dtype, what: str, dev
     return t.data_ptr()
 
 
+class _CurrentStream(NamedTuple):
+    device: torch.device
+    cuda_stream: int
+
+
 def _call_stream(stream):
     if stream is None:
-        return torch.cuda.current_stream()
+        # its address alone: the object that torch.cuda.current_stream() makes of it takes 2.6 us, a quarter of a small call
+        index = torch.cuda.current_device()
+        return _CurrentStream(torch.device("cuda", index), torch._C._cuda_getCurrentRawStream(index))
     s = stream
     if s.device != torch.device("cuda", torch.cuda.current_device()):
         raise ValueError(f"the stream belongs to {s.device}, which is not the current device")
@@ -434,6 +443,8 @@ def _head_rows(t: Optional[torch.Tensor], shape, row: int, dtype: torch.dtype, w
     if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{what}: {dtype} of shape {tuple(shape)} expected, got {t.dtype} of shape {tuple(t.shape)}")
     strides = (row or shape[1] * shape[2], shape[2], 1)
+    if t.device == device and t.stride() == strides:
+        return t.data_ptr()
     if t.device != device or any(n > 1 and s != want for n, s, want in zip(shape, t.stride(), strides)):
         raise ValueError(f"{what}: strides {strides} and on {device} (the device of the call's stream) expected")
     return t.data_ptr()

@@ -320,11 +320,11 @@ struct Parts {
   int ld = 0;                            // head_dim in whole fours
 };
 __device__ __forceinline__ int turn_from(int part, int parts, int turns) { return (int)((long)part * turns / parts); }
-// The n that fills the chip's `slots` places for workgroups, with eight turns a part left on average; grid: workgroups of one part's launch,
+// The n that fills the chip's `slots` places for workgroups, with four turns a part left on average; grid: workgroups of one part's launch,
 // empty ones too
 inline int parts_of(long workgroups, long grid, long slots, long turns) {
   long n = (slots + workgroups - 1) / workgroups;
-  for (const long most : {turns / 8, kMaxGrid / grid, 16L}) n = n < most ? n : most;
+  for (const long most : {turns / 4, kMaxGrid / grid, 16L}) n = n < most ? n : most;
   return (int)(n > 1 ? n : 1);
 }
 
