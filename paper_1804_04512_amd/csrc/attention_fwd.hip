@@ -15,26 +15,37 @@ using namespace attn;
 
 namespace {
 
-constexpr int kQueries = 128, kThreads = 256;
+constexpr int kThreads = 256, kMostRows = 4;
 
-// keys of a tile: 64 KB of LDS at most for both halves of a workgroup's tiles of keys and values, or 96 for the three planes of the largest
-template <class T, int DP> constexpr int keys_of() { return DP > 128 || (sizeof(T) == 4 && DP > 64) ? 32 : 64; }
+// A workgroup's four wavefronts are ROWS groups of 32 queries times 4 / ROWS groups that share a tile's keys.
+template <class T, int DP, int ROWS>
+struct Shape {
+  // keys of a tile: 32 or 64 a wavefront, and 128 KB of LDS at most for the keys' and the values' two tiles (single precision: three planes)
+  static constexpr int kKeyGroups = 4 / ROWS, kPer = ROWS < 4 || DP > 128 || (sizeof(T) == 4 && DP > 64) ? 32 : 64, kKeys = kPer * kKeyGroups;
+  static constexpr int kQueries = 32 * ROWS;
+  typedef Stager<T, DP, kKeys, kThreads> Rows;
+  static constexpr int kLeft = DP * 128 + 512;   // bytes that a wavefront leaves for another one: its outputs, maxima and sums
+  static constexpr int kLds = 2 * Rows::kBytes > (kKeyGroups - 1) * ROWS * kLeft ? 2 * Rows::kBytes : (kKeyGroups - 1) * ROWS * kLeft;
+  static constexpr bool kExists = ROWS == 4 || (sizeof(T) == 2 && kLds <= 128 * 1024);
+  // workgroups that a compute unit holds
+  static constexpr int kResident = (sizeof(T) == 2 ? DP <= 128 : DP <= 96) && kLds <= 80 * 1024 ? 2 : 1;
+};
 
-// workgroups that a compute unit holds, by their registers
-template <class T, int DP> constexpr int residents() { return (sizeof(T) == 2 ? DP <= 128 : DP <= 96) ? 2 : 1; }
-
-template <class T, int DP, int BN>
-__global__ __launch_bounds__(kThreads, (residents<T, DP>())) void attention_fwd_kernel(const AttentionArgs a, const Parts parts, const int tiles) {
-  typedef Stager<T, DP, BN, kThreads> S;
+template <class T, int DP, int ROWS>
+__global__ __launch_bounds__(kThreads, (Shape<T, DP, ROWS>::kResident)) void attention_fwd_kernel(const AttentionArgs a, const Parts parts, const int tiles) {
+  typedef Shape<T, DP, ROWS> Sh;
+  typedef typename Sh::Rows S;
+  constexpr int BN = Sh::kKeys, kPer = Sh::kPer, kQueries = Sh::kQueries;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+  const int mine = wave / ROWS * kPer;   // this wavefront's keys of a tile
   // heads of one key head side by side, on as few XCDs as may be; the last tiles, which see most keys, first
   const int part = blockIdx.x % parts.n, id = blockIdx.x / parts.n, kv = id % a.KV, rest = id / a.KV, group = a.H / a.KV, head = kv * group + rest % group,
             tile = tiles - 1 - rest / group;
   const Place pq = place_of(a.q_starts, a.S, a.Tq, tile, kQueries);
   if (pq.at >= pq.count) return;
   const int kv_first = start_of(a.kv_starts, pq.sequence, a.Tk), keys = max(0, start_of(a.kv_starts, pq.sequence + 1, a.Tk) - kv_first);
-  const int row0 = pq.at + 32 * wave, row = row0 + (lane & 31), shift = keys - pq.count;
+  const int row0 = pq.at + 32 * (wave % ROWS), row = row0 + (lane & 31), shift = keys - pq.count;
   const int seen = a.causal ? max(0, min(keys, row + shift + 1)) : keys;                                    // by this lane's query
   const int seen_first = a.causal ? max(0, min(keys, row0 + shift + 1)) : keys;                             // by the wavefront's first
   const int seen_last = row0 >= pq.count ? 0 : a.causal ? max(0, min(keys, min(row0 + 32, pq.count) + shift)) : keys;   // by its last
@@ -61,23 +72,23 @@ __global__ __launch_bounds__(kThreads, (residents<T, DP>())) void attention_fwd_
     const char *lk = sk.turn(wave, odd, k, key0 + BN, keys), *lv = sv.turn(wave, odd, v, key0 + BN, keys);
     landed<T, 2 * S::kLoads>();
     barrier();
-    if (key0 < seen_last) {
-      floatx16 z[BN / 32];
+    if (key0 + mine < seen_last) {
+      floatx16 z[kPer / 32];
 #pragma unroll
-      for (int b = 0; b < BN / 32; ++b) z[b] = floatx16{};
+      for (int b = 0; b < kPer / 32; ++b) z[b] = floatx16{};
 #pragma unroll
       for (int s = 0; s < DP / 16; ++s)
 #pragma unroll
-        for (int b = 0; b < BN / 32; ++b) z[b] = mma(reader.along(lk, 32 * b, s), q[s], z[b]);
-      if (key0 + BN > seen_first)
+        for (int b = 0; b < kPer / 32; ++b) z[b] = mma(reader.along(lk, mine + 32 * b, s), q[s], z[b]);
+      if (key0 + mine + kPer > seen_first)
 #pragma unroll
-        for (int b = 0; b < BN / 32; ++b)
+        for (int b = 0; b < kPer / 32; ++b)
 #pragma unroll
           for (int r = 0; r < 16; ++r)
-            if (key0 + 32 * b + token_of(r) + 4 * half >= seen) z[b][r] = -INFINITY;
+            if (key0 + mine + 32 * b + token_of(r) + 4 * half >= seen) z[b][r] = -INFINITY;
       float top = -INFINITY;
 #pragma unroll
-      for (int b = 0; b < BN / 32; ++b)
+      for (int b = 0; b < kPer / 32; ++b)
 #pragma unroll
         for (int r = 0; r < 16; ++r) top = fmaxf(top, z[b][r]);
       top = fmaxf(top, other_half(top)) * c;
@@ -92,25 +103,64 @@ __global__ __launch_bounds__(kThreads, (residents<T, DP>())) void attention_fwd_
       }
       const float from = m == -INFINITY ? 0.0f : m;
 #pragma unroll
-      for (int b = 0; b < BN / 32; ++b)
+      for (int b = 0; b < kPer / 32; ++b)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           z[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[b][r], c, -from));
           l += z[b][r];
         }
 #pragma unroll
-      for (int s = 0; s < BN / 16; ++s) {
+      for (int s = 0; s < kPer / 16; ++s) {
         const Frag<T> p = frag_of<T>(z[s / 2], s % 2);
 #pragma unroll
-        for (int i = 0; i < DP / 32; ++i) o[i] = mma(reader.across(lv, 16 * s, 32 * i), p, o[i]);
+        for (int i = 0; i < DP / 32; ++i) o[i] = mma(reader.across(lv, mine + 16 * s, 32 * i), p, o[i]);
       }
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     barrier();
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // of the tile of zeros too
-  if (row >= pq.count) return;
   l += other_half(l);
+  if constexpr (ROWS < 4) {   // the groups' outputs together, in the tiles' place, in the groups' order
+    constexpr int kLeft = Sh::kLeft;
+    barrier();
+    if (wave >= ROWS) {
+      char *to = smem + (wave - ROWS) * kLeft;
+#pragma unroll
+      for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          *reinterpret_cast<floatx4 *>(to + ((i * 4 + r) * 64 + lane) * 16) = floatx4{o[i][4 * r], o[i][4 * r + 1], o[i][4 * r + 2], o[i][4 * r + 3]};
+      float *ml = reinterpret_cast<float *>(to + DP * 128);
+      ml[lane] = m;
+      ml[64 + lane] = l;
+    }
+    __syncthreads();
+    if (wave >= ROWS) return;
+    float top = m;
+#pragma unroll
+    for (int g = 1; g < 4 / ROWS; ++g) top = fmaxf(top, reinterpret_cast<const float *>(smem + (wave + (g - 1) * ROWS) * kLeft + DP * 128)[lane]);
+    const float from = top == -INFINITY ? 0.0f : top, own = __builtin_amdgcn_exp2f(m - from);
+    l *= own;
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i) o[i] *= own;
+#pragma unroll
+    for (int g = 1; g < 4 / ROWS; ++g) {
+      const char *other = smem + (wave + (g - 1) * ROWS) * kLeft;
+      const float *ml = reinterpret_cast<const float *>(other + DP * 128), f = __builtin_amdgcn_exp2f(ml[lane] - from);
+      l += f * ml[64 + lane];
+#pragma unroll
+      for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const floatx4 v = *reinterpret_cast<const floatx4 *>(other + ((i * 4 + r) * 64 + lane) * 16);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[i][4 * r + j] += f * v[j];
+        }
+    }
+    m = top;
+  }
+  if (row >= pq.count) return;
   const long at = pq.first + row;
   if (parts.n > 1) {
     const long to = (long)part * a.Tq + at;
@@ -154,49 +204,71 @@ __global__ __launch_bounds__(kThreads) void attention_join_kernel(const Attentio
 
 // The workspace's parts, the same walk for the query and the call
 struct FwdPlan {
+  int rows = kMostRows;
   Parts parts;
   size_t bytes;
-  FwdPlan(const AttentionArgs &a, int keys, int resident, char *base) {
-    Take take{base};
-    parts.n = parts_of((a.Tq + kQueries - 1) / kQueries * (long)a.H, tiles_of(a.Tq, a.S, kQueries) * a.H, (long)resident * chip().cus, a.Tk / a.S / keys);
-    parts.ld = (a.D + 3) & ~3;
-    if (parts.n > 1) {
-      parts.sums[0] = (float *)take((size_t)parts.n * a.Tq * a.H * parts.ld * sizeof(float));
-      parts.ml = (float *)take((size_t)parts.n * a.Tq * a.H * 2 * sizeof(float));
-    }
-    bytes = take.used;
-  }
 };
-
+template <class T, int DP, int ROWS>
+FwdPlan plan_as(const AttentionArgs &a, char *base) {
+  typedef Shape<T, DP, ROWS> S;
+  FwdPlan p;
+  Take take{base};
+  p.rows = ROWS;
+  p.parts.n = parts_of((a.Tq + S::kQueries - 1) / S::kQueries * (long)a.H, tiles_of(a.Tq, a.S, S::kQueries) * a.H, (long)S::kResident * chip().cus, a.Tk / a.S / S::kKeys);
+  p.parts.ld = (a.D + 3) & ~3;
+  if (p.parts.n > 1) {
+    p.parts.sums[0] = (float *)take((size_t)p.parts.n * a.Tq * a.H * p.parts.ld * sizeof(float));
+    p.parts.ml = (float *)take((size_t)p.parts.n * a.Tq * a.H * 2 * sizeof(float));
+  }
+  p.bytes = take.used;
+  return p;
+}
 template <class T, int DP>
-hipError_t fwd_as(const AttentionArgs &a, char *scratch, hipStream_t stream) {
-  constexpr int BN = keys_of<T, DP>();
-  constexpr size_t lds = 2 * Stager<T, DP, BN, kThreads>::kBytes;
-  const auto kernel = attention_fwd_kernel<T, DP, BN>;
-  DLL_TRY(allow_large_lds(reinterpret_cast<const void *>(kernel), lds));
-  const FwdPlan p(a, BN, residents<T, DP>(), scratch);
-  const long tiles = tiles_of(a.Tq, a.S, kQueries);
-  kernel<<<dim3((unsigned)(tiles * a.H * p.parts.n)), dim3(kThreads), lds, stream>>>(a, p.parts, (int)tiles);
-  DLL_TRY(hipGetLastError());
-  if (p.parts.n == 1) return hipSuccess;
-  const long units = (long)a.Tq * a.H * (p.parts.ld / 4), blocks = (units + kThreads - 1) / kThreads;
-  attention_join_kernel<T><<<dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(kThreads), 0, stream>>>(a, p.parts, units);
-  return hipGetLastError();
+FwdPlan plan(const AttentionArgs &a, char *base) {
+  // as many workgroups of 128 queries as there are at least
+  const long all = (a.Tq + 127) / 128 > a.S ? (a.Tq + 127) / 128 : a.S, workgroups = all * a.H;
+  if constexpr (Shape<T, DP, 2>::kExists) {
+    if constexpr (Shape<T, DP, 1>::kExists)
+      if (2 * workgroups < chip().cus && a.Tk / a.S >= 512) return plan_as<T, DP, 1>(a, base);
+    if (workgroups < 2 * chip().cus) return plan_as<T, DP, 2>(a, base);
+  }
+  return plan_as<T, DP, 4>(a, base);
+}
+
+template <class T, int DP, int ROWS>
+hipError_t fwd_as(const AttentionArgs &a, const FwdPlan &p, hipStream_t stream) {
+  typedef Shape<T, DP, ROWS> S;
+  if constexpr (S::kExists) {
+    const auto kernel = attention_fwd_kernel<T, DP, ROWS>;
+    DLL_TRY(allow_large_lds(reinterpret_cast<const void *>(kernel), S::kLds));
+    const long tiles = tiles_of(a.Tq, a.S, S::kQueries);
+    kernel<<<dim3((unsigned)(tiles * a.H * p.parts.n)), dim3(kThreads), S::kLds, stream>>>(a, p.parts, (int)tiles);
+    DLL_TRY(hipGetLastError());
+    if (p.parts.n == 1) return hipSuccess;
+    const long units = (long)a.Tq * a.H * (p.parts.ld / 4), blocks = (units + kThreads - 1) / kThreads;
+    attention_join_kernel<T><<<dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(kThreads), 0, stream>>>(a, p.parts, units);
+    return hipGetLastError();
+  }
+  return hipErrorInvalidValue;   // not planned
 }
 
 template <class T>
 hipError_t fwd(const AttentionArgs &a, char *scratch, hipStream_t stream) {
-  return instance(a.D, [&](auto dp) { return fwd_as<T, decltype(dp)::value>(a, scratch, stream); });
+  return instance(a.D, [&](auto dp) {
+    constexpr int DP = decltype(dp)::value;
+    const FwdPlan p = plan<T, DP>(a, scratch);
+    return p.rows == 4 ? fwd_as<T, DP, 4>(a, p, stream) : p.rows == 2 ? fwd_as<T, DP, 2>(a, p, stream) : fwd_as<T, DP, 1>(a, p, stream);
+  });
 }
 template <class T>
 size_t fwd_bytes(const AttentionArgs &a) {
-  return instance(a.D, [&](auto dp) { return FwdPlan(a, keys_of<T, decltype(dp)::value>(), residents<T, decltype(dp)::value>(), nullptr).bytes; });
+  return instance(a.D, [&](auto dp) { return plan<T, decltype(dp)::value>(a, nullptr).bytes; });
 }
 
 }  // namespace
 
 bool attention_fits(int q_tokens, int kv_tokens, int sequences, int heads) {
-  return tiles_of(q_tokens > kv_tokens ? q_tokens : kv_tokens, sequences, kQueries) * heads <= kMaxGrid;
+  return tiles_of(q_tokens > kv_tokens ? q_tokens : kv_tokens, sequences, 32) * heads <= kMaxGrid;
 }
 
 size_t attention_fwd_scratch(const AttentionArgs &a) { return (a.dtype == TYPE_BF16 ? fwd_bytes<bf16>(a) : fwd_bytes<float>(a)) + 1; }   // never nothing
