@@ -43,7 +43,7 @@ __device__ __forceinline__ float row_product(const T *x, const T *y, int dim, in
 #pragma unroll
     for (int j = 0; j < 8; ++j) sum += to_float(e.v[j]) * to_float(f.v[j]);
   }
-  return sum + other_half(sum);
+  return sum_of_halves(sum);
 }
 
 // ------------------------------------------------------------------------------------------------ dq
@@ -95,9 +95,9 @@ __global__ __launch_bounds__(kThreads, (dq_residents<T, DP>())) void attention_d
   const Reader<T, DP, BN> reader(lane);
   int odd = 1;
   for (int key0 = begin; key0 < end; key0 += BN, odd ^= 1) {
+    landed<T>();
     const char *lk = sk.turn(wave, odd, k, key0 + BN, keys), *lv = sv.turn(wave, odd, v, key0 + BN, keys);
-    landed<T, 2 * S::kLoads>();
-    barrier();
+    written<T>();
 #pragma unroll 1
     for (int b = 0; b < BN && key0 + b < seen_last; b += 32) {
       floatx16 z = {}, d;
@@ -123,8 +123,6 @@ __global__ __launch_bounds__(kThreads, (dq_residents<T, DP>())) void attention_d
         for (int i = 0; i < DP / 32; ++i) dq[i] = mma(reader.across(lk, b + 16 * s, 32 * i), ds, dq[i]);
       }
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    barrier();
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   if (row >= pq.count) return;
@@ -197,11 +195,11 @@ __global__ __launch_bounds__(kThreads, (dkv_residents<T, DP>())) void attention_
   int odd = 1;
   for (int turn = begin; turn < end; ++turn, odd ^= 1) {
     const Turn next = turn_of(turn + 1);
+    landed<T>();
     const char *lq = sq.turn(wave, odd, next.q, next.i0, queries), *lg = sg.turn(wave, odd, next.g, next.i0, queries);
     if constexpr (sizeof(T) == 4) reinterpret_cast<float *>(figures)[(2 * (odd ^ 1) + (wave & 1)) * (kFigures / 4) + lane] = held;
     load_figures(next, odd);
-    landed<T, 2 * S::kLoads + 1>();
-    barrier();
+    written<T>();
     const float *lse2 = reinterpret_cast<const float *>(figures + 2 * (odd ^ 1) * kFigures), *minus_delta = lse2 + kFigures / 4;
     const int i0 = from + (turn % tiles) * BN;
 #pragma unroll 1
@@ -250,8 +248,6 @@ __global__ __launch_bounds__(kThreads, (dkv_residents<T, DP>())) void attention_
         }
       }
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    barrier();
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   if (key >= pk.count) return;

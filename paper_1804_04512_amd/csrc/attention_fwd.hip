@@ -69,17 +69,28 @@ __global__ __launch_bounds__(kThreads, (Shape<T, DP, ROWS>::kResident)) void att
   const Reader<T, DP, BN> reader(lane);
   int odd = 1;
   for (int key0 = begin; key0 < end; key0 += BN, odd ^= 1) {
+    landed<T>();
     const char *lk = sk.turn(wave, odd, k, key0 + BN, keys), *lv = sv.turn(wave, odd, v, key0 + BN, keys);
-    landed<T, 2 * S::kLoads>();
-    barrier();
+    written<T>();
     if (key0 + mine < seen_last) {
       floatx16 z[kPer / 32];
 #pragma unroll
       for (int b = 0; b < kPer / 32; ++b) z[b] = floatx16{};
+      // keys are read a step ahead of the products that take them
+      Frag<T> kf[2][kPer / 32];
+      const auto read = [&](int s) {
 #pragma unroll
-      for (int s = 0; s < DP / 16; ++s)
+        for (int b = 0; b < kPer / 32; ++b) kf[s & 1][b] = reader.along(lk, mine + 32 * b, s);
+      };
+      read(0);
 #pragma unroll
-        for (int b = 0; b < kPer / 32; ++b) z[b] = mma(reader.along(lk, mine + 32 * b, s), q[s], z[b]);
+      for (int s = 0; s < DP / 16; ++s) {
+        if (s + 1 < DP / 16) read(s + 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int b = 0; b < kPer / 32; ++b) z[b] = mma(kf[s & 1][b], q[s], z[b]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
       if (key0 + mine + kPer > seen_first)
 #pragma unroll
         for (int b = 0; b < kPer / 32; ++b)
@@ -91,7 +102,7 @@ __global__ __launch_bounds__(kThreads, (Shape<T, DP, ROWS>::kResident)) void att
       for (int b = 0; b < kPer / 32; ++b)
 #pragma unroll
         for (int r = 0; r < 16; ++r) top = fmaxf(top, z[b][r]);
-      top = fmaxf(top, other_half(top)) * c;
+      top = most_of_halves(top) * c;
       if (__any(top > m + 8.0f)) {
         const float grown = fmaxf(m, top), shrink = grown == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - grown);
         m = grown;
@@ -116,11 +127,9 @@ __global__ __launch_bounds__(kThreads, (Shape<T, DP, ROWS>::kResident)) void att
         for (int i = 0; i < DP / 32; ++i) o[i] = mma(reader.across(lv, mine + 16 * s, 32 * i), p, o[i]);
       }
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    barrier();
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // of the tile of zeros too
-  l += other_half(l);
+  l = sum_of_halves(l);
   if constexpr (ROWS < 4) {   // the groups' outputs together, in the tiles' place, in the groups' order
     constexpr int kLeft = Sh::kLeft;
     barrier();

@@ -65,12 +65,12 @@ struct Tile {
   }
 };
 
-// NR tokens' rows from memory into LDS, for a loop over tiles of them: `start` sends the first tile on its way; `turn` sees to it that tile
-// `now` is in LDS (behind the caller's barrier), sends `next` on its way and says where the tile lies.  What lies behind the last row, and behind a
-// row's dim elements, is zeros.
+// NR tokens' rows from memory into LDS, for a loop over tiles of them: `start` sends the first tile on its way; `turn`, called by everyone behind a
+// barrier at which the former tile is done with and, `landed`, this one has come, sends the next one on its way and says where this one lies.  What
+// lies behind the last row, and behind a row's dim elements, is zeros.
 //
-// bfloat16 goes straight into LDS, the next tile into the other half of the area.  Single precision comes through registers, where it is split once for
-// all wavefronts, and has one area, written between the caller's barriers.
+// bfloat16 goes straight into LDS, the tiles into the halves of the area in turn.  Single precision comes through registers, where it is split once for
+// all wavefronts, and has one area, which `turn` writes: `written` has to follow.
 template <class T, int DP, int NR, int THREADS>
 struct Stager;
 
@@ -163,11 +163,19 @@ struct Stager<float, DP, NR, THREADS> {
   }
 };
 
-// What the caller's barrier of a turn stands behind: all loads straight into LDS but the LATER newest ones have landed, and LDS is written
-template <class T, int LATER>
+// The barrier in front of `turn`: all loads straight into LDS have landed
+template <class T>
 __device__ __forceinline__ void landed() {
-  if constexpr (sizeof(T) == 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LATER) : "memory");
-  else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  if constexpr (sizeof(T) == 2) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  barrier();
+}
+// The one behind it
+template <class T>
+__device__ __forceinline__ void written() {
+  if constexpr (sizeof(T) == 4) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    barrier();
+  }
 }
 
 // Fragments of a tile of NR rows in LDS for lane l: of scores, elements 16 s + 8 (l / 32) on of row x0 + l % 32; of sums over tokens, element
@@ -279,8 +287,27 @@ __device__ __forceinline__ void store_sums(float *p, const floatx16 (&c)[N], int
         *reinterpret_cast<floatx4 *>(p + 32 * i + 8 * q + 4 * half) = floatx4{c[i][4 * q], c[i][4 * q + 1], c[i][4 * q + 2], c[i][4 * q + 3]};
 }
 
-// What the other half of the wavefront's lanes holds for the same column
-__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+// Here is where a fragment's value is made: it is not moved behind what follows
+__device__ __forceinline__ void made(bf16x8 &f) {
+  uintx4 v = __builtin_bit_cast(uintx4, f);
+  asm volatile("" : "+v"(v));
+  f = __builtin_bit_cast(bf16x8, v);
+}
+__device__ __forceinline__ void made(Split &f) {
+#pragma unroll
+  for (int k = 0; k < 3; ++k) made(f.p[k]);
+}
+
+// Over both halves of the wavefront's lanes.  The swap of the one's upper with the other's lower half leaves both halves' values in two registers.
+struct Halves { float a, b; };
+__device__ __forceinline__ Halves halves(float v) {
+  const unsigned u = __builtin_bit_cast(unsigned, v);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  const unsigned a = r[0], b = r[1];
+  return Halves{__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)};
+}
+__device__ __forceinline__ float most_of_halves(float v) { const Halves h = halves(v); return fmaxf(h.a, h.b); }
+__device__ __forceinline__ float sum_of_halves(float v) { const Halves h = halves(v); return h.a + h.b; }
 
 // Packed sequences in tiles of B tokens: sequence s has its tiles from starts[s] / B + s on, which leaves room for the last, part-filled one
 // of each, so no table of tiles is needed.  The last s with starts[s] / B + s <= t is found by sixty-four probes at a time.
