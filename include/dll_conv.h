@@ -433,7 +433,8 @@ typedef struct {
  *   free_pages [n_free] pages that nobody has, taken from entry *free_at on (NULL: 0; n_free = 0: free_pages may be NULL) in the requests' order
  *   table   [requests][table_pages]  entries of the pages that the requests had before are read, those of the new pages are written,
  *           the others left as they are
- *   starts  [requests + 1]  receives where each request's new tokens lie when they are packed (q_starts of dll_attention_fwd)
+ *   starts  [requests + 1]  receives where each request's new tokens lie when they are packed (q_starts of dll_attention_fwd); sums
+ *           stop at 2^30, and so do those of state
  *   slots   [tokens]  receives page * page_tokens + place for each new token; -1 where it has no page.  tokens, at least 1, is the array's room:
  *           new tokens behind it get neither slot nor table entry; what lies behind the new tokens is left as it is
  *   state   [2]  receives the first entry of free_pages that is still free, and how many pages were missing, as the list was too short (their

@@ -103,10 +103,19 @@ __global__ __launch_bounds__(kThreads, (dq_residents<T, DP>())) void attention_d
       floatx16 z = {}, d;
 #pragma unroll
       for (int r = 0; r < 16; ++r) d[r] = minus_delta;
+      Frag<T> kf[2], vf[2];   // read a step ahead of the products that take them
+      kf[0] = reader.along(lk, b, 0);
+      vf[0] = reader.along(lv, b, 0);
 #pragma unroll
       for (int s = 0; s < DP / 16; ++s) {
-        z = mma(reader.along(lk, b, s), q[s], z);
-        d = mma(reader.along(lv, b, s), g[s], d);
+        if (s + 1 < DP / 16) {
+          kf[(s + 1) & 1] = reader.along(lk, b, s + 1);
+          vf[(s + 1) & 1] = reader.along(lv, b, s + 1);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        z = mma(kf[s & 1], q[s], z);
+        d = mma(vf[s & 1], g[s], d);
+        __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
       for (int r = 0; r < 16; ++r) z[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[r], c, -lse2));
@@ -213,10 +222,19 @@ __global__ __launch_bounds__(kThreads, (dkv_residents<T, DP>())) void attention_
 #pragma unroll
           for (int j = 0; j < 4; ++j) d[4 * r + j] = w[j];
         }
+      Frag<T> qf[2], gf[2];
+      qf[0] = reader.along(lq, b, 0);
+      if constexpr (DK) gf[0] = reader.along(lg, b, 0);
 #pragma unroll
       for (int s = 0; s < DP / 16; ++s) {
-        z = mma(reader.along(lq, b, s), k[s], z);
-        if constexpr (DK) d = mma(reader.along(lg, b, s), v[s], d);
+        if (s + 1 < DP / 16) {
+          qf[(s + 1) & 1] = reader.along(lq, b, s + 1);
+          if constexpr (DK) gf[(s + 1) & 1] = reader.along(lg, b, s + 1);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        z = mma(qf[s & 1], k[s], z);
+        if constexpr (DK) d = mma(gf[s & 1], v[s], d);
+        __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
       for (int r = 0; r < 4; ++r) {

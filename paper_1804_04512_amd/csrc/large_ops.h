@@ -16,6 +16,16 @@ inline long padded(long n) { return (n + 63) & ~63L; }
 // first.
 inline bool loadable(long n, int dtype) { return n * (long)type_bytes(dtype) % 4 == 0; }
 
+// n / d for n from 0 to 2^31 - 1: n * (floor(2^(31 + shift) / d) + 1) / 2^(31 + shift), off by less than 1 / d where 2^shift >= d
+struct Divisor {
+  unsigned factor, shift;
+  explicit Divisor(int d) : shift(0) {
+    while (1L << shift < d) ++shift;
+    factor = (unsigned)((1L << (31 + shift)) / d + 1);
+  }
+  __device__ __forceinline__ int of(int n) const { return (int)(__umulhi((unsigned)n << 1, factor) >> shift); }
+};
+
 // ---- gated feed-forward block -------------------------------------------------------------------------------------
 struct GatedArgs {
   int T = 0, D = 0, H = 0, gate = 0, dtype = 0;

@@ -20,18 +20,8 @@ using namespace attn;
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = 4, kTile = 32, kUnit = 128, kHeads = 16;
+constexpr int kThreads = 256, kWaves = 4, kTile = 32, kUnit = kWaves * kTile, kHeads = 16;
 constexpr int kMaxGroups = 1024;   // workgroups of a launch
-
-// n / d for n below 2^30: n * (floor(2^(30 + shift) / d) + 1) / 2^(30 + shift), off by less than 1 / d where 2^shift >= d
-struct Divisor {
-  unsigned factor, shift;
-  explicit Divisor(int d) : shift(0) {
-    while (1L << shift < d) ++shift;
-    factor = (unsigned)((1L << (30 + shift)) / d + 1);
-  }
-  __device__ __forceinline__ int of(int n) const { return (int)(__umulhi((unsigned)n << 2, factor) >> shift); }
-};
 
 // workgroups that a compute unit holds, by their registers
 template <class T, int DP> constexpr int residents() { return (sizeof(T) == 2 ? DP <= 128 : DP <= 96) ? 2 : 1; }
@@ -97,7 +87,7 @@ __device__ __forceinline__ int owner_of(long unit, long all, int n) { return (in
 // behind the wavefronts' areas in LDS
 struct Shared {
   long scratch[kWaves + 1];
-  int found;
+  int found, keys, empty[kWaves];
   float ml[kWaves][kHeads][2];
 };
 
@@ -117,26 +107,32 @@ __global__ __launch_bounds__(kThreads, (residents<T, DP>())) void paged_attentio
   const int group = a.H / a.KV, blocks = parts.blocks, VH = a.KV * blocks;
   const float c = fmaxf(fabsf(a.scale) * kLog2e, 0x1p-126f);
 
-  // requests without keys
-  for (int r = blockIdx.x; r < a.R; r += gridDim.x)
-    if (keys_of(a, r) == 0)
-      for (int i = threadIdx.x; i < a.H * a.D; i += kThreads) {
-        ((T *)a.o)[(long)r * a.H * a.D + i] = (T)0.0f;
-        if (a.lse && i < a.H) a.lse[(long)r * a.H + i] = -INFINITY;
-      }
-
   // this workgroup's units, and the request that the first of them belongs to
   const int each = (a.R + kThreads - 1) / kThreads, r0 = min((int)threadIdx.x * each, a.R), r1 = min(r0 + each, a.R);
   long mine = 0;
-  for (int r = r0; r < r1; ++r) mine += units_of(keys_of(a, r));
+  int empty = 0, keys = 0;   // some request has no keys; the last one's
+  for (int r = r0; r < r1; ++r) {
+    keys = keys_of(a, r);
+    mine += units_of(keys);
+    empty |= keys == 0;
+  }
   long up = mine;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
     const long o = __shfl_up(up, d);
     if (lane >= d) up += o;
   }
-  if (lane == 63) scratch[wave] = up;
+  const int some = __any(empty);
+  if (lane == 63) scratch[wave] = up, shared.empty[wave] = some;
   __syncthreads();
+  if (shared.empty[0] | shared.empty[1] | shared.empty[2] | shared.empty[3]) {   // their outputs, by all workgroups in turn
+    for (int r = blockIdx.x; r < a.R; r += gridDim.x)
+      if (keys_of(a, r) == 0)
+        for (int i = threadIdx.x; i < a.H * a.D; i += kThreads) {
+          ((T *)a.o)[(long)r * a.H * a.D + i] = (T)0.0f;
+          if (a.lse && i < a.H) a.lse[(long)r * a.H + i] = -INFINITY;
+        }
+  }
   long before = up - mine, all = 0;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
@@ -150,9 +146,11 @@ __global__ __launch_bounds__(kThreads, (residents<T, DP>())) void paged_attentio
   if (before * VH <= first && first < (before + mine) * VH) {
     long base = before * VH;
     for (int r = r0; r < r1; ++r) {
-      const long n = (long)units_of(keys_of(a, r)) * VH;
+      if (each > 1) keys = keys_of(a, r);
+      const long n = (long)units_of(keys) * VH;
       if (first < base + n) {
         shared.found = r;
+        shared.keys = keys;
         scratch[kWaves] = base;
         break;
       }
@@ -162,6 +160,7 @@ __global__ __launch_bounds__(kThreads, (residents<T, DP>())) void paged_attentio
   __syncthreads();
   int r = __builtin_amdgcn_readfirstlane(shared.found);
   long base = scratch[kWaves];
+  keys = __builtin_amdgcn_readfirstlane(shared.keys);
 
   int off[kSteps];   // a lane's run of each step in its row, in bytes
 #pragma unroll
@@ -169,11 +168,7 @@ __global__ __launch_bounds__(kThreads, (residents<T, DP>())) void paged_attentio
   const long row_bytes = (long)a.D * (int)sizeof(T), head_bytes = a.page * row_bytes, page_bytes = a.KV * head_bytes;
 
   for (long u = first; u < end;) {
-    const int keys = __builtin_amdgcn_readfirstlane(keys_of(a, r)), per = units_of(keys);
-    if (per == 0) {   // r stays in range: units before `end` are somebody's
-      ++r;
-      continue;
-    }
+    const int per = units_of(keys);
     const long rel = u - base;
     const int vh = (int)(rel / per), unit0 = (int)(rel % per), units = (int)min((long)(per - unit0), end - u);
     const int kv = vh / blocks, block = vh % blocks, heads = min(kHeads, group - block * kHeads), head0 = kv * group + block * kHeads;
@@ -370,66 +365,72 @@ __global__ __launch_bounds__(kThreads, (residents<T, DP>())) void paged_attentio
     u += units;
     if (rel + units == (long)per * VH) {
       base += (long)per * VH;
-      ++r;
+      if (u < end)   // some later request has the next unit
+        do keys = __builtin_amdgcn_readfirstlane(keys_of(a, ++r));
+        while (keys == 0);
     }
   }
 }
 
-// One request's head, where more than one workgroup had a part of it: the parts' factors first, then their outputs, four elements a thread
-// and as many parts side by side as there are threads
+// One request's heads that share a key head, or one of them, where more than one workgroup had a part of them: each head's factors by sixteen
+// threads or a wavefront, then the outputs, four elements a thread and as many parts side by side as there are threads
 template <class T>
-__global__ __launch_bounds__(kThreads) void paged_join_kernel(const CacheArgs a, const Runs parts, int groups) {
+__global__ __launch_bounds__(kThreads) void paged_join_kernel(const CacheArgs a, const Runs parts, int groups, const int single) {
   __shared__ long scratch[2 * kWaves];
-  __shared__ float factor[kMaxGroups], level[2][kWaves];
+  __shared__ float from[kHeads], total[kHeads], shift[kHeads];
   __shared__ floatx4 sums[kThreads];
-  const int r = blockIdx.x / a.H, head = blockIdx.x % a.H, group = a.H / a.KV, VH = a.KV * parts.blocks, t = threadIdx.x;
+  const int group = a.H / a.KV, VH = a.KV * parts.blocks, t = threadIdx.x;
+  const int wide_group = min(kHeads, group), id = single ? blockIdx.x / wide_group : blockIdx.x, r = id / VH, vh = id % VH;
   const int per = units_of(keys_of(a, r));
   if (per <= 1) return;
   long before, all;
   add_units(a, r, &before, &all, scratch);
   all *= VH;
   groups = working(all, groups);
-  const int in = head % group, h = in % kHeads;
-  const long unit = before * VH + (long)((head / group) * parts.blocks + in / kHeads) * per;
+  const long unit = before * VH + (long)vh * per;
   const int w0 = owner_of(unit, all, groups), n = owner_of(unit + per - 1, all, groups) - w0 + 1;
   if (n == 1) return;
   const int slot0 = 2 * w0 + (unit == run_of(w0, all, groups) ? 0 : 1);
-  const auto row_of = [&](int i) { return (i == 0 ? slot0 : 2 * (w0 + i)) * kHeads + h; };
-  float top = -INFINITY;
-  for (int i = t; i < n; i += kThreads) top = fmaxf(top, parts.ml[row_of(i) * 2]);
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-  if ((t & 63) == 0) level[0][t >> 6] = top;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, level[0][w]);
-  const float from = top == -INFINITY ? 0.0f : top;
-  float sum = 0.0f;
-  for (int i = t; i < n; i += kThreads) {
-    const float f = __builtin_amdgcn_exp2f(parts.ml[row_of(i) * 2] - from);
-    factor[i] = f;
-    sum += f * parts.ml[row_of(i) * 2 + 1];
+  const int block = vh % parts.blocks, all_heads = min(kHeads, group - block * kHeads),
+            skip = single ? blockIdx.x % wide_group : 0, heads = single ? 1 : all_heads, head0 = vh / parts.blocks * group + block * kHeads + skip;
+  if (skip >= all_heads) return;
+  const auto row_of = [&](int i, int h) { return (long)(i == 0 ? slot0 : 2 * (w0 + i)) * kHeads + skip + h; };
+  {
+    const int lanes = single ? 64 : 16, h = single ? 0 : t / 16;
+    float top = -INFINITY, sum = 0.0f;
+    if (h < heads)
+      for (int i = t % lanes; i < n; i += lanes) top = fmaxf(top, parts.ml[row_of(i, h) * 2]);
+    for (int d = 1; d < lanes; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+    const float base = top == -INFINITY ? 0.0f : top;
+    if (h < heads)
+      for (int i = t % lanes; i < n; i += lanes) sum += __builtin_amdgcn_exp2f(parts.ml[row_of(i, h) * 2] - base) * parts.ml[row_of(i, h) * 2 + 1];
+    for (int d = 1; d < lanes; d *= 2) sum += __shfl_xor(sum, d);
+    if (t % lanes == 0 && (!single || t == 0)) from[h] = base, total[h] = sum, shift[h] = top;
   }
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-  if ((t & 63) == 0) level[1][t >> 6] = sum;
   __syncthreads();
-  sum = 0.0f;
+  const int wide = parts.ld / 4, items = heads * wide, side = max(1, kThreads / items);   // wide: 1 to 64
+  for (int first = 0; first < items; first += kThreads) {   // more than one turn with more items than threads
+    const int item = first + t % (side > 1 ? items : kThreads), p = side > 1 ? t / items : 0, h = min(item / wide, heads - 1), c = item % wide;
+    floatx4 out = {};
+    if (item < items && p < side)
+#pragma unroll 4
+      for (int i = p; i < n; i += side) {
+        const long row = row_of(i, h);
+        out += __builtin_amdgcn_exp2f(parts.ml[row * 2] - from[h]) * *reinterpret_cast<const floatx4 *>(parts.o + row * parts.ld + 4 * c);
+      }
+    if (side > 1) {
+      sums[t] = out;
+      __syncthreads();
+      if (p > 0) return;
+      for (int i = 1; i < side; ++i) out += sums[i * items + item];
+    }
+    if (item >= items) return;
+    const long to = (long)r * a.H + head0 + h;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) sum += level[1][w];
-  const int wide = parts.ld / 4, side = kThreads / wide, c = t % wide, p = t / wide;   // wide: 1 to 64
-  floatx4 out = {};
-  if (p < side)
-    for (int i = p; i < n; i += side) out += factor[i] * *reinterpret_cast<const floatx4 *>(parts.o + (long)row_of(i) * parts.ld + 4 * c);
-  sums[t] = out;
-  __syncthreads();
-  if (p > 0) return;
-  for (int i = 1; i < side; ++i) out += sums[i * wide + c];
-  const long to = (long)r * a.H + head;
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (4 * c + j < a.D) ((T *)a.o)[to * a.D + 4 * c + j] = (T)(sum == 0.0f ? 0.0f : out[j] / sum);
-  if (a.lse && t == 0) a.lse[to] = sum == 0.0f ? -INFINITY : top * kLn2 + logf(sum);
+    for (int j = 0; j < 4; ++j)
+      if (4 * c + j < a.D) ((T *)a.o)[to * a.D + 4 * c + j] = (T)(total[h] == 0.0f ? 0.0f : out[j] / total[h]);
+    if (a.lse && c == 0) a.lse[to] = total[h] == 0.0f ? -INFINITY : shift[h] * kLn2 + logf(total[h]);
+  }
 }
 
 int blocks_of(const CacheArgs &a) { return (a.H / a.KV + kHeads - 1) / kHeads; }
@@ -463,7 +464,11 @@ hipError_t paged_as(const CacheArgs &a, const Runs &parts, hipStream_t stream) {
   kernel<<<dim3((unsigned)groups), dim3(kThreads), lds, stream>>>(a, parts, Divisor(a.page));
   DLL_TRY(hipGetLastError());
   if ((long)a.columns * a.page <= kUnit) return hipSuccess;   // one unit a request and head
-  paged_join_kernel<T><<<dim3((unsigned)(a.R * a.H)), dim3(kThreads), 0, stream>>>(a, parts, groups);
+  // a workgroup a head while that makes no more than the chip takes at a time: 8 requests with 32 heads on 2 key heads 15.9 us, by key heads 20.0;
+  // 64 requests with 32 on 8, 199.4 and 195.7
+  const int single = (long)a.R * a.H <= 4L * chip().cus;
+  const int wide_group = a.H / a.KV < kHeads ? a.H / a.KV : kHeads;
+  paged_join_kernel<T><<<dim3((unsigned)(a.R * a.KV * parts.blocks * (single ? wide_group : 1))), dim3(kThreads), 0, stream>>>(a, parts, groups, single);
   return hipGetLastError();
 }
 
