@@ -51,27 +51,29 @@ __device__ __forceinline__ float row_product(const T *x, const T *y, int dim, in
 template <class T, int DP> constexpr int dq_residents() { return (sizeof(T) == 2 ? DP <= 128 : DP <= 64) ? 2 : 1; }
 
 // dq may be NULL: then the rows' figures are all that is wanted
-template <class T, int DP, int BN>
+// ROWS groups of 32 queries; with two, the wavefronts share a tile's keys two by two
+template <class T, int DP, int BN, int ROWS>
 __global__ __launch_bounds__(kThreads, (dq_residents<T, DP>())) void attention_dq_kernel(const AttentionArgs a, const Rows rows, const Parts parts, const int tiles) {
+  constexpr int kQueries = 32 * ROWS, kPer = BN * ROWS / 4;   // keys of a tile that a wavefront takes
   typedef Stager<T, DP, BN, kThreads> S;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
   const int part = blockIdx.x % parts.n, id = blockIdx.x / parts.n, kv = id % a.KV, rest = id / a.KV, group = a.H / a.KV, head = kv * group + rest % group,
             tile = tiles - 1 - rest / group;
-  const Place pq = place_of(a.q_starts, a.S, a.Tq, tile, kRows);
+  const Place pq = place_of(a.q_starts, a.S, a.Tq, tile, kQueries);
   if (pq.at >= pq.count) return;
   const int kv_first = start_of(a.kv_starts, pq.sequence, a.Tk), keys = max(0, start_of(a.kv_starts, pq.sequence + 1, a.Tk) - kv_first);
-  const int row0 = pq.at + 32 * wave, row = row0 + (lane & 31), shift = keys - pq.count;
+  const int mine = wave / ROWS * kPer, row0 = pq.at + 32 * (wave % ROWS), row = row0 + (lane & 31), shift = keys - pq.count;
   const int seen = a.causal ? max(0, min(keys, row + shift + 1)) : keys;
   const int seen_first = a.causal ? max(0, min(keys, row0 + shift + 1)) : keys;
   const int seen_last = row0 >= pq.count ? 0 : a.causal ? max(0, min(keys, min(row0 + 32, pq.count) + shift)) : keys;
-  const int seen_all = a.causal ? max(0, min(keys, min(pq.at + kRows, pq.count) + shift)) : keys;
+  const int seen_all = a.causal ? max(0, min(keys, min(pq.at + kQueries, pq.count) + shift)) : keys;
 
   const long at = pq.first + min(row, pq.count - 1);
   const T *g_row = (const T *)a.d_o + at * a.H * a.D + head * a.D;
   const float minus_delta = -row_product<T, DP>(g_row, (const T *)a.o + at * a.H * a.D + head * a.D, a.D, half);
   const float lse2 = a.lse[(long)head * a.Tq + at] * kLog2e;
-  if (part == 0 && half == 0 && row < pq.count) {
+  if (part == 0 && wave < ROWS && half == 0 && row < pq.count) {
     rows.lse2[(long)head * a.Tq + at] = lse2;
     rows.minus_delta[(long)head * a.Tq + at] = minus_delta;
   }
@@ -99,7 +101,7 @@ __global__ __launch_bounds__(kThreads, (dq_residents<T, DP>())) void attention_d
     const char *lk = sk.turn(wave, odd, k, key0 + BN, keys), *lv = sv.turn(wave, odd, v, key0 + BN, keys);
     written<T>();
 #pragma unroll 1
-    for (int b = 0; b < BN && key0 + b < seen_last; b += 32) {
+    for (int b = mine; b < mine + kPer && key0 + b < seen_last; b += 32) {
       floatx16 z = {}, d;
 #pragma unroll
       for (int r = 0; r < 16; ++r) d[r] = minus_delta;
@@ -134,20 +136,55 @@ __global__ __launch_bounds__(kThreads, (dq_residents<T, DP>())) void attention_d
     }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  if constexpr (ROWS == 2) {   // the second pair's sums to the first, in the tiles' place
+    constexpr int kLeft = DP * 128;
+    static_assert(2 * kLeft <= 2 * S::kBytes, "");
+    barrier();
+    if (wave >= ROWS)
+#pragma unroll
+      for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          *reinterpret_cast<floatx4 *>(smem + (wave - ROWS) * kLeft + ((i * 4 + r) * 64 + lane) * 16) =
+              floatx4{dq[i][4 * r], dq[i][4 * r + 1], dq[i][4 * r + 2], dq[i][4 * r + 3]};
+    __syncthreads();
+    if (wave >= ROWS) return;
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const floatx4 v = *reinterpret_cast<const floatx4 *>(smem + wave * kLeft + ((i * 4 + r) * 64 + lane) * 16);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) dq[i][4 * r + j] += v[j];
+      }
+  }
   if (row >= pq.count) return;
   if (parts.n > 1) return store_sums(parts.sums[0] + (((long)part * a.Tq + at) * a.H + head) * parts.ld, dq, parts.ld, half);
   store_row<T>((T *)a.dq + at * a.q_row + head * a.D, dq, a.scale, a.D, half);
 }
 
 // ------------------------------------------------------------------------------------------------ dk, dv
-// DK, DV: which of the two this instance takes (single precision with more than 128 elements a head takes them one after the other, as their
-// sums and both rows would not fit the registers)
-template <class T, int DP> constexpr int dkv_residents() { return (sizeof(T) == 2 ? DP <= 64 : DP <= 32) ? 2 : 1; }
+// The kernel's forms.  BOTH: both gradients.  HELD_LESS: both, the values' rows in LDS instead of registers, so that two workgroups fit a compute unit.
+// KEYS, VALUES: one of the two gradients (single precision with more than 128 elements a head takes them one after the other, as their
+// sums and both rows would not fit the registers).
+enum Form { BOTH, HELD_LESS, KEYS, VALUES };
+template <class T, int DP, Form F>
+struct DkvShape {
+  static constexpr bool kDK = F != VALUES, kDV = F != KEYS, kInLds = F == HELD_LESS;
+  static constexpr int kQueries = kInLds ? 32 : tile_rows<T, DP>();   // of a tile
+  static constexpr int kFigures = 256;                                // bytes of one kind of figures of a tile
+  typedef Stager<T, DP, kQueries, kThreads> Rows;
+  typedef Stager<T, DP, kRows, kThreads> Values;
+  static constexpr int kLds = 2 * Rows::kBytes + 4 * kFigures + (kInLds ? Values::kTile : 0);
+  static constexpr int kResident = kInLds || (sizeof(T) == 2 ? DP <= 64 : DP <= 32) ? 2 : 1;
+};
 
-template <class T, int DP, int BN, bool DK, bool DV>
-__global__ __launch_bounds__(kThreads, (dkv_residents<T, DP>())) void attention_dkv_kernel(const AttentionArgs a, const Rows rows, const Parts parts) {
-  typedef Stager<T, DP, BN, kThreads> S;
-  constexpr int kFigures = 256;   // bytes of one kind of figures of a tile
+template <class T, int DP, Form F>
+__global__ __launch_bounds__(kThreads, (DkvShape<T, DP, F>::kResident)) void attention_dkv_kernel(const AttentionArgs a, const Rows rows, const Parts parts) {
+  typedef DkvShape<T, DP, F> Sh;
+  typedef typename Sh::Rows S;
+  constexpr bool DK = Sh::kDK, DV = Sh::kDV;
+  constexpr int BN = Sh::kQueries, kFigures = Sh::kFigures;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
   const int part = blockIdx.x % parts.n, id = blockIdx.x / parts.n, kv = id % a.KV, tile = id / a.KV, group = a.H / a.KV;
@@ -162,7 +199,20 @@ __global__ __launch_bounds__(kThreads, (dkv_residents<T, DP>())) void attention_
   const long at = pk.first + min(key, pk.count - 1);
   RowFrags<T, DP> k, v;
   k.load((const T *)a.k + at * a.kv_row + kv * a.D, a.D, half);
-  if (DK) v.load((const T *)a.v + at * a.kv_row + kv * a.D, a.D, half);
+  char *const values = smem + 2 * S::kBytes + 4 * kFigures;
+  if constexpr (Sh::kInLds) {   // landed, as the first tile is
+    typename Sh::Values sv;
+    const T *p = (const T *)a.v + (long)pk.first * a.kv_row + kv * a.D;
+    sv.init(values, p, a.kv_row, a.D);
+    sv.start(wave, p, pk.at, pk.count);
+  } else if (DK) {
+    v.load((const T *)a.v + at * a.kv_row + kv * a.D, a.D, half);
+  }
+  const Reader<T, DP, kRows> values_reader(lane);
+  const auto value = [&](int s) {
+    if constexpr (Sh::kInLds) return values_reader.along(values, 32 * wave, s);
+    else return v[s];
+  };
   const float c = a.scale * kLog2e;
   floatx16 dk[DK ? DP / 32 : 1], dv[DV ? DP / 32 : 1];
 #pragma unroll
@@ -233,7 +283,7 @@ __global__ __launch_bounds__(kThreads, (dkv_residents<T, DP>())) void attention_
         }
         __builtin_amdgcn_sched_barrier(0);
         z = mma(qf[s & 1], k[s], z);
-        if constexpr (DK) d = mma(gf[s & 1], v[s], d);
+        if constexpr (DK) d = mma(gf[s & 1], value(s), d);
         __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
@@ -320,55 +370,80 @@ hipError_t launch_sums(const Sums &s, hipStream_t stream) {
 // ------------------------------------------------------------------------------------------------ host
 // The workspace's parts, the same walk for the query and the call
 struct BwdPlan {
-  Rows rows;
+  int rows = 4;          // groups of 32 queries of a workgroup that takes dq
+  bool less = false;     // HELD_LESS
+  Rows figures;
   Parts dq, dkv;
   size_t bytes;
-  BwdPlan(const AttentionArgs &a, int tile, int dq_resident, int dkv_resident, char *base) {
-    Take take{base};
-    rows.lse2 = (float *)take((size_t)a.H * a.Tq * sizeof(float));
-    rows.minus_delta = (float *)take((size_t)a.H * a.Tq * sizeof(float));
-    dq.n = parts_of((a.Tq + kRows - 1) / kRows * (long)a.H, tiles_of(a.Tq, a.S, kRows) * a.H, (long)dq_resident * chip().cus, a.Tk / a.S / tile);
-    dkv.n = parts_of((a.Tk + kRows - 1) / kRows * (long)a.KV, tiles_of(a.Tk, a.S, kRows) * a.KV, (long)dkv_resident * chip().cus,
-                      (long)a.Tq / a.S * (a.H / a.KV) / tile);
-    dq.ld = dkv.ld = (a.D + 3) & ~3;
-    if (dq.n > 1) dq.sums[0] = (float *)take((size_t)dq.n * a.Tq * a.H * dq.ld * sizeof(float));
-    if (dkv.n > 1)
-      for (float *&s : dkv.sums) s = (float *)take((size_t)dkv.n * a.Tk * a.KV * dkv.ld * sizeof(float));
-    bytes = take.used;
-  }
 };
 template <class T, int DP>
-BwdPlan plan_of(const AttentionArgs &a, char *scratch) { return BwdPlan(a, tile_rows<T, DP>(), dq_residents<T, DP>(), dkv_residents<T, DP>(), scratch); }
-
-template <class T, int DP, bool DK, bool DV>
-hipError_t launch_dkv(const AttentionArgs &a, const BwdPlan &p, hipStream_t stream) {
+BwdPlan plan(const AttentionArgs &a, char *base) {
   constexpr int BN = tile_rows<T, DP>();
-  constexpr size_t lds = 2 * Stager<T, DP, BN, kThreads>::kBytes + 4 * 256;
-  const auto kernel = attention_dkv_kernel<T, DP, BN, DK, DV>;
+  constexpr bool kTwo = sizeof(T) == 2 && BN == 64, kLess = sizeof(T) == 2 && DP > 64 && DP <= 128;
+  const long cus = chip().cus, all_q = (a.Tq + kRows - 1) / kRows, all_k = (a.Tk + kRows - 1) / kRows;
+  const long q_work = (all_q > a.S ? all_q : a.S) * a.H, k_work = (all_k > a.S ? all_k : a.S) * a.KV;
+  BwdPlan p;
+  Take take{base};
+  p.figures.lse2 = (float *)take((size_t)a.H * a.Tq * sizeof(float));
+  p.figures.minus_delta = (float *)take((size_t)a.H * a.Tq * sizeof(float));
+  // 64 queries a workgroup where 128 leave most of the chip idle, or where a causal mask's longest row of tiles decides; microseconds of a training
+  // pass with 128 / 64: 1000 tokens in two sequences, 8 heads of 128 68.4 / 64.1; 4096 in one, 16 heads of 128 386 / 370, of 64 258 / 242; in six
+  // 138 / 142; in one, all keys seen, 649 / 668
+  const bool chain = a.causal && a.Tk / a.S >= 2048;
+  if (kTwo && (2 * q_work <= cus || (chain && q_work <= 2 * cus))) p.rows = 2;
+  const int queries = 32 * p.rows;
+  p.dq.n = parts_of((a.Tq + queries - 1) / queries * (long)a.H, tiles_of(a.Tq, a.S, queries) * a.H, dq_residents<T, DP>() * cus, a.Tk / a.S / BN);
+  // values in LDS and two workgroups a unit, but for the smallest calls, and where one round of them has such a row of tiles that a lone workgroup
+  // finishes sooner; values in registers / in LDS: 4096 tokens, 16 heads of 128 on 4 key heads 501 / 439, all keys seen 649 / 591, causal 386 / 424; 8192 in
+  // three sequences 610 / 577; 1000 in two, 8 heads on 2, 68.4 / 72.2
+  p.less = kLess && 4 * k_work >= cus && !(chain && k_work >= 2 * cus && 2 * k_work < 5 * cus);
+  const int resident = p.less ? DkvShape<T, DP, kLess ? HELD_LESS : BOTH>::kResident : DkvShape<T, DP, BOTH>::kResident;
+  p.dkv.n = parts_of(all_k * a.KV, tiles_of(a.Tk, a.S, kRows) * a.KV, resident * cus, (long)a.Tq / a.S * (a.H / a.KV) / BN);
+  p.dq.ld = p.dkv.ld = (a.D + 3) & ~3;
+  if (p.dq.n > 1) p.dq.sums[0] = (float *)take((size_t)p.dq.n * a.Tq * a.H * p.dq.ld * sizeof(float));
+  if (p.dkv.n > 1)
+    for (float *&s : p.dkv.sums) s = (float *)take((size_t)p.dkv.n * a.Tk * a.KV * p.dkv.ld * sizeof(float));
+  p.bytes = take.used;
+  return p;
+}
+
+template <class T, int DP, int ROWS>
+hipError_t launch_dq(const AttentionArgs &a, const BwdPlan &p, hipStream_t stream) {
+  constexpr int BN = tile_rows<T, DP>();
+  constexpr size_t lds = 2 * Stager<T, DP, BN, kThreads>::kBytes;
+  const auto kernel = attention_dq_kernel<T, DP, BN, ROWS>;
   DLL_TRY(allow_large_lds(reinterpret_cast<const void *>(kernel), lds));
-  kernel<<<dim3((unsigned)(tiles_of(a.Tk, a.S, kRows) * a.KV * p.dkv.n)), dim3(kThreads), lds, stream>>>(a, p.rows, p.dkv);
+  const long tiles = tiles_of(a.Tq, a.S, 32 * ROWS);
+  const Parts one, &dq = a.dq ? p.dq : one;
+  kernel<<<dim3((unsigned)(tiles * a.H * dq.n)), dim3(kThreads), lds, stream>>>(a, p.figures, dq, (int)tiles);
+  DLL_TRY(hipGetLastError());
+  return dq.n > 1 ? launch_sums<T>(Sums{dq, a.q_starts, a.S, a.Tq, a.H, a.D, a.q_row, {a.dq, nullptr}, {a.scale, 0.0f}}, stream) : hipSuccess;
+}
+
+template <class T, int DP, Form F>
+hipError_t launch_dkv(const AttentionArgs &a, const BwdPlan &p, hipStream_t stream) {
+  typedef DkvShape<T, DP, F> S;
+  const auto kernel = attention_dkv_kernel<T, DP, F>;
+  DLL_TRY(allow_large_lds(reinterpret_cast<const void *>(kernel), S::kLds));
+  kernel<<<dim3((unsigned)(tiles_of(a.Tk, a.S, kRows) * a.KV * p.dkv.n)), dim3(kThreads), S::kLds, stream>>>(a, p.figures, p.dkv);
   return hipGetLastError();
 }
 
 template <class T, int DP>
 hipError_t bwd_as(const AttentionArgs &a, char *scratch, hipStream_t stream) {
-  constexpr int BN = tile_rows<T, DP>();
-  constexpr size_t lds = 2 * Stager<T, DP, BN, kThreads>::kBytes;
-  const BwdPlan p = plan_of<T, DP>(a, scratch);
-  const auto kernel = attention_dq_kernel<T, DP, BN>;
-  DLL_TRY(allow_large_lds(reinterpret_cast<const void *>(kernel), lds));
-  const long tiles = tiles_of(a.Tq, a.S, kRows);
-  const Parts one;
-  const Parts &dq = a.dq ? p.dq : one;
-  kernel<<<dim3((unsigned)(tiles * a.H * dq.n)), dim3(kThreads), lds, stream>>>(a, p.rows, dq, (int)tiles);
-  DLL_TRY(hipGetLastError());
-  if (dq.n > 1) DLL_TRY(launch_sums<T>(Sums{dq, a.q_starts, a.S, a.Tq, a.H, a.D, a.q_row, {a.dq, nullptr}, {a.scale, 0.0f}}, stream));
+  const BwdPlan p = plan<T, DP>(a, scratch);
+  if constexpr (sizeof(T) == 2 && tile_rows<T, DP>() == 64)
+    DLL_TRY((p.rows == 2 ? launch_dq<T, DP, 2>(a, p, stream) : launch_dq<T, DP, 4>(a, p, stream)));
+  else
+    DLL_TRY((launch_dq<T, DP, 4>(a, p, stream)));
   if (!a.dk && !a.dv) return hipSuccess;
   if constexpr (sizeof(T) == 4 && DP > 128) {
-    if (a.dv) DLL_TRY((launch_dkv<T, DP, false, true>(a, p, stream)));
-    if (a.dk) DLL_TRY((launch_dkv<T, DP, true, false>(a, p, stream)));
+    if (a.dv) DLL_TRY((launch_dkv<T, DP, VALUES>(a, p, stream)));
+    if (a.dk) DLL_TRY((launch_dkv<T, DP, KEYS>(a, p, stream)));
+  } else if constexpr (sizeof(T) == 2 && DP > 64 && DP <= 128) {
+    DLL_TRY((p.less ? launch_dkv<T, DP, HELD_LESS>(a, p, stream) : launch_dkv<T, DP, BOTH>(a, p, stream)));
   } else {
-    DLL_TRY((launch_dkv<T, DP, true, true>(a, p, stream)));
+    DLL_TRY((launch_dkv<T, DP, BOTH>(a, p, stream)));
   }
   if (p.dkv.n == 1) return hipSuccess;
   return launch_sums<T>(Sums{p.dkv, a.kv_starts, a.S, a.Tk, a.KV, a.D, a.kv_row, {a.dk, a.dv}, {a.scale, 1.0f}}, stream);
@@ -380,7 +455,7 @@ hipError_t bwd(const AttentionArgs &a, char *scratch, hipStream_t stream) {
 }
 template <class T>
 size_t bwd_bytes(const AttentionArgs &a) {
-  return instance(a.D, [&](auto dp) { return plan_of<T, decltype(dp)::value>(a, nullptr).bytes; });
+  return instance(a.D, [&](auto dp) { return plan<T, decltype(dp)::value>(a, nullptr).bytes; });
 }
 
 }  // namespace
