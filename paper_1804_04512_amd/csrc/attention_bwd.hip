@@ -392,13 +392,13 @@ BwdPlan plan(const AttentionArgs &a, char *base) {
   const bool chain = a.causal && a.Tk / a.S >= 2048;
   if (kTwo && (2 * q_work <= cus || (chain && q_work <= 2 * cus))) p.rows = 2;
   const int queries = 32 * p.rows;
-  p.dq.n = parts_of((a.Tq + queries - 1) / queries * (long)a.H, tiles_of(a.Tq, a.S, queries) * a.H, dq_residents<T, DP>() * cus, a.Tk / a.S / BN);
+  p.dq.n = parts_of((a.Tq + queries - 1) / queries * (long)a.H, tiles_of(a.Tq, a.S, queries) * a.H, dq_residents<T, DP>() * cus, a.Tk / a.S / BN, 2);
   // values in LDS and two workgroups a unit, but for the smallest calls, and where one round of them has such a row of tiles that a lone workgroup
   // finishes sooner; values in registers / in LDS: 4096 tokens, 16 heads of 128 on 4 key heads 501 / 439, all keys seen 649 / 591, causal 386 / 424; 8192 in
   // three sequences 610 / 577; 1000 in two, 8 heads on 2, 68.4 / 72.2
   p.less = kLess && 4 * k_work >= cus && !(chain && k_work >= 2 * cus && 2 * k_work < 5 * cus);
   const int resident = p.less ? DkvShape<T, DP, kLess ? HELD_LESS : BOTH>::kResident : DkvShape<T, DP, BOTH>::kResident;
-  p.dkv.n = parts_of(all_k * a.KV, tiles_of(a.Tk, a.S, kRows) * a.KV, resident * cus, (long)a.Tq / a.S * (a.H / a.KV) / BN);
+  p.dkv.n = parts_of(all_k * a.KV, tiles_of(a.Tk, a.S, kRows) * a.KV, resident * cus, (long)a.Tq / a.S * (a.H / a.KV) / BN, 2);
   p.dq.ld = p.dkv.ld = (a.D + 3) & ~3;
   if (p.dq.n > 1) p.dq.sums[0] = (float *)take((size_t)p.dq.n * a.Tq * a.H * p.dq.ld * sizeof(float));
   if (p.dkv.n > 1)

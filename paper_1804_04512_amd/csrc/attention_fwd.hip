@@ -223,7 +223,8 @@ FwdPlan plan_as(const AttentionArgs &a, char *base) {
   FwdPlan p;
   Take take{base};
   p.rows = ROWS;
-  p.parts.n = parts_of((a.Tq + S::kQueries - 1) / S::kQueries * (long)a.H, tiles_of(a.Tq, a.S, S::kQueries) * a.H, (long)S::kResident * chip().cus, a.Tk / a.S / S::kKeys);
+  p.parts.n = parts_of((a.Tq + S::kQueries - 1) / S::kQueries * (long)a.H, tiles_of(a.Tq, a.S, S::kQueries) * a.H, (long)(ROWS == 4 ? S::kResident : 1) * chip().cus,
+                       a.Tk / a.S / S::kKeys, 4);
   p.parts.ld = (a.D + 3) & ~3;
   if (p.parts.n > 1) {
     p.parts.sums[0] = (float *)take((size_t)p.parts.n * a.Tq * a.H * p.parts.ld * sizeof(float));

@@ -347,14 +347,14 @@ struct Parts {
   int ld = 0;                            // head_dim in whole fours
 };
 __device__ __forceinline__ int turn_from(int part, int parts, int turns) { return (int)((long)part * turns / parts); }
-// The n that fills the chip's `slots` places for workgroups, with four turns a part left on average; grid: workgroups of one part's launch,
-// empty ones too
-inline int parts_of(long workgroups, long grid, long slots, long turns) {
+// The n that fills the chip's `slots` places for workgroups, with `least` turns a part left on average; grid: workgroups of one part's launch,
+// empty ones too.  Forced n, microseconds of a training pass: 2001 ragged tokens, six heads of 80 in single precision, n = 1 / 2 / 3 / 4 / 6: 460 / 266 / 230 / 202 / 205;
+// 1024 tokens, 8 heads of 64 on 2, n = 1 / 4 / 6 / 12: 121 / 69 / 55 / 49; 6000 tokens, 8 heads of 128, n = 1 / 2 / 4: 503 / 452 / 528.
+inline int parts_of(long workgroups, long grid, long slots, long turns, long least) {
   long n = (slots + workgroups - 1) / workgroups;
-  for (const long most : {turns / 4, kMaxGrid / grid, 16L}) n = n < most ? n : most;
+  for (const long most : {turns / least, kMaxGrid / grid, 16L}) n = n < most ? n : most;
   return (int)(n > 1 ? n : 1);
 }
-
 
 // What `call` makes of the smallest instance that holds a head
 template <class F>
