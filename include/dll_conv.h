@@ -399,7 +399,8 @@ typedef struct {
  * A query that may see no key has o = 0 and lse = -infinity.  Rows outside the sequences are neither read nor written.  What other
  * sequences hold does not matter; a NaN or an infinity in a sequence may reach all of its own outputs.  scale is finite
  * (else DLL_ERR_SHAPE).  Starts outside [0, tokens] are taken as the nearest of these.  With DLL_BF16 p is rounded, relative to its row's
- * maximum, before it meets v. */
+ * maximum, before it meets v.  Products of DLL_FP32 tensors are taken on three bfloat16 parts of each number, here without a second
+ * pass: numbers from 3.39e38 on count as infinite.  (q_tokens / 32 + sequences) * heads, and the same of kv_tokens, at most 2^24 - 1. */
 size_t dll_attention_fwd_workspace_bytes(const dll_attention_desc *d);
 dll_status dll_attention_fwd(const dll_attention_desc *d, const void *q, const void *k, const void *v,
                              const int *q_starts, const int *kv_starts, float scale, void *o, float *lse,
@@ -409,7 +410,8 @@ dll_status dll_attention_fwd(const dll_attention_desc *d, const void *q, const v
  *   delta_i = d_o_i . o_i,  ds_ij = p_ij (d_o_i . v_j - delta_i)
  *   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij d_o_i   (over the heads that read j, too)
  * dq in rows like q's, dk and dv in rows like k's; each may be NULL (that gradient is not taken), not all three.  A key that no
- * query may see has gradients of 0.  With DLL_BF16 p and ds are rounded before the sums, and delta takes o as it was rounded. */
+ * query may see has gradients of 0.  With DLL_BF16 p and ds are rounded before the sums, and delta takes o as it was rounded, but for queries that
+ * see few keys. */
 size_t dll_attention_bwd_workspace_bytes(const dll_attention_desc *d);
 dll_status dll_attention_bwd(const dll_attention_desc *d, const void *q, const void *k, const void *v,
                              const int *q_starts, const int *kv_starts, float scale, const void *o,

@@ -7,6 +7,13 @@
 // the five of one kernel that would have to add its dq up in memory.  32 rows a wavefront stay in registers as fragments; the others come
 // through LDS tile by tile, read along a head's elements for the scores and across tokens for the sums.  p and ds go from one
 // product's result to the next one's operand in registers, rounded to the operands' type there.
+//
+// Bound by the matrix pipe and by what stands between its products (exponentials, waits for fragments).  4096 tokens, causal, 16 heads of 128 in
+// bfloat16: dq 128 us, dk and dv 188 us, 172 GFLOP of five products at 545 TFLOP/s, and of the seven that are done at 760; all keys seen, 1030 to
+// 1050 for dq.  2001 tokens in three sequences, six heads of 80 on three in single precision: dq 72, dk and dv 77 and their parts' sums 12 us.
+// Tried and slower: two blocks of scores a turn with one's exponentials between the other's products (twice the registers, sums moved
+// between the register files at each product: 390 to 840 us for the pass), fragments three steps ahead instead of one (the same), all
+// fragments of the second products ahead of the exponentials (3 % slower).
 #include "attention_tile.h"
 
 namespace dllk {
@@ -71,30 +78,96 @@ __global__ __launch_bounds__(kThreads, (dq_residents<T, DP>())) void attention_d
 
   const long at = pq.first + min(row, pq.count - 1);
   const T *g_row = (const T *)a.d_o + at * a.H * a.D + head * a.D;
-  const float minus_delta = -row_product<T, DP>(g_row, (const T *)a.o + at * a.H * a.D + head * a.D, a.D, half);
+  float minus_delta = -row_product<T, DP>(g_row, (const T *)a.o + at * a.H * a.D + head * a.D, a.D, half);
   const float lse2 = a.lse[(long)head * a.Tq + at] * kLog2e;
-  if (part == 0 && wave < ROWS && half == 0 && row < pq.count) {
+  const auto leave_figures = [&] {
+    if (part > 0 || wave >= ROWS || half > 0 || row >= pq.count) return;
     rows.lse2[(long)head * a.Tq + at] = lse2;
     rows.minus_delta[(long)head * a.Tq + at] = minus_delta;
+  };
+  // Rows that see few keys take delta as sum_j p_ij (do_i . v_j) instead, in a pass of its own: o was rounded, and where a few keys have most of p,
+  // ds is small beside that error (of a row with one key it is 0).  600 tokens in 24 sequences in bfloat16: dq and dk off by
+  // 2.8e-3, with it by 2.4e-3, for 1.2 us of 21.
+  const int turns = (seen_all + BN - 1) / BN;
+  const bool measures = sizeof(T) == 2 && turns > 0 && seen_all <= 128;
+  if (!measures) {
+    leave_figures();
+    if (!a.dq) return;
   }
-  if (!a.dq) return;
 
   const T *k = (const T *)a.k + (long)kv_first * a.kv_row + kv * a.D, *v = (const T *)a.v + (long)kv_first * a.kv_row + kv * a.D;
   S sk, sv;
   sk.init(smem, k, a.kv_row, a.D);
   sv.init(smem + S::kBytes, v, a.kv_row, a.D);
-  const int turns = (seen_all + BN - 1) / BN, begin = turn_from(part, parts.n, turns) * BN, end = min(seen_all, turn_from(part + 1, parts.n, turns) * BN);
-  sk.start(wave, k, begin, keys);
-  sv.start(wave, v, begin, keys);
   RowFrags<T, DP> q, g;
   q.load((const T *)a.q + at * a.q_row + head * a.D, a.D, half);
   g.load(g_row, a.D, half);
   const float c = a.scale * kLog2e;
 
+  const Reader<T, DP, BN> reader(lane);
+  // p (dp + from) of the 32 keys from b on in a tile
+  const auto ds_of = [&](const char *lk, const char *lv, int key0, int b, float from) {
+    floatx16 z = {}, d;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) d[r] = from;
+    Frag<T> kf[2], vf[2];   // read a step ahead of the products that take them
+    kf[0] = reader.along(lk, b, 0);
+    vf[0] = reader.along(lv, b, 0);
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) {
+      if (s + 1 < DP / 16) {
+        kf[(s + 1) & 1] = reader.along(lk, b, s + 1);
+        vf[(s + 1) & 1] = reader.along(lv, b, s + 1);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      z = mma(kf[s & 1], q[s], z);
+      d = mma(vf[s & 1], g[s], d);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) z[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[r], c, -lse2));
+    if (key0 + b + 32 > seen_first)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (key0 + b + token_of(r) + 4 * half >= seen) z[r] = 0.0f, d[r] = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) d[r] *= z[r];
+    return d;
+  };
+  if constexpr (sizeof(T) == 2)
+    if (measures) {
+      sk.start(wave, k, 0, keys);
+      sv.start(wave, v, 0, keys);
+      float delta = 0.0f;
+      for (int key0 = 0, odd = 1; key0 < seen_all; key0 += BN, odd ^= 1) {
+        landed<T>();
+        const char *lk = sk.turn(wave, odd, k, key0 + BN, keys), *lv = sv.turn(wave, odd, v, key0 + BN, keys);
+        for (int b = mine; b < mine + kPer && key0 + b < seen_last; b += 32) {
+          const floatx16 d = ds_of(lk, lv, key0, b, 0.0f);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) delta += d[r];
+        }
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      barrier();   // everyone is done with the tiles
+      delta = sum_of_halves(delta);
+      if constexpr (ROWS == 2) {   // of both pairs' keys
+        float *shared = reinterpret_cast<float *>(smem);
+        shared[wave * 64 + lane] = delta;
+        __syncthreads();
+        delta = shared[wave % 2 * 64 + lane] + shared[(wave % 2 + 2) * 64 + lane];
+        __syncthreads();
+      }
+      minus_delta = -delta;
+      leave_figures();
+      if (!a.dq) return;
+    }
+  const int begin = turn_from(part, parts.n, turns) * BN, end = min(seen_all, turn_from(part + 1, parts.n, turns) * BN);
+  sk.start(wave, k, begin, keys);
+  sv.start(wave, v, begin, keys);
   floatx16 dq[DP / 32];
 #pragma unroll
   for (int i = 0; i < DP / 32; ++i) dq[i] = floatx16{};
-  const Reader<T, DP, BN> reader(lane);
   int odd = 1;
   for (int key0 = begin; key0 < end; key0 += BN, odd ^= 1) {
     landed<T>();
@@ -102,31 +175,7 @@ __global__ __launch_bounds__(kThreads, (dq_residents<T, DP>())) void attention_d
     written<T>();
 #pragma unroll 1
     for (int b = mine; b < mine + kPer && key0 + b < seen_last; b += 32) {
-      floatx16 z = {}, d;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) d[r] = minus_delta;
-      Frag<T> kf[2], vf[2];   // read a step ahead of the products that take them
-      kf[0] = reader.along(lk, b, 0);
-      vf[0] = reader.along(lv, b, 0);
-#pragma unroll
-      for (int s = 0; s < DP / 16; ++s) {
-        if (s + 1 < DP / 16) {
-          kf[(s + 1) & 1] = reader.along(lk, b, s + 1);
-          vf[(s + 1) & 1] = reader.along(lv, b, s + 1);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        z = mma(kf[s & 1], q[s], z);
-        d = mma(vf[s & 1], g[s], d);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-#pragma unroll
-      for (int r = 0; r < 16; ++r) z[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[r], c, -lse2));
-      if (key0 + b + 32 > seen_first)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (key0 + b + token_of(r) + 4 * half >= seen) z[r] = 0.0f, d[r] = 0.0f;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) d[r] *= z[r];
+      const floatx16 d = ds_of(lk, lv, key0, b, minus_delta);
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         const Frag<T> ds = frag_of<T>(d, s);

@@ -6,7 +6,15 @@
 //
 // A workgroup has 128 queries of one head, 32 a wavefront, which hold their rows of q as fragments.  Tiles of keys and values come
 // straight into LDS, the next one while one is worked on.  Scores are taken transposed (keys are registers, the query is the lane), so
-// maximum and sum are a lane's own but for the two halves, and p goes into the second product as it lies.
+// maximum and sum are a lane's own but for the two halves, and p goes into the second product as it lies.  Where workgroups are few their
+// wavefronts share 64 or 32 queries and take a tile's keys between them, joined in LDS at the end; where they are few still, the keys are
+// cut into parts that a second launch joins.
+//
+// Bound by the matrix pipe beside the exponentials: a tile of 64 keys is 1024 cycles of products and 980 of vector instructions for a wavefront, and
+// two wavefronts a SIMD overlap them only in part.  bfloat16, heads of 128: 4096 tokens, all keys seen, 16 heads, 134 us = 1030 TFLOP/s; causal
+// 88 us = 780 (its longest row of 64 tiles decides); 16384 tokens in five sequences 290 to 303 us = 940 to 980.  777 tokens, 16 heads of 64,
+// 9.7 us (latency).  Tried and slower: exponentials of one block of keys beside the products of the next and the former (134 to 162 us), wavefront
+// priorities around the products (the same), the second products beside the other half's exponentials (the same).
 #include "attention_tile.h"
 
 namespace dllk {
@@ -235,7 +243,9 @@ FwdPlan plan_as(const AttentionArgs &a, char *base) {
 }
 template <class T, int DP>
 FwdPlan plan(const AttentionArgs &a, char *base) {
-  // as many workgroups of 128 queries as there are at least
+  // as many workgroups of 128 queries as there are at least.  Microseconds with 128 / 64 / 32 queries a workgroup: 777 tokens, 16 heads of 64 18 / 17 / 11; 1000, 8 of 128
+  // 24 / 22 / 18; 300, 8 of 128 11.6 / 10.2 / 11.1; 2048, 8 of 128 33 / 33 / 34; 3000, 16 of 64 44 / 39 / 48; 4096 in 50 sequences, 16 of 64 14 / 15 / 28.  Single
+  // precision gains nothing from fewer (1000, 8 of 128: 42 / 43 / 43) as its rows are split by four wavefronts for four.
   const long all = (a.Tq + 127) / 128 > a.S ? (a.Tq + 127) / 128 : a.S, workgroups = all * a.H;
   if constexpr (Shape<T, DP, 2>::kExists) {
     if constexpr (Shape<T, DP, 1>::kExists)

@@ -46,6 +46,8 @@ def sequence(q, k, v, scale, causal, d_o=None):
         dp = d_o @ vT
         delta = (d_o * o).sum(2, keepdim=True)
         edelta = (d_o.abs() * (eo + gamma(D) * o.abs())).sum(2, keepdim=True)
+        # rows that see few keys take delta as sum p dp, whose terms are off by p's and dp's errors
+        edelta = edelta + (p * gamma(D) * (d_o.abs() @ vT.abs()) + ep * dp.abs() + gamma(nk) * (p * dp).abs()).sum(2, keepdim=True)
         edp = gamma(D) * (d_o.abs() @ vT.abs() + delta.abs()) + edelta
         ep = p * (ez + out["lse"][1][..., None] + 4 * U32 * (z.abs() + torch.where(empty, 0.0, lse)[..., None].abs()) + EXP) + TINY * seen
         ds = p * (dp - delta)
