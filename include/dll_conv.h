@@ -397,7 +397,8 @@ typedef struct {
  *   (so that one projection's output may hold all three), at any multiple of their elements
  *   o [q_tokens][heads][head_dim] contiguous;  lse [heads][q_tokens] fp32, may be NULL
  * A query that may see no key has o = 0 and lse = -infinity.  Rows outside the sequences are neither read nor written.  What other
- * sequences hold does not matter; a NaN or an infinity in a sequence may reach all of its own outputs.  scale is finite
+ * sequences hold does not matter, and what keys, values, queries and d_o hold that is not finite reaches the results of those that see them
+ * or are seen by them alone (as NaN, where they would be infinite, too).  scale is finite
  * (else DLL_ERR_SHAPE).  Starts outside [0, tokens] are taken as the nearest of these.  With DLL_BF16 p is rounded, relative to its row's
  * maximum, before it meets v.  Products of DLL_FP32 tensors are taken on three bfloat16 parts of each number, here without a second
  * pass: numbers from 3.39e38 on count as infinite.  (q_tokens / 32 + sequences) * heads, and the same of kv_tokens, at most 2^24 - 1. */

@@ -163,9 +163,11 @@ __global__ __launch_bounds__(kThreads, (dq_residents<T, DP>())) void attention_d
       if (!a.dq) return;
     }
   const int begin = turn_from(part, parts.n, turns) * BN, end = min(seen_all, turn_from(part + 1, parts.n, turns) * BN);
+  floatx16 dq[DP / 32];
+  bool reached = false;   // by a key that is not finite, in a careful pass
+  for (bool careful = false;; careful = true) {
   sk.start(wave, k, begin, keys);
   sv.start(wave, v, begin, keys);
-  floatx16 dq[DP / 32];
 #pragma unroll
   for (int i = 0; i < DP / 32; ++i) dq[i] = floatx16{};
   int odd = 1;
@@ -173,6 +175,10 @@ __global__ __launch_bounds__(kThreads, (dq_residents<T, DP>())) void attention_d
     landed<T>();
     const char *lk = sk.turn(wave, odd, k, key0 + BN, keys), *lv = sv.turn(wave, odd, v, key0 + BN, keys);
     written<T>();
+    if (careful && key0 + BN > pq.at + shift + 1) {
+      const Cleared c = clear_rows<T, DP, BN>(const_cast<char *>(lk), smem + 2 * S::kBytes);
+      reached = reached || (c.first < BN && key0 + c.first < seen);
+    }
 #pragma unroll 1
     for (int b = mine; b < mine + kPer && key0 + b < seen_last; b += 32) {
       const floatx16 d = ds_of(lk, lv, key0, b, minus_delta);
@@ -185,6 +191,11 @@ __global__ __launch_bounds__(kThreads, (dq_residents<T, DP>())) void attention_d
     }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  if (!a.causal || careful || !anyone(!all_finite(dq), smem + 2 * S::kBytes, wave)) break;
+  }
+  if (reached)
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i) dq[i] += NAN;
   if constexpr (ROWS == 2) {   // the second pair's sums to the first, in the tiles' place
     constexpr int kLeft = DP * 128;
     static_assert(2 * kLeft <= 2 * S::kBytes, "");
@@ -224,7 +235,7 @@ struct DkvShape {
   static constexpr int kFigures = 256;                                // bytes of one kind of figures of a tile
   typedef Stager<T, DP, kQueries, kThreads> Rows;
   typedef Stager<T, DP, kRows, kThreads> Values;
-  static constexpr int kLds = 2 * Rows::kBytes + 4 * kFigures + (kInLds ? Values::kTile : 0);
+  static constexpr int kTiles = 2 * Rows::kBytes + 4 * kFigures + (kInLds ? Values::kTile : 0), kLds = kTiles + kCareful;
   static constexpr int kResident = kInLds || (sizeof(T) == 2 ? DP <= 64 : DP <= 32) ? 2 : 1;
 };
 
@@ -264,11 +275,6 @@ __global__ __launch_bounds__(kThreads, (DkvShape<T, DP, F>::kResident)) void att
   };
   const float c = a.scale * kLog2e;
   floatx16 dk[DK ? DP / 32 : 1], dv[DV ? DP / 32 : 1];
-#pragma unroll
-  for (int i = 0; i < DP / 32; ++i) {
-    if (DK) dk[i] = floatx16{};
-    if (DV) dv[i] = floatx16{};
-  }
   const Reader<T, DP, BN> reader(lane);
   S sq, sg;
   sq.init(smem, a.q, a.q_row, a.D);
@@ -294,6 +300,13 @@ __global__ __launch_bounds__(kThreads, (DkvShape<T, DP, F>::kResident)) void att
     const uintx4 rs = buffer_of((const char *)t.figures, (unsigned)max(0, min(queries - t.i0, BN)) * 4u);
     load_words_to_lds(rs, lane * 4, (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)(figures + (2 * odd + (wave & 1)) * kFigures));
   };
+  bool reached = false;   // by a query, or its outputs' gradients, that is not finite, in a careful pass
+  for (bool careful = false;; careful = true) {
+#pragma unroll
+  for (int i = 0; i < DP / 32; ++i) {
+    if (DK) dk[i] = floatx16{};
+    if (DV) dv[i] = floatx16{};
+  }
   if (begin < end) {
     const Turn t = turn_of(begin);
     sq.start(wave, t.q, t.i0, queries);
@@ -310,6 +323,11 @@ __global__ __launch_bounds__(kThreads, (DkvShape<T, DP, F>::kResident)) void att
     written<T>();
     const float *lse2 = reinterpret_cast<const float *>(figures + 2 * (odd ^ 1) * kFigures), *minus_delta = lse2 + kFigures / 4;
     const int i0 = from + (turn % tiles) * BN;
+    if (careful && i0 < pk.at + kRows - 1 - shift) {   // a query that does not see all of the workgroup's keys
+      const Cleared of_q = clear_rows<T, DP, BN>(const_cast<char *>(lq), smem + Sh::kTiles), of_g = clear_rows<T, DP, BN>(const_cast<char *>(lg), smem + Sh::kTiles);
+      const int last = max(of_q.last, of_g.last);
+      reached = reached || (last >= 0 && i0 + last >= sees);
+    }
 #pragma unroll 1
     for (int b = 0; b < BN && i0 + b < queries; b += 32) {
       if (a.causal && i0 + b + 31 < sees_first) continue;
@@ -367,6 +385,17 @@ __global__ __launch_bounds__(kThreads, (DkvShape<T, DP, F>::kResident)) void att
     }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  bool finite = true;
+  if (DK) finite = all_finite(dk);
+  if (DV) finite = finite && all_finite(dv);
+  if (!a.causal || careful || !anyone(!finite, smem + Sh::kTiles, wave)) break;
+  }
+  if (reached)
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i) {
+      if (DK) dk[i] += NAN;
+      if (DV) dv[i] += NAN;
+    }
   if (key >= pk.count) return;
   if (parts.n > 1) {
     const long to = (((long)part * a.Tk + at) * a.KV + kv) * parts.ld;
@@ -459,7 +488,7 @@ BwdPlan plan(const AttentionArgs &a, char *base) {
 template <class T, int DP, int ROWS>
 hipError_t launch_dq(const AttentionArgs &a, const BwdPlan &p, hipStream_t stream) {
   constexpr int BN = tile_rows<T, DP>();
-  constexpr size_t lds = 2 * Stager<T, DP, BN, kThreads>::kBytes;
+  constexpr size_t lds = 2 * Stager<T, DP, BN, kThreads>::kBytes + kCareful;
   const auto kernel = attention_dq_kernel<T, DP, BN, ROWS>;
   DLL_TRY(allow_large_lds(reinterpret_cast<const void *>(kernel), lds));
   const long tiles = tiles_of(a.Tq, a.S, 32 * ROWS);

@@ -33,8 +33,8 @@ struct Shape {
   static constexpr int kQueries = 32 * ROWS;
   typedef Stager<T, DP, kKeys, kThreads> Rows;
   static constexpr int kLeft = DP * 128 + 512;   // bytes that a wavefront leaves for another one: its outputs, maxima and sums
-  static constexpr int kLds = 2 * Rows::kBytes > (kKeyGroups - 1) * ROWS * kLeft ? 2 * Rows::kBytes : (kKeyGroups - 1) * ROWS * kLeft;
-  static constexpr bool kExists = ROWS == 4 || (sizeof(T) == 2 && kLds <= 128 * 1024);
+  static constexpr int kTiles = 2 * Rows::kBytes > (kKeyGroups - 1) * ROWS * kLeft ? 2 * Rows::kBytes : (kKeyGroups - 1) * ROWS * kLeft, kLds = kTiles + kCareful;
+  static constexpr bool kExists = ROWS == 4 || (sizeof(T) == 2 && kTiles <= 128 * 1024);
   // workgroups that a compute unit holds
   static constexpr int kResident = (sizeof(T) == 2 ? DP <= 128 : DP <= 96) && kLds <= 80 * 1024 ? 2 : 1;
 };
@@ -64,22 +64,29 @@ __global__ __launch_bounds__(kThreads, (Shape<T, DP, ROWS>::kResident)) void att
   sk.init(smem, k, a.kv_row, a.D);
   sv.init(smem + S::kBytes, v, a.kv_row, a.D);
   const int turns = (seen_all + BN - 1) / BN, begin = turn_from(part, parts.n, turns) * BN, end = min(seen_all, turn_from(part + 1, parts.n, turns) * BN);
-  sk.start(wave, k, begin, keys);
-  sv.start(wave, v, begin, keys);
   RowFrags<T, DP> q;   // with a scale below 0 the maximum of the scores is that of -q k
   q.load((const T *)a.q + (long)(pq.first + min(row, pq.count - 1)) * a.q_row + head * a.D, a.D, half, a.scale < 0.0f);
   const float c = fmaxf(fabsf(a.scale) * kLog2e, 0x1p-126f);   // a masked score of -infinity stays one where the scale is 0
 
   floatx16 o[DP / 32];
+  float m, l;
+  const Reader<T, DP, BN> reader(lane);
+  bool reached = false;   // by a value that is not finite, in a careful pass
+  for (bool careful = false;; careful = true) {
+  sk.start(wave, k, begin, keys);
+  sv.start(wave, v, begin, keys);
 #pragma unroll
   for (int i = 0; i < DP / 32; ++i) o[i] = floatx16{};
-  float m = -INFINITY, l = 0.0f;
-  const Reader<T, DP, BN> reader(lane);
+  m = -INFINITY, l = 0.0f;
   int odd = 1;
   for (int key0 = begin; key0 < end; key0 += BN, odd ^= 1) {
     landed<T>();
     const char *lk = sk.turn(wave, odd, k, key0 + BN, keys), *lv = sv.turn(wave, odd, v, key0 + BN, keys);
     written<T>();
+    if (careful && key0 + BN > pq.at + shift + 1) {   // more keys than the workgroup's first query sees
+      const Cleared c = clear_rows<T, DP, BN>(const_cast<char *>(lv), smem + Sh::kTiles);
+      reached = reached || (c.first < BN && key0 + c.first < seen);
+    }
     if (key0 + mine < seen_last) {
       floatx16 z[kPer / 32];
 #pragma unroll
@@ -137,6 +144,11 @@ __global__ __launch_bounds__(kThreads, (Shape<T, DP, ROWS>::kResident)) void att
     }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // of the tile of zeros too
+  if (!a.causal || careful || !anyone(!all_finite(o), smem + Sh::kTiles, wave)) break;
+  }
+  if (reached)
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i) o[i] += NAN;
   l = sum_of_halves(l);
   if constexpr (ROWS < 4) {   // the groups' outputs together, in the tiles' place, in the groups' order
     constexpr int kLeft = Sh::kLeft;

@@ -178,6 +178,57 @@ __device__ __forceinline__ void written() {
   }
 }
 
+// A product's 0 for a token that a mask leaves out stays 0 only while the other operand is finite.  Where sums turn out not to be finite under a mask, a
+// workgroup takes its tiles again: in those that the mask cuts, rows with such numbers lose them, and the lanes that see one of these rows are
+// told, whose results are NaN.  All of this is off the usual path but for one look at the sums.
+constexpr int kCareful = 256;   // bytes of LDS for it
+template <int N>
+__device__ __forceinline__ bool all_finite(const floatx16 (&c)[N]) {
+  bool finite = true;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) finite = finite && fabsf(c[i][r]) < INFINITY;
+  return finite;
+}
+// Whether any of a workgroup's four wavefronts says so
+__device__ __forceinline__ bool anyone(bool here, char *lds, int wave) {
+  unsigned *flags = reinterpret_cast<unsigned *>(lds);
+  const unsigned any = __any(here) ? 1u : 0u;
+  if ((threadIdx.x & 63) == 0) flags[wave] = any;
+  __syncthreads();
+  const unsigned all = flags[0] | flags[1] | flags[2] | flags[3];
+  __syncthreads();
+  return __builtin_amdgcn_readfirstlane((int)all) != 0;
+}
+// Clears what is not finite in a tile of NR rows, by everyone; the first and the last row that had any, NR and -1 where none had
+struct Cleared { int first, last; };
+template <class T, int DP, int NR>
+__device__ __forceinline__ Cleared clear_rows(char *tile, char *lds) {
+  int *rows = reinterpret_cast<int *>(lds);
+  if (threadIdx.x == 0) rows[0] = NR, rows[1] = -1;
+  __syncthreads();
+  for (int at = threadIdx.x; at < NR * Tile<DP>::kGroups; at += 256) {
+    uintx4 keep = {~0u, ~0u, ~0u, ~0u};   // of all parts of a number, where all are numbers
+#pragma unroll
+    for (int k = 0; k < planes<T>(); ++k) {
+      const uintx4 v = *reinterpret_cast<const uintx4 *>(tile + k * NR * Tile<DP>::kRowBytes + at * 16);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) keep[j] &= ((v[j] & 0x7F80u) == 0x7F80u ? 0u : 0xFFFFu) | ((v[j] & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u);
+    }
+    if ((keep[0] & keep[1] & keep[2] & keep[3]) == ~0u) continue;
+    const int row = at / Tile<DP>::kGroups;
+    atomicMin(&rows[0], row);
+    atomicMax(&rows[1], row);
+#pragma unroll
+    for (int k = 0; k < planes<T>(); ++k) *reinterpret_cast<uintx4 *>(tile + k * NR * Tile<DP>::kRowBytes + at * 16) &= keep;
+  }
+  __syncthreads();
+  const Cleared c{rows[0], rows[1]};
+  __syncthreads();
+  return c;
+}
+
 // Fragments of a tile of NR rows in LDS for lane l: of scores, elements 16 s + 8 (l / 32) on of row x0 + l % 32; of sums over tokens, element
 // d0 + l % 32 of the sixteen tokens from x0 on, in the order of a result's registers.  x0 is a multiple of 32 and of 16.
 template <class T, int DP, int NR>
