@@ -72,80 +72,81 @@ __global__ __launch_bounds__(kThreads, (Shape<T, DP, ROWS>::kResident)) void att
   float m, l;
   const Reader<T, DP, BN> reader(lane);
   bool reached = false;   // by a value that is not finite, in a careful pass
-  for (bool careful = false;; careful = true) {
-  sk.start(wave, k, begin, keys);
-  sv.start(wave, v, begin, keys);
+  const auto pass = [&](auto careful) {
+    sk.start(wave, k, begin, keys);
+    sv.start(wave, v, begin, keys);
 #pragma unroll
-  for (int i = 0; i < DP / 32; ++i) o[i] = floatx16{};
-  m = -INFINITY, l = 0.0f;
-  int odd = 1;
-  for (int key0 = begin; key0 < end; key0 += BN, odd ^= 1) {
-    landed<T>();
-    const char *lk = sk.turn(wave, odd, k, key0 + BN, keys), *lv = sv.turn(wave, odd, v, key0 + BN, keys);
-    written<T>();
-    if (careful && key0 + BN > pq.at + shift + 1) {   // more keys than the workgroup's first query sees
-      const Cleared c = clear_rows<T, DP, BN>(const_cast<char *>(lv), smem + Sh::kTiles);
-      reached = reached || (c.first < BN && key0 + c.first < seen);
-    }
-    if (key0 + mine < seen_last) {
-      floatx16 z[kPer / 32];
-#pragma unroll
-      for (int b = 0; b < kPer / 32; ++b) z[b] = floatx16{};
-      // keys are read a step ahead of the products that take them
-      Frag<T> kf[2][kPer / 32];
-      const auto read = [&](int s) {
-#pragma unroll
-        for (int b = 0; b < kPer / 32; ++b) kf[s & 1][b] = reader.along(lk, mine + 32 * b, s);
-      };
-      read(0);
-#pragma unroll
-      for (int s = 0; s < DP / 16; ++s) {
-        if (s + 1 < DP / 16) read(s + 1);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int b = 0; b < kPer / 32; ++b) z[b] = mma(kf[s & 1][b], q[s], z[b]);
-        __builtin_amdgcn_sched_barrier(0);
+    for (int i = 0; i < DP / 32; ++i) o[i] = floatx16{};
+    m = -INFINITY, l = 0.0f;
+    int odd = 1;
+    for (int key0 = begin; key0 < end; key0 += BN, odd ^= 1) {
+      landed<T>();
+      const char *lk = sk.turn(wave, odd, k, key0 + BN, keys), *lv = sv.turn(wave, odd, v, key0 + BN, keys);
+      written<T>();
+      if (decltype(careful)::value && key0 + BN > pq.at + shift + 1) {   // more keys than the workgroup's first query sees
+        const Cleared c = clear_rows<T, DP, BN>(const_cast<char *>(lv), smem + Sh::kTiles);
+        reached = reached || (c.first < BN && key0 + c.first < seen);
       }
-      if (key0 + mine + kPer > seen_first)
+      if (key0 + mine < seen_last) {
+        floatx16 z[kPer / 32];
+#pragma unroll
+        for (int b = 0; b < kPer / 32; ++b) z[b] = floatx16{};
+        // keys are read a step ahead of the products that take them
+        Frag<T> kf[2][kPer / 32];
+        const auto read = [&](int s) {
+#pragma unroll
+          for (int b = 0; b < kPer / 32; ++b) kf[s & 1][b] = reader.along(lk, mine + 32 * b, s);
+        };
+        read(0);
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s) {
+          if (s + 1 < DP / 16) read(s + 1);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int b = 0; b < kPer / 32; ++b) z[b] = mma(kf[s & 1][b], q[s], z[b]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (key0 + mine + kPer > seen_first)
+#pragma unroll
+          for (int b = 0; b < kPer / 32; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              if (key0 + mine + 32 * b + token_of(r) + 4 * half >= seen) z[b][r] = -INFINITY;
+        float top = -INFINITY;
 #pragma unroll
         for (int b = 0; b < kPer / 32; ++b)
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (key0 + mine + 32 * b + token_of(r) + 4 * half >= seen) z[b][r] = -INFINITY;
-      float top = -INFINITY;
+          for (int r = 0; r < 16; ++r) top = fmaxf(top, z[b][r]);
+        top = most_of_halves(top) * c;
+        if (__any(top > m + 8.0f)) {
+          const float grown = fmaxf(m, top), shrink = grown == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - grown);
+          m = grown;
+          l *= shrink;
 #pragma unroll
-      for (int b = 0; b < kPer / 32; ++b)
+          for (int i = 0; i < DP / 32; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) top = fmaxf(top, z[b][r]);
-      top = most_of_halves(top) * c;
-      if (__any(top > m + 8.0f)) {
-        const float grown = fmaxf(m, top), shrink = grown == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - grown);
-        m = grown;
-        l *= shrink;
-#pragma unroll
-        for (int i = 0; i < DP / 32; ++i)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[i][r] *= shrink;
-      }
-      const float from = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-      for (int b = 0; b < kPer / 32; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          z[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[b][r], c, -from));
-          l += z[b][r];
+            for (int r = 0; r < 16; ++r) o[i][r] *= shrink;
         }
+        const float from = m == -INFINITY ? 0.0f : m;
 #pragma unroll
-      for (int s = 0; s < kPer / 16; ++s) {
-        const Frag<T> p = frag_of<T>(z[s / 2], s % 2);
+        for (int b = 0; b < kPer / 32; ++b)
 #pragma unroll
-        for (int i = 0; i < DP / 32; ++i) o[i] = mma(reader.across(lv, mine + 16 * s, 32 * i), p, o[i]);
+          for (int r = 0; r < 16; ++r) {
+            z[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[b][r], c, -from));
+            l += z[b][r];
+          }
+#pragma unroll
+        for (int s = 0; s < kPer / 16; ++s) {
+          const Frag<T> p = frag_of<T>(z[s / 2], s % 2);
+#pragma unroll
+          for (int i = 0; i < DP / 32; ++i) o[i] = mma(reader.across(lv, mine + 16 * s, 32 * i), p, o[i]);
+        }
       }
     }
-  }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // of the tile of zeros too
-  if (!a.causal || careful || !anyone(!all_finite(o), smem + Sh::kTiles, wave)) break;
-  }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // of the tile of zeros too
+  };
+  pass(std::false_type{});
+  if (a.causal && anyone(!all_finite(o), smem + Sh::kTiles, wave)) pass(std::true_type{});
   if (reached)
 #pragma unroll
     for (int i = 0; i < DP / 32; ++i) o[i] += NAN;
