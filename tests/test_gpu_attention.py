@@ -9,7 +9,7 @@ torch = pytest.importorskip("torch")
 import attention_ref
 import large_ref as ref
 from paper_1804_04512_amd import binding as B
-from paper_1804_04512_amd.workloads import AttentionSpec
+from paper_1804_04512_amd.workloads import AttentionSpec, GatedSpec, VocabSpec
 
 pytestmark = pytest.mark.gpu
 
@@ -294,3 +294,61 @@ def test_many_sequences():
         # sums of at most 16 and 3 terms of numbers below 6, exponents below 40
         assert (c.o[rows, 0] - want).abs().max() <= 6 * (ref.EXP * 2 + 64 * ref.gamma(16))
     assert torch.isfinite(c.dq).all() and torch.isfinite(c.dk).all() and torch.isfinite(c.dv).all()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_a_training_step(dtype):
+    """Attention, a gated block and the loss over a vocabulary, then their gradients back to one buffer of q, k and v, cut to a norm.  Every operator is checked on
+    what it was given; the step is captured and replayed with other inputs."""
+    lengths, H, KV, D, hidden, classes = [70, 1, 129], 4, 2, 32, 96, 300
+    T, width, t = sum(lengths), H * D, TYPES[dtype]
+    c = Case(lengths, lengths, H, KV, D, True, dtype, seed=31, fused=True)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(32)
+    wg, wu, wd, wv = (torch.randn(s, generator=gen, device="cuda").mul(0.1).to(t) for s in ((hidden, width), (hidden, width), (width, hidden), (classes, width)))
+    labels = torch.randint(-30, classes, (T,), generator=gen, device="cuda", dtype=torch.int32)
+    block, head = GatedSpec(T, width, hidden, "silu", dtype), VocabSpec(T, width, classes, dtype)
+    nan = lambda *s, t=t: torch.full(s, NAN, dtype=t, device="cuda")
+    y, dy, a, b = nan(T, width), nan(T, width), nan(T, hidden), nan(T, hidden)
+    dwg, dwu, dwd, dwv = nan(hidden, width), nan(hidden, width), nan(width, hidden), nan(classes, width)
+    row_loss, row_lse, loss, norm = nan(T, t=torch.float32), nan(T, t=torch.float32), nan(1, t=torch.float32), nan(1, t=torch.float32)
+    grads = [c.dbuffer, dwg, dwu, dwd, dwv]
+    cut, several = [torch.full_like(g, NAN) for g in grads], B.tensor_list(grads)
+    ws = {f: B.workspace(getattr(B, f + "_workspace_bytes")(s)) for f, s in (
+        ("dll_attention_fwd", c.spec), ("dll_attention_bwd", c.spec), ("dll_gated_fwd", block), ("dll_gated_bwd", block), ("dll_vocab_loss_grad", head),
+        ("dll_grad_norm", several))}
+
+    def step():
+        B.dll_attention_fwd(c.spec, *c.inputs(), c.o, c.lse, ws["dll_attention_fwd"])
+        rows = c.o.view(T, width)
+        B.dll_gated_fwd(block, rows, wg, wu, wd, y, a, b, ws["dll_gated_fwd"])
+        B.dll_vocab_loss_grad(head, y, wv, None, labels, 8.0, row_loss, row_lse, loss, dy, dwv, None, ws["dll_vocab_loss_grad"])
+        B.dll_gated_bwd(block, rows, wg, wu, wd, a, b, dy, c.d_o.view(T, width), dwg, dwu, dwd, ws["dll_gated_bwd"])
+        B.dll_attention_bwd(c.spec, *c.inputs(), c.o, c.lse, c.d_o, c.dq, c.dk, c.dv, ws["dll_attention_bwd"])
+        B.dll_grad_clip(several, grads, cut, 0.25, norm, ws["dll_grad_norm"])
+
+    results = lambda: [r.clone() for r in (c.o, c.lse, c.d_o, y, dy, loss, row_loss, row_lse, norm, *grads, *cut)]
+    step()
+    c.check()
+    rows = c.o.view(T, width)
+    want = ref.gated(rows, wg, wu, wd, "silu", dy)
+    for k, v in {"y": y, "gate_pre": a, "up_pre": b, "dx": c.d_o.view(T, width), "dw_gate": dwg, "dw_up": dwu, "dw_down": dwd}.items():
+        ref.check(v, want[k], k)
+    want = ref.vocab(y, wv, None, labels, scale=8.0)
+    for k, v in {"loss": loss, "row_loss": row_loss, "row_lse": row_lse, "dx": dy, "dw": dwv}.items():
+        ref.check(v, want[k], k)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for turn in range(3):
+        c.buffer.copy_(Case(lengths, lengths, H, KV, D, True, dtype, seed=33 + turn, fused=True).buffer)
+        step()
+        eager = results()
+        for r in (c.o, c.lse, c.d_o, y, a, b, dy, loss, row_loss, row_lse, norm, *grads, *cut):
+            r.fill_(NAN)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for i, (x, z) in enumerate(zip(results(), eager)):
+            assert torch.isfinite(z).all() and torch.equal(x, z), (turn, i)
