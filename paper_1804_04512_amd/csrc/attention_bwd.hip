@@ -35,7 +35,17 @@ __device__ __forceinline__ void load_words_to_lds(const uintx4 &rs, unsigned off
 // Per query, [H][Tq]: lse in the exponent's base, and -delta, which the products with v start from
 struct Rows {
   float *lse2, *minus_delta;
+  unsigned *again = nullptr;   // per workgroup, where the careful pass is a launch of its own: whether it is to be taken
 };
+
+// Where a kernel's careful pass is.  NONE: without a mask there is none; HERE: a second copy of the loop; a launch of its own, after that of
+// the workgroups that leave word where it is needed (LEAVE), by those that find it (TAKE).  The copy costs no registers in most kernels.  Where sums and
+// rows fill them it makes the usual pass slower: 2048 tokens in two sequences, causal, 4 heads on 2, of 128 in single precision, microseconds without it / HERE / as a
+// launch: 171 / 235 / 176; of 256, 725 / 839 / 749; in bfloat16 332 / 408 / 341; 2001 ragged ones, six heads of 80 in single precision 146 / 162 / 153.
+// Without a mask the same call takes 200 us with NONE, 214 with HERE.
+enum Careful { NONE, HERE, LEAVE, TAKE };
+template <class T, int DP> constexpr bool dq_apart() { return DP > 128; }
+template <class T, int DP> constexpr bool dkv_apart() { return DP > (sizeof(T) == 2 ? 128 : 64); }
 
 // The sum of two rows' products, over both lane halves
 template <class T, int DP>
@@ -59,7 +69,7 @@ template <class T, int DP> constexpr int dq_residents() { return (sizeof(T) == 2
 
 // dq may be NULL: then the rows' figures are all that is wanted
 // ROWS groups of 32 queries; with two, the wavefronts share a tile's keys two by two
-template <class T, int DP, int BN, int ROWS>
+template <class T, int DP, int BN, int ROWS, Careful CARE>
 __global__ __launch_bounds__(kThreads, (dq_residents<T, DP>())) void attention_dq_kernel(const AttentionArgs a, const Rows rows, const Parts parts, const int tiles) {
   constexpr int kQueries = 32 * ROWS, kPer = BN * ROWS / 4;   // keys of a tile that a wavefront takes
   typedef Stager<T, DP, BN, kThreads> S;
@@ -68,7 +78,7 @@ __global__ __launch_bounds__(kThreads, (dq_residents<T, DP>())) void attention_d
   const int part = blockIdx.x % parts.n, id = blockIdx.x / parts.n, kv = id % a.KV, rest = id / a.KV, group = a.H / a.KV, head = kv * group + rest % group,
             tile = tiles - 1 - rest / group;
   const Place pq = place_of(a.q_starts, a.S, a.Tq, tile, kQueries);
-  if (pq.at >= pq.count) return;
+  if (pq.at >= pq.count || (CARE == TAKE && !rows.again[blockIdx.x])) return;
   const int kv_first = start_of(a.kv_starts, pq.sequence, a.Tk), keys = max(0, start_of(a.kv_starts, pq.sequence + 1, a.Tk) - kv_first);
   const int mine = wave / ROWS * kPer, row0 = pq.at + 32 * (wave % ROWS), row = row0 + (lane & 31), shift = keys - pq.count;
   const int seen = a.causal ? max(0, min(keys, row + shift + 1)) : keys;
@@ -192,8 +202,19 @@ __global__ __launch_bounds__(kThreads, (dq_residents<T, DP>())) void attention_d
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   };
-  pass(std::false_type{});
-  if (a.causal && anyone(!all_finite(dq), smem + 2 * S::kBytes, wave)) pass(std::true_type{});
+  if constexpr (CARE == TAKE) {
+    pass(std::true_type{});
+  } else {
+    pass(std::false_type{});
+    if (CARE != NONE && a.causal) {
+      const bool again = anyone(!all_finite(dq), smem + 2 * S::kBytes, wave);
+      if constexpr (CARE == LEAVE) {
+        if (threadIdx.x == 0) rows.again[blockIdx.x] = again;
+      } else if (again) {
+        pass(std::true_type{});
+      }
+    }
+  }
   if (reached)
 #pragma unroll
     for (int i = 0; i < DP / 32; ++i) dq[i] += NAN;
@@ -240,10 +261,8 @@ struct DkvShape {
   static constexpr int kResident = kInLds || (sizeof(T) == 2 ? DP <= 64 : DP <= 32) ? 2 : 1;
 };
 
-// CAUSAL as a.causal: the careful pass is in the causal kernel alone, as it costs single precision registers.  2001 ragged tokens, six heads of 80,
-// single precision, no mask: 200 us, 214 with the pass in it; causal, 162, and 146 without it.
-template <class T, int DP, Form F, bool CAUSAL>
-__global__ __launch_bounds__(kThreads, (DkvShape<T, DP, F>::kResident)) void attention_dkv_kernel(const AttentionArgs a, const Rows rows, const Parts parts) {
+template <class T, int DP, Form F, Careful CARE>
+__global__ __launch_bounds__(kThreads, (DkvShape<T, DP, F>::kResident)) void attention_dkv_kernel(const AttentionArgs a, const Rows rows, const Parts parts, int) {
   typedef DkvShape<T, DP, F> Sh;
   typedef typename Sh::Rows S;
   constexpr bool DK = Sh::kDK, DV = Sh::kDV;
@@ -252,7 +271,7 @@ __global__ __launch_bounds__(kThreads, (DkvShape<T, DP, F>::kResident)) void att
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
   const int part = blockIdx.x % parts.n, id = blockIdx.x / parts.n, kv = id % a.KV, tile = id / a.KV, group = a.H / a.KV;
   const Place pk = place_of(a.kv_starts, a.S, a.Tk, tile, kRows);
-  if (pk.at >= pk.count) return;
+  if (pk.at >= pk.count || (CARE == TAKE && !rows.again[blockIdx.x])) return;
   const int q_first = start_of(a.q_starts, pk.sequence, a.Tq), queries = max(0, start_of(a.q_starts, pk.sequence + 1, a.Tq) - q_first);
   const int key0 = pk.at + 32 * wave, key = key0 + (lane & 31), shift = pk.count - queries;
   const int from = a.causal ? max(0, pk.at - shift) : 0;         // the first query that sees any of the workgroup's keys
@@ -389,12 +408,21 @@ __global__ __launch_bounds__(kThreads, (DkvShape<T, DP, F>::kResident)) void att
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   };
-  pass(std::false_type{});
-  if constexpr (CAUSAL) {
-    bool finite = true;
-    if (DK) finite = all_finite(dk);
-    if (DV) finite = finite && all_finite(dv);
-    if (anyone(!finite, smem + Sh::kTiles, wave)) pass(std::true_type{});
+  if constexpr (CARE == TAKE) {
+    pass(std::true_type{});
+  } else {
+    pass(std::false_type{});
+    if constexpr (CARE != NONE) {
+      bool finite = true;
+      if (DK) finite = all_finite(dk);
+      if (DV) finite = finite && all_finite(dv);
+      const bool again = anyone(!finite, smem + Sh::kTiles, wave);
+      if constexpr (CARE == LEAVE) {
+        if (threadIdx.x == 0) rows.again[blockIdx.x] = again;
+      } else if (again) {
+        pass(std::true_type{});
+      }
+    }
   }
   if (reached)
 #pragma unroll
@@ -487,30 +515,47 @@ BwdPlan plan(const AttentionArgs &a, char *base) {
   if (p.dq.n > 1) p.dq.sums[0] = (float *)take((size_t)p.dq.n * a.Tq * a.H * p.dq.ld * sizeof(float));
   if (p.dkv.n > 1)
     for (float *&s : p.dkv.sums) s = (float *)take((size_t)p.dkv.n * a.Tk * a.KV * p.dkv.ld * sizeof(float));
+  if (a.causal && dkv_apart<T, DP>()) {   // of one launch at a time
+    const long q_grid = tiles_of(a.Tq, a.S, queries) * a.H * p.dq.n, k_grid = tiles_of(a.Tk, a.S, kRows) * a.KV * p.dkv.n;
+    p.figures.again = (unsigned *)take((size_t)(q_grid > k_grid ? q_grid : k_grid) * sizeof(unsigned));
+  }
   p.bytes = take.used;
   return p;
+}
+
+template <class K>
+hipError_t launch(K kernel, long grid, size_t lds, const AttentionArgs &a, const BwdPlan &p, const Parts &parts, int tiles, hipStream_t stream) {
+  DLL_TRY(allow_large_lds(reinterpret_cast<const void *>(kernel), lds));
+  kernel<<<dim3((unsigned)grid), dim3(kThreads), lds, stream>>>(a, p.figures, parts, tiles);
+  return hipGetLastError();
 }
 
 template <class T, int DP, int ROWS>
 hipError_t launch_dq(const AttentionArgs &a, const BwdPlan &p, hipStream_t stream) {
   constexpr int BN = tile_rows<T, DP>();
   constexpr size_t lds = 2 * Stager<T, DP, BN, kThreads>::kBytes + kCareful;
-  const auto kernel = attention_dq_kernel<T, DP, BN, ROWS>;
-  DLL_TRY(allow_large_lds(reinterpret_cast<const void *>(kernel), lds));
   const long tiles = tiles_of(a.Tq, a.S, 32 * ROWS);
   const Parts one, &dq = a.dq ? p.dq : one;
-  kernel<<<dim3((unsigned)(tiles * a.H * dq.n)), dim3(kThreads), lds, stream>>>(a, p.figures, dq, (int)tiles);
-  DLL_TRY(hipGetLastError());
+  const auto run = [&](auto kernel) { return launch(kernel, tiles * a.H * dq.n, lds, a, p, dq, (int)tiles, stream); };
+  if constexpr (dq_apart<T, DP>()) {
+    DLL_TRY(run(a.causal ? attention_dq_kernel<T, DP, BN, ROWS, LEAVE> : attention_dq_kernel<T, DP, BN, ROWS, NONE>));
+    if (a.causal && a.dq) DLL_TRY(run(attention_dq_kernel<T, DP, BN, ROWS, TAKE>));
+  } else {
+    DLL_TRY(run(attention_dq_kernel<T, DP, BN, ROWS, HERE>));
+  }
   return dq.n > 1 ? launch_sums<T>(Sums{dq, a.q_starts, a.S, a.Tq, a.H, a.D, a.q_row, {a.dq, nullptr}, {a.scale, 0.0f}}, stream) : hipSuccess;
 }
 
 template <class T, int DP, Form F>
 hipError_t launch_dkv(const AttentionArgs &a, const BwdPlan &p, hipStream_t stream) {
-  typedef DkvShape<T, DP, F> S;
-  const auto kernel = a.causal ? attention_dkv_kernel<T, DP, F, true> : attention_dkv_kernel<T, DP, F, false>;
-  DLL_TRY(allow_large_lds(reinterpret_cast<const void *>(kernel), S::kLds));
-  kernel<<<dim3((unsigned)(tiles_of(a.Tk, a.S, kRows) * a.KV * p.dkv.n)), dim3(kThreads), S::kLds, stream>>>(a, p.figures, p.dkv);
-  return hipGetLastError();
+  const auto run = [&](auto kernel) { return launch(kernel, tiles_of(a.Tk, a.S, kRows) * a.KV * p.dkv.n, DkvShape<T, DP, F>::kLds, a, p, p.dkv, 0, stream); };
+  if (!a.causal) return run(attention_dkv_kernel<T, DP, F, NONE>);
+  if constexpr (dkv_apart<T, DP>()) {
+    DLL_TRY(run(attention_dkv_kernel<T, DP, F, LEAVE>));
+    return run(attention_dkv_kernel<T, DP, F, TAKE>);
+  } else {
+    return run(attention_dkv_kernel<T, DP, F, HERE>);
+  }
 }
 
 template <class T, int DP>

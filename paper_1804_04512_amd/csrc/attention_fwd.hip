@@ -12,8 +12,8 @@
 //
 // Bound by the matrix pipe beside the exponentials: a tile of 64 keys is 1024 cycles of products and 980 of vector instructions for a wavefront, and
 // two wavefronts a SIMD overlap them only in part.  bfloat16, heads of 128: 4096 tokens, all keys seen, 16 heads, 134 us = 1030 TFLOP/s; causal
-// 88 us = 780 (its longest row of 64 tiles decides); 16384 tokens in five sequences 290 to 303 us = 940 to 980.  777 tokens, 16 heads of 64,
-// 9.7 us (latency).  Tried and slower: exponentials of one block of keys beside the products of the next and the former (134 to 162 us), wavefront
+// 88 us = 780 (its longest row of 64 tiles decides); 16384 tokens in five sequences 295 to 312 us = 910 to 970.  777 tokens, 16 heads of 64,
+// 9.9 us (latency).  Tried and slower: exponentials of one block of keys beside the products of the next and the former (134 to 162 us), wavefront
 // priorities around the products (the same), the second products beside the other half's exponentials (the same).
 #include "attention_tile.h"
 

@@ -179,7 +179,7 @@ __device__ __forceinline__ void written() {
 }
 
 // A product's 0 for a token that a mask leaves out stays 0 only while the other operand is finite.  Where sums turn out not to be finite under a mask, a
-// workgroup takes its tiles again: in those that the mask cuts, rows with such numbers lose them, and the lanes that see one of these rows are
+// workgroup takes its tiles again (or another launch's does): in those that the mask cuts, rows with such numbers lose them, and the lanes that see one of these rows are
 // told, whose results are NaN.  All of this is off the usual path but for one look at the sums and the registers that a second copy of the loop
 // takes.  With it / without, microseconds: 16384 prompt tokens in five sequences, 16 heads of 128 on 4, 304 / 296; 777, 10.7 / 10.2; a training pass
 // over 4096, 16 heads of 128, 368 / 367; 1024 in single precision, 8 heads of 64 on 2, 98 / 93.
