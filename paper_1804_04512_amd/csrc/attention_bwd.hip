@@ -158,7 +158,7 @@ __global__ __launch_bounds__(kThreads, (dq_residents<T, DP>())) void attention_d
           for (int r = 0; r < 16; ++r) delta += d[r];
         }
       }
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      arrived();
       barrier();   // everyone is done with the tiles
       delta = sum_of_halves(delta);
       if constexpr (ROWS == 2) {   // of both pairs' keys
@@ -200,7 +200,7 @@ __global__ __launch_bounds__(kThreads, (dq_residents<T, DP>())) void attention_d
         }
       }
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    arrived();
   };
   if constexpr (CARE == TAKE) {
     pass(std::true_type{});
@@ -406,7 +406,7 @@ __global__ __launch_bounds__(kThreads, (DkvShape<T, DP, F>::kResident)) void att
         }
       }
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    arrived();
   };
   if constexpr (CARE == TAKE) {
     pass(std::true_type{});

@@ -143,7 +143,7 @@ __global__ __launch_bounds__(kThreads, (Shape<T, DP, ROWS>::kResident)) void att
         }
       }
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // of the tile of zeros too
+    arrived();
   };
   pass(std::false_type{});
   if (a.causal && anyone(!all_finite(o), smem + Sh::kTiles, wave)) pass(std::true_type{});

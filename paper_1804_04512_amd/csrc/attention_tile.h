@@ -163,10 +163,13 @@ struct Stager<float, DP, NR, THREADS> {
   }
 };
 
-// The barrier in front of `turn`: all loads straight into LDS have landed
+// All that this wavefront has on its way into LDS has arrived: the loads that go there, and the stores of rows that do not come whole.  It stands in front
+// of every barrier behind which others may write or read those places, and behind a loop over tiles, whose last `turn` still sends a tile of zeros.
+__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+// The barrier in front of `turn`
 template <class T>
 __device__ __forceinline__ void landed() {
-  if constexpr (sizeof(T) == 2) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  if constexpr (sizeof(T) == 2) arrived();
   barrier();
 }
 // The one behind it
