@@ -24,7 +24,8 @@ constexpr int kPlanThreads = 256, kEach = 4, kTokens = kPlanThreads * kEach;   /
 constexpr int kRequests = 8;
 constexpr int kMost = 1 << 30;   // sums stop there, above any token that has a slot
 
-__device__ __forceinline__ int add(int a, int b) { return min(a + b, kMost); }   // of two up to kMost
+// of two up to kMost, whose sum may pass 31 bits
+__device__ __forceinline__ int add(int a, int b) { return (int)min((unsigned)a + (unsigned)b, (unsigned)kMost); }
 
 // What a request asks for: its figures with lengths below 0 taken as 0 and no more new tokens than there are tokens
 struct Asked {
