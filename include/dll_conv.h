@@ -457,7 +457,8 @@ dll_status dll_cache_write(const dll_cache_desc *d, int tokens, int row, const v
  *   o[r][h] = sum_t p_t v_t,  p = softmax_t(scale q[r][h] . k_t),  t < lengths[r], keys and values of head h / (heads / kv_heads)
  *   q, o [requests][heads][head_dim];  table [requests][table_pages], lengths [requests] int32;  lse [requests][heads] fp32, may be NULL
  * A length below 0 counts as 0, one that the table has no room for as that room.  Keys whose table entry lies outside [0, pages)
- * are left out, and nothing that pages hold behind a request's last token is used.  A request without keys has o = 0 and lse = -infinity.
+ * are left out, and nothing that pages hold behind a request's last token is used.  A request without keys has o = 0 and lse = -infinity.  What keys
+ * and values hold that is not finite reaches the outputs of the heads that read it alone; a key whose score is -infinity has no weight.
  * scale is finite (else DLL_ERR_SHAPE).  With DLL_BF16 p is rounded, relative to its maximum, before it meets v. */
 size_t dll_paged_attention_workspace_bytes(const dll_cache_desc *d);
 dll_status dll_paged_attention(const dll_cache_desc *d, const void *q, const void *k_cache, const void *v_cache,

@@ -96,11 +96,13 @@ struct Shared {
 };
 
 // WHOLE: a head's rows are whole runs of eight elements, so every load is 16 bytes or more from a place that exists and no branch stands
-// between the loads; what a lane has no run for it takes from its row's last one, against zeros of q.
+// between the loads; what a lane has no run for it takes from its row's last one, and is cleared before it meets the zeros of q: 0 times an
+// infinity would make a score of -infinity NaN.
 template <class T, int DP, bool WHOLE>
 __global__ __launch_bounds__(kThreads, (residents<T, DP>())) void paged_attention_kernel(const CacheArgs a, const Runs parts, const Divisor page) {
   typedef Rows<T, DP> G;
   constexpr int kSteps = DP / 32, kArea = kTile * G::kRowBytes;   // LDS of a wavefront: its values, or at the end its sums [16][DP] fp32
+  constexpr int kLeast = DP == 256 ? 136 : DP - 24;               // the shortest WHOLE row that comes here
   static_assert(kArea >= kHeads * DP * 4, "");
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   Shared &shared = *reinterpret_cast<Shared *>(smem + kWaves * kArea);
@@ -274,9 +276,13 @@ __global__ __launch_bounds__(kThreads, (residents<T, DP>())) void paged_attentio
       __builtin_amdgcn_sched_barrier(0);
       floatx4 z[2] = {};
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s)
+      for (int s = 0; s < kSteps; ++s) {
+        if (WHOLE && 32 * (s + 1) > kLeast && 32 * (s + 1) > a.D && 32 * s + 8 * quarter >= a.D)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) k[h][s] = Numbers<T>{};
 #pragma unroll
         for (int h = 0; h < 2; ++h) z[h] = mma16(k[h][s], q[s], z[h]);
+      }
       __builtin_amdgcn_sched_barrier(0);
       load(k, k_head, next);
       __builtin_amdgcn_sched_barrier(0);
