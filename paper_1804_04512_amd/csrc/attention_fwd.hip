@@ -2,7 +2,8 @@
 //
 // One pass over the keys with a running maximum m and sum l for each query: p = exp2(s - m), l += sum p, o += p v, and where m grows,
 // o and l shrink by exp2(old m - m).  The scale and log2 e are one factor.  m follows the true maximum only where that has grown by
-// more than 2^8: until then p is at most 256, which neither its rounding nor the sums mind, and o is left alone.
+// more than 2^8: until then p is at most 256, which its rounding does not mind, and o is left alone.  Sums that get near the largest number on their way
+// are taken again with p times a power of two that brings all of a row's below 1 (the careful pass, with the same digits).
 //
 // A workgroup has 128 queries of one head, 32 a wavefront, which hold their rows of q as fragments.  Tiles of keys and values come
 // straight into LDS, the next one while one is worked on.  Scores are taken transposed (keys are registers, the query is the lane), so
@@ -72,7 +73,10 @@ __global__ __launch_bounds__(kThreads, (Shape<T, DP, ROWS>::kResident)) void att
   float m, l;
   const Reader<T, DP, BN> reader(lane);
   bool reached = false;   // by a value that is not finite, in a careful pass
+  float lift = 1.0f;      // what o has to be multiplied with behind it
   const auto pass = [&](auto careful) {
+    const float weight = power(-fold_of(keys));
+    if (decltype(careful)::value) lift = power(fold_of(keys));
     sk.start(wave, k, begin, keys);
     sv.start(wave, v, begin, keys);
 #pragma unroll
@@ -83,7 +87,7 @@ __global__ __launch_bounds__(kThreads, (Shape<T, DP, ROWS>::kResident)) void att
       landed<T>();
       const char *lk = sk.turn(wave, odd, k, key0 + BN, keys), *lv = sv.turn(wave, odd, v, key0 + BN, keys);
       written<T>();
-      if (decltype(careful)::value && key0 + BN > pq.at + shift + 1) {   // more keys than the workgroup's first query sees
+      if (decltype(careful)::value && a.causal && key0 + BN > pq.at + shift + 1) {   // more keys than the workgroup's first query sees
         const Cleared c = clear_rows<T, DP, BN>(const_cast<char *>(lv), smem + Sh::kTiles);
         reached = reached || (c.first < BN && key0 + c.first < seen);
       }
@@ -134,6 +138,7 @@ __global__ __launch_bounds__(kThreads, (Shape<T, DP, ROWS>::kResident)) void att
           for (int r = 0; r < 16; ++r) {
             z[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[b][r], c, -from));
             l += z[b][r];
+            if (decltype(careful)::value) z[b][r] *= weight;
           }
 #pragma unroll
         for (int s = 0; s < kPer / 16; ++s) {
@@ -146,7 +151,7 @@ __global__ __launch_bounds__(kThreads, (Shape<T, DP, ROWS>::kResident)) void att
     arrived();
   };
   pass(std::false_type{});
-  if (a.causal && anyone(!all_finite(o), smem + Sh::kTiles, wave)) pass(std::true_type{});
+  if (anyone(!all_small(o), smem + Sh::kTiles, wave)) pass(std::true_type{});
   if (reached)
 #pragma unroll
     for (int i = 0; i < DP / 32; ++i) o[i] += NAN;
@@ -192,9 +197,10 @@ __global__ __launch_bounds__(kThreads, (Shape<T, DP, ROWS>::kResident)) void att
   }
   if (row >= pq.count) return;
   const long at = pq.first + row;
+  const float by = l == 0.0f ? 0.0f : lift * (1.0f / l);
   if (parts.n > 1) {
     const long to = (long)part * a.Tq + at;
-    store_sums(parts.sums[0] + (to * a.H + head) * parts.ld, o, parts.ld, half);
+    store_sums(parts.sums[0] + (to * a.H + head) * parts.ld, o, parts.ld, half, by);
     if (half == 0) {
       float *ml = parts.ml + (((long)part * a.H + head) * a.Tq + at) * 2;
       ml[0] = m;
@@ -202,11 +208,11 @@ __global__ __launch_bounds__(kThreads, (Shape<T, DP, ROWS>::kResident)) void att
     }
     return;
   }
-  store_row<T>((T *)a.o + at * a.H * a.D + head * a.D, o, l == 0.0f ? 0.0f : 1.0f / l, a.D, half);
+  store_row<T>((T *)a.o + at * a.H * a.D + head * a.D, o, by, a.D, half);
   if (a.lse && half == 0) a.lse[(long)head * a.Tq + at] = l == 0.0f ? -INFINITY : m * kLn2 + logf(l);
 }
 
-// A row's parts, each relative to its own maximum: four elements a thread
+// A row's parts, each with its own maximum and sum: a mean of their outputs.  Four elements a thread
 template <class T>
 __global__ __launch_bounds__(kThreads) void attention_join_kernel(const AttentionArgs a, const Parts parts, const long units) {
   const int wide = parts.ld / 4, first = start_of(a.q_starts, 0, a.Tq), end = start_of(a.q_starts, a.S, a.Tq);
@@ -214,20 +220,27 @@ __global__ __launch_bounds__(kThreads) void attention_join_kernel(const Attentio
     const int d = (int)(u % wide) * 4;
     const long row = u / wide, head = row % a.H, at = row / a.H;
     if (at < first || at >= end) continue;   // nobody's
+    floatx2 ml[kMostParts];   // all on their way at once
+#pragma unroll
+    for (int p = 0; p < kMostParts; ++p) ml[p] = p < parts.n ? *reinterpret_cast<const floatx2 *>(parts.ml + ((p * (long)a.H + head) * a.Tq + at) * 2) : floatx2{-INFINITY, 0.0f};
     float top = -INFINITY, l = 0.0f;
-    for (int p = 0; p < parts.n; ++p) top = fmaxf(top, parts.ml[((p * (long)a.H + head) * a.Tq + at) * 2]);
+#pragma unroll
+    for (int p = 0; p < kMostParts; ++p) top = fmaxf(top, ml[p][0]);
     const float from = top == -INFINITY ? 0.0f : top;
-    floatx4 o = {};
-    for (int p = 0; p < parts.n; ++p) {
-      const float *ml = parts.ml + ((p * (long)a.H + head) * a.Tq + at) * 2, f = __builtin_amdgcn_exp2f(ml[0] - from);
-      l += f * ml[1];
-      o += f * *reinterpret_cast<const floatx4 *>(parts.sums[0] + ((p * (long)a.Tq + at) * a.H + head) * parts.ld + d);
+#pragma unroll
+    for (int p = 0; p < kMostParts; ++p) {
+      ml[p][1] *= __builtin_amdgcn_exp2f(ml[p][0] - from);
+      l += ml[p][1];
     }
     const float by = l == 0.0f ? 0.0f : 1.0f / l;
+    floatx4 o = {};
+#pragma unroll
+    for (int p = 0; p < kMostParts; ++p)
+      if (p < parts.n) o += ml[p][1] * by * *reinterpret_cast<const floatx4 *>(parts.sums[0] + ((p * (long)a.Tq + at) * a.H + head) * parts.ld + d);
     T *to = (T *)a.o + row * a.D + d;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (d + j < a.D) to[j] = (T)(o[j] * by);
+      if (d + j < a.D) to[j] = (T)o[j];
     if (a.lse && d == 0) a.lse[head * a.Tq + at] = l == 0.0f ? -INFINITY : top * kLn2 + logf(l);
   }
 }

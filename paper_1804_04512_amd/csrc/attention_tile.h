@@ -19,6 +19,7 @@ namespace attn {
 
 using namespace tile;
 
+typedef float floatx2 __attribute__((ext_vector_type(2)));
 typedef float floatx8 __attribute__((ext_vector_type(8)));
 // Eight elements as the 32 x 32 x 16 products take them.  Single precision is three bfloat16 parts of each number (split3): six products on
 // a pipe of sixteen times the rate.
@@ -181,7 +182,8 @@ __device__ __forceinline__ void written() {
   }
 }
 
-// A product's 0 for a token that a mask leaves out stays 0 only while the other operand is finite.  Where sums turn out not to be finite under a mask, a
+// A product's 0 for a token that a mask leaves out stays 0 only while the other operand is finite.  Where sums turn out not to be finite under a mask (outputs:
+// not small, and without a mask too, as sums of large values may overflow on their way to a mean that does not), a
 // workgroup takes its tiles again (or another launch's does): in those that the mask cuts, rows with such numbers lose them, and the lanes that see one of these rows are
 // told, whose results are NaN.  All of this is off the usual path but for one look at the sums and the registers that a second copy of the loop
 // takes.  With it / without, microseconds: 16384 prompt tokens in five sequences, 16 heads of 128 on 4, 304 / 296; 777, 10.7 / 10.2; a training pass
@@ -196,6 +198,22 @@ __device__ __forceinline__ bool all_finite(const floatx16 (&c)[N]) {
     for (int r = 0; r < 16; ++r) zero[r % 4] = __builtin_fmaf(c[i][r], 0.0f, zero[r % 4]);
   return (zero[0] + zero[1]) + (zero[2] + zero[3]) == 0.0f;
 }
+// Whether all sums are below 2^120, so that a few wavefronts' may be added up; what is not finite is not
+template <int N>
+__device__ __forceinline__ bool all_small(const floatx16 (&c)[N]) {
+  float x[4] = {};   // finite as long as every sum's 2^8 fold is
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[r % 4] = __builtin_fmaf(c[i][r], 256.0f, x[r % 4]);
+#pragma unroll
+  for (float &f : x) f -= f;   // 0 or NaN
+  return (x[0] + x[1]) + (x[2] + x[3]) == 0.0f;
+}
+// An exponential follows the running maximum at up to 2^8 above it.  The power of two that brings the sum of that many of them below 1: products with it
+// lose no digits, and sums of values that it has made weights of cannot pass the largest of them.
+__device__ __forceinline__ int fold_of(int keys) { return 8 + 32 - __builtin_clz((unsigned)keys | 1u); }
+__device__ __forceinline__ float power(int e) { return __builtin_bit_cast(float, (127 + e) << 23); }   // 2^e, -126 <= e <= 127
 // Whether any of a workgroup's four wavefronts says so, once all of them are done with the tiles; its flags lie behind clear_rows's, so that no one
 // needs to wait until all have read them
 __device__ __forceinline__ bool anyone(bool here, char *lds, int wave) {
@@ -334,13 +352,13 @@ __device__ __forceinline__ void store_row(T *p, const floatx16 (&c)[N], float fa
 
 // The same unrounded, into a row of sums whose length is a multiple of four
 template <int N>
-__device__ __forceinline__ void store_sums(float *p, const floatx16 (&c)[N], int ld, int half) {
+__device__ __forceinline__ void store_sums(float *p, const floatx16 (&c)[N], int ld, int half, float factor = 1.0f) {
 #pragma unroll
   for (int i = 0; i < N; ++i)
 #pragma unroll
     for (int q = 0; q < 4; ++q)
       if (32 * i + 8 * q + 4 * half < ld)
-        *reinterpret_cast<floatx4 *>(p + 32 * i + 8 * q + 4 * half) = floatx4{c[i][4 * q], c[i][4 * q + 1], c[i][4 * q + 2], c[i][4 * q + 3]};
+        *reinterpret_cast<floatx4 *>(p + 32 * i + 8 * q + 4 * half) = floatx4{c[i][4 * q], c[i][4 * q + 1], c[i][4 * q + 2], c[i][4 * q + 3]} * factor;
 }
 
 // Here is where a fragment's value is made: it is not moved behind what follows
@@ -396,9 +414,10 @@ inline long tiles_of(int tokens, int sequences, int B) { return (long)tokens / B
 
 // Work split along the axis that a workgroup goes over: part k of n of a workgroup's `turns`, its sums left in 32 bits for a launch that adds them
 // up in order.  Taken where there are too few workgroups for the chip.
+constexpr int kMostParts = 16;
 struct Parts {
   int n = 1;
-  float *sums[2] = {nullptr, nullptr};   // [n][tokens][heads][ld]: un-normalised outputs; or a gradient's, or both gradients'
+  float *sums[2] = {nullptr, nullptr};   // [n][tokens][heads][ld]: the parts' own outputs; or a gradient's sums, or both gradients'
   float *ml = nullptr;                   // [n][heads][tokens][2]: maximum in the exponent's base, sum
   int ld = 0;                            // head_dim in whole fours
 };
@@ -408,7 +427,7 @@ __device__ __forceinline__ int turn_from(int part, int parts, int turns) { retur
 // 1024 tokens, 8 heads of 64 on 2, n = 1 / 4 / 6 / 12: 121 / 69 / 55 / 49; 6000 tokens, 8 heads of 128, n = 1 / 2 / 4: 503 / 452 / 528.
 inline int parts_of(long workgroups, long grid, long slots, long turns, long least) {
   long n = (slots + workgroups - 1) / workgroups;
-  for (const long most : {turns / least, kMaxGrid / grid, 16L}) n = n < most ? n : most;
+  for (const long most : {turns / least, kMaxGrid / grid, (long)kMostParts}) n = n < most ? n : most;
   return (int)(n > 1 ? n : 1);
 }
 

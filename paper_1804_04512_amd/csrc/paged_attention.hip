@@ -5,8 +5,8 @@
 //
 // The work is units of kUnit keys of one request and key head, dealt to the workgroups in equal runs whatever the lengths are: each
 // workgroup finds its run by adding the lengths up.  Where a run holds all of a request's head the result is written; where it
-// begins or ends inside one, sums, maximum and un-normalised outputs go to the workspace (two places a workgroup) and a second
-// launch joins them, in the order of the keys.
+// begins or ends inside one, its outputs with their maximum and sum go to the workspace (two places a workgroup) and a second
+// launch makes their mean, in the order of the keys.
 //
 // Inside a workgroup the wavefronts take tiles of 32 keys in turn, each with its own running maximum and sums.  A lane holds eight elements of
 // two keys a step, straight from memory into the operand's registers; values have the same addresses, and go through the
@@ -59,7 +59,7 @@ __device__ __forceinline__ int keys_of(const CacheArgs &a, int r) { return (int)
 __device__ __forceinline__ int units_of(int keys) { return (keys + kUnit - 1) / kUnit; }
 
 struct Runs {
-  float *o;    // [2 groups][kHeads][ld], relative to the maximum
+  float *o;    // [2 groups][kHeads][ld]
   float *ml;   // [2 groups][kHeads][2]: maximum in the exponent's base, sum
   int ld;      // head_dim in whole fours
   int blocks;  // of at most kHeads heads that share a key head
@@ -232,6 +232,9 @@ __global__ __launch_bounds__(kThreads, (residents<T, DP>())) void paged_attentio
 #pragma unroll
     for (int i = 0; i < DP / 16; ++i) o[i] = floatx4{};
     float m = -INFINITY, l = 0.0f;
+    // p times a power of two that brings all of a request's below 1, as sums of large values would overflow on their way to a mean that does not.  (Of
+    // 60000 keys, those with weights below 2^-102 of the largest lose digits.)
+    const float weight = power(-fold_of(keys));
     // On their way while a tile is worked on: the next one's values and keys, and the pages of the one behind it, which are asked
     // for first: loads come back in order, and the next rows' addresses must not wait for rows.
     int key0 = key_begin + wave * kTile, id[2], id_next[2];
@@ -309,7 +312,7 @@ __global__ __launch_bounds__(kThreads, (residents<T, DP>())) void paged_attentio
       Numbers<T> p;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j >> 2][j & 3], c, -from));
+        const float e = weight * __builtin_amdgcn_exp2f(__builtin_fmaf(z[j >> 2][j & 3], c, -from));
         l += e;
         p[j] = (T)e;
       }
@@ -340,31 +343,32 @@ __global__ __launch_bounds__(kThreads, (residents<T, DP>())) void paged_attentio
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
-    l = sum4(l);
+    const float lift = power(fold_of(keys));
+    l = sum4(l) * lift;
 
-    // the wavefronts' sums joined: o and l relative to the largest maximum
+    // the wavefronts' outputs joined
     if (quarter == 0) ml[wave][col][0] = m, ml[wave][col][1] = l;
+    const float by = l == 0.0f ? 0.0f : lift / l;
 #pragma unroll
-    for (int i = 0; i < DP / 16; ++i) *reinterpret_cast<floatx4 *>(area + (col * DP + 16 * i + 4 * quarter) * 4) = o[i];
+    for (int i = 0; i < DP / 16; ++i) *reinterpret_cast<floatx4 *>(area + (col * DP + 16 * i + 4 * quarter) * 4) = o[i] * by;
     __syncthreads();
     const bool full = units == per;
     const int slot = 2 * (int)blockIdx.x + (u == first ? 0 : 1);
     for (int i = threadIdx.x; i < heads * DP; i += kThreads) {
       const int h = i / DP, d = i % DP;
-      float top = -INFINITY, sum = 0.0f, out = 0.0f;
+      float top = -INFINITY, sum = 0.0f, out = 0.0f, f[kWaves];
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[w][h][0]);
       const float from = top == -INFINITY ? 0.0f : top;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        const float f = __builtin_amdgcn_exp2f(ml[w][h][0] - from);
-        sum += f * ml[w][h][1];
-        out += f * *reinterpret_cast<const float *>(smem + w * kArea + i * 4);
-      }
+      for (int w = 0; w < kWaves; ++w) sum += f[w] = __builtin_amdgcn_exp2f(ml[w][h][0] - from) * ml[w][h][1];
+      const float share = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) out += f[w] * share * *reinterpret_cast<const float *>(smem + w * kArea + i * 4);
       if (d >= a.D) continue;
       if (full) {
         const long to = (long)r * a.H + head0 + h;
-        ((T *)a.o)[to * a.D + d] = (T)(sum == 0.0f ? 0.0f : out / sum);
+        ((T *)a.o)[to * a.D + d] = (T)out;
         if (a.lse && d == 0) a.lse[to] = sum == 0.0f ? -INFINITY : top * kLn2 + logf(sum);
       } else {
         parts.o[((long)slot * kHeads + h) * parts.ld + d] = out;
@@ -421,12 +425,13 @@ __global__ __launch_bounds__(kThreads) void paged_join_kernel(const CacheArgs a,
   const int wide = parts.ld / 4, items = heads * wide, side = max(1, kThreads / items);   // wide: 1 to 64
   for (int first = 0; first < items; first += kThreads) {   // more than one turn with more items than threads
     const int item = first + t % (side > 1 ? items : kThreads), p = side > 1 ? t / items : 0, h = min(item / wide, heads - 1), c = item % wide;
+    const float share = total[h] == 0.0f ? 0.0f : 1.0f / total[h];
     floatx4 out = {};
     if (item < items && p < side)
 #pragma unroll 4
       for (int i = p; i < n; i += side) {
         const long row = row_of(i, h);
-        out += __builtin_amdgcn_exp2f(parts.ml[row * 2] - from[h]) * *reinterpret_cast<const floatx4 *>(parts.o + row * parts.ld + 4 * c);
+        out += __builtin_amdgcn_exp2f(parts.ml[row * 2] - from[h]) * parts.ml[row * 2 + 1] * share * *reinterpret_cast<const floatx4 *>(parts.o + row * parts.ld + 4 * c);
       }
     if (side > 1) {
       sums[t] = out;
@@ -438,7 +443,7 @@ __global__ __launch_bounds__(kThreads) void paged_join_kernel(const CacheArgs a,
     const long to = (long)r * a.H + head0 + h;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (4 * c + j < a.D) ((T *)a.o)[to * a.D + 4 * c + j] = (T)(total[h] == 0.0f ? 0.0f : out[j] / total[h]);
+      if (4 * c + j < a.D) ((T *)a.o)[to * a.D + 4 * c + j] = (T)out[j];
     if (a.lse && c == 0) a.lse[to] = total[h] == 0.0f ? -INFINITY : shift[h] * kLn2 + logf(total[h]);
   }
 }
