@@ -112,6 +112,9 @@ CacheArgs cache_args(const dll_cache_desc *d) {
   return a;
 }
 
+// Scores are scale * log2 e times a product: that factor has to be a number
+bool off_scale(float scale) { return !(std::fabs(scale) <= 0x1p127f); }
+
 // q, k, v and their gradients stand at any multiple of their elements; o and its gradient at 16 bytes
 bool off_type(const void *p, int dtype) { return reinterpret_cast<uintptr_t>(p) % type_bytes(dtype) != 0; }
 
@@ -282,7 +285,7 @@ dll_status dll_attention_fwd(const dll_attention_desc *d, const void *q, const v
   if (!q || !k || !v || !q_starts || !kv_starts || !o) return DLL_ERR_NULL;
   const void *in[] = {q, k, v, q_starts, kv_starts}, *out[] = {o, lse, ws};
   if (aliased(in, 5, out, 3) || misaligned(o) || off_element(lse) || off_element(q_starts) || off_element(kv_starts)) return DLL_ERR_SHAPE;
-  if (off_type(q, d->dtype) || off_type(k, d->dtype) || off_type(v, d->dtype) || !std::isfinite(scale)) return DLL_ERR_SHAPE;
+  if (off_type(q, d->dtype) || off_type(k, d->dtype) || off_type(v, d->dtype) || off_scale(scale)) return DLL_ERR_SHAPE;
   if ((st = check_ws(ws, ws_bytes, dll_attention_fwd_workspace_bytes(d))) != DLL_OK) return st;
   AttentionArgs a = attention_args(d);
   a.q = q; a.k = k; a.v = v; a.q_starts = q_starts; a.kv_starts = kv_starts; a.scale = scale; a.o = o; a.lse = lse;
@@ -302,7 +305,7 @@ dll_status dll_attention_bwd(const dll_attention_desc *d, const void *q, const v
   if (aliased(in, 8, out, 4) || misaligned(o) || misaligned(d_o) || off_element(lse) || off_element(q_starts) || off_element(kv_starts)) return DLL_ERR_SHAPE;
   for (const void *p : {q, k, v, (const void *)dq, (const void *)dk, (const void *)dv})
     if (off_type(p, d->dtype)) return DLL_ERR_SHAPE;
-  if (!std::isfinite(scale)) return DLL_ERR_SHAPE;
+  if (off_scale(scale)) return DLL_ERR_SHAPE;
   if ((st = check_ws(ws, ws_bytes, dll_attention_bwd_workspace_bytes(d))) != DLL_OK) return st;
   AttentionArgs a = attention_args(d);
   a.q = q; a.k = k; a.v = v; a.q_starts = q_starts; a.kv_starts = kv_starts; a.scale = scale;
@@ -354,7 +357,7 @@ dll_status dll_paged_attention(const dll_cache_desc *d, const void *q, const voi
   if (!q || !k_cache || !v_cache || !table || !lengths || !o) return DLL_ERR_NULL;
   const void *in[] = {q, k_cache, v_cache, table, lengths}, *out[] = {o, lse, ws};
   if (aliased(in, 5, out, 3) || misaligned(q) || misaligned(k_cache) || misaligned(v_cache) || misaligned(o)) return DLL_ERR_SHAPE;
-  if (off_element(table) || off_element(lengths) || off_element(lse) || !std::isfinite(scale)) return DLL_ERR_SHAPE;
+  if (off_element(table) || off_element(lengths) || off_element(lse) || off_scale(scale)) return DLL_ERR_SHAPE;
   if ((st = check_ws(ws, ws_bytes, dll_paged_attention_workspace_bytes(d))) != DLL_OK) return st;
   CacheArgs a = cache_args(d);
   a.q = q; a.k_cache = const_cast<void *>(k_cache); a.v_cache = const_cast<void *>(v_cache); a.table = const_cast<int *>(table); a.lengths = lengths;

@@ -67,7 +67,7 @@ __global__ __launch_bounds__(kThreads, (Shape<T, DP, ROWS>::kResident)) void att
   const int turns = (seen_all + BN - 1) / BN, begin = turn_from(part, parts.n, turns) * BN, end = min(seen_all, turn_from(part + 1, parts.n, turns) * BN);
   RowFrags<T, DP> q;   // with a scale below 0 the maximum of the scores is that of -q k
   q.load((const T *)a.q + (long)(pq.first + min(row, pq.count - 1)) * a.q_row + head * a.D, a.D, half, a.scale < 0.0f);
-  const float c = fmaxf(fabsf(a.scale) * kLog2e, 0x1p-126f);   // a masked score of -infinity stays one where the scale is 0
+  const float c = factor_of(a.scale);
 
   floatx16 o[DP / 32];
   float m, l;

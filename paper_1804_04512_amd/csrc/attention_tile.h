@@ -31,6 +31,10 @@ template <class T> constexpr int planes() { return sizeof(T) == 2 ? 1 : 3; }
 
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
 
+// What makes exponents to the base 2 of scores.  A masked score of -infinity stays one where the scale is 0: the smallest number takes its place, with
+// which no score passes 2^-21.
+__device__ __forceinline__ float factor_of(float scale) { return fmaxf(fabsf(scale) * kLog2e, 0x1p-149f); }
+
 // c += a b over sixteen: a's 32 rows become c's registers, b's its lanes
 __device__ __forceinline__ floatx16 mma(bf16x8 a, bf16x8 b, floatx16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ floatx16 mma(const Split &a, const Split &b, floatx16 c) { return mfma6(a, b, c); }

@@ -111,7 +111,7 @@ __global__ __launch_bounds__(kThreads, (residents<T, DP>())) void paged_attentio
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4, col = lane & 15;
   char *area = smem + wave * kArea;
   const int group = a.H / a.KV, blocks = parts.blocks, VH = a.KV * blocks;
-  const float c = fmaxf(fabsf(a.scale) * kLog2e, 0x1p-126f);
+  const float c = factor_of(a.scale);
 
   // this workgroup's units, and the request that the first of them belongs to
   const int each = (a.R + kThreads - 1) / kThreads, r0 = min((int)threadIdx.x * each, a.R), r1 = min(r0 + each, a.R);
