@@ -309,12 +309,13 @@ __global__ __launch_bounds__(kThreads, (residents<T, DP>())) void paged_attentio
         for (int i = 0; i < DP / 16; ++i) o[i] *= shrink;
       }
       const float from = m == -INFINITY ? 0.0f : m;
-      Numbers<T> p;
+      Numbers<T> p, rest;   // bfloat16: in two parts, as the second's products cost nothing beside memory
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float e = weight * __builtin_amdgcn_exp2f(__builtin_fmaf(z[j >> 2][j & 3], c, -from));
         l += e;
         p[j] = (T)e;
+        rest[j] = (T)(e - (float)p[j]);
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       constexpr int kAhead = DP * (int)sizeof(T) <= 256 ? DP / 16 : DP % 64 ? 3 : 4;   // fragments read at a time
@@ -340,6 +341,9 @@ __global__ __launch_bounds__(kThreads, (residents<T, DP>())) void paged_attentio
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int b = 0; b < kAhead; ++b) o[i - kAhead + 1 + b] = mma16(w[b], p, o[i - kAhead + 1 + b]);
+        if constexpr (sizeof(T) == 2)
+#pragma unroll
+          for (int b = 0; b < kAhead; ++b) o[i - kAhead + 1 + b] = mma16(w[b], rest, o[i - kAhead + 1 + b]);
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
