@@ -498,23 +498,42 @@ BwdPlan plan(const AttentionArgs &a, char *base) {
   Take take{base};
   p.figures.lse2 = (float *)take((size_t)a.H * a.Tq * sizeof(float));
   p.figures.minus_delta = (float *)take((size_t)a.H * a.Tq * sizeof(float));
-  // 64 queries a workgroup where 128 leave most of the chip idle, or where a causal mask's longest row of tiles decides; microseconds of a training
-  // pass with 128 / 64: 1000 tokens in two sequences, 8 heads of 128 68.4 / 64.1; 4096 in one, 16 heads of 128 386 / 370, of 64 258 / 242; in six
-  // 138 / 142; in one, all keys seen, 649 / 668
-  const bool chain = a.causal && a.Tk / a.S >= 2048;
-  if (kTwo && (2 * q_work <= cus || (chain && q_work <= 2 * cus))) p.rows = 2;
-  const int queries = 32 * p.rows;
-  p.dq.n = parts_of((a.Tq + queries - 1) / queries * (long)a.H, tiles_of(a.Tq, a.S, queries) * a.H, dq_residents<T, DP>() * cus, a.Tk / a.S / BN, 2);
-  // values in LDS and two workgroups a unit, but for the smallest calls, and where one round of them has such a row of tiles that a lone workgroup
-  // finishes sooner; values in registers / in LDS: 4096 tokens, 16 heads of 128 on 4 key heads 501 / 439, all keys seen 649 / 591, causal 386 / 424; 8192 in
-  // three sequences 610 / 577; 1000 in two, 8 heads on 2, 68.4 / 72.2
-  p.less = kLess && 4 * k_work >= cus && !(chain && k_work >= 2 * cus && 2 * k_work < 5 * cus);
-  const int resident = p.less ? DkvShape<T, DP, kLess ? HELD_LESS : BOTH>::kResident : DkvShape<T, DP, BOTH>::kResident;
-  p.dkv.n = parts_of(all_k * a.KV, tiles_of(a.Tk, a.S, kRows) * a.KV, resident * cus, (long)a.Tq / a.S * (a.H / a.KV) / BN, 2);
+  const auto dq_parts = [&](int rows) {
+    const int queries = 32 * rows;
+    return parts_of((a.Tq + queries - 1) / queries * (long)a.H, tiles_of(a.Tq, a.S, queries) * a.H, dq_residents<T, DP>() * cus, a.Tk / a.S / BN, 2);
+  };
+  const auto dkv_parts = [&](int resident) {
+    return parts_of(all_k * a.KV, tiles_of(a.Tk, a.S, kRows) * a.KV, resident * cus, (long)a.Tq / a.S * (a.H / a.KV) / BN, 2);
+  };
+  // Both rules below come from 207 causal and open calls taken either way: 500 to 20480 tokens in one to forty sequences, 4 to 128 heads, groups of 1, 2, 4 and 8.  They
+  // lose 0.4 and 0.3 % to the better way on average and 11 and 8 % at most.
+  // Sequences so long that, under a causal mask, their first keys' and last queries' workgroups last: 1365 and 1536 tokens 9 and 4 % faster the other way, 2000 and 2048
+  // 8 and 4 % slower (dk and dv).
+  const bool chain = a.causal && a.Tk / a.S >= 1792;
+  // 64 queries a workgroup where 128 have their keys cut into parts, whose sums cost a pass; where they leave most of the chip idle; and where a causal
+  // mask's longest workgroups decide, as all of them run at once (heads up to 64: nearly so).  Microseconds of a backward pass with 128 / 64, causal: 40 heads of 128, 1024 tokens
+  // 111 / 85; 16, 3328 tokens 233 / 207, 4096 in one 291 / 282, in two 182 / 168, in four 126 / 128, 4480 348 / 347, 4992 422 / 430; 16 of 64, 4096 188 / 172, 5120 244 / 229, 6400
+  // 324 / 323, 8192 522 / 521, 4096 in twenty 46 / 48; all keys seen, 16 of 64, 2560 161 / 143, 4096 256 / 270.
+  p.dq.n = dq_parts(4);
+  if (kTwo && (p.dq.n > 1 || 2 * q_work <= cus || (chain && q_work <= (DP <= 64 ? 3 : 2) * cus))) {
+    p.rows = 2;
+    p.dq.n = dq_parts(2);
+  }
+  // values in LDS, so that a unit has two workgroups: where there are two for it, but for causal calls with so few that all run at once and nothing evens out their long
+  // and short ones; and where that takes more parts than values in registers do, only if the parts are long enough for their sums.  Values in registers / in LDS: 16 heads
+  // of 128, causal, 3328 tokens 233 / 245, 3968 296 / 315, 4096 291 / 327, 4480 348 / 367, 5120 438 / 439, 5632 509 / 493, 8192 991 / 927; in two 537 / 488; 8 heads, 3500 tokens 165 / 167,
+  // 4500 249 / 232, 8192 540 / 620, 10000 792 / 811; 16 on 4, 2048 141 / 133, 4096 406 / 348, 16384 3911 / 5065; 32 on 8, 9216 2526 / 2825, 10240 3172 / 3340; 3000 in thirty, 16 heads, 67 / 60;
+  // all keys seen, 16 heads, 2048 160 / 166, 2560 315 / 285, 4096 507 / 449
+  const int apart = dkv_parts(DkvShape<T, DP, BOTH>::kResident), beside = kLess ? dkv_parts(DkvShape<T, DP, kLess ? HELD_LESS : BOTH>::kResident) : apart;
+  const bool at_once = chain && k_work >= 2 * cus && 2 * k_work < 5 * cus;
+  const long part_work = (long)a.Tq / a.S * (a.H / a.KV) * (a.causal ? 1 : 2);
+  p.less = kLess && !at_once && (beside == apart ? k_work * beside > cus : part_work >= 4096);
+  p.dkv.n = p.less ? beside : apart;
   p.dq.ld = p.dkv.ld = (a.D + 3) & ~3;
   if (p.dq.n > 1) p.dq.sums[0] = (float *)take((size_t)p.dq.n * a.Tq * a.H * p.dq.ld * sizeof(float));
   if (p.dkv.n > 1)
     for (float *&s : p.dkv.sums) s = (float *)take((size_t)p.dkv.n * a.Tk * a.KV * p.dkv.ld * sizeof(float));
+  const int queries = 32 * p.rows;
   if (a.causal && dkv_apart<T, DP>()) {   // of one launch at a time
     const long q_grid = tiles_of(a.Tq, a.S, queries) * a.H * p.dq.n, k_grid = tiles_of(a.Tk, a.S, kRows) * a.KV * p.dkv.n;
     p.figures.again = (unsigned *)take((size_t)(q_grid > k_grid ? q_grid : k_grid) * sizeof(unsigned));

@@ -15,6 +15,7 @@ BACKWARD = {
     "float32": [(40, 40, 1, 2, 1, d, True) for d in (20, 64, 90, 128, 200)] + [(700, 700, 1, 4, 2, d, True) for d in (30, 64, 96, 127, 256)] +
                [(90, 150, 2, 4, 2, d, False) for d in (24, 48, 80, 120, 160)],
 }
+BACKWARD["bfloat16"] += [(1100, 1100, 1, 8, 2, d, False) for d in (96, 128)]
 CACHES = {t: [(3, 100, 2, 1, d, 16) for d in (16, 64, 72, 128, 192)] + [(3, 300, 4, 2, d, 7) for d in (13, 65, 130)] + [(2, 2000, 3, 1, 64, 16), (40, 700, 32, 4, 32, 16)]
           for t in ("bfloat16", "float32")}
 
