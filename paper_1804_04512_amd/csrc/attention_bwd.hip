@@ -39,10 +39,12 @@ struct Rows {
 };
 
 // Where a kernel's careful pass is.  NONE: without a mask there is none; HERE: a second copy of the loop; a launch of its own, after that of
-// the workgroups that leave word where it is needed (LEAVE), by those that find it (TAKE).  The copy costs no registers in most kernels.  Where sums and
-// rows fill them it makes the usual pass slower: 2048 tokens in two sequences, causal, 4 heads on 2, of 128 in single precision, microseconds without it / HERE / as a
-// launch: 171 / 235 / 176; of 256, 725 / 839 / 749; in bfloat16 332 / 408 / 341; 2001 ragged ones, six heads of 80 in single precision 146 / 162 / 153.
-// Without a mask the same call takes 200 us with NONE, 214 with HERE.
+// the workgroups that leave word where it is needed (LEAVE), by those that find it (TAKE).  As compiled, the copy makes no kernel spill but dq's of 97 to 128 elements in
+// bfloat16 with 128 queries (36 bytes a lane, outside the loop: 4224 tokens, 16 heads, 310 us, as a launch 319).  Where sums and rows fill the registers anyway it makes the usual
+// pass slower: 2048 tokens in two sequences, causal, 4 heads on 2, of 128 in single precision, microseconds without it / HERE / as a launch: 171 / 235 / 176; of 256, 725 / 839 / 749; in
+// bfloat16 332 / 408 / 341; 2001 ragged ones, six heads of 80 in single precision 146 / 162 / 153.  Without a mask the latter take 200 with NONE, 214 with HERE.
+// Scratch of the usual pass, bytes a lane: single precision, dk and dv of 97 to 128 elements 240, of 129 to 256 dq 1250 to 1270, dk 510, dv 1210 to 1230; bfloat16, dk and dv
+// of 129 to 256 870.
 enum Careful { NONE, HERE, LEAVE, TAKE };
 template <class T, int DP> constexpr bool dq_apart() { return DP > 128; }
 template <class T, int DP> constexpr bool dkv_apart() { return DP > (sizeof(T) == 2 ? 128 : 64); }
@@ -64,8 +66,11 @@ __device__ __forceinline__ float row_product(const T *x, const T *y, int dim, in
 }
 
 // ------------------------------------------------------------------------------------------------ dq
-// workgroups that a compute unit holds, by their registers
-template <class T, int DP> constexpr int dq_residents() { return (sizeof(T) == 2 ? DP <= 128 : DP <= 64) ? 2 : 1; }
+// workgroups that a compute unit holds, by their registers.  Single precision of 33 to 64 elements spills 75 of them with two; backward pass, microseconds with two / one:
+// 1024 tokens, 8 heads of 64 on 2, 74.1 / 66.3, all keys seen 79.3 / 71.4; 2048 in two, 4 on 2, 77.4 / 66.3; 600 in 24, 8 heads, 22.5 / 20.0; 8192 in four, 16 heads, 749 / 685,
+// all keys seen 1240 / 1231; 4096, 8 heads, 529 / 565 (as many workgroups as units, so not cut into parts).  Two with the careful pass as a launch of its own
+// spill 33 and take 72.9, 76.4, 76.4, 22.7, 718, 1213 and 512.
+template <class T, int DP> constexpr int dq_residents() { return (sizeof(T) == 2 ? DP <= 128 : DP <= 32) ? 2 : 1; }
 
 // dq may be NULL: then the rows' figures are all that is wanted
 // ROWS groups of 32 queries; with two, the wavefronts share a tile's keys two by two
@@ -560,7 +565,7 @@ hipError_t launch_dq(const AttentionArgs &a, const BwdPlan &p, hipStream_t strea
     DLL_TRY(run(a.causal ? attention_dq_kernel<T, DP, BN, ROWS, LEAVE> : attention_dq_kernel<T, DP, BN, ROWS, NONE>));
     if (a.causal && a.dq) DLL_TRY(run(attention_dq_kernel<T, DP, BN, ROWS, TAKE>));
   } else {
-    DLL_TRY(run(attention_dq_kernel<T, DP, BN, ROWS, HERE>));
+    DLL_TRY(run(attention_dq_kernel<T, DP, BN, ROWS, HERE>));   // without a mask the copy costs less than 1 % (instances without it: 14 calls in 0.993 to 1.007 of the time)
   }
   return dq.n > 1 ? launch_sums<T>(Sums{dq, a.q_starts, a.S, a.Tq, a.H, a.D, a.q_row, {a.dq, nullptr}, {a.scale, 0.0f}}, stream) : hipSuccess;
 }

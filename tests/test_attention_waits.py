@@ -37,3 +37,11 @@ def test_the_walk_itself():
             (20, "s_waitcnt", "vmcnt(0)", None), (24, "s_barrier", "", None), (28, "s_endpgm", "", None)]
     before = device_code.reaching(code, step)
     assert not before[3] and before[5]
+
+
+def test_registers_that_are_spilled(tmp_path):
+    """Sums and rows of heads up to 96 elements stay in registers: no gradient kernel writes any of them to memory and reads them again."""
+    for kernel in ("attention_dq_kernel", "attention_dkv_kernel"):
+        for name, code in device_code.kernels(B.LIB_PATH, tmp_path, kernel).items():
+            if any(f"Li{dim}EL" in name for dim in (32, 64, 96)) and not any(f"Li{dim}EL" in name for dim in (128, 256)):
+                assert not any(op.startswith("scratch_") for _, op, _, _ in code), name
