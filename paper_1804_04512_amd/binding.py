@@ -336,9 +336,13 @@ class _CurrentStream(NamedTuple):
 
 def _call_stream(stream):
     if stream is None:
-        # its address alone: the object that torch.cuda.current_stream() makes of it takes 2.6 us, a quarter of a small call
         index = torch.cuda.current_device()
-        return _CurrentStream(torch.device("cuda", index), torch._C._cuda_getCurrentRawStream(index))
+        try:
+            # its address alone: the object that torch.cuda.current_stream() makes of it takes 2.6 us, a quarter of a small call
+            address = torch._C._cuda_getCurrentRawStream(index)
+        except AttributeError:   # a private name, which another version need not have
+            address = torch.cuda.current_stream(index).cuda_stream
+        return _CurrentStream(torch.device("cuda", index), address)
     s = stream
     if s.device != torch.device("cuda", torch.cuda.current_device()):
         raise ValueError(f"the stream belongs to {s.device}, which is not the current device")
