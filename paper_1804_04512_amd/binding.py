@@ -435,6 +435,9 @@ def dll_vocab_loss_grad(v: VocabSpec, x, w, bias, labels, scale, row_loss, row_l
         "dll_vocab_loss_grad")
 
 
+_MOST = (1 << 31) - 1   # of the library's int arguments
+
+
 def attention_desc(a: AttentionSpec) -> dll_attention_desc:
     return dll_attention_desc(a.q_tokens, a.kv_tokens, a.sequences, a.heads, a.kv_heads, a.head_dim, int(a.causal), DTYPE[a.dtype],
                               a.q_row, a.kv_row)
@@ -444,6 +447,8 @@ def _head_rows(t: Optional[torch.Tensor], shape, row: int, dtype: torch.dtype, w
     """The address of a tensor [tokens][heads][head_dim] whose tokens lie `row` elements apart (0: contiguous)."""
     if t is None:
         return _tensor(t, shape, dtype, what, device, optional)
+    if row > _MOST:   # ctypes would cut it
+        raise ValueError(f"{what}: tokens {row} elements apart, {_MOST} at most")
     if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{what}: {dtype} of shape {tuple(shape)} expected, got {t.dtype} of shape {tuple(t.shape)}")
     strides = (row or shape[1] * shape[2], shape[2], 1)
@@ -498,6 +503,8 @@ def _ints(t, n, what: str, dev, optional: bool = False):
     """The address of a vector of whole numbers; n: its length, or None (any), or a shape."""
     if t is not None and n is None:
         n = t.numel()
+        if n > _MOST:
+            raise ValueError(f"{what}: {n} entries, {_MOST} at most")
     return _tensor(t, n if isinstance(n, tuple) else (n,), torch.int32, what, dev, optional)
 
 
