@@ -398,9 +398,9 @@ typedef struct {
  *   o [q_tokens][heads][head_dim] contiguous;  lse [heads][q_tokens] fp32, may be NULL
  * A query that may see no key has o = 0 and lse = -infinity.  Rows outside the sequences are neither read nor written.  What other
  * sequences hold does not matter, and what keys, values, queries and d_o hold that is not finite reaches the results of those that see them
- * or are seen by them alone (as NaN, where they would be infinite, too).  scale is at most 2^127 in size (else DLL_ERR_SHAPE); q_i . k_j and
- * s_ij count as infinite from 2.3e38 on.  Starts outside [0, tokens] are taken as the nearest of these.  With DLL_BF16 p is rounded, relative to
- * its row's maximum, before it meets v.  Products of DLL_FP32 tensors are taken on three bfloat16 parts of each number, here without a second
+ * or are seen by them alone (as NaN, where they would be infinite, too, and in any elements of their rows).  scale is at most 2^127 in size
+ * (else DLL_ERR_SHAPE); q_i . k_j and s_ij count as infinite from 2.3e38 on.  Starts outside [0, tokens] are taken as the nearest of these.  With
+ * DLL_BF16 p is rounded, relative to its row's maximum, before it meets v.  Products of DLL_FP32 tensors are taken on three bfloat16 parts of each number, here without a second
  * pass: numbers from 3.39e38 on count as infinite.  (q_tokens / 32 + sequences) * heads, and the same of kv_tokens, at most 2^24 - 1. */
 size_t dll_attention_fwd_workspace_bytes(const dll_attention_desc *d);
 dll_status dll_attention_fwd(const dll_attention_desc *d, const void *q, const void *k, const void *v,
@@ -459,7 +459,7 @@ dll_status dll_cache_write(const dll_cache_desc *d, int tokens, int row, const v
  * A length below 0 counts as 0, one that the table has no room for as that room.  Keys whose table entry lies outside [0, pages)
  * are left out, and nothing that pages hold behind a request's last token is used.  A request without keys has o = 0 and lse = -infinity.  What keys
  * and values hold that is not finite reaches the outputs of the heads that read it alone; a key whose score is -infinity has no weight.
- * scale as for dll_attention_fwd.  With DLL_BF16 p is rounded, relative to its maximum, before it meets v. */
+ * scale as for dll_attention_fwd.  With DLL_BF16 p meets v in two parts of that type. */
 size_t dll_paged_attention_workspace_bytes(const dll_cache_desc *d);
 dll_status dll_paged_attention(const dll_cache_desc *d, const void *q, const void *k_cache, const void *v_cache,
                                const int *table, const int *lengths, float scale, void *o, float *lse, void *ws,

@@ -6,11 +6,12 @@
 // other 128 keys of a key head and goes over the queries of its heads (dk, dv).  Both take scores and do.v again, seven products for
 // the five of one kernel that would have to add its dq up in memory.  32 rows a wavefront stay in registers as fragments; the others come
 // through LDS tile by tile, read along a head's elements for the scores and across tokens for the sums.  p and ds go from one
-// product's result to the next one's operand in registers, rounded to the operands' type there.
+// product's result to the next one's operand in registers, rounded to the operands' type there (in bfloat16 a second part of each would be two products
+// more, of nine).
 //
 // Bound by the matrix pipe and by what stands between its products (exponentials, waits for fragments).  4096 tokens, causal, 16 heads of 128 in
-// bfloat16: dq 128 us, dk and dv 188 us, 172 GFLOP of five products at 545 TFLOP/s, and of the seven that are done at 760; all keys seen, 1030 to
-// 1050 for dq.  2001 tokens in three sequences, six heads of 80 on three in single precision: dq 72, dk and dv 77 and their parts' sums 12 us.
+// bfloat16: dq 126 us, dk and dv 183 us, 172 GFLOP of five products at 555 TFLOP/s, and of the seven that are done at 780.
+// 2001 tokens in three sequences, six heads of 80 on three in single precision: dq 68, dk and dv 73 and their parts' sums 12 us.
 // Tried and slower: two blocks of scores a turn with one's exponentials between the other's products (twice the registers, sums moved
 // between the register files at each product: 390 to 840 us for the pass), fragments three steps ahead instead of one (the same), all
 // fragments of the second products ahead of the exponentials (3 % slower).

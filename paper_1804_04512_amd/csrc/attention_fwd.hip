@@ -12,9 +12,10 @@
 // cut into parts that a second launch joins.
 //
 // Bound by the matrix pipe beside the exponentials: a tile of 64 keys is 1024 cycles of products and 980 of vector instructions for a wavefront, and
-// two wavefronts a SIMD overlap them only in part.  bfloat16, heads of 128: 4096 tokens, all keys seen, 16 heads, 134 us = 1030 TFLOP/s; causal
-// 88 us = 780 (its longest row of 64 tiles decides); 16384 tokens in five sequences 295 to 312 us = 910 to 970.  777 tokens, 16 heads of 64,
-// 9.9 us (latency).  Tried and slower: exponentials of one block of keys beside the products of the next and the former (134 to 162 us), wavefront
+// two wavefronts a SIMD overlap them only in part.  In bfloat16 p is rounded on its way into the second product: its rest in a second part would be half as many
+// products again.  Heads of 128: 4096 tokens, all keys seen, 16 heads, 134 to 144 us = 950 to 1030 TFLOP/s; causal
+// 88 to 94 us = 730 to 780 (its longest row of 64 tiles decides); 16384 tokens in five sequences 305 to 317 us = 900 to 940.  777 tokens, 16 heads of 64,
+// 9.7 us (latency).  Tried and slower: exponentials of one block of keys beside the products of the next and the former (134 to 162 us), wavefront
 // priorities around the products (the same), the second products beside the other half's exponentials (the same).
 #include "attention_tile.h"
 
@@ -257,6 +258,8 @@ FwdPlan plan_as(const AttentionArgs &a, char *base) {
   FwdPlan p;
   Take take{base};
   p.rows = ROWS;
+  // four turns a part at least.  Microseconds with 2 / 4 / 8 / 16: 777 tokens, 4 heads of 64, 12.3 / 9.6 / 9.6 / 9.6; 1500, 4 of 128 on one, 24.4 / 24.4 / 21.2 / 21.2, in two 23.5 / 18.2 / 18.2 / 18.2;
+  // 600, 8 of 256, 33.8 / 26.3 / 25.1 / 25.1; in single precision 500, 8 of 64, 20.6 / 28.4 / 28.4 / 28.4, 1000, 8 of 128, 43.5 / 43.4 / 49.7 / 96.1, 2001 ragged, six of 80, 51.2 / 48.8 / 54.0 / 82.5
   p.parts.n = parts_of((a.Tq + S::kQueries - 1) / S::kQueries * (long)a.H, tiles_of(a.Tq, a.S, S::kQueries) * a.H, (long)(ROWS == 4 ? S::kResident : 1) * chip().cus,
                        a.Tk / a.S / S::kKeys, 4);
   p.parts.ld = (a.D + 3) & ~3;

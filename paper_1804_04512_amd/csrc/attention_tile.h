@@ -190,8 +190,8 @@ __device__ __forceinline__ void written() {
 // not small, and without a mask too, as sums of large values may overflow on their way to a mean that does not), a
 // workgroup takes its tiles again (or another launch's does): in those that the mask cuts, rows with such numbers lose them, and the lanes that see one of these rows are
 // told, whose results are NaN.  All of this is off the usual path but for one look at the sums and the registers that a second copy of the loop
-// takes.  With it / without, microseconds: 16384 prompt tokens in five sequences, 16 heads of 128 on 4, 304 / 296; 777, 10.7 / 10.2; a training pass
-// over 4096, 16 heads of 128, 368 / 367; 1024 in single precision, 8 heads of 64 on 2, 98 / 93.
+// takes.  With it / without, microseconds: forward 16384 tokens in five sequences, 16 heads of 128 on 4, 310 / 305; 4096, 16 heads, 91.3 / 89.1, all keys seen 139 / 138; 777, 10.6 /
+// 10.4; 1024 in single precision, 8 heads of 64 on 2, 25.1 / 24.8; the gradients of a training pass over 4096, 16 heads of 128, 373 / 373; 1024 in single precision 91.0 / 89.3.
 constexpr int kCareful = 256;   // bytes of LDS for it
 template <int N>
 __device__ __forceinline__ bool all_finite(const floatx16 (&c)[N]) {

@@ -13,8 +13,8 @@
 // wavefront's own LDS to be read across keys, in the order in which the scores' registers hold them: register r of quarter c is key 4 c + r of
 // its sixteen, so eight registers of two results are keys 4 c + j and 16 + 4 c + j.
 //
-// 64 requests of up to 8192 keys, 32 heads of 128 on 8, bfloat16: 193 us for 1.04 GB = 5.4 TB/s, above what a copy reaches (4.8); three of up to 60000, eight heads of
-// 96 in single precision, 161 us = 5.5.  One request of 1000 keys 13.5 us: two launches, each a chain of loads.  What it took: pages asked for before the
+// 64 requests of up to 8192 keys, 32 heads of 128 on 8, bfloat16: 196 us for 1.04 GB = 5.3 TB/s, above what a copy reaches (4.8); three of up to 60000, eight heads of
+// 96 in single precision, 163 us = 5.4.  One request of 1000 keys 13.5 us: two launches, each a chain of loads.  What it took: pages asked for before the
 // rows of the tile in between, as loads come back in order (312 to 193 us), and no branch between loads.
 #include "attention_tile.h"
 

@@ -9,7 +9,7 @@
 // Store.  Rows go from [token][head] to [page][head][place in page], so that a head's keys of a page lie together for the
 // attention that streams them; both sides move 16 bytes or more a lane.
 //
-// The plan is bound by latency: 64 requests with a new token each 4.1 us on the GPU, 2000 prompts with 272 000 tokens 7.4 (as much for an empty
+// The plan is bound by latency: 64 requests with a new token each 4.3 us on the GPU, 2000 prompts with 272 000 tokens 7.3 (as much for an empty
 // kernel: 2.7).  The store is bound by memory: 15 000 tokens of 8 heads of 128 in single precision, 236 MB, 41 us = 5.8 TB/s.
 #include "large_ops.h"
 #include "tile_product.h"
